@@ -53,6 +53,8 @@ extern "C" {
 #define GT_MAX_K 16u           /* classes */
 #define GT_MAX_TAU 20u         /* fractional bits of the Gini quotients */
 #define GT_STATIC_MAX_N (1u << 18) /* rows of gt_oaa_static */
+#define GT_MAX_DIM (1u << 20)  /* rows, inputs and outputs of a layer */
+#define GT_MAX_EXPERTS 64u     /* experts of a mixture */
 
 typedef struct gt_ctx gt_ctx;     /* keys, operation counter, stream, scratch for partial sums */
 typedef struct gt_train gt_train; /* per-party shares of T, F, M, C, gamma and the data */
@@ -108,7 +110,9 @@ enum {
     GT_KC_EQGRID_STORE = 7, /* equality grid that stores the per-sample leaf one-hot */
     GT_KC_INFER = 8,        /* one-launch inference */
     GT_KC_PARTMM = 9,       /* data partition by products on the matrix cores */
-    GT_KC_N = 10
+    GT_KC_DENSE = 10,       /* matrix products of layers, with the conversion of their operands */
+    GT_KC_FINISH = 11,      /* completion of layers: rounding, activation, residual */
+    GT_KC_N = 12
 };
 typedef struct { double ms[GT_KC_N]; uint64_t launches[GT_KC_N]; } gt_prof;
 
@@ -247,6 +251,41 @@ int gt_forest_create(gt_ctx *ctx, const gt_tree *const *trees, size_t ntrees, gt
 int gt_forest_destroy(gt_forest *forest);
 int gt_infer_forest(gt_ctx *ctx, const gt_forest *forest, const gt_shares *I, size_t N_I,
                     uint32_t d, const gt_shares *R_out);
+
+/* ---- layers in fixed point: tau fraction bits (no part of the paper: the layers of a small network on
+ * the same shares, for users who keep such a model beside trees).  All values are
+ * signed words x = round(real * 2^tau); all matrices row-major without gaps; results are exact. */
+#define GT_ACT_NONE 0
+#define GT_ACT_RELU 1
+typedef struct gt_dense gt_dense; /* weights din x dout, bias */
+typedef struct gt_moe gt_moe;     /* router, experts, workspace for max_rows rows */
+/* W: din x dout, b: dout words or NULL.  The shares are copied. */
+int gt_dense_create(gt_ctx *ctx, const gt_shares *W, const gt_shares *b, uint32_t din, uint32_t dout, gt_dense **out);
+/* new weights of the same sizes, as after a training step; b as at creation (NULL where it was NULL).  Allocates nothing. */
+int gt_dense_set(gt_ctx *ctx, gt_dense *layer, const gt_shares *W, const gt_shares *b);
+int gt_dense_destroy(gt_dense *layer);
+/* y = act(floor((x W + (b << tau) + 2^(tau-1)) / 2^tau)) + residual, x: rows x din, y, residual (NULL: none), gate: rows x dout.
+ * Sums are added up modulo 2^64 and have to stay below 2^62 in absolute value, with GT_ACT_RELU below
+ * 2^(tau+31) (results below 2^31).  gate (NULL: not wanted, GT_EINVAL without ReLU) receives ReLU's bit, 1 where the
+ * value before the activation is at least 0.  y may be the residual's buffers, not those of x.  One operation id; rounds: 7, with ReLU 9.
+ * The context's workspace grows on first use or for larger calls (then the call waits for the stream and allocates). */
+int gt_dense_forward(gt_ctx *ctx, const gt_dense *layer, const gt_shares *x, size_t rows, int act, const gt_shares *residual,
+                     const gt_shares *y, const gt_shares *gate);
+/* dz = gate dy (gate NULL: dz = dy), dx = floor((dz W^T + 2^(tau-1)) / 2^tau), dW = the same of x^T dz, db = column sums of dz; outputs
+ * that are NULL are not computed (x is needed for dW alone).  The gradient of the residual is dy.  Up to three operation ids: dz (with
+ * a gate), dx, dW, in this order, each if computed. */
+int gt_dense_backward(gt_ctx *ctx, const gt_dense *layer, const gt_shares *x, const gt_shares *gate, const gt_shares *dy, size_t rows,
+                      const gt_shares *dx, const gt_shares *dW, const gt_shares *db);
+/* Router Wr: d x experts, br: experts; W1: experts x d x ff, b1: experts x ff; W2: experts x ff x d, b2: experts x d; biases may be
+ * NULL.  1 <= top <= experts <= GT_MAX_EXPERTS.  The shares are copied; the workspace for max_rows rows is allocated here. */
+int gt_moe_create(gt_ctx *ctx, const gt_shares *Wr, const gt_shares *br, const gt_shares *W1, const gt_shares *b1, const gt_shares *W2,
+                  const gt_shares *b2, uint32_t d, uint32_t ff, uint32_t experts, uint32_t top, uint32_t max_rows, gt_moe **out);
+int gt_moe_destroy(gt_moe *moe);
+/* Per row: scores s = ReLU(x Wr + br); the `top` experts of the largest scores, ties to the lower index; gates
+ * g = floor(s 2^tau / (1 + sum of s)); y = sum over them of g (ReLU(x W1 + b1) W2 + b2), the hidden values scaled by g, rounded once,
+ * plus the residual (NULL: none).  Which experts a row takes is not revealed: the row's inputs are multiplied by the shared choice and meet
+ * all experts' weights.  rows <= max_rows, x, y, residual: rows x d; y may be the residual's buffers.  10 + tau operation ids. */
+int gt_moe_forward(gt_ctx *ctx, gt_moe *moe, const gt_shares *x, size_t rows, const gt_shares *residual, const gt_shares *y);
 
 #ifdef __cplusplus
 }

@@ -1511,3 +1511,293 @@ int orc_infer_rows(orc_ctx *c, const uint64_t *featf, const uint64_t *thrf, cons
     rowsel rs = { rows, nrows };
     return infer_rs(c, featf, thrf, leaff, H, If, NI, d, Rf, &rs);
 }
+
+/* ------------------------------------------------------------------------- */
+/* Layers in fixed point with f = tau fraction bits.                          */
+
+/* A party's part of the matrix product of X (m x k) and W (k x n): the three-term products added up over k.
+ * xt, wt: the factor is stored transposed (k x m, n x k). */
+static void product_parts(const sh *X, int xt, const sh *W, int wt, size_t m, size_t k, size_t n, sh *z)
+{
+#pragma omp parallel for schedule(static)
+    for (size_t i = 0; i < m; i++) {
+        for (size_t j = 0; j < n; j++) { u64 o[3] = { 0, 0, 0 }; sh_set(z, i * n + j, o); }
+        for (size_t q = 0; q < k; q++) {
+            u64 x[3], w[3], t[3];
+            sh_get(X, xt ? q * m + i : i * k + q, x);
+            for (size_t j = 0; j < n; j++) {
+                sh_get(W, wt ? j * k + q : q * n + j, w);
+                prod3(x, w, t);
+                for (int p = 0; p < 3; p++) z->c[p][i * n + j] += t[p];
+            }
+        }
+    }
+}
+
+/* Block e of stream 5 under the dealer's key: the words of a completion beside the edaBit and daBit of stream 0: an arithmetic
+ * sharing of r >> f and of r's top bit, and a second daBit. */
+typedef struct { u64 shift[3], top[3], bA[3], bB[3]; } finish_t;
+static void dealer_finish(const orc_ctx *c, u32 op, u64 e, u64 r, u32 f, finish_t *G)
+{
+    u32 out[16];
+    u64 w[8], beta;
+    orc_chacha_block(c->key[KEY_DEALER], (u32)e, (u32)(e >> 32), op, 5, PRF_ROUNDS, out);
+    for (int i = 0; i < 8; i++) w[i] = (u64)out[2 * i] | ((u64)out[2 * i + 1] << 32);
+    beta = w[6] & 1;
+    G->shift[0] = w[0]; G->shift[1] = w[1]; G->shift[2] = (r >> f) - w[0] - w[1];
+    G->top[0] = w[2]; G->top[1] = w[3]; G->top[2] = (r >> 63) - w[2] - w[3];
+    G->bA[0] = w[4]; G->bA[1] = w[5]; G->bA[2] = beta - w[4] - w[5];
+    G->bB[0] = (w[6] >> 1) & 1; G->bB[1] = (w[6] >> 2) & 1; G->bB[2] = beta ^ G->bB[0] ^ G->bB[1];
+}
+
+/* [c < r] for public c and bitwise shared r, on the low `width` bits of both: the prefix pairs of ge_el, levels up to
+ * blocks of 64 or 32 bits.  low: the pair G of bits 0..31 (before the last level of 64). */
+static void less_el(const orc_ctx *c, u32 op, u64 e, u64 cw, const u64 rw[3], int levels, u64 low[3], u64 all[3])
+{
+    u64 AG[3], AE[3], G[64][3], E[64][3];
+    int n = 1 << levels;
+    for (int i = 0; i < n; i++) {
+        u64 nc = (~cw >> i) & 1;
+        for (int j = 0; j < 3; j++) { u64 rb = (rw[j] >> i) & 1; G[i][j] = nc & rb; E[i][j] = rb; }
+        E[i][0] ^= nc;
+        if (i == 63) for (int j = 0; j < 3; j++) { G[i][j] = 0; E[i][j] = j == 0; }
+    }
+    zero_b(c, op, 1, e, AG);
+    zero_b(c, op, 2, e, AE);
+    for (int k = 0; k < levels; k++) {
+        int s = 1 << k;
+        if (k == 5) memcpy(low, G[0], sizeof G[0]);
+        for (int i = 0; i < n; i += 2 * s) {
+            int hi = i + s, lo = i, bit = i + s - 1;
+            u64 al[3], p[3];
+            for (int j = 0; j < 3; j++) al[j] = (AG[j] >> bit) & 1;
+            and_el(E[hi], G[lo], al, 1, p);
+            for (int j = 0; j < 3; j++) G[lo][j] = G[hi][j] ^ p[j];
+            if (k < levels - 1) {
+                for (int j = 0; j < 3; j++) al[j] = (AE[j] >> bit) & 1;
+                and_el(E[hi], E[lo], al, 1, E[lo]);
+            }
+        }
+    }
+    if (levels == 5) memcpy(low, G[0], sizeof G[0]);
+    memcpy(all, G[0], sizeof G[0]);
+}
+
+/* Completion of sums v whose additive parts the parties hold: y = floor((v + 2^(f-1)) / 2^f), with ReLU times its sign bit (the gate),
+ * plus a residual.  Open c = v + 2^(f-1) + O + r with O = 2^62, or 2^(f+31) with ReLU (z_p + alpha_p + r_p to both others, one round); then
+ * y = (c >> f) - (r >> f) + 2^(64-f) [c_63 = 0 and r_63 = 1] - [c mod 2^f < r mod 2^f] - (O >> f), and the sign is bit f+31 of c - r. */
+static void finish(orc_ctx *c, u32 op, const sh *z, size_t n, int relu, const sh *res, sh *y, sh *gate)
+{
+    const u32 f = c->tau;
+    const u64 off = relu ? (u64)1 << (f + 31) : (u64)1 << 62;
+#pragma omp parallel for schedule(static)
+    for (size_t e = 0; e < n; e++) {
+        dealer_t D; finish_t G;
+        u64 al[3], v[3], cw, low[3], all[3], rw[3], b[3], o[3];
+        sh_get(z, e, v);
+        dealer(c, op, e, &D);
+        dealer_finish(c, op, e, D.r, f, &G);
+        zero_a(c, op, 0, e, al);
+        cw = ((u64)1 << (f - 1)) + off;
+        for (int j = 0; j < 3; j++) cw += v[j] + al[j] + D.rA[j];          /* opened */
+        for (int j = 0; j < 3; j++) rw[j] = D.rho[j] << (32 - f);
+        less_el(c, op, e, cw << (32 - f), rw, relu ? 6 : 5, low, all);
+        b2a_el(low, &D, b);
+        for (int j = 0; j < 3; j++) {
+            o[j] = (cw >> 63 ? 0 : G.top[j] << (64 - f)) - G.shift[j] - b[j];
+            if (j == 0) o[j] += (cw >> f) - (off >> f);
+        }
+        if (relu) {
+            dealer_t D2;
+            u64 s[3], sA[3], a3[3], r[3];
+            memcpy(D2.bA, G.bA, sizeof G.bA); memcpy(D2.bB, G.bB, sizeof G.bB);
+            for (int j = 0; j < 3; j++) s[j] = ((D.rho[j] >> (f + 31)) & 1) ^ all[j];
+            s[0] ^= (cw >> (f + 31)) & 1;
+            b2a_el(s, &D2, sA);
+            zero_a(c, op, 3, e, a3);
+            mult_el(sA, o, a3, r);
+            memcpy(o, r, sizeof o);
+            if (gate) sh_set(gate, e, sA);
+        }
+        if (res) for (int j = 0; j < 3; j++) o[j] += res->c[j][e];
+        sh_set(y, e, o);
+    }
+    wire(c, +1, n, 64); wire(c, -1, n, 64);
+    for (int k = 0; k < (relu ? 5 : 4); k++) wire(c, -1, n, 2 * ((relu ? 32u : 16u) >> k));
+    wire(c, -1, n, 1);
+    wire(c, +1, n, relu ? 2 : 1);
+    if (relu) wire(c, -1, n, 64);
+    c->rounds += relu ? 9 : 7;
+}
+
+static sh sh_flat(const u64 *flat, size_t n) { sh v = sh_alloc(n); if (flat) sh_from_flat(&v, flat); return v; }
+
+static void dense(orc_ctx *c, const sh *X, const sh *W, const sh *b, size_t m, size_t k, size_t n, int relu, const sh *res, sh *y, sh *gate)
+{
+    sh z = sh_alloc(m * n);
+    product_parts(X, 0, W, 0, m, k, n, &z);
+    if (b) for (int p = 0; p < 3; p++) for (size_t e = 0; e < m * n; e++) z.c[p][e] += b->c[p][e % n] << c->tau;
+    finish(c, c->op++, &z, m * n, relu, res, y, gate);
+    sh_free(&z);
+}
+
+void orc_dense_forward(orc_ctx *c, const uint64_t *Xf, const uint64_t *Wf, const uint64_t *bf, const uint64_t *resf, size_t rows, size_t din,
+                       size_t dout, int relu, uint64_t *yf, uint64_t *gatef)
+{
+    sh X = sh_flat(Xf, rows * din), W = sh_flat(Wf, din * dout), b = sh_flat(bf, dout), res = sh_flat(resf, resf ? rows * dout : 0);
+    sh y = sh_alloc(rows * dout), gate = sh_alloc(rows * dout);
+    dense(c, &X, &W, bf ? &b : NULL, rows, din, dout, relu, resf ? &res : NULL, &y, &gate);
+    sh_to_flat(&y, yf);
+    if (gatef) sh_to_flat(&gate, gatef);
+    sh_free(&X); sh_free(&W); sh_free(&b); sh_free(&res); sh_free(&y); sh_free(&gate);
+}
+
+void orc_dense_backward(orc_ctx *c, const uint64_t *Xf, const uint64_t *Wf, const uint64_t *gatef, const uint64_t *dyf, size_t rows, size_t din,
+                        size_t dout, uint64_t *dxf, uint64_t *dWf, uint64_t *dbf)
+{
+    const size_t n = rows * dout;
+    sh X = sh_flat(Xf, rows * din), W = sh_flat(Wf, din * dout), dz = sh_flat(dyf, n);
+    if (gatef) {
+        u64 *t = (u64 *)malloc(3 * (n ? n : 1) * sizeof(u64));
+        orc_mult(c, gatef, dyf, n, t);
+        sh_from_flat(&dz, t);
+        free(t);
+    }
+    if (dxf) {
+        sh z = sh_alloc(rows * din), o = sh_alloc(rows * din);
+        product_parts(&dz, 0, &W, 1, rows, dout, din, &z);
+        finish(c, c->op++, &z, rows * din, 0, NULL, &o, NULL);
+        sh_to_flat(&o, dxf);
+        sh_free(&z); sh_free(&o);
+    }
+    if (dWf) {
+        sh z = sh_alloc(din * dout), o = sh_alloc(din * dout);
+        product_parts(&X, 1, &dz, 0, din, rows, dout, &z);
+        finish(c, c->op++, &z, din * dout, 0, NULL, &o, NULL);
+        sh_to_flat(&o, dWf);
+        sh_free(&z); sh_free(&o);
+    }
+    if (dbf)
+        for (int p = 0; p < 3; p++)
+            for (size_t j = 0; j < dout; j++) {
+                u64 s = 0;
+                for (size_t i = 0; i < rows; i++) s += dz.c[p][i * dout + j];
+                dbf[p * dout + j] = s;
+            }
+    sh_free(&X); sh_free(&W); sh_free(&dz);
+}
+
+/* Mixture of experts.  Scores s = ReLU(x Wr + br); rank of an expert = how many others beat it (all pairs a < b: bit [s_a >= s_b], a tie goes
+ * to the lower index); o_j[a] = [rank_a = j], j < k; gate g_j = floor(S_j 2^f / (1 + sum of s)), S_j the score with rank j; per chosen
+ * expert h_j = ReLU(x W1 + b1) from the inputs o_j[a] x[i] against the experts' stacked weights, scaled by g_j, and
+ * y = sum_j g_j (h_j W2 + b2) likewise, completed once, plus a residual. */
+void orc_moe_forward(orc_ctx *c, const uint64_t *Xf, const uint64_t *Wrf, const uint64_t *brf, const uint64_t *W1f, const uint64_t *b1f,
+                     const uint64_t *W2f, const uint64_t *b2f, const uint64_t *resf, size_t rows, size_t d, size_t ff, size_t E, size_t k, uint64_t *yf)
+{
+    const u32 f = c->tau;
+    const size_t P = E * (E - 1) / 2, rk = rows * k, n1 = E * d + E, n2 = E * ff + E;
+    sh X = sh_flat(Xf, rows * d), Wr = sh_flat(Wrf, d * E), br = sh_flat(brf, E), res = sh_flat(resf, resf ? rows * d : 0);
+    sh W1 = sh_alloc(n1 * ff), W2 = sh_alloc(n2 * d);
+    for (int p = 0; p < 3; p++) {                                     /* biases as further rows of the weights */
+        memcpy(W1.c[p], W1f + p * E * d * ff, E * d * ff * 8);
+        memcpy(W2.c[p], W2f + p * E * ff * d, E * ff * d * 8);
+        if (b1f) memcpy(W1.c[p] + E * d * ff, b1f + p * E * ff, E * ff * 8);
+        if (b2f) memcpy(W2.c[p] + E * ff * d, b2f + p * E * d, E * d * 8);
+    }
+    sh s = sh_alloc(rows * E), rank = sh_alloc(rows * E), o = sh_alloc(rk * E), S = sh_alloc(rk), Q = sh_alloc(rk), g = sh_alloc(rk);
+    dense(c, &X, &Wr, brf ? &br : NULL, rows, d, E, 1, NULL, &s, NULL);
+    u32 op = c->op++;
+    for (size_t t = 0; t < rows; t++) {
+        size_t e = t * P;
+        for (size_t a = 0; a < E; a++)
+            for (size_t b = a + 1; b < E; b++, e++) {
+                dealer_t D;
+                u64 v[3], ge[3], w[3];
+                for (int p = 0; p < 3; p++) v[p] = s.c[p][t * E + a] - s.c[p][t * E + b];
+                dealer(c, op, e, &D);
+                ge_el(c, op, e, v, &D, ge);
+                b2a_el(ge, &D, w);                                    /* a beats b */
+                for (int p = 0; p < 3; p++) { rank.c[p][t * E + b] += w[p]; rank.c[p][t * E + a] += (u64)(p == 0) - w[p]; }
+            }
+    }
+    wire_ge(c, rows * P); wire_b2a(c, rows * P);
+    op = c->op++;
+    for (size_t e = 0; e < rk * E; e++) {
+        dealer_t D;
+        u64 v[3], A[3], t[3], w[3];
+        sh_get(&rank, e / (k * E) * E + e % E, v);
+        v[0] -= e / E % k;
+        dealer(c, op, e, &D);
+        eq_el(c, op, e, v, &D, A, t);
+        b2a_el(t, &D, w);
+        sh_set(&o, e, w);
+    }
+    wire_eq(c, rk * E); wire_b2a(c, rk * E);
+    op = c->op++;
+    for (size_t e = 0; e < rk; e++) {
+        u64 al[3], z[3];
+        zero_a(c, op, 0, e, al);
+        memcpy(z, al, sizeof z);
+        Q.c[0][e] = 1;
+        for (size_t a = 0; a < E; a++) {
+            u64 x[3], y[3], t[3];
+            sh_get(&o, e * E + a, x); sh_get(&s, e / k * E + a, y);
+            prod3(x, y, t);
+            for (int p = 0; p < 3; p++) { z[p] += t[p]; Q.c[p][e] += y[p]; }
+        }
+        sh_set(&S, e, z);
+    }
+    wire_reshare(c, rk, 1);
+    {
+        u64 *Sf = (u64 *)malloc(9 * (rk ? rk : 1) * 8), *Qf = Sf + 3 * rk, *gf = Qf + 3 * rk;
+        sh_to_flat(&S, Sf); sh_to_flat(&Q, Qf);
+        orc_div(c, Sf, Qf, rk, gf);
+        sh_from_flat(&g, gf);
+        free(Sf);
+    }
+    sh xe = sh_alloc(rk * n1), h = sh_alloc(rk * ff), z = sh_alloc(rk * ff), hg = sh_alloc(rk * ff), he = sh_alloc(rows * n2), y = sh_alloc(rows * d);
+    op = c->op++;
+    for (size_t r = 0; r < rk; r++)
+        for (size_t a = 0; a < E; a++) {
+            u64 w[3], x[3], al[3], t[3];
+            sh_get(&o, r * E + a, w);
+            for (size_t i = 0; i < d; i++) {
+                sh_get(&X, r / k * d + i, x);
+                zero_a(c, op, 0, (r * E + a) * d + i, al);
+                mult_el(w, x, al, t);
+                sh_set(&xe, r * n1 + a * d + i, t);
+            }
+            for (int p = 0; p < 3; p++) xe.c[p][r * n1 + E * d + a] = w[p] << f;
+        }
+    wire_reshare(c, rk * E * d, 1);
+    dense(c, &xe, &W1, NULL, rk, n1, ff, 1, NULL, &h, NULL);
+    for (size_t e = 0; e < rk * ff; e++) {
+        u64 a[3], b[3], t[3];
+        sh_get(&g, e / ff, a); sh_get(&h, e, b);
+        prod3(a, b, t);
+        sh_set(&z, e, t);
+    }
+    finish(c, c->op++, &z, rk * ff, 0, NULL, &hg, NULL);
+    op = c->op++;
+    for (size_t t = 0; t < rows; t++)
+        for (size_t q = 0; q < n2; q++) {
+            u64 al[3], sum[3];
+            const int tail = q >= E * ff;
+            const size_t a = tail ? q - E * ff : q / ff;
+            zero_a(c, op, 0, t * n2 + q, al);
+            memcpy(sum, al, sizeof sum);
+            for (size_t j = 0; j < k; j++) {
+                u64 w[3], v[3], r[3];
+                sh_get(&o, (t * k + j) * E + a, w);
+                if (tail) sh_get(&g, t * k + j, v); else sh_get(&hg, (t * k + j) * ff + q % ff, v);
+                prod3(w, v, r);
+                for (int p = 0; p < 3; p++) sum[p] += r[p];
+            }
+            sh_set(&he, t * n2 + q, sum);
+        }
+    wire_reshare(c, rows * n2, 1);
+    dense(c, &he, &W2, NULL, rows, n2, d, 0, resf ? &res : NULL, &y, NULL);
+    sh_to_flat(&y, yf);
+    sh *all[] = { &X, &Wr, &br, &res, &W1, &W2, &s, &rank, &o, &S, &Q, &g, &xe, &h, &z, &hg, &he, &y };
+    for (size_t i = 0; i < sizeof all / sizeof *all; i++) sh_free(all[i]);
+}

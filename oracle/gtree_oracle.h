@@ -141,6 +141,18 @@ int orc_infer_rows(orc_ctx *, const uint64_t *feat, const uint64_t *thr, const u
                    uint32_t H, const uint64_t *I, size_t NI, uint32_t d, const size_t *rows,
                    size_t nrows, uint64_t *R);
 
+/* ---- layers in fixed point, tau fraction bits ------------------------------ */
+/* y = act(floor((X W + (b << tau) + 2^(tau-1)) / 2^tau)) + res; X rows x din, W din x dout; b, res, gate (ReLU's bit, [y >= 0] before
+ * the activation) may be NULL; one op */
+void orc_dense_forward(orc_ctx *, const uint64_t *X, const uint64_t *W, const uint64_t *b, const uint64_t *res, size_t rows, size_t din,
+                       size_t dout, int relu, uint64_t *y, uint64_t *gate);
+/* dz = gate dy (op, if gate), dx = dz W^T (op), dW = X^T dz (op), db = column sums of dz; outputs may be NULL */
+void orc_dense_backward(orc_ctx *, const uint64_t *X, const uint64_t *W, const uint64_t *gate, const uint64_t *dy, size_t rows, size_t din,
+                        size_t dout, uint64_t *dx, uint64_t *dW, uint64_t *db);
+/* mixture of experts, see the source; Wr d x E, W1 E x d x ff, W2 E x ff x d; 10 + tau ops */
+void orc_moe_forward(orc_ctx *, const uint64_t *X, const uint64_t *Wr, const uint64_t *br, const uint64_t *W1, const uint64_t *b1,
+                     const uint64_t *W2, const uint64_t *b2, const uint64_t *res, size_t rows, size_t d, size_t ff, size_t E, size_t k, uint64_t *y);
+
 #ifdef __cplusplus
 }
 #endif

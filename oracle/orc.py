@@ -73,6 +73,9 @@ def _load():
         "orc_ge_a": (None, [vp, _u64p, _u64p, sz, _u64p]),
         "orc_oaa": (None, [vp, _u64p, sz, _u64p, sz, _u64p]),
         "orc_div": (None, [vp, _u64p, _u64p, sz, _u64p]),
+        "orc_dense_forward": (None, [vp, _u64p, _u64p, _u64p, _u64p, sz, sz, sz, i, _u64p, _u64p]),
+        "orc_dense_backward": (None, [vp, _u64p, _u64p, _u64p, _u64p, sz, sz, sz, _u64p, _u64p, _u64p]),
+        "orc_moe_forward": (None, [vp] + [_u64p] * 8 + [sz] * 5 + [_u64p]),
         "orc_train_create": (vp, [vp, _u64p, _u64p, sz, u32, u32]),
         "orc_train_destroy": (None, [vp]),
         "orc_train_level": (i, [vp, vp, u32]),
@@ -257,6 +260,32 @@ class Oracle:
         z = np.zeros_like(S)
         self.L.orc_div(self.ctx, _p(S.reshape(-1)), _p(Q.reshape(-1)), S.shape[1], _p(z.reshape(-1)))
         return z
+
+    # -- layers ------------------------------------------------------------
+    def _flat(self, a):
+        return None if a is None else self._c(a).reshape(-1)
+
+    def dense_forward(self, X, W, rows, din, dout, b=None, relu=False, residual=None):
+        """(y, gate); gate is None without ReLU."""
+        y = np.zeros((3, rows * dout), dtype=np.uint64)
+        gate = np.zeros_like(y) if relu else None
+        a = [self._flat(t) for t in (X, W, b, residual)]
+        self.L.orc_dense_forward(self.ctx, *[_p(t) for t in a], rows, din, dout, int(relu), _p(y.reshape(-1)),
+                                 None if gate is None else _p(gate.reshape(-1)))
+        return y, gate
+
+    def dense_backward(self, X, W, dy, rows, din, dout, gate=None, want=(True, True, True)):
+        """(dx, dW, db), None where not wanted."""
+        out = [np.zeros((3, n), dtype=np.uint64) if w else None for n, w in zip((rows * din, din * dout, dout), want)]
+        a = [self._flat(t) for t in (X, W, gate, dy)]
+        self.L.orc_dense_backward(self.ctx, *[_p(t) for t in a], rows, din, dout, *[None if t is None else _p(t.reshape(-1)) for t in out])
+        return tuple(out)
+
+    def moe_forward(self, X, Wr, W1, W2, rows, d, ff, experts, top, br=None, b1=None, b2=None, residual=None):
+        y = np.zeros((3, rows * d), dtype=np.uint64)
+        a = [self._flat(t) for t in (X, Wr, br, W1, b1, W2, b2, residual)]
+        self.L.orc_moe_forward(self.ctx, *[_p(t) for t in a], rows, d, ff, experts, top, _p(y.reshape(-1)))
+        return y
 
     # -- training ----------------------------------------------------------
     def train_create(self, X, Y, N, d, H):

@@ -1,0 +1,395 @@
+// Layers in fixed point on shares, f = tau fraction bits: matrix products with bias, activation and residual, and a mixture
+// of experts for a few tokens.
+//   product:     the parties' parts z_p of v = X W (three-term products added up, Sec. II-B), 64-bit words
+//   completion:  y = floor((v + (b << f) + 2^(f-1)) / 2^f), with ReLU times its sign bit, plus a residual (k_finish)
+// The completion opens v once, masked with the edaBit r of the element: party p sends z_p + alpha_p + r_p to both others, which
+// replaces the reshare and the opening of its result.  With c = v + 2^(f-1) + O + r, 0 <= v + 2^(f-1) + O < 2^63,
+//   y = (c >> f) - (r >> f) + 2^(64-f) [c_63 = 0 and r_63 = 1] - [c mod 2^f < r mod 2^f] - (O >> f)
+// where r >> f and r_63 are dealer material and the last bit comes from a tree of ANDs.  With ReLU O = 2^(f+31): v + 2^(f-1) >= 0 iff bit
+// f+31 of c - r is set, and the borrow into that bit is the root of the tree whose lower half is the borrow of the rounding; so one
+// opening and one tree of 64 leaves (bits 0 .. f+31, shifted up to end at leaf 63) serve both.
+#pragma once
+#include "gt_kernels.hpp"
+
+#define GT_FIN_EL 16                              // elements of a wavefront's tile
+#define GT_FIN_ROWS 31                            // rows of material: 19 of the dealer's, 4 streams x 3 keys
+
+// The wavefront model with 16 lanes per party (lanes 48-63 repeat party 2's and neither store nor count): a tile starts at a multiple of
+// 8, so that its words under the three keys are whole blocks, and two dealer blocks per element, six blocks per stream make up one pass
+// of the block function (56 of 64 lanes with four streams).
+struct FWire : WWire {
+    __device__ __forceinline__ void init(uint4 *region, u64 *s_cnt)
+    {
+        const u32 l = threadIdx.x & (GT_LANES - 1);
+        real = l < 3 * GT_FIN_EL; t = l & 15; p = l < 16 ? 0 : (l < 32 ? 1 : 2); pn = p == 2 ? 0 : p + 1;
+        m = 16 * (u32)p + t;
+        nx = 16 * (u32)pn + t; pv = 16 * (p == 0 ? 2u : (u32)p - 1) + t;
+        buf = region; cnt = s_cnt; nopen = 0; nresh = 0;
+        if (l < 6) cnt[l] = 0;
+        wave_sync();
+    }
+    // a word to both others; the sum of the three
+    __device__ __forceinline__ u64 open_both(u64 v, u32 bits)
+    {
+        nopen += bits; nresh += bits;
+        wave_sync();
+        *(uint2 *)&buf[m] = make_uint2((u32)v, (u32)(v >> 32));
+        wave_sync();
+        const uint2 a = *(const uint2 *)&buf[nx], b = *(const uint2 *)&buf[pv];
+        return v + ((u64)a.x | ((u64)a.y << 32)) + ((u64)b.x | ((u64)b.y << 32));
+    }
+};
+
+// Material of a tile: rows of GT_FIN_EL words.  0-2 r, 3-5 bits of r shifted up by 32 - f, 6-8 and 9 the daBit (arithmetic, both Boolean
+// ones), 10-12 r >> f, 13-15 r_63 << (64 - f), 16-18 the second daBit, then [stream][key].
+template <int NS>
+struct FinTile {
+    const u32 *keys;
+    u64 *mat;
+    u32 f;
+    __device__ __forceinline__ void deal(u32 op, u64 e0)
+    {
+        const u32 l = threadIdx.x & (GT_LANES - 1), el = l & 15, q = l - 32, i = q / 6, j = (q % 6) / 2, g = q & 1;
+        const bool dealer = l < 32;
+        wave_sync();
+        Key kv;
+        const u32 *from = keys + 8 * (dealer ? GT_KEY_DEALER : (int)(j < 3 ? j : 0));
+#pragma unroll
+        for (int w = 0; w < 8; w++) kv.k[w] = from[w];
+        u64 D[8];
+        chacha8<PRF_PAIR>(kv, dealer ? e0 + el : (e0 >> 3) + g, op, l < 16 ? 0u : (dealer ? 5u : i), D);
+        const u64 r = (u64)__shfl((unsigned long long)D[0], (int)el, GT_LANES);          // of the element's first block
+        const u64 bits = dealer ? (l < 16 ? D[5] : D[6]) : 0, beta = bits & 1;
+        const u32 b0 = (u32)(bits >> 1) & 1, b1 = (u32)(bits >> 2) & 1, bb = b0 | (b1 << 1) | ((((u32)beta ^ b0 ^ b1) & 1) << 2);
+        const u32 other = (u32)__shfl((int)bb, (int)el + 16, GT_LANES);
+        u64 *to = mat + el;
+        if (l < 16) {
+            to[0] = D[1]; to[16] = D[2]; to[32] = r - D[1] - D[2];
+            to[48] = D[3] << (32 - f); to[64] = D[4] << (32 - f); to[80] = (r ^ D[3] ^ D[4]) << (32 - f);
+            to[96] = D[6]; to[112] = D[7]; to[128] = beta - D[6] - D[7];
+            to[144] = bb | (other << 3);
+        } else if (dealer) {
+            to[160] = D[0]; to[176] = D[1]; to[192] = (r >> f) - D[0] - D[1];
+            to[208] = D[2] << (64 - f); to[224] = D[3] << (64 - f); to[240] = ((r >> 63) - D[2] - D[3]) << (64 - f);
+            to[256] = D[4]; to[272] = D[5]; to[288] = beta - D[4] - D[5];
+        } else if (q < 6 * NS) {
+#pragma unroll
+            for (int w = 0; w < 8; w++) mat[(19 + q / 2) * GT_FIN_EL + g * 8 + w] = D[w];
+        }
+        wave_sync();
+    }
+    __device__ __forceinline__ Sh pair(const WWire &W, int row) const { return Sh{ mat[(row + W.p) * GT_FIN_EL + W.t], mat[(row + W.pn) * GT_FIN_EL + W.t] }; }
+    __device__ __forceinline__ u64 za(const WWire &W, int i) const { const Sh w = pair(W, 19 + 3 * i); return w.o - w.n; }
+    __device__ __forceinline__ u64 zb(const WWire &W, int i) const { const Sh w = pair(W, 19 + 3 * i); return w.o ^ w.n; }
+};
+
+// [c < r] on the low 63 bits (the prefix pairs of ge_bit_masks); low: on the low 32 bits
+__device__ __forceinline__ Sh less64(FWire &W, u64 c, Sh rho, u64 AG, u64 AE, bool act, Sh &low)
+{
+    const u64 LOW63 = 0x7fffffffffffffffull, TOP = 0x8000000000000000ull, nc = ~c;
+    Sh G, E;
+    G.o = nc & rho.o & LOW63; G.n = nc & rho.n & LOW63;
+    E.o = rho.o & LOW63; E.n = rho.n & LOW63;
+    if (W.p == 0) E.o = ((rho.o ^ nc) & LOW63) | TOP;
+    if (W.p == 2) E.n = ((rho.n ^ nc) & LOW63) | TOP;
+#pragma unroll
+    for (int k = 0; k < 6; k++) {
+        const int s = 1 << k;
+        const u64 sm = k == 0 ? 0x5555555555555555ull : k == 1 ? 0x1111111111111111ull
+                     : k == 2 ? 0x0101010101010101ull : k == 3 ? 0x0001000100010001ull
+                     : k == 4 ? 0x0000000100000001ull : 0x1ull;
+        Sh Eh, Gh;
+        Eh.o = E.o >> s; Eh.n = E.n >> s; Gh.o = G.o >> s; Gh.n = G.n >> s;
+        const u64 zg = (and3(Eh, G) ^ (AG >> (s - 1))) & sm;
+        if (k == 5) low = Sh{ G.o & 1, G.n & 1 };
+        if (k < 5) {
+            const u64 ze = (and3(Eh, E) ^ (AE >> (s - 1))) & sm;
+            u64 snd[2] = { zg, ze }, rcv[2];
+            W.template reshare<2>(snd, rcv, act ? 2u * (32u >> k) : 0u);
+            G.o = (Gh.o & sm) ^ zg; G.n = (Gh.n & sm) ^ rcv[0];
+            E.o = ze; E.n = rcv[1];
+        } else {
+            const u64 r = W.reshare1(zg, act ? 1u : 0u);
+            G.o = (Gh.o & sm) ^ zg; G.n = (Gh.n & sm) ^ r;
+        }
+    }
+    return G;
+}
+// [c < r] of 32-bit words
+__device__ __forceinline__ Sh less32(FWire &W, u32 c, u32 ro, u32 rn, u32 AG, u32 AE, bool act)
+{
+    const u32 nc = ~c;
+    u32 Go = nc & ro, Gn = nc & rn, Eo = ro, En = rn;
+    if (W.p == 0) Eo ^= nc;
+    if (W.p == 2) En ^= nc;
+#pragma unroll
+    for (int k = 0; k < 5; k++) {
+        const int s = 1 << k;
+        const u32 sm = k == 0 ? 0x55555555u : k == 1 ? 0x11111111u : k == 2 ? 0x01010101u : k == 3 ? 0x00010001u : 1u;
+        const u32 eo = Eo >> s, en = En >> s;
+        const u32 zg = (and3l(eo, en, Go, Gn) ^ (AG >> (s - 1))) & sm;
+        if (k < 4) {
+            const u32 ze = (and3l(eo, en, Eo, En) ^ (AE >> (s - 1))) & sm;
+            u32 snd[2] = { zg, ze }, rcv[2];
+            W.template reshare<2>(snd, rcv);
+            Go = ((Go >> s) & sm) ^ zg; Gn = ((Gn >> s) & sm) ^ rcv[0];
+            Eo = ze; En = rcv[1];
+        } else {
+            u32 snd[1] = { zg }, rcv[1];
+            W.template reshare<1>(snd, rcv);
+            Go = ((Go >> s) & sm) ^ zg; Gn = ((Gn >> s) & sm) ^ rcv[0];
+        }
+    }
+    W.nresh += act ? 61u : 0u;
+    return Sh{ Go, Gn };
+}
+
+// Completion.  Z: the parties' parts, [3][n] words, left at zero for the next product; bias: ncol words or none.
+enum { FIN_PARTS = 0, FIN_SCALE = 1 };            // parts in memory; z = row factor S[e / ncol] times x (experts' gates)
+struct FinArgs { KCommon c; u64 *Z; P6 bias, res, y, gate, S, x; u64 n; u32 ncol, f; int has_bias, has_res, has_gate; };
+template <int SRC, bool RELU>
+__global__ __launch_bounds__(64) void k_finish(FinArgs a)
+{
+    __shared__ uint4 s_msg[GT_LANES];
+    __shared__ u64 s_mat[GT_FIN_ROWS * GT_FIN_EL];
+    __shared__ u64 s_cnt[6];
+    FWire W; W.init(s_msg, s_cnt);
+    FinTile<RELU ? 4 : 3> T; T.keys = a.c.keys; T.mat = s_mat; T.f = a.f;
+    const int p = W.p;
+    const u32 f = a.f;
+    const bool narrow = a.n <= 0xffffffffu;
+    const u64 off = RELU ? 1ull << (f + 31) : 1ull << 62;
+    for (u64 tile = blockIdx.x; tile < (a.n + GT_FIN_EL - 1) / GT_FIN_EL; tile += gridDim.x) {
+        const u64 e0 = tile * GT_FIN_EL, e = e0 + W.t;
+        const bool act = e < a.n;
+        const u32 on = act ? 1u : 0u;
+        const u64 row = !act ? 0 : (narrow ? (u64)((u32)e / a.ncol) : e / a.ncol), col = act ? e - row * a.ncol : 0;
+        u64 z = 0;
+        if (act) {
+            if (SRC == FIN_PARTS) { z = a.Z[(u64)p * a.n + e]; if (W.real) a.Z[(u64)p * a.n + e] = 0; }
+            else z = prod3(ld(a.S, p, row), ld(a.x, p, e));
+            if (a.has_bias) z += own_of(a.bias, p)[col] << f;
+        }
+        T.deal(a.c.op, e0);
+        z += T.za(W, 0) + T.pair(W, 0).o;
+        const u64 c = W.open_both(z, 64u * on) + ((1ull << (f - 1)) + off);
+        const u32 bits = (u32)T.mat[9 * GT_FIN_EL + W.t];
+        const Sh rho = T.pair(W, 3), d = T.pair(W, 6), one = pub(p, 1);
+        Sh low, s = { 0, 0 };
+        if (RELU) {
+            const Sh all = less64(W, c << (32 - f), rho, T.zb(W, 1), T.zb(W, 2), act, low);
+            s.o = ((rho.o >> 63) ^ all.o) & 1; s.n = ((rho.n >> 63) ^ all.n) & 1;
+            const u64 ct = (c >> (f + 31)) & 1;
+            if (p == 0) s.o ^= ct;
+            if (p == 2) s.n ^= ct;
+        } else low = less32(W, (u32)(c << (32 - f)), (u32)rho.o, (u32)rho.n, (u32)T.zb(W, 1), (u32)T.zb(W, 2), act);
+        // the bits to arithmetic: one message
+        u32 fo[1] = { ((u32)low.o ^ (bits >> p)) & 1 }, fr[1];
+        u32 fn = ((u32)low.n ^ (bits >> W.pn)) & 1;
+        if (RELU) { fo[0] |= (((u32)s.o ^ (bits >> (3 + p))) & 1) << 1; fn |= (((u32)s.n ^ (bits >> (3 + W.pn))) & 1) << 1; }
+        W.template pass<1>(fo, fr, W.pv);
+        W.nopen += (RELU ? 2u : 1u) * on;
+        const u32 ff = fo[0] ^ fn ^ fr[0];
+        const Sh b = ff & 1 ? one - d : d;
+        Sh y = Sh{ 0, 0 } - T.pair(W, 10) - b + pub(p, (c >> f) - (off >> f));
+        if (!(c >> 63)) y = y + T.pair(W, 13);
+        if (RELU) {
+            const Sh d2 = T.pair(W, 16), sa = ff & 2 ? one - d2 : d2;
+            y = mult_sh(W, sa, y, T.za(W, 3), act);
+            if (a.has_gate && act && W.real) st(a.gate, p, e, sa);
+        }
+        if (act && W.real) {
+            if (a.has_res) y = y + ld(a.res, p, e);
+            st(a.y, p, e, y);
+        }
+        W.drain();
+    }
+    W.flush(a.c.wire);
+}
+
+// ---------------------------------------------------------------------------------
+// A matrix of shared words by component, element (row, k) at c[j][row * rs + k * ks].
+struct MatView { const u64 *c[3]; u64 rs, ks; };
+
+// Parts of the product of A (M x K) and B (N x K): one output per thread.
+struct MmArgs { MatView A, B; u64 *Z; u64 M, N, K; };
+__global__ __launch_bounds__(256) void k_mm(MmArgs a)
+{
+    const u64 n = a.M * a.N;
+    for (u64 e = (u64)blockIdx.x * blockDim.x + threadIdx.x; e < n; e += (u64)gridDim.x * blockDim.x) {
+        const u64 r = e / a.N, col = e % a.N;
+        u64 z[3] = { 0, 0, 0 };
+        for (u64 k = 0; k < a.K; k++) {
+            u64 x[3], w[3];
+#pragma unroll
+            for (int j = 0; j < 3; j++) { x[j] = a.A.c[j][r * a.A.rs + k * a.A.ks]; w[j] = a.B.c[j][col * a.B.rs + k * a.B.ks]; }
+#pragma unroll
+            for (int j = 0; j < 3; j++) { const int q = (j + 1) % 3; z[j] += x[j] * (w[j] + w[q]) + x[q] * w[j]; }
+        }
+#pragma unroll
+        for (int j = 0; j < 3; j++) a.Z[(u64)j * n + e] = z[j];
+    }
+}
+
+// components (own planes) of a rows x cols matrix into a padded one, rows from row0 on; padding stays at zero
+struct PutArgs { P6 src; u64 *dst; u64 plane, ld, row0, rows, cols; };
+__global__ __launch_bounds__(256) void k_put(PutArgs a)
+{
+    const u64 n = a.rows * a.cols;
+    for (u64 e = (u64)blockIdx.x * blockDim.x + threadIdx.x; e < n; e += (u64)gridDim.x * blockDim.x) {
+        const u64 r = e / a.cols, to = (a.row0 + r) * a.ld + (e - r * a.cols);
+#pragma unroll
+        for (int j = 0; j < 3; j++) a.dst[j * a.plane + to] = a.src.o[j][e];
+    }
+}
+
+// column sums of a shared matrix (local): a workgroup per 64 columns
+struct ColsumArgs { P6 x, out; u64 rows; u32 cols; };
+__global__ __launch_bounds__(256) void k_colsum(ColsumArgs a)
+{
+    __shared__ u64 s_sum[4][GT_LANES];
+    const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6, pl = blockIdx.y;
+    const u64 col = (u64)blockIdx.x * GT_LANES + lane;
+    const u64 *x = pl == 0 ? a.x.o[0] : (pl == 1 ? a.x.o[1] : a.x.o[2]);
+    u64 s = 0;
+    if (col < a.cols) for (u64 r = wave; r < a.rows; r += 4) s += x[r * a.cols + col];
+    s_sum[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && col < a.cols) {
+        s += s_sum[1][lane] + s_sum[2][lane] + s_sum[3][lane];
+        // component pl: party pl's own, its predecessor's next one
+        own_of(a.out, (int)pl)[col] = s;
+        nxt_of(a.out, pl == 0 ? 2 : (int)pl - 1)[col] = s;
+    }
+}
+
+// ---------------------------------------------------------------------------------
+// Mixture of experts: choice of the experts of a few tokens.
+// w[t * P + q] = [s_a >= s_b] of the q-th pair a < b (a beats b: ties go to the lower index)
+__device__ __forceinline__ void pair_of(u32 q, u32 E, u32 &a, u32 &b)
+{
+    a = 0;
+    while (q >= E - 1 - a) { q -= E - 1 - a; a++; }
+    b = a + 1 + q;
+}
+__device__ __forceinline__ u32 pair_at(u32 a, u32 b, u32 E) { return a * (2 * E - a - 1) / 2 + b - a - 1; }      // a < b
+struct MoeArgs { KCommon c; P6 s, w, o, S, Q, g, x, xe, hg, he; u64 rows; u32 E, k, d, ff, f; };
+__global__ __launch_bounds__(64) void k_moe_pairs(MoeArgs a)
+{
+    GT_EL_SHARED(2, PRF_ALONE)
+    const u32 P = a.E * (a.E - 1) / 2;
+    const u64 n = a.rows * P;
+    GT_FOR_EL(n) {
+        const u64 e0 = tile_ * GT_EL, e = e0 + W.t;
+        const bool act = W.t < GT_EL && e < n;
+        Sh v = { 0, 0 };
+        if (act) {
+            u32 x, y;
+            pair_of((u32)(e % P), a.E, x, y);
+            v = ld(a.s, p, e / P * a.E + x) - ld(a.s, p, e / P * a.E + y);
+        }
+        const u32 st2[2] = { 1, 2 }, w = (u32)(e0 & 7) + W.t;
+        T.deal(W, a.c.op, e0, st2, el_live(e0, n));
+        const Dealer D = T.dealer(W);
+        const Sh b = b2a(W, p, ge_bit_masks(W, p, v, D, T.zb(W, 0, w), T.zb(W, 1, w), act), D, act);
+        if (act && W.real) st(a.w, p, e, b);
+        W.drain();
+    }
+    W.flush(a.c.wire);
+}
+// o[(t * k + j) * E + a] = [rank of a = j], the rank: how many others beat it; and the same times 2^f behind the row's inputs
+__global__ __launch_bounds__(64) void k_moe_hot(MoeArgs a)
+{
+    GT_EL_SHARED(1, PRF_ALONE)
+    const u64 n = a.rows * a.k * a.E, P = a.E * (a.E - 1) / 2;
+    GT_FOR_EL(n) {
+        const u64 e0 = tile_ * GT_EL, e = e0 + W.t;
+        const bool act = W.t < GT_EL && e < n;
+        Sh v = { 0, 0 };
+        const u32 x = (u32)(e % a.E);
+        if (act) {
+            const u64 t = e / ((u64)a.E * a.k);
+            for (u32 y = 0; y < a.E; y++)
+                if (y < x) v = v + ld(a.w, p, t * P + pair_at(y, x, a.E));
+                else if (y > x) v = v + pub(p, 1) - ld(a.w, p, t * P + pair_at(x, y, a.E));
+            v = v - pub(p, e / a.E % a.k);
+        }
+        T.deal_mask(W, a.c.op, e0, 1, el_live(e0, n));
+        const Dealer D = T.dealer(W);
+        const Sh b = b2a(W, p, eq_bit_mask(W, p, v, D, T.zb(W, 0, (u32)(e0 & 7) + W.t), act), D, act);
+        if (act && W.real) {
+            st(a.o, p, e, b);
+            st(a.xe, p, e / a.E * ((u64)a.E * (a.d + 1)) + (u64)a.E * a.d + x, scale(b, 1ull << a.f));
+        }
+        W.drain();
+    }
+    W.flush(a.c.wire);
+}
+// S = sum_a o[a] s[a] (one reshare), Q = 1 + sum_a s[a]
+__global__ __launch_bounds__(64) void k_moe_pick(MoeArgs a)
+{
+    GT_EL_SHARED(1, PRF_ALONE)
+    const u64 n = a.rows * a.k;
+    GT_FOR_EL(n) {
+        const u64 e0 = tile_ * GT_EL, e = e0 + W.t;
+        const bool act = W.t < GT_EL && e < n;
+        Sh q = pub(p, 1), z;
+        u64 s = 0;
+        if (act)
+            for (u32 x = 0; x < a.E; x++) {
+                const Sh v = ld(a.s, p, e / a.k * a.E + x);
+                s += prod3(ld(a.o, p, e * a.E + x), v);
+                q = q + v;
+            }
+        T.deal_mask(W, a.c.op, e0, 0, 0);
+        z.o = s + T.za(W, 0, (u32)(e0 & 7) + W.t);
+        z.n = W.reshare1(z.o, act ? 64u : 0u);
+        if (act && W.real) { st(a.S, p, e, z); st(a.Q, p, e, q); }
+        W.drain();
+    }
+    W.flush(a.c.wire);
+}
+// xe[r][a * d + i] = o[r][a] x[r / k][i]
+__global__ __launch_bounds__(64) void k_moe_spread(MoeArgs a)
+{
+    GT_EL_SHARED(1, PRF_PAIR)
+    const u64 Ed = (u64)a.E * a.d, n = a.rows * a.k * Ed;
+    GT_FOR_EL(n) {
+        const u64 e0 = tile_ * GT_EL, e = e0 + W.t;
+        const bool act = W.t < GT_EL && e < n;
+        const u64 r = e / Ed, q = e - r * Ed;
+        u64 s = 0;
+        if (act) s = prod3(ld(a.o, p, r * a.E + q / a.d), ld(a.x, p, r / a.k * a.d + q % a.d));
+        T.deal_mask(W, a.c.op, e0, 0, 0);
+        Sh z;
+        z.o = s + T.za(W, 0, (u32)(e0 & 7) + W.t);
+        z.n = W.reshare1(z.o, act ? 64u : 0u);
+        if (act && W.real) st(a.xe, p, r * (Ed + a.E) + q, z);
+        W.drain();
+    }
+    W.flush(a.c.wire);
+}
+// he[t][a * ff + i] = sum_j o_j[a] hg_j[i]; behind them sum_j o_j[a] g_j
+__global__ __launch_bounds__(64) void k_moe_gather(MoeArgs a)
+{
+    GT_EL_SHARED(1, PRF_PAIR)
+    const u64 Ef = (u64)a.E * a.ff, len = Ef + a.E, n = a.rows * len;
+    GT_FOR_EL(n) {
+        const u64 e0 = tile_ * GT_EL, e = e0 + W.t;
+        const bool act = W.t < GT_EL && e < n;
+        const u64 t = e / len, q = e - t * len, x = q >= Ef ? q - Ef : q / a.ff;
+        u64 s = 0;
+        if (act)
+            for (u32 j = 0; j < a.k; j++) {
+                const u64 r = t * a.k + j;
+                s += prod3(ld(a.o, p, r * a.E + x), q >= Ef ? ld(a.g, p, r) : ld(a.hg, p, r * a.ff + q % a.ff));
+            }
+        T.deal_mask(W, a.c.op, e0, 0, 0);
+        Sh z;
+        z.o = s + T.za(W, 0, (u32)(e0 & 7) + W.t);
+        z.n = W.reshare1(z.o, act ? 64u : 0u);
+        if (act && W.real) st(a.he, p, e, z);
+        W.drain();
+    }
+    W.flush(a.c.wire);
+}

@@ -1,0 +1,252 @@
+// Host side of the layers: argument checks, the operation schedule, message accounting, launches (part of gtree.hip).
+#pragma once
+
+// Words of a weight matrix by component, rows padded to a multiple of 64, columns to one of 16, zero there.
+struct WMat {
+    u64 *base = nullptr;
+    u64 K = 0, N = 0, Kp = 0, Np = 0;
+    u64 plane() const { return Kp * Np; }
+};
+static int wmat_alloc(WMat &w, u64 K, u64 N, hipStream_t st)
+{
+    w.K = K; w.N = N; w.Kp = (K + 63) & ~(u64)63; w.Np = (N + 15) & ~(u64)15;
+    if (hipMalloc(&w.base, 3 * w.plane() * 8) != hipSuccess) { w.base = nullptr; return GT_ENOMEM; }
+    HIPCHK(hipMemsetAsync(w.base, 0, 3 * w.plane() * 8, st));
+    return GT_OK;
+}
+static int wmat_put(gt_ctx *c, const WMat &w, const gt_shares *src, u64 row0, u64 rows)
+{
+    PutArgs a{};
+    a.src = to_p6(src); a.dst = w.base; a.plane = w.plane(); a.ld = w.Np; a.row0 = row0; a.rows = rows; a.cols = w.N;
+    return launch(c, GT_KC_LOCAL, k_put, g1(rows * w.N), B256, a);
+}
+// rows: the matrix's columns (outputs), k: its rows
+static MatView wmat_t(const WMat &w) { MatView v; for (int j = 0; j < 3; j++) v.c[j] = w.base + j * w.plane(); v.rs = 1; v.ks = w.Np; return v; }
+static MatView wmat(const WMat &w) { MatView v; for (int j = 0; j < 3; j++) v.c[j] = w.base + j * w.plane(); v.rs = w.Np; v.ks = 1; return v; }
+static MatView view(P6 a, u64 rs, u64 ks) { MatView v; for (int j = 0; j < 3; j++) v.c[j] = a.o[j]; v.rs = rs; v.ks = ks; return v; }
+
+struct gt_dense { u32 din, dout; bool has_b; WMat W; DSh b; };
+struct gt_moe {
+    u32 d, ff, E, k, max_rows;
+    bool has_br;
+    WMat Wr, W1, W2;             // biases of the experts' layers as further rows
+    DSh br, s, w, o, S, Q, g, xe, h, hg, he;
+};
+
+static void acct_finish(gt_ctx *c, u64 n, bool relu)
+{
+    wire_add(c, +1, n, 64); wire_add(c, -1, n, 64);
+    for (int k = 0; k < (relu ? 5 : 4); k++) wire_add(c, -1, n, 2 * ((relu ? 32u : 16u) >> k));
+    wire_add(c, -1, n, 1);
+    wire_add(c, +1, n, relu ? 2 : 1);
+    if (relu) wire_add(c, -1, n, 64);
+    c->acc.rounds += relu ? 9 : 7;
+}
+
+struct FinOut { P6 y{}, gate{}, res{}, bias{}; bool has_res = false, has_gate = false, has_bias = false; };
+static dim3 gF(u64 n) { return dim3((unsigned)std::min<u64>((n + GT_FIN_EL - 1) / GT_FIN_EL, 1u << 16)); }
+static int do_finish(gt_ctx *c, int src, bool relu, u64 n, u32 ncol, const FinOut &o, P6 S = {}, P6 x = {})
+{
+    FinArgs a{};
+    a.c = kc(c, c->op++); a.Z = c->dacc; a.n = n; a.ncol = ncol; a.f = c->tau; a.S = S; a.x = x;
+    a.y = o.y; a.gate = o.gate; a.res = o.res; a.bias = o.bias; a.has_res = o.has_res; a.has_gate = o.has_gate; a.has_bias = o.has_bias;
+    if (n) GTCHK(src == FIN_SCALE ? launch(c, GT_KC_FINISH, k_finish<FIN_SCALE, false>, gF(n), B64, a)
+                 : relu ? launch(c, GT_KC_FINISH, k_finish<FIN_PARTS, true>, gF(n), B64, a)
+                 : launch(c, GT_KC_FINISH, k_finish<FIN_PARTS, false>, gF(n), B64, a));
+    acct_finish(c, n, relu);
+    return GT_OK;
+}
+// completion of the product of A (M x K) and B (N x K)
+static int do_dense(gt_ctx *c, const MatView &A, const MatView &B, u64 M, u64 N, u64 K, bool relu, const FinOut &o)
+{
+    if (M && N) {
+        GTCHK(grow_dacc(c, 3 * M * N));
+        MmArgs a{}; a.A = A; a.B = B; a.Z = c->dacc; a.M = M; a.N = N; a.K = K;
+        GTCHK(launch(c, GT_KC_DENSE, k_mm, g1(M * N), B256, a));
+    }
+    return do_finish(c, FIN_PARTS, relu, M * N, (u32)N, o);
+}
+
+static bool dim_ok(u64 n) { return n >= 1 && n <= GT_MAX_DIM; }
+static void dense_free(gt_dense *l)
+{
+    if (l->W.base) (void)hipFree(l->W.base);
+    dsh_free(l->b);
+    delete l;
+}
+extern "C" int gt_dense_set(gt_ctx *c, gt_dense *l, const gt_shares *W, const gt_shares *b)
+{
+    if (!c || !l || !shares_ok(W, (size_t)l->din * l->dout) || l->has_b != (b != nullptr) || (b && !shares_ok(b, l->dout))) return GT_EINVAL;
+    Timed T(c);
+    int rc = wmat_put(c, l->W, W, 0, l->din);
+    if (rc == GT_OK && b) rc = copy6(c, l->b.v, 0, to_p6(b), 0, l->dout);
+    return T.finish(rc);
+}
+extern "C" int gt_dense_create(gt_ctx *c, const gt_shares *W, const gt_shares *b, uint32_t din, uint32_t dout, gt_dense **out)
+{
+    if (!c || !out || !dim_ok(din) || !dim_ok(dout) || !shares_ok(W, (size_t)din * dout) || (b && !shares_ok(b, dout))) return GT_EINVAL;
+    gt_dense *l = new (std::nothrow) gt_dense();
+    if (!l) return GT_ENOMEM;
+    l->din = din; l->dout = dout; l->has_b = b != nullptr;
+    int rc = wmat_alloc(l->W, din, dout, c->stream);
+    if (rc == GT_OK && b) rc = dsh_alloc(l->b, dout, c->stream);
+    if (rc == GT_OK) rc = gt_dense_set(c, l, W, b);
+    if (rc != GT_OK) { dense_free(l); return rc; }
+    *out = l;
+    return GT_OK;
+}
+extern "C" int gt_dense_destroy(gt_dense *l)
+{
+    if (!l) return GT_EINVAL;
+    dense_free(l);
+    return GT_OK;
+}
+
+extern "C" int gt_dense_forward(gt_ctx *c, const gt_dense *l, const gt_shares *x, size_t rows, int act, const gt_shares *res, const gt_shares *y,
+                                const gt_shares *gate)
+{
+    if (!c || !l || rows > GT_MAX_DIM || (act != GT_ACT_NONE && act != GT_ACT_RELU)) return GT_EINVAL;
+    const size_t n = rows * l->dout;
+    if (!shares_ok(x, rows * l->din) || !shares_ok(y, n) || (res && !shares_ok(res, n)) || (gate && (act != GT_ACT_RELU || !shares_ok(gate, n)))) return GT_EINVAL;
+    Timed T(c);
+    FinOut o;
+    o.y = to_p6(y);
+    if (res) { o.has_res = true; o.res = to_p6(res); }
+    if (gate) { o.has_gate = true; o.gate = to_p6(gate); }
+    if (l->has_b) { o.has_bias = true; o.bias = l->b.v; }
+    return T.finish(do_dense(c, view(to_p6(x), l->din, 1), wmat_t(l->W), rows, l->dout, l->din, act == GT_ACT_RELU, o));
+}
+
+static int ws_grow(gt_ctx *c, DSh &w, size_t n)
+{
+    if (w.base && w.n >= n) return GT_OK;
+    (void)hipStreamSynchronize(c->stream);
+    dsh_free(w);
+    return dsh_alloc(w, n, c->stream);
+}
+extern "C" int gt_dense_backward(gt_ctx *c, const gt_dense *l, const gt_shares *x, const gt_shares *gate, const gt_shares *dy, size_t rows,
+                                 const gt_shares *dx, const gt_shares *dW, const gt_shares *db)
+{
+    if (!c || !l || rows > GT_MAX_DIM) return GT_EINVAL;
+    const size_t n = rows * l->dout, nx = rows * l->din, nw = (size_t)l->din * l->dout;
+    if (!shares_ok(dy, n) || (gate && !shares_ok(gate, n)) || (dW && !shares_ok(x, nx)) || (dx && !shares_ok(dx, nx)) || (dW && !shares_ok(dW, nw)) ||
+        (db && !shares_ok(db, l->dout))) return GT_EINVAL;
+    Timed T(c);
+    P6 dz = to_p6(dy);
+    if (gate) {
+        int rc = ws_grow(c, c->ws_dz, n);
+        if (rc != GT_OK) return rc;
+        dz = c->ws_dz.v;
+        MultArgs m{}; m.x = once(to_p6(gate)); m.y = once(to_p6(dy)); m.z = dz; m.n = n;
+        m.c = kc(c, c->op++);
+        if (n) GTCHK(launch(c, GT_KC_MULT, k_mult, dim3(tiles8(n)), GT_BLOCK, m));
+        acct_reshare(c, n, 1);
+    }
+    if (dx) {
+        FinOut o;
+        o.y = to_p6(dx);
+        GTCHK(do_dense(c, view(dz, l->dout, 1), wmat(l->W), rows, l->din, l->dout, false, o));
+    }
+    if (dW) {
+        FinOut o;
+        o.y = to_p6(dW);
+        GTCHK(do_dense(c, view(to_p6(x), 1, l->din), view(dz, 1, l->dout), l->din, l->dout, rows, false, o));
+    }
+    if (db) {
+        ColsumArgs a{}; a.x = dz; a.out = to_p6(db); a.rows = rows; a.cols = l->dout;
+        GTCHK(launch(c, GT_KC_LOCAL, k_colsum, dim3((l->dout + GT_LANES - 1) / GT_LANES, 3), B256, a));
+    }
+    return T.finish(GT_OK);
+}
+
+static void moe_free(gt_moe *m)
+{
+    for (WMat *w : { &m->Wr, &m->W1, &m->W2 }) if (w->base) (void)hipFree(w->base);
+    DSh *all[] = { &m->br, &m->s, &m->w, &m->o, &m->S, &m->Q, &m->g, &m->xe, &m->h, &m->hg, &m->he };
+    for (DSh *s : all) dsh_free(*s);
+    delete m;
+}
+static int moe_init(gt_ctx *c, gt_moe *m, const gt_shares *Wr, const gt_shares *br, const gt_shares *W1, const gt_shares *b1, const gt_shares *W2,
+                    const gt_shares *b2)
+{
+    const u64 E = m->E, d = m->d, ff = m->ff, rows = m->max_rows, rk = rows * m->k, P = E * (E - 1) / 2;
+    GTCHK(wmat_alloc(m->Wr, d, E, c->stream));
+    GTCHK(wmat_alloc(m->W1, E * (d + 1), ff, c->stream));
+    GTCHK(wmat_alloc(m->W2, E * (ff + 1), d, c->stream));
+    GTCHK(wmat_put(c, m->Wr, Wr, 0, d));
+    GTCHK(wmat_put(c, m->W1, W1, 0, E * d));
+    GTCHK(wmat_put(c, m->W2, W2, 0, E * ff));
+    if (b1) GTCHK(wmat_put(c, m->W1, b1, E * d, E));
+    if (b2) GTCHK(wmat_put(c, m->W2, b2, E * ff, E));
+    if (br) { GTCHK(dsh_alloc(m->br, E, c->stream)); GTCHK(copy6(c, m->br.v, 0, to_p6(br), 0, E)); }
+    GTCHK(dsh_alloc(m->s, rows * E, c->stream)); GTCHK(dsh_alloc(m->w, rows * P, c->stream)); GTCHK(dsh_alloc(m->o, rk * E, c->stream));
+    for (DSh *s : { &m->S, &m->Q, &m->g }) GTCHK(dsh_alloc(*s, rk, c->stream));
+    GTCHK(dsh_alloc(m->xe, rk * E * (d + 1), c->stream));
+    GTCHK(dsh_alloc(m->h, rk * ff, c->stream)); GTCHK(dsh_alloc(m->hg, rk * ff, c->stream));
+    return dsh_alloc(m->he, rows * E * (ff + 1), c->stream);
+}
+extern "C" int gt_moe_create(gt_ctx *c, const gt_shares *Wr, const gt_shares *br, const gt_shares *W1, const gt_shares *b1, const gt_shares *W2,
+                             const gt_shares *b2, uint32_t d, uint32_t ff, uint32_t experts, uint32_t top, uint32_t max_rows, gt_moe **out)
+{
+    const size_t E = experts, w = (size_t)d * ff;
+    if (!c || !out || !dim_ok(d) || !dim_ok(ff) || !dim_ok(max_rows) || E < 1 || E > GT_MAX_EXPERTS || top < 1 || top > E) return GT_EINVAL;
+    if (!shares_ok(Wr, E * d) || (br && !shares_ok(br, E)) || !shares_ok(W1, E * w) || (b1 && !shares_ok(b1, E * ff)) || !shares_ok(W2, E * w) ||
+        (b2 && !shares_ok(b2, E * d))) return GT_EINVAL;
+    gt_moe *m = new (std::nothrow) gt_moe();
+    if (!m) return GT_ENOMEM;
+    m->d = d; m->ff = ff; m->E = experts; m->k = top; m->max_rows = max_rows; m->has_br = br != nullptr;
+    const int rc = moe_init(c, m, Wr, br, W1, b1, W2, b2);
+    if (rc != GT_OK) { (void)hipStreamSynchronize(c->stream); moe_free(m); return rc; }
+    *out = m;
+    return GT_OK;
+}
+extern "C" int gt_moe_destroy(gt_moe *m)
+{
+    if (!m) return GT_EINVAL;
+    moe_free(m);
+    return GT_OK;
+}
+
+extern "C" int gt_moe_forward(gt_ctx *c, gt_moe *m, const gt_shares *x, size_t rows, const gt_shares *res, const gt_shares *y)
+{
+    if (!c || !m || rows > m->max_rows) return GT_EINVAL;
+    const u64 E = m->E, d = m->d, ff = m->ff, rk = rows * m->k, P = E * (E - 1) / 2;
+    if (!shares_ok(x, rows * d) || !shares_ok(y, rows * d) || (res && !shares_ok(res, rows * d))) return GT_EINVAL;
+    Timed T(c);
+    MoeArgs a{};
+    a.s = m->s.v; a.w = m->w.v; a.o = m->o.v; a.S = m->S.v; a.Q = m->Q.v; a.g = m->g.v; a.x = to_p6(x); a.xe = m->xe.v; a.hg = m->hg.v; a.he = m->he.v;
+    a.rows = rows; a.E = (u32)E; a.k = m->k; a.d = m->d; a.ff = m->ff; a.f = c->tau;
+    FinOut o;
+    o.y = m->s.v;
+    if (m->has_br) { o.has_bias = true; o.bias = m->br.v; }
+    GTCHK(do_dense(c, view(a.x, d, 1), wmat_t(m->Wr), rows, E, d, true, o));
+    a.c = kc(c, c->op++);
+    if (rows * P) GTCHK(launch(c, GT_KC_SMALL, k_moe_pairs, gE(rows * P), B64, a));
+    acct_ge(c, rows * P); acct_b2a(c, rows * P);
+    a.c = kc(c, c->op++);
+    if (rk) GTCHK(launch(c, GT_KC_SMALL, k_moe_hot, gE(rk * E), B64, a));
+    acct_eq(c, rk * E); acct_b2a(c, rk * E);
+    a.c = kc(c, c->op++);
+    if (rk) GTCHK(launch(c, GT_KC_SMALL, k_moe_pick, gE(rk), B64, a));
+    acct_reshare(c, rk, 1);
+    DivArgs q{}; q.c = kc(c, c->op); q.S = m->S.v; q.Q = m->Q.v; q.quo = m->g.v; q.n = rk; q.nsteps = c->tau + 1;
+    c->op += c->tau + 1;
+    if (rk) GTCHK(few_elements(c, rk) ? launch(c, GT_KC_SMALL, k_div<4>, gE(rk), dim3(4 * GT_LANES), q) : launch(c, GT_KC_SMALL, k_div<1>, gE(rk), B64, q));
+    acct_div(c, rk);
+    a.c = kc(c, c->op++);
+    if (rk) GTCHK(launch(c, GT_KC_MULT, k_moe_spread, gE(rk * E * d), B64, a));
+    acct_reshare(c, rk * E * d, 1);
+    FinOut oh;
+    oh.y = m->h.v;
+    GTCHK(do_dense(c, view(m->xe.v, E * (d + 1), 1), wmat_t(m->W1), rk, ff, E * (d + 1), true, oh));
+    FinOut og;
+    og.y = m->hg.v;
+    GTCHK(do_finish(c, FIN_SCALE, false, rk * ff, m->ff, og, m->g.v, m->h.v));
+    a.c = kc(c, c->op++);
+    if (rk) GTCHK(launch(c, GT_KC_MULT, k_moe_gather, gE(rows * E * (ff + 1)), B64, a));
+    acct_reshare(c, rows * E * (ff + 1), 1);
+    FinOut oy;
+    oy.y = to_p6(y);
+    if (res) { oy.has_res = true; oy.res = to_p6(res); }
+    return T.finish(do_dense(c, view(m->he.v, E * (ff + 1), 1), wmat_t(m->W2), rows, d, E * (ff + 1), false, oy));
+}

@@ -5,6 +5,7 @@
 #include "gt_kernels.hpp"
 #include "gt_infer.hpp"
 #include "gt_partmm.hpp"
+#include "gt_layers.hpp"
 #include <algorithm>
 #include <cstdio>
 #include <cstring>
@@ -51,6 +52,7 @@ struct gt_ctx {
     std::vector<int> ev_cls;
     gt_prof prof;
     DSh ws[5];                // inference workspace, grown on demand, kept between calls
+    DSh ws_dz;                // a layer's gradient behind its activation, likewise
     u64 *dacc;                // partial inner products of split equality grids
     size_t dacc_words;
     u64 *scratch_d;           // this device's copy of the static scratch array
@@ -299,6 +301,7 @@ extern "C" int gt_ctx_destroy(gt_ctx *c)
     (void)hipStreamSynchronize(c->stream);
     for (hipEvent_t e : c->ev_pool) (void)hipEventDestroy(e);
     for (DSh &w : c->ws) dsh_free(w);
+    dsh_free(c->ws_dz);
     if (c->dacc) (void)hipFree(c->dacc);
     (void)hipFree(c->wire_d);
     (void)hipFree(c->keys_d);
@@ -1300,3 +1303,5 @@ extern "C" int gt_infer_forest(gt_ctx *c, const gt_forest *f, const gt_shares *I
     Timed T(c);
     return T.finish(infer_one_launch(c, f->feat.v, f->has_thr ? f->thr.v : f->feat.v, f->leaf.v, f->has_thr, f->H, f->ntrees, I, NI, d, R));
 }
+
+#include "gt_layers_host.hpp"

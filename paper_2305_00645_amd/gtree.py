@@ -40,11 +40,12 @@ class _Stats(C.Structure):
 GT_FLAG_PROFILE = 1
 GT_FLAG_LEVELWISE_INFER = 2
 GT_FLAG_INFER_TILE = {16: 0x100, 32: 0x200, 64: 0x300}
-KC_NAMES = ("share", "mult", "eqgrid", "count", "small", "local", "eqgrid_rows", "eqgrid_store", "infer", "partmm")
+KC_NAMES = ("share", "mult", "eqgrid", "count", "small", "local", "eqgrid_rows", "eqgrid_store", "infer", "partmm", "dense",
+            "finish")
 
 
 class _Prof(C.Structure):
-    _fields_ = [("ms", C.c_double * 10), ("launches", C.c_uint64 * 10)]
+    _fields_ = [("ms", C.c_double * len(KC_NAMES)), ("launches", C.c_uint64 * len(KC_NAMES))]
 
 
 class _Params(C.Structure):
@@ -107,6 +108,14 @@ def load():
         "gt_forest_create": (i, [vp, C.POINTER(vp), sz, C.POINTER(vp)]),
         "gt_forest_destroy": (i, [vp]),
         "gt_infer_forest": (i, [vp, vp, S, sz, u32, S]),
+        "gt_dense_create": (i, [vp, S, S, u32, u32, C.POINTER(vp)]),
+        "gt_dense_set": (i, [vp, vp, S, S]),
+        "gt_dense_destroy": (i, [vp]),
+        "gt_dense_forward": (i, [vp, vp, S, sz, i, S, S, S]),
+        "gt_dense_backward": (i, [vp, vp, S, S, S, sz, S, S, S]),
+        "gt_moe_create": (i, [vp, S, S, S, S, S, S, u32, u32, u32, u32, u32, C.POINTER(vp)]),
+        "gt_moe_destroy": (i, [vp]),
+        "gt_moe_forward": (i, [vp, vp, S, sz, S, S]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -363,6 +372,81 @@ class GTree:
         R = self._out(NI * forest.ntrees)
         _chk(self.L.gt_infer_forest(self.ctx, forest.h, _ref(I), NI, d, _ref(R)), "gt_infer_forest")
         return R
+
+    # -- layers (fixed point, tau fraction bits) ---------------------------
+    def fixed(self, real):
+        """Real tensor or array -> device int64 tensor round(real * 2^tau), for share_a."""
+        t = self.torch.as_tensor(real, dtype=self.torch.float64, device=self.device)
+        return self.torch.round(t * 2.0 ** self.tau).to(self.torch.int64)
+
+    def real(self, s):
+        """The real numbers that shares of fixed-point values stand for (float64, reconstructed)."""
+        return self.reconstruct_a(s).double() / 2.0 ** self.tau
+
+    def dense_create(self, W, din, dout, b=None):
+        h = C.c_void_p()
+        _chk(self.L.gt_dense_create(self.ctx, _ref(W), _ref(b), din, dout, C.byref(h)), "gt_dense_create")
+        return Dense(self, h, din, dout)
+
+    def dense_set(self, layer, W, b=None):
+        """New weights in place, as after a training step."""
+        _chk(self.L.gt_dense_set(self.ctx, layer.h, _ref(W), _ref(b)), "gt_dense_set")
+
+    def dense_forward(self, layer, x, rows, relu=False, residual=None, want_gate=False):
+        """y, or (y, gate) with want_gate (ReLU's bits, for dense_backward)."""
+        y = self._out(rows * layer.dout)
+        gate = self._out(rows * layer.dout) if want_gate else None
+        _chk(self.L.gt_dense_forward(self.ctx, layer.h, _ref(x), rows, int(bool(relu)), _ref(residual), _ref(y), _ref(gate)), "gt_dense_forward")
+        return (y, gate) if want_gate else y
+
+    def dense_backward(self, layer, x, dy, rows, gate=None, want=(True, True, True)):
+        """(dx, dW, db); want: which of them to compute, None in the place of the others."""
+        out = [self._out(n) if w else None for n, w in zip((rows * layer.din, layer.din * layer.dout, layer.dout), want)]
+        _chk(self.L.gt_dense_backward(self.ctx, layer.h, _ref(x), _ref(gate), _ref(dy), rows, *[_ref(t) for t in out]), "gt_dense_backward")
+        return tuple(out)
+
+    def moe_create(self, Wr, W1, W2, d, ff, experts, top, max_rows, br=None, b1=None, b2=None):
+        h = C.c_void_p()
+        _chk(self.L.gt_moe_create(self.ctx, _ref(Wr), _ref(br), _ref(W1), _ref(b1), _ref(W2), _ref(b2), d, ff, experts, top, max_rows,
+                                  C.byref(h)), "gt_moe_create")
+        return Moe(self, h, d)
+
+    def moe_forward(self, moe, x, rows, residual=None):
+        y = self._out(rows * moe.d)
+        _chk(self.L.gt_moe_forward(self.ctx, moe.h, _ref(x), rows, _ref(residual), _ref(y)), "gt_moe_forward")
+        return y
+
+
+class Dense:
+    def __init__(self, g, h, din, dout):
+        self.g, self.h, self.din, self.dout = g, h, din, dout
+
+    def close(self):
+        if self.h:
+            self.g.L.gt_dense_destroy(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Moe:
+    def __init__(self, g, h, d):
+        self.g, self.h, self.d = g, h, d
+
+    def close(self):
+        if self.h:
+            self.g.L.gt_moe_destroy(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 class Forest:
