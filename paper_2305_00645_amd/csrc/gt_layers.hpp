@@ -231,6 +231,149 @@ __global__ __launch_bounds__(256) void k_mm(MmArgs a)
     }
 }
 
+// Parts of the product of a few rows with a weight matrix, on the matrix cores in signed 8-bit limbs (36 products of
+// limbs per ring product, as in k_count).  A wavefront owns 16 columns, a workgroup 64 and `per` steps of 64 terms of the long axis;
+// the splits' parts meet by atomic adds of 64-bit words (exact, order-free).  z_p = (x_p + x_{p+1}) w_p + x_p w_{p+1}: the sum is made of
+// the few rows' words, so each component of the weights is read once and meets both factors.  Up to 8 rows both factors share a 16-row tile:
+//   rows 0-7: x_j + x_{j+1} -> z_j     rows 8-15: x_{j-1} -> z_{j-1}      (times w_j)
+// so that a term costs 36 instructions a component and not 72.  The weights stay words in memory, 24 bytes each, and are
+// turned into limbs in registers (byte permutes; a quarter of the time in which they arrive): one copy serves both passes, KC: k contiguous (the
+// transposed product of the backward pass).
+// Bound: the rate at which the weights arrive.
+struct FewArgs { const u64 *x[3]; const u64 *w; u64 *Z; u64 plane, ldx, ldw, M, N, K; u32 per, nsplit; };
+template <int ROWS, bool KC>
+__global__ __launch_bounds__(256) void k_mm_few(FewArgs a)
+{
+    constexpr int SLOTS = ROWS == 8 ? 3 : 6;                         // tiles of the left factor: both factors in one, or three of each
+    __shared__ __align__(16) unsigned char s_a[2][SLOTS * 8 * 1024];  // [tile][limb][lane of the operand][16 bytes]
+    const u32 tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const u32 lr = lane & 15, kq = lane >> 4;
+    const u32 split = blockIdx.x % a.nsplit;
+    const u64 c0 = ((u64)(blockIdx.x / a.nsplit) * 4 + wave) * 16, r0 = (u64)blockIdx.y * ROWS;
+    const u32 nsteps = (u32)((a.K + 63) / 64), s0 = split * a.per, s1 = s0 + a.per < nsteps ? s0 + a.per : nsteps;
+    const bool cols = c0 < a.N;                                      // whole wavefront; it takes part in the barriers
+    const u32 nrow = a.M - r0 < (u64)ROWS ? (u32)(a.M - r0) : ROWS;
+    // units of 8 terms of a tile's row: 3 x 16 x 8 or 6 x 16 x 8
+    constexpr int UNITS = SLOTS * 128, PASSES = (UNITS + 255) / 256;
+    u64 xw[PASSES][8];
+    auto fetch = [&](u32 s) {
+#pragma unroll
+        for (int q = 0; q < PASSES; q++) {
+            const u32 u = tid + q * 256, slot = u >> 7, row = (u >> 3) & 15, g = u & 7;
+            const bool sum = ROWS == 8 ? row < 8 : slot < 3;
+            const u32 j = ROWS == 8 ? (sum ? slot : (slot + 2) % 3) : slot % 3, r = ROWS == 8 ? row & 7 : row;
+            const u64 k0 = (u64)s * 64 + g * 8;
+            const u64 *x0 = j == 0 ? a.x[0] : (j == 1 ? a.x[1] : a.x[2]), *x1 = j == 0 ? a.x[1] : (j == 1 ? a.x[2] : a.x[0]);
+            const bool on = u < UNITS && r < nrow;
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                u64 v = 0;
+                if (on && k0 + i < a.K) {
+                    const u64 at = (r0 + r) * a.ldx + k0 + i;
+                    v = x0[at];
+                    if (sum) v += x1[at];
+                }
+                xw[q][i] = v;
+            }
+        }
+    };
+    auto put = [&](int buf) {
+#pragma unroll
+        for (int q = 0; q < PASSES; q++) {
+            const u32 u = tid + q * 256, slot = u >> 7, row = (u >> 3) & 15, g = u & 7;
+            if (u < UNITS) {
+                u64 y[8];
+#pragma unroll
+                for (int i = 0; i < 8; i++) y[i] = (xw[q][i] + GT_BIAS) ^ GT_BIAS;
+                transpose8x8(y);
+                unsigned char *to = s_a[buf] + slot * 8192 + (row + 16 * (g >> 1)) * 16 + (g & 1) * 8;
+#pragma unroll
+                for (int sl = 0; sl < 8; sl++) *(u64 *)(to + sl * 1024) = y[sl];
+            }
+        }
+    };
+    u64 raw[3][16];
+    const u64 *wl = KC ? a.w + (c0 + lr) * a.ldw + kq * 16 : a.w + (u64)kq * 16 * a.ldw + c0 + lr;
+    auto load = [&](int j, u32 s) {
+        const u64 *from = wl + (u64)j * a.plane + (KC ? (u64)s * 64 : (u64)s * 64 * a.ldw);
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) {
+            if (KC) { const ulonglong2 v = *(const ulonglong2 *)(from + i); raw[j][i] = v.x; raw[j][i + 1] = v.y; }
+            else { raw[j][i] = from[(u64)i * a.ldw]; raw[j][i + 1] = from[(u64)(i + 1) * a.ldw]; }
+        }
+    };
+    v4i acc[3][8];
+#pragma unroll
+    for (int j = 0; j < 3; j++)
+#pragma unroll
+        for (int u = 0; u < 8; u++) acc[j][u] = v4i{ 0, 0, 0, 0 };
+    if (cols)
+#pragma unroll
+        for (int j = 0; j < 3; j++) load(j, s0);
+    fetch(s0);
+    put(0);
+    __syncthreads();
+    for (u32 s = s0; s < s1; s++) {
+        const int buf = (s - s0) & 1;
+        if (s + 1 < s1) fetch(s + 1);
+        if (cols) {
+#pragma unroll
+            for (int j = 0; j < 3; j++) {
+                v4i B[8];
+                {
+                    u64 y[8], z[8];
+#pragma unroll
+                    for (int i = 0; i < 8; i++) { y[i] = (raw[j][i] + GT_BIAS) ^ GT_BIAS; z[i] = (raw[j][8 + i] + GT_BIAS) ^ GT_BIAS; }
+                    transpose8x8(y); transpose8x8(z);
+#pragma unroll
+                    for (int i = 0; i < 8; i++) B[i] = v4i{ (int)(u32)y[i], (int)(u32)(y[i] >> 32), (int)(u32)z[i], (int)(u32)(z[i] >> 32) };
+                }
+                if (s + 1 < s1) load(j, s + 1);
+#pragma unroll
+                for (int h = 0; h < (ROWS == 8 ? 1 : 2); h++) {
+                    // the sums' tile with w_j gives z_j; x_{j-1} with w_j gives z_{j-1}
+                    const int slot = h == 0 ? j : 3 + (j + 2) % 3, to = h == 0 ? j : (j + 2) % 3;
+                    const unsigned char *A0 = s_a[buf] + slot * 8192 + lane * 16;
+#pragma unroll
+                    for (int sl = 0; sl < 8; sl++) {
+                        const v4i A = *(const v4i *)(A0 + sl * 1024);
+#pragma unroll
+                        for (int t = 0; t < 8 - sl; t++) acc[to][sl + t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(A, B[t], acc[to][sl + t], 0, 0, 0);
+                    }
+                }
+            }
+        }
+        if (s + 1 < s1) put(buf ^ 1);
+        __syncthreads();
+    }
+    if (!cols) return;
+#pragma unroll
+    for (int v = 0; v < 4; v++) {
+        u64 z[3];
+#pragma unroll
+        for (int j = 0; j < 3; j++) {
+            z[j] = 0;
+#pragma unroll
+            for (int u = 0; u < 8; u++) z[j] += (u64)(long long)acc[j][u][v] << (8 * u);
+        }
+        if (ROWS == 8) {                                             // rows 8-15 of the next component's tile belong to this party
+            u64 o[3];
+#pragma unroll
+            for (int j = 0; j < 3; j++) o[j] = (u64)__shfl_xor((unsigned long long)z[j], 32, GT_LANES);
+#pragma unroll
+            for (int j = 0; j < 3; j++) z[j] += o[(j + 1) % 3];
+        }
+        const u32 row = 4 * kq + v;
+        const u64 c = c0 + lr;
+        if (row < nrow && c < a.N)
+#pragma unroll
+            for (int j = 0; j < 3; j++) {
+                u64 *to = &a.Z[((u64)j * a.M + r0 + row) * a.N + c];
+                if (a.nsplit > 1) atomicAdd((unsigned long long *)to, (unsigned long long)z[j]); else *to = z[j];
+            }
+    }
+}
+
 // components (own planes) of a rows x cols matrix into a padded one, rows from row0 on; padding stays at zero
 struct PutArgs { P6 src; u64 *dst; u64 plane, ld, row0, rows, cols; };
 __global__ __launch_bounds__(256) void k_put(PutArgs a)

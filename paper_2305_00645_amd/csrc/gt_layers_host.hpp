@@ -10,8 +10,9 @@ struct WMat {
 static int wmat_alloc(WMat &w, u64 K, u64 N, hipStream_t st)
 {
     w.K = K; w.N = N; w.Kp = (K + 63) & ~(u64)63; w.Np = (N + 15) & ~(u64)15;
-    if (hipMalloc(&w.base, 3 * w.plane() * 8) != hipSuccess) { w.base = nullptr; return GT_ENOMEM; }
-    HIPCHK(hipMemsetAsync(w.base, 0, 3 * w.plane() * 8, st));
+    const u64 words = 3 * w.plane() + 64;                  // a step of the transposed product reads up to 48 words past a row
+    if (hipMalloc(&w.base, words * 8) != hipSuccess) { w.base = nullptr; return GT_ENOMEM; }
+    HIPCHK(hipMemsetAsync(w.base, 0, words * 8, st));
     return GT_OK;
 }
 static int wmat_put(gt_ctx *c, const WMat &w, const gt_shares *src, u64 row0, u64 rows)
@@ -67,6 +68,23 @@ static int do_dense(gt_ctx *c, const MatView &A, const MatView &B, u64 M, u64 N,
     return do_finish(c, FIN_PARTS, relu, M * N, (u32)N, o);
 }
 
+// the same for few rows of x and weights: x (M rows of K words), W or, transposed, its rows as columns
+static int do_dense_w(gt_ctx *c, P6 x, u64 ldx, const WMat &W, bool transposed, u64 M, bool relu, const FinOut &o)
+{
+    const u64 N = transposed ? W.K : W.N, K = transposed ? W.N : W.K;
+    if (M == 0 || M > GT_FEW_ROWS) return do_dense(c, view(x, ldx, 1), transposed ? wmat(W) : wmat_t(W), M, N, K, relu, o);
+    GTCHK(grow_dacc(c, 3 * M * N));
+    FewArgs a{};
+    for (int j = 0; j < 3; j++) a.x[j] = x.o[j];
+    a.w = W.base; a.Z = c->dacc; a.plane = W.plane(); a.ldx = ldx; a.ldw = W.Np; a.M = M; a.N = N; a.K = K;
+    const FewShape s = few_shape(c->simds, M, N, K);
+    a.per = s.per; a.nsplit = s.nsplit;
+    const dim3 g((unsigned)(s.ngrp * s.nsplit), (unsigned)s.ntile);
+    GTCHK(s.rows == 8 ? (transposed ? launch(c, GT_KC_DENSE, k_mm_few<8, true>, g, B256, a) : launch(c, GT_KC_DENSE, k_mm_few<8, false>, g, B256, a))
+          : (transposed ? launch(c, GT_KC_DENSE, k_mm_few<16, true>, g, B256, a) : launch(c, GT_KC_DENSE, k_mm_few<16, false>, g, B256, a)));
+    return do_finish(c, FIN_PARTS, relu, M * N, (u32)N, o);
+}
+
 static bool dim_ok(u64 n) { return n >= 1 && n <= GT_MAX_DIM; }
 static void dense_free(gt_dense *l)
 {
@@ -114,7 +132,7 @@ extern "C" int gt_dense_forward(gt_ctx *c, const gt_dense *l, const gt_shares *x
     if (res) { o.has_res = true; o.res = to_p6(res); }
     if (gate) { o.has_gate = true; o.gate = to_p6(gate); }
     if (l->has_b) { o.has_bias = true; o.bias = l->b.v; }
-    return T.finish(do_dense(c, view(to_p6(x), l->din, 1), wmat_t(l->W), rows, l->dout, l->din, act == GT_ACT_RELU, o));
+    return T.finish(do_dense_w(c, to_p6(x), l->din, l->W, false, rows, act == GT_ACT_RELU, o));
 }
 
 static int ws_grow(gt_ctx *c, DSh &w, size_t n)
@@ -145,7 +163,7 @@ extern "C" int gt_dense_backward(gt_ctx *c, const gt_dense *l, const gt_shares *
     if (dx) {
         FinOut o;
         o.y = to_p6(dx);
-        GTCHK(do_dense(c, view(dz, l->dout, 1), wmat(l->W), rows, l->din, l->dout, false, o));
+        GTCHK(do_dense_w(c, dz, l->dout, l->W, true, rows, false, o));
     }
     if (dW) {
         FinOut o;
@@ -219,7 +237,7 @@ extern "C" int gt_moe_forward(gt_ctx *c, gt_moe *m, const gt_shares *x, size_t r
     FinOut o;
     o.y = m->s.v;
     if (m->has_br) { o.has_bias = true; o.bias = m->br.v; }
-    GTCHK(do_dense(c, view(a.x, d, 1), wmat_t(m->Wr), rows, E, d, true, o));
+    GTCHK(do_dense_w(c, a.x, d, m->Wr, false, rows, true, o));
     a.c = kc(c, c->op++);
     if (rows * P) GTCHK(launch(c, GT_KC_SMALL, k_moe_pairs, gE(rows * P), B64, a));
     acct_ge(c, rows * P); acct_b2a(c, rows * P);
@@ -238,7 +256,7 @@ extern "C" int gt_moe_forward(gt_ctx *c, gt_moe *m, const gt_shares *x, size_t r
     acct_reshare(c, rk * E * d, 1);
     FinOut oh;
     oh.y = m->h.v;
-    GTCHK(do_dense(c, view(m->xe.v, E * (d + 1), 1), wmat_t(m->W1), rk, ff, E * (d + 1), true, oh));
+    GTCHK(do_dense_w(c, m->xe.v, E * (d + 1), m->W1, false, rk, true, oh));
     FinOut og;
     og.y = m->hg.v;
     GTCHK(do_finish(c, FIN_SCALE, false, rk * ff, m->ff, og, m->g.v, m->h.v));
@@ -248,5 +266,5 @@ extern "C" int gt_moe_forward(gt_ctx *c, gt_moe *m, const gt_shares *x, size_t r
     FinOut oy;
     oy.y = to_p6(y);
     if (res) { oy.has_res = true; oy.res = to_p6(res); }
-    return T.finish(do_dense(c, view(m->he.v, E * (ff + 1), 1), wmat_t(m->W2), rows, d, E * (ff + 1), false, oy));
+    return T.finish(do_dense_w(c, m->he.v, E * (ff + 1), m->W2, false, rows, false, oy));
 }
