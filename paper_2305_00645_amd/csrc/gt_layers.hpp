@@ -144,30 +144,149 @@ __device__ __forceinline__ Sh less32(FWire &W, u32 c, u32 ro, u32 rn, u32 AG, u3
     return Sh{ Go, Gn };
 }
 
+// ---------------------------------------------------------------------------------
+// Residues.  Products of many rows run as products of small residues: words are taken as signed numbers, their products
+// added up exactly, |S| <= 2 * RNS_TERMS * 2^126, from 18 coprime moduli whose product M is 2^140.4 > 2 |S| / 0.74, and only then
+// reduced modulo 2^64.  A modulus costs one int8 product per term, so a ring product costs 18 of them where signed limbs cost 36.
+//   r_i = (sum of the products of residues, the right factor's times (M / m_i)^-1) mod m_i, balanced
+//   S = sum_i r_i M / m_i - q M,  q = round(sum_i r_i / m_i)
+// q is exact: |S / M| <= 0.367 and the fixed-point sum below is off by at most 18 * 128 / 2^15 = 0.071 < 0.5 - 0.367.
+#define RNS_N 18
+#define RNS_TERMS 4096                            // terms of the long axis in a product (two products of words each)
+struct RnsTable {
+    int m[RNS_N];                                 // moduli
+    float inv[RNS_N];
+    u32 left[RNS_N][2], right[RNS_N][2];          // balanced 256^s mod m_i, the right factor's times (M / m_i)^-1, four s a word
+    int c13[RNS_N];                               // 2^13 mod m_i, balanced
+    u32 join[8][5];                               // signed byte s of (M / m_i) mod 2^64, four i a word; byte 2 of the last one: of M
+    u32 quot[5];                                  // round(2^14 / m_i)
+};
+constexpr u32 rns_byte(int v, int at) { return ((u32)v & 0xffu) << (8 * at); }
+constexpr int rns_balanced(u64 v, int m) { const int r = (int)(v % (u64)m); return 2 * r > m - 1 + (m & 1) ? r - m : r; }
+constexpr RnsTable rns_make()
+{
+    const int m[RNS_N] = { 256, 255, 253, 251, 247, 241, 239, 233, 229, 227, 223, 217, 211, 199, 197, 193, 191, 181 };
+    RnsTable t{};
+    u64 all = 1;
+    for (int i = 0; i < RNS_N; i++) all *= (u64)m[i];
+    for (int i = 0; i < RNS_N; i++) {
+        t.m[i] = m[i]; t.inv[i] = 1.0f / (float)m[i];
+        u64 rest = 1, word = 1, inverse = 0;      // M / m_i modulo m_i and modulo 2^64
+        for (int j = 0; j < RNS_N; j++) if (j != i) { rest = rest * (u64)m[j] % (u64)m[i]; word *= (u64)m[j]; }
+        for (int v = 1; v < m[i]; v++) if (rest * (u64)v % (u64)m[i] == 1) inverse = (u64)v;
+        u64 power = 1;
+        for (int b = 0; b < 8; b++) {
+            t.left[i][b / 4] |= rns_byte(rns_balanced(power, m[i]), b % 4);
+            t.right[i][b / 4] |= rns_byte(rns_balanced(power * inverse, m[i]), b % 4);
+            power = power * 256 % (u64)m[i];
+        }
+        t.c13[i] = rns_balanced(8192, m[i]);
+        const u64 y = (word + GT_BIAS) ^ GT_BIAS;
+        for (int b = 0; b < 8; b++) t.join[b][i / 4] |= rns_byte((int)(y >> (8 * b)), i % 4);
+        t.quot[i / 4] |= rns_byte((16384 + m[i] / 2) / m[i], i % 4);
+    }
+    const u64 y = (all + GT_BIAS) ^ GT_BIAS;
+    for (int b = 0; b < 8; b++) t.join[b][4] |= rns_byte((int)(y >> (8 * b)), 2);
+    return t;
+}
+constexpr RnsTable RNS = rns_make();
+static __device__ const RnsTable d_rns = rns_make();             // for a modulus that is not known when the kernel is compiled
+#define RNS_MAGIC 0x4b400000u                     // 1.5 * 2^23: this plus an integer is the float 1.5 * 2^23 plus it
+
+// an integer t, |t| < 2^21.1, given as RNS_MAGIC + t, to the balanced residue: in the low byte
+__device__ __forceinline__ u32 rns_reduce(u32 tm, float m, float inv)
+{
+    const float magic = __uint_as_float(RNS_MAGIC), x = __uint_as_float(tm);
+    const float q = __builtin_fmaf(x - magic, inv, magic) - magic;
+    return __float_as_uint(__builtin_fmaf(-q, m, x));
+}
+__device__ __forceinline__ u32 low_bytes(u32 a, u32 b, u32 c, u32 d)
+{
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u), 0x05040100u);
+}
+// four bytes of four words to four words of a byte of each
+__device__ __forceinline__ void transpose4x4(u32 (&x)[4])
+{
+    const u32 a = __builtin_amdgcn_perm(x[1], x[0], 0x06020400u), b = __builtin_amdgcn_perm(x[1], x[0], 0x07030501u);
+    const u32 c = __builtin_amdgcn_perm(x[3], x[2], 0x06020400u), d = __builtin_amdgcn_perm(x[3], x[2], 0x07030501u);
+    x[0] = __builtin_amdgcn_perm(c, a, 0x05040100u); x[1] = __builtin_amdgcn_perm(d, b, 0x05040100u);
+    x[2] = __builtin_amdgcn_perm(c, a, 0x07060302u); x[3] = __builtin_amdgcn_perm(d, b, 0x07060302u);
+}
+// the word that 18 residues (bytes of five words, four a word, the last two bytes zero) stand for
+__device__ __forceinline__ u64 rns_join(const u32 (&r)[5])
+{
+    int qs = 1 << 13;
+#pragma unroll
+    for (int g = 0; g < 5; g++) qs = __builtin_amdgcn_sdot4((int)r[g], (int)RNS.quot[g], qs, false);
+    const u32 last = r[4] | (((u32)-(qs >> 14) & 0xffu) << 16);
+    int D[8];
+#pragma unroll
+    for (int b = 0; b < 8; b++) {
+        int d = __builtin_amdgcn_sdot4((int)last, (int)RNS.join[b][4], 0, false);
+#pragma unroll
+        for (int g = 0; g < 4; g++) d = __builtin_amdgcn_sdot4((int)r[g], (int)RNS.join[b][g], d, false);
+        D[b] = d;
+    }
+    return (u64)(long long)(D[0] + D[1] * 256) + ((u64)(long long)(D[2] + D[3] * 256) << 16) + ((u64)(u32)(D[4] + D[5] * 256) << 32) +
+           ((u64)(u32)(D[6] + D[7] * 256) << 48);
+}
+
 // Completion.  Z: the parties' parts, [3][n] words, left at zero for the next product; bias: ncol words or none.
-enum { FIN_PARTS = 0, FIN_SCALE = 1 };            // parts in memory; z = row factor S[e / ncol] times x (experts' gates)
-struct FinArgs { KCommon c; u64 *Z; P6 bias, res, y, gate, S, x; u64 n; u32 ncol, f; int has_bias, has_res, has_gate; };
+// FIN_RES: R: residues of the elements from `first` on, planes [chunk][party][modulus] of `plane` bytes, chunks added up; a workgroup takes
+// 128 elements at a time: a lane of a party turns the residues of eight adjacent ones into words and leaves them in LDS.
+enum { FIN_PARTS = 0, FIN_SCALE = 1, FIN_RES = 2 };   // parts in memory; z = row factor S[e / ncol] times x (experts' gates); residues
+struct FinArgs { KCommon c; u64 *Z; P6 bias, res, y, gate, S, x; u64 n; u32 ncol, f; int has_bias, has_res, has_gate; const unsigned char *R; u64 first, plane; u32 nchunk; };
 template <int SRC, bool RELU>
 __global__ __launch_bounds__(64) void k_finish(FinArgs a)
 {
     __shared__ uint4 s_msg[GT_LANES];
     __shared__ u64 s_mat[GT_FIN_ROWS * GT_FIN_EL];
     __shared__ u64 s_cnt[6];
+    __shared__ u64 s_z[SRC == FIN_RES ? 3 : 1][SRC == FIN_RES ? 8 * GT_FIN_EL + 8 : 1];
     FWire W; W.init(s_msg, s_cnt);
     FinTile<RELU ? 4 : 3> T; T.keys = a.c.keys; T.mat = s_mat; T.f = a.f;
     const int p = W.p;
     const u32 f = a.f;
-    const bool narrow = a.n <= 0xffffffffu;
+    const bool narrow = a.first + a.n <= 0xffffffffu;
     const u64 off = RELU ? 1ull << (f + 31) : 1ull << 62;
-    for (u64 tile = blockIdx.x; tile < (a.n + GT_FIN_EL - 1) / GT_FIN_EL; tile += gridDim.x) {
-        const u64 e0 = tile * GT_FIN_EL, e = e0 + W.t;
-        const bool act = e < a.n;
+    constexpr u32 PER = SRC == FIN_RES ? 8 : 1;                       // tiles at a time
+    const u64 tiles = (a.n + GT_FIN_EL - 1) / GT_FIN_EL;
+    for (u64 tile = (u64)blockIdx.x * PER, sub = 0; tile < tiles; sub++, tile += sub == PER ? (u64)(gridDim.x - 1) * PER + 1 : 1, sub = sub == PER ? 0 : sub) {
+        if (SRC == FIN_RES && sub == 0) {
+            u64 zw[8] = { 0, 0, 0, 0, 0, 0, 0, 0 };
+            for (u32 ch = 0; ch < a.nchunk; ch++) {
+                const unsigned char *R = a.R + (u64)(ch * 3 + p) * RNS_N * a.plane + tile * GT_FIN_EL + 8 * W.t;
+                u32 r[2][20];
+#pragma unroll
+                for (int i = 0; i < RNS_N; i++) { const uint2 v = *(const uint2 *)(R + (u64)i * a.plane); r[0][i] = v.x; r[1][i] = v.y; }
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    r[h][18] = 0; r[h][19] = 0;
+                    u32 q[5][4];
+#pragma unroll
+                    for (int g = 0; g < 5; g++) {
+#pragma unroll
+                        for (int i = 0; i < 4; i++) q[g][i] = r[h][4 * g + i];
+                        transpose4x4(q[g]);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; i++) { const u32 w[5] = { q[0][i], q[1][i], q[2][i], q[3][i], q[4][i] }; zw[4 * h + i] += rns_join(w); }
+                }
+            }
+            wave_sync();
+#pragma unroll
+            for (int i = 0; i < 8; i++) s_z[p][8 * W.t + i] = zw[i];
+            wave_sync();
+        }
+        const u64 e0 = a.first + tile * GT_FIN_EL, e = e0 + W.t;
+        const bool act = tile * GT_FIN_EL + W.t < a.n;
         const u32 on = act ? 1u : 0u;
         const u64 row = !act ? 0 : (narrow ? (u64)((u32)e / a.ncol) : e / a.ncol), col = act ? e - row * a.ncol : 0;
         u64 z = 0;
         if (act) {
             if (SRC == FIN_PARTS) { z = a.Z[(u64)p * a.n + e]; if (W.real) a.Z[(u64)p * a.n + e] = 0; }
-            else z = prod3(ld(a.S, p, row), ld(a.x, p, e));
+            else if (SRC == FIN_SCALE) z = prod3(ld(a.S, p, row), ld(a.x, p, e));
+            else z = s_z[p][sub * GT_FIN_EL + W.t];
             if (a.has_bias) z += own_of(a.bias, p)[col] << f;
         }
         T.deal(a.c.op, e0);
@@ -210,26 +329,6 @@ __global__ __launch_bounds__(64) void k_finish(FinArgs a)
 // ---------------------------------------------------------------------------------
 // A matrix of shared words by component, element (row, k) at c[j][row * rs + k * ks].
 struct MatView { const u64 *c[3]; u64 rs, ks; };
-
-// Parts of the product of A (M x K) and B (N x K): one output per thread.
-struct MmArgs { MatView A, B; u64 *Z; u64 M, N, K; };
-__global__ __launch_bounds__(256) void k_mm(MmArgs a)
-{
-    const u64 n = a.M * a.N;
-    for (u64 e = (u64)blockIdx.x * blockDim.x + threadIdx.x; e < n; e += (u64)gridDim.x * blockDim.x) {
-        const u64 r = e / a.N, col = e % a.N;
-        u64 z[3] = { 0, 0, 0 };
-        for (u64 k = 0; k < a.K; k++) {
-            u64 x[3], w[3];
-#pragma unroll
-            for (int j = 0; j < 3; j++) { x[j] = a.A.c[j][r * a.A.rs + k * a.A.ks]; w[j] = a.B.c[j][col * a.B.rs + k * a.B.ks]; }
-#pragma unroll
-            for (int j = 0; j < 3; j++) { const int q = (j + 1) % 3; z[j] += x[j] * (w[j] + w[q]) + x[q] * w[j]; }
-        }
-#pragma unroll
-        for (int j = 0; j < 3; j++) a.Z[(u64)j * n + e] = z[j];
-    }
-}
 
 // Parts of the product of a few rows with a weight matrix, on the matrix cores in signed 8-bit limbs (36 products of
 // limbs per ring product, as in k_count).  A wavefront owns 16 columns, a workgroup 64 and `per` steps of 64 terms of the long axis;
@@ -371,6 +470,158 @@ __global__ __launch_bounds__(256) void k_mm_few(FewArgs a)
                 u64 *to = &a.Z[((u64)j * a.M + r0 + row) * a.N + c];
                 if (a.nsplit > 1) atomicAdd((unsigned long long *)to, (unsigned long long)z[j]); else *to = z[j];
             }
+    }
+}
+
+// ---------------------------------------------------------------------------------
+// Residues of a matrix of words (rows x K) as operands of v_mfma_i32_32x32x32_i8: [matrix][modulus][32 terms][32 rows][64 lanes][16 bytes],
+// lane l of an operand holds row l % 32 and the 16 terms from 16 (l / 32) on.  Matrices: the sums of adjacent components (0-2) and the components
+// (3-5), or the components alone (0-2).  Rows and terms beyond the matrix are zero.  A residue: two four-byte dot products of the word's
+// signed bytes with the powers of 256, a rounded quotient in floating point.  RIGHT: times (M / m_i)^-1.
+// A wavefront makes an operand of 32 x 32 words, all moduli.
+struct ResArgs { MatView x; unsigned char *out; u64 rows, K, k0; u32 nrb, nkb; int sums; };
+template <bool RIGHT>
+__global__ __launch_bounds__(256) void k_residues(ResArgs a)
+{
+    const u32 lane = threadIdx.x & 63, lr = lane & 31, hi = lane >> 5;
+    const u64 nfr = (u64)a.nrb * a.nkb, mat = nfr * 1024;
+    const u64 fr = (u64)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (fr >= nfr) return;
+    // neighbours along the axis that is contiguous in memory
+    const u32 rb = (u32)(a.x.ks == 1 ? fr / a.nkb : fr % a.nrb), kb = (u32)(a.x.ks == 1 ? fr % a.nkb : fr / a.nrb);
+    const u64 row = (u64)rb * 32 + lr, k = (u64)kb * 32 + hi * 16;
+    u64 x[3][16];
+#pragma unroll
+    for (int j = 0; j < 3; j++)
+#pragma unroll
+        for (int i = 0; i < 16; i++) x[j][i] = row < a.rows && k + i < a.K ? a.x.c[j][row * a.x.rs + (a.k0 + k + i) * a.x.ks] : 0;
+    unsigned char *out = a.out + ((u64)kb * a.nrb + rb) * 1024 + lane * 16;
+#pragma unroll
+    for (int q = 0; q < 6; q++) {
+        if (q >= 3 && !a.sums) break;
+        u32 lo[16], hh[16];
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+            const u64 w = q >= 3 ? x[q - 3][i] : a.sums ? x[q][i] + x[(q + 1) % 3][i] : x[q][i];
+            const u64 y = (w + GT_BIAS) ^ GT_BIAS;
+            lo[i] = (u32)y; hh[i] = (u32)(y >> 32);
+        }
+#pragma unroll
+        for (int i = 0; i < RNS_N; i++) {
+            const int cl = (int)(RIGHT ? RNS.right[i][0] : RNS.left[i][0]), ch = (int)(RIGHT ? RNS.right[i][1] : RNS.left[i][1]);
+            u32 b[16];
+#pragma unroll
+            for (int e = 0; e < 16; e++)
+                b[e] = rns_reduce((u32)__builtin_amdgcn_sdot4((int)lo[e], cl, __builtin_amdgcn_sdot4((int)hh[e], ch, (int)RNS_MAGIC, false), false),
+                                  (float)RNS.m[i], RNS.inv[i]);
+            uint4 v;
+            v.x = low_bytes(b[0], b[1], b[2], b[3]); v.y = low_bytes(b[4], b[5], b[6], b[7]);
+            v.z = low_bytes(b[8], b[9], b[10], b[11]); v.w = low_bytes(b[12], b[13], b[14], b[15]);
+            *(uint4 *)(out + ((u64)q * RNS_N + i) * mat) = v;
+        }
+    }
+}
+
+// The products of residues: for every party and modulus the sum of two products, party p's
+//   (a_p + a_{p+1}) b_p + a_p b_{p+1}      or      a_p (b_p + b_{p+1}) + a_{p+1} b_p
+// (sums in the left or the right factor), reduced to balanced residues, [party][modulus] planes of bytes, row-major M x N.
+// A workgroup of 2 x 2 wavefronts owns 64 WM x 64 WN outputs, a wavefront 32 WM x 32 WN; a step of 64 terms of both operands goes through LDS (its loads are in
+// flight during the step before), where an operand lies as it is loaded: no bank conflicts.  The right factor takes the role of rows, so
+// that a lane holds four adjacent columns of a result.  Consecutive workgroups of an XCD take the tiles of one product.
+struct RmmArgs { const unsigned char *A, *B; unsigned char *R; u64 amat, bmat, plane; u32 M, N, narb, nbrb, nstep, ntm, ntn, total; int asums; };   // amat, bmat: bytes of a modulus's matrix; narb: blocks of 32 rows
+template <int WM, int WN>
+__global__ __launch_bounds__(256, WM == 4 ? 2 : 4) void k_rns_mm(RmmArgs a)
+{
+    constexpr int FA = 2 * WM, FB = 2 * WN, STEP = 2 * (FA + FB) * 1024;       // operands of 32 rows a workgroup, bytes of a step
+    constexpr int LD = 64 * WN + 16, OUT = 64 * WM * LD;
+    constexpr int LOADS = STEP / 4096;                                         // of 16 bytes a lane
+    __shared__ __align__(16) unsigned char s_buf[2 * STEP > OUT ? 2 * STEP : OUT];
+    const u32 tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave & 1, wn = wave >> 1;
+    // blocks go to the XCDs in turn: XCD x takes the x-th eighth of the work
+    const u32 per = (a.total + 7) / 8, id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    if ((blockIdx.x >> 3) >= per || id >= a.total) return;
+    const u32 tiles = a.ntm * a.ntn, batch = id / tiles, tile = id % tiles, p = batch / RNS_N, mi = batch % RNS_N;
+    // groups of 8 row tiles, column tiles one after the other
+    const u32 grp = tile / (8 * a.ntn), gm = a.ntm - grp * 8 < 8 ? a.ntm - grp * 8 : 8, in = tile - grp * 8 * a.ntn;
+    const u32 tm = grp * 8 + in % gm, tn = in / gm, pn = p == 2 ? 0 : p + 1;
+    const unsigned char *A0 = a.A + ((u64)p * RNS_N + mi) * a.amat, *A1 = a.A + ((u64)(a.asums ? 3 + p : pn) * RNS_N + mi) * a.amat;
+    const unsigned char *B0 = a.B + ((u64)p * RNS_N + mi) * a.bmat, *B1 = a.B + ((u64)(a.asums ? pn : 3 + p) * RNS_N + mi) * a.bmat;
+    const u32 half = a.nstep / 2;                                              // steps of a product
+    uint4 st[LOADS];
+    auto fetch = [&](u32 s) {
+        const u32 k = s >= half ? s - half : s;
+        const unsigned char *A = (s >= half ? A1 : A0) + ((u64)k * 2 * a.narb + tm * FA) * 1024, *B = (s >= half ? B1 : B0) + ((u64)k * 2 * a.nbrb + tn * FB) * 1024;
+#pragma unroll
+        for (int q = 0; q < LOADS; q++) {
+            const u32 o = q * 4 + wave;                                        // operand: [2 blocks of terms][FA] of A, then of B
+            const bool isA = o < 2 * FA;
+            const u32 w = isA ? o : o - 2 * FA, kb = isA ? w / FA : w / FB, r = isA ? w % FA : w % FB;
+            st[q] = *(const uint4 *)((isA ? A + ((u64)kb * a.narb + r) * 1024 : B + ((u64)kb * a.nbrb + r) * 1024) + lane * 16);
+        }
+    };
+    auto put = [&](u32 buf) {
+#pragma unroll
+        for (int q = 0; q < LOADS; q++) *(uint4 *)(s_buf + buf * STEP + (q * 4 + wave) * 1024 + lane * 16) = st[q];
+    };
+    v16i acc[WM][WN];
+#pragma unroll
+    for (int i = 0; i < WM; i++)
+#pragma unroll
+        for (int j = 0; j < WN; j++)
+#pragma unroll
+            for (int v = 0; v < 16; v++) acc[i][j][v] = 0;
+    fetch(0);
+    put(0);
+    __syncthreads();
+    for (u32 s = 0; s < a.nstep; s++) {
+        if (s + 1 < a.nstep) fetch(s + 1);
+        const unsigned char *buf = s_buf + (s & 1) * STEP + lane * 16;
+#pragma unroll
+        for (int kb = 0; kb < 2; kb++) {
+            v4i x[WM], w[WN];
+#pragma unroll
+            for (int i = 0; i < WM; i++) x[i] = *(const v4i *)(buf + (kb * FA + wm * WM + i) * 1024);
+#pragma unroll
+            for (int j = 0; j < WN; j++) w[j] = *(const v4i *)(buf + (2 * FA + kb * FB + wn * WN + j) * 1024);
+#pragma unroll
+            for (int i = 0; i < WM; i++)
+#pragma unroll
+                for (int j = 0; j < WN; j++) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[j], x[i], acc[i][j], 0, 0, 0);
+        }
+        if (s + 1 < a.nstep) put((s + 1) & 1);
+        __syncthreads();
+    }
+    // |sum| < 2^28: low 13 bits and the rest times 2^13 mod m, below 2^21.1, then the balanced residue; through LDS to rows
+    const float m = (float)d_rns.m[mi], inv = d_rns.inv[mi];
+    const int c13 = d_rns.c13[mi];
+#pragma unroll
+    for (int i = 0; i < WM; i++)
+#pragma unroll
+        for (int j = 0; j < WN; j++)
+#pragma unroll
+            for (int g = 0; g < 4; g++) {
+                u32 b[4];
+#pragma unroll
+                for (int v = 0; v < 4; v++) {
+                    const int z = acc[i][j][4 * g + v];
+                    b[v] = rns_reduce((u32)((z >> 13) * c13) + (((u32)z & 8191u) | RNS_MAGIC), m, inv);
+                }
+                *(u32 *)(s_buf + ((wm * WM + i) * 32 + (lane & 31)) * LD + (wn * WN + j) * 32 + 8 * g + 4 * (lane >> 5)) = low_bytes(b[0], b[1], b[2], b[3]);
+            }
+    __syncthreads();
+    unsigned char *R = a.R + (u64)batch * a.plane;
+    constexpr u32 SEG = 4 * WN;                                                // of 16 bytes a row
+    for (u32 u = tid; u < 64 * WM * SEG; u += 256) {
+        const u32 r = u / SEG, c = (u % SEG) * 16;
+        const u32 row = tm * 64 * WM + r, col = tn * 64 * WN + c;
+        if (row >= a.M || col >= a.N) continue;
+        const uint4 v = *(const uint4 *)(s_buf + r * LD + c);
+        unsigned char *to = R + (u64)row * a.N + col;
+        if (col + 16 <= a.N) __builtin_memcpy(to, &v, 16);
+        else {
+            const u32 w[4] = { v.x, v.y, v.z, v.w };
+            for (u32 i = 0; i < a.N - col; i++) to[i] = (unsigned char)(w[i >> 2] >> (8 * (i & 3)));
+        }
     }
 }
 

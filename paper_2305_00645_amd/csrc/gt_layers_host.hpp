@@ -57,17 +57,62 @@ static int do_finish(gt_ctx *c, int src, bool relu, u64 n, u32 ncol, const FinOu
     acct_finish(c, n, relu);
     return GT_OK;
 }
-// completion of the product of A (M x K) and B (N x K)
-static int do_dense(gt_ctx *c, const MatView &A, const MatView &B, u64 M, u64 N, u64 K, bool relu, const FinOut &o)
+// The context's workspace of residues.
+static int grow_res(gt_ctx *c, size_t need)
 {
-    if (M && N) {
-        GTCHK(grow_dacc(c, 3 * M * N));
-        MmArgs a{}; a.A = A; a.B = B; a.Z = c->dacc; a.M = M; a.N = N; a.K = K;
-        GTCHK(launch(c, GT_KC_DENSE, k_mm, g1(M * N), B256, a));
-    }
-    return do_finish(c, FIN_PARTS, relu, M * N, (u32)N, o);
+    if (c->res_bytes >= need) return GT_OK;
+    (void)hipStreamSynchronize(c->stream);
+    if (c->res) (void)hipFree(c->res);
+    c->res = nullptr; c->res_bytes = 0;
+    if (hipMalloc(&c->res, need) != hipSuccess) { c->res = nullptr; return GT_ENOMEM; }
+    c->res_bytes = need;
+    return GT_OK;
 }
-
+template <bool RIGHT>
+static int residues(gt_ctx *c, const MatView &x, unsigned char *out, u64 rows, u64 K, u64 k0, u32 nrb, u32 nkb, bool sums)
+{
+    ResArgs a{};
+    a.x = x; a.out = out; a.rows = rows; a.K = K; a.k0 = k0; a.nrb = nrb; a.nkb = nkb; a.sums = sums;
+    return launch(c, GT_KC_DENSE, k_residues<RIGHT>, dim3((unsigned)(((u64)nrb * nkb + 3) / 4)), B256, a);
+}
+// completion of the product of A (M x K) and B (N x K), by residues: rows in blocks, the long axis in chunks of RNS_TERMS
+static int do_dense(gt_ctx *c, MatView A, const MatView &B, u64 M, u64 N, u64 K, bool relu, const FinOut &o)
+{
+    FinArgs f{};
+    f.c = kc(c, c->op++); f.ncol = (u32)N; f.f = c->tau;
+    f.y = o.y; f.gate = o.gate; f.res = o.res; f.bias = o.bias; f.has_res = o.has_res; f.has_gate = o.has_gate; f.has_bias = o.has_bias;
+    const u32 nchunk = (u32)((K + RNS_TERMS - 1) / RNS_TERMS);
+    const u64 step = rns_rows(N);
+    for (u64 r0 = 0; r0 < M; r0 += step) {
+        const u64 m = std::min<u64>(M - r0, step);
+        const RmmShape s = rmm_shape(c->simds, m, N);
+        const u32 narb = (u32)(s.ntm * 2 * s.wm), nbrb = (u32)(s.ntn * 2 * s.wn);
+        const bool asums = m <= N;                                       // the factor with fewer rows is converted twice
+        const u32 nkb = (u32)((std::min<u64>(K, RNS_TERMS) + 63) / 64 * 2);
+        const u64 amat = (u64)narb * nkb * 1024, bmat = (u64)nbrb * nkb * 1024, plane = (m * N + 127) & ~(u64)127;
+        const u64 abytes = (asums ? 6 : 3) * RNS_N * amat, bbytes = (asums ? 3 : 6) * RNS_N * bmat, rbytes = 3 * RNS_N * plane;
+        GTCHK(grow_res(c, abytes + bbytes + nchunk * rbytes));
+        MatView Ar = A;
+        for (int j = 0; j < 3; j++) Ar.c[j] += r0 * A.rs;
+        for (u32 ch = 0; ch < nchunk; ch++) {
+            const u64 k0 = (u64)ch * RNS_TERMS, k = std::min<u64>(K - k0, RNS_TERMS);
+            const u32 kb = (u32)((k + 63) / 64 * 2);
+            GTCHK(residues<false>(c, Ar, c->res, m, k, k0, narb, kb, asums));
+            GTCHK(residues<true>(c, B, c->res + abytes, N, k, k0, nbrb, kb, !asums));
+            RmmArgs a{};
+            a.A = c->res; a.B = c->res + abytes; a.R = c->res + abytes + bbytes + ch * rbytes; a.amat = (u64)narb * kb * 1024; a.bmat = (u64)nbrb * kb * 1024;
+            a.plane = plane; a.M = (u32)m; a.N = (u32)N; a.narb = narb; a.nbrb = nbrb; a.nstep = kb; a.ntm = (u32)s.ntm; a.ntn = (u32)s.ntn; a.asums = asums;
+            a.total = (u32)(3 * RNS_N * s.ntm * s.ntn);
+            const dim3 g((a.total + 7) / 8 * 8);
+            GTCHK(s.wm == 4 ? launch(c, GT_KC_DENSE, k_rns_mm<4, 2>, g, B256, a) : launch(c, GT_KC_DENSE, k_rns_mm<1, 1>, g, B256, a));
+        }
+        f.R = c->res + abytes + bbytes; f.first = r0 * N; f.plane = plane; f.nchunk = nchunk; f.n = m * N;
+        const dim3 g((unsigned)std::min<u64>((f.n + 127) / 128, 1u << 16));
+        GTCHK(relu ? launch(c, GT_KC_FINISH, k_finish<FIN_RES, true>, g, B64, f) : launch(c, GT_KC_FINISH, k_finish<FIN_RES, false>, g, B64, f));
+    }
+    acct_finish(c, M * N, relu);
+    return GT_OK;
+}
 // the same for few rows of x and weights: x (M rows of K words), W or, transposed, its rows as columns
 static int do_dense_w(gt_ctx *c, P6 x, u64 ldx, const WMat &W, bool transposed, u64 M, bool relu, const FinOut &o)
 {

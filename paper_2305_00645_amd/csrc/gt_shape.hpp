@@ -227,3 +227,17 @@ static inline FewShape few_shape(u64 simds, u64 M, u64 N, u64 K)
     s.nsplit = (u32)((steps + s.per - 1) / s.per);
     return s;
 }
+
+// Product by residues (k_rns_mm): tiles of 64 wm x 64 wn outputs.
+// rows of a pass, a multiple of 128: its outputs' residues, 54 bytes each, stay below 7 GB (more for over 2^20 columns)
+static inline u64 rns_rows(u64 N) { return std::max<u64>(128, std::min<u64>(16384, ((u64)1 << 27) / N / 128 * 128)); }
+struct RmmShape { u32 wm, wn; u64 ntm, ntn; };
+static inline RmmShape rmm_shape(u64 simds, u64 M, u64 N)
+{
+    RmmShape s = { 4, 2, 0, 0 };
+    const u64 cus = simds / 4, big = (M + 255) / 256 * ((N + 127) / 128) * 54;
+    if (big < 2 * cus || M <= 64 || N <= 64) { s.wm = 1; s.wn = 1; }
+    s.ntm = (M + 64 * s.wm - 1) / (64 * s.wm);
+    s.ntn = (N + 64 * s.wn - 1) / (64 * s.wn);
+    return s;
+}

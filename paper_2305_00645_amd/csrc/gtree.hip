@@ -52,6 +52,8 @@ struct gt_ctx {
     std::vector<int> ev_cls;
     gt_prof prof;
     DSh ws[5];                // inference workspace, grown on demand, kept between calls
+    unsigned char *res;       // residues of a layer's product, likewise
+    size_t res_bytes;
     DSh ws_dz;                // a layer's gradient behind its activation, likewise
     u64 *dacc;                // partial inner products of split equality grids
     size_t dacc_words;
@@ -265,7 +267,7 @@ extern "C" int gt_ctx_create(gt_ctx **out, const gt_params *prm)
     gt_ctx *c = new (std::nothrow) gt_ctx();
     if (!c) return GT_ENOMEM;
     c->noalloc = false; c->scratch_d = nullptr;
-    c->op = 0; c->ev_used = 0; c->keys_d = nullptr; c->wire_d = nullptr; c->dacc = nullptr; c->dacc_words = 0; c->simds = 1024;
+    c->op = 0; c->ev_used = 0; c->keys_d = nullptr; c->wire_d = nullptr; c->dacc = nullptr; c->dacc_words = 0; c->res = nullptr; c->res_bytes = 0; c->simds = 1024;
     memset(&c->acc, 0, sizeof c->acc); memset(&c->prof, 0, sizeof c->prof);
     c->profile = (prm->flags & GT_FLAG_PROFILE) != 0;
     c->levelwise_infer = (prm->flags & GT_FLAG_LEVELWISE_INFER) != 0;
@@ -302,6 +304,7 @@ extern "C" int gt_ctx_destroy(gt_ctx *c)
     for (hipEvent_t e : c->ev_pool) (void)hipEventDestroy(e);
     for (DSh &w : c->ws) dsh_free(w);
     dsh_free(c->ws_dz);
+    if (c->res) (void)hipFree(c->res);
     if (c->dacc) (void)hipFree(c->dacc);
     (void)hipFree(c->wire_d);
     (void)hipFree(c->keys_d);
