@@ -547,7 +547,7 @@ __global__ __launch_bounds__(256, WM == 4 ? 2 : 4) void k_rns_mm(RmmArgs a)
     const unsigned char *A0 = a.A + ((u64)p * RNS_N + mi) * a.amat, *A1 = a.A + ((u64)(a.asums ? 3 + p : pn) * RNS_N + mi) * a.amat;
     const unsigned char *B0 = a.B + ((u64)p * RNS_N + mi) * a.bmat, *B1 = a.B + ((u64)(a.asums ? pn : 3 + p) * RNS_N + mi) * a.bmat;
     const u32 half = a.nstep / 2;                                              // steps of a product
-    uint4 st[LOADS];
+    v4i st[LOADS];
     auto fetch = [&](u32 s) {
         const u32 k = s >= half ? s - half : s;
         const unsigned char *A = (s >= half ? A1 : A0) + ((u64)k * 2 * a.narb + tm * FA) * 1024, *B = (s >= half ? B1 : B0) + ((u64)k * 2 * a.nbrb + tn * FB) * 1024;
@@ -556,12 +556,12 @@ __global__ __launch_bounds__(256, WM == 4 ? 2 : 4) void k_rns_mm(RmmArgs a)
             const u32 o = q * 4 + wave;                                        // operand: [2 blocks of terms][FA] of A, then of B
             const bool isA = o < 2 * FA;
             const u32 w = isA ? o : o - 2 * FA, kb = isA ? w / FA : w / FB, r = isA ? w % FA : w % FB;
-            st[q] = *(const uint4 *)((isA ? A + ((u64)kb * a.narb + r) * 1024 : B + ((u64)kb * a.nbrb + r) * 1024) + lane * 16);
+            st[q] = *(const v4i *)((isA ? A + ((u64)kb * a.narb + r) * 1024 : B + ((u64)kb * a.nbrb + r) * 1024) + lane * 16);
         }
     };
     auto put = [&](u32 buf) {
 #pragma unroll
-        for (int q = 0; q < LOADS; q++) *(uint4 *)(s_buf + buf * STEP + (q * 4 + wave) * 1024 + lane * 16) = st[q];
+        for (int q = 0; q < LOADS; q++) *(v4i *)(s_buf + buf * STEP + (q * 4 + wave) * 1024 + lane * 16) = st[q];
     };
     v16i acc[WM][WN];
 #pragma unroll
@@ -619,8 +619,9 @@ __global__ __launch_bounds__(256, WM == 4 ? 2 : 4) void k_rns_mm(RmmArgs a)
         unsigned char *to = R + (u64)row * a.N + col;
         if (col + 16 <= a.N) __builtin_memcpy(to, &v, 16);
         else {
-            const u32 w[4] = { v.x, v.y, v.z, v.w };
-            for (u32 i = 0; i < a.N - col; i++) to[i] = (unsigned char)(w[i >> 2] >> (8 * (i & 3)));
+#pragma unroll
+            for (u32 i = 0; i < 15; i++)
+                if (i < a.N - col) to[i] = (unsigned char)((i < 4 ? v.x : i < 8 ? v.y : i < 12 ? v.z : v.w) >> (8 * (i & 3)));
         }
     }
 }
