@@ -340,10 +340,12 @@ struct MatView { const u64 *c[3]; u64 rs, ks; };
 // transposed product of the backward pass).
 // Bound: the rate at which the weights arrive.
 struct FewArgs { const u64 *x[3]; const u64 *w; u64 *Z; u64 plane, ldx, ldw, M, N, K; u32 per, nsplit; };
+// a word at a wave-uniform address plus a lane's offset in bytes
+template <class T> __device__ __forceinline__ T ld_at(const void *base, u32 off) { return *(const T *)((const char *)base + off); }
 template <int ROWS, bool KC>
-__global__ __launch_bounds__(256) void k_mm_few(FewArgs a)
+__global__ __launch_bounds__(256, 1) void k_mm_few(FewArgs a)
 {
-    constexpr int SLOTS = ROWS == 8 ? 3 : 6;                         // tiles of the left factor: both factors in one, or three of each
+    constexpr int SLOTS = ROWS == 8 ? 3 : 6, XP = ROWS / 8;           // tiles of the left factor: both factors in one, or three of each
     __shared__ __align__(16) unsigned char s_a[2][SLOTS * 8 * 1024];  // [tile][limb][lane of the operand][16 bytes]
     const u32 tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const u32 lr = lane & 15, kq = lane >> 4;
@@ -351,54 +353,53 @@ __global__ __launch_bounds__(256) void k_mm_few(FewArgs a)
     const u64 c0 = ((u64)(blockIdx.x / a.nsplit) * 4 + wave) * 16, r0 = (u64)blockIdx.y * ROWS;
     const u32 nsteps = (u32)((a.K + 63) / 64), s0 = split * a.per, s1 = s0 + a.per < nsteps ? s0 + a.per : nsteps;
     const bool cols = c0 < a.N;                                      // whole wavefront; it takes part in the barriers
-    const u32 nrow = a.M - r0 < (u64)ROWS ? (u32)(a.M - r0) : ROWS;
-    // units of 8 terms of a tile's row: 3 x 16 x 8 or 6 x 16 x 8
-    constexpr int UNITS = SLOTS * 128, PASSES = (UNITS + 255) / 256;
-    u64 xw[PASSES][8];
+    const u32 nrow = a.M - r0 < (u64)ROWS ? (u32)(a.M - r0) : ROWS, K = (u32)a.K, ldx = (u32)a.ldx;
+    // The left factor: wavefront j < 3 makes x_j + x_{j+1} (tile j) and x_j (meets w_{j+1}), a lane eight terms of a row.
+    const u64 *xa = (wave == 0 ? a.x[0] : wave == 1 ? a.x[1] : a.x[2]) + r0 * a.ldx, *xb = (wave == 0 ? a.x[1] : wave == 1 ? a.x[2] : a.x[0]) + r0 * a.ldx;
+    const u32 xr = lane >> 3, xg = lane & 7;
+    u64 va[XP][8], vb[XP][8];
     auto fetch = [&](u32 s) {
 #pragma unroll
-        for (int q = 0; q < PASSES; q++) {
-            const u32 u = tid + q * 256, slot = u >> 7, row = (u >> 3) & 15, g = u & 7;
-            const bool sum = ROWS == 8 ? row < 8 : slot < 3;
-            const u32 j = ROWS == 8 ? (sum ? slot : (slot + 2) % 3) : slot % 3, r = ROWS == 8 ? row & 7 : row;
-            const u64 k0 = (u64)s * 64 + g * 8;
-            const u64 *x0 = j == 0 ? a.x[0] : (j == 1 ? a.x[1] : a.x[2]), *x1 = j == 0 ? a.x[1] : (j == 1 ? a.x[2] : a.x[0]);
-            const bool on = u < UNITS && r < nrow;
+        for (int q = 0; q < XP; q++) {
+            const u32 r = xr + 8 * q, base = (r < nrow ? r : 0) * ldx, k0 = s * 64 + xg * 8;
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                u64 v = 0;
-                if (on && k0 + i < a.K) {
-                    const u64 at = (r0 + r) * a.ldx + k0 + i;
-                    v = x0[at];
-                    if (sum) v += x1[at];
-                }
-                xw[q][i] = v;
+            for (int i = 0; i < 8; i++) {                             // (words that exist where these do not: loads without branches)
+                const u32 at = (base + (k0 + i < K ? k0 + i : K - 1)) * 8;
+                va[q][i] = ld_at<u64>(xa, at); vb[q][i] = ld_at<u64>(xb, at);
             }
         }
     };
-    auto put = [&](int buf) {
+    auto put = [&](u32 s, int buf) {
 #pragma unroll
-        for (int q = 0; q < PASSES; q++) {
-            const u32 u = tid + q * 256, slot = u >> 7, row = (u >> 3) & 15, g = u & 7;
-            if (u < UNITS) {
-                u64 y[8];
+        for (int q = 0; q < XP; q++) {
+            const u32 r = xr + 8 * q, k0 = s * 64 + xg * 8;
+            const bool on = r < nrow;
+            u64 ys[8], yp[8];
 #pragma unroll
-                for (int i = 0; i < 8; i++) y[i] = (xw[q][i] + GT_BIAS) ^ GT_BIAS;
-                transpose8x8(y);
-                unsigned char *to = s_a[buf] + slot * 8192 + (row + 16 * (g >> 1)) * 16 + (g & 1) * 8;
+            for (int i = 0; i < 8; i++) {
+                const u64 live = 0 - (u64)(on && k0 + i < K);
+                ys[i] = (((va[q][i] + vb[q][i]) + GT_BIAS) ^ GT_BIAS) & live;
+                yp[i] = ((va[q][i] + GT_BIAS) ^ GT_BIAS) & live;
+            }
+            transpose8x8(ys); transpose8x8(yp);
+            const u32 slot = ROWS == 8 ? (wave == 2 ? 0 : wave + 1) : 3 + wave, row = ROWS == 8 ? 8 + r : r;     // of the component
+            unsigned char *to = s_a[buf] + 256 * (xg >> 1) + 8 * (xg & 1);
 #pragma unroll
-                for (int sl = 0; sl < 8; sl++) *(u64 *)(to + sl * 1024) = y[sl];
+            for (int sl = 0; sl < 8; sl++) {
+                *(u64 *)(to + wave * 8192 + r * 16 + sl * 1024) = ys[sl];
+                *(u64 *)(to + slot * 8192 + row * 16 + sl * 1024) = yp[sl];
             }
         }
     };
     u64 raw[3][16];
-    const u64 *wl = KC ? a.w + (c0 + lr) * a.ldw + kq * 16 : a.w + (u64)kq * 16 * a.ldw + c0 + lr;
+    const u32 ldw = (u32)a.ldw, woff = (KC ? lr * ldw + kq * 16 : kq * 16 * ldw + lr) * 8;
+    const u64 *w0 = a.w + (KC ? c0 * ldw : c0);
     auto load = [&](int j, u32 s) {
-        const u64 *from = wl + (u64)j * a.plane + (KC ? (u64)s * 64 : (u64)s * 64 * a.ldw);
+        const u64 *from = w0 + (u64)j * a.plane + (KC ? (u64)s * 64 : (u64)s * 64 * ldw);
 #pragma unroll
         for (int i = 0; i < 16; i += 2) {
-            if (KC) { const ulonglong2 v = *(const ulonglong2 *)(from + i); raw[j][i] = v.x; raw[j][i + 1] = v.y; }
-            else { raw[j][i] = from[(u64)i * a.ldw]; raw[j][i + 1] = from[(u64)(i + 1) * a.ldw]; }
+            if (KC) { const ulonglong2 v = ld_at<ulonglong2>(from + i, woff); raw[j][i] = v.x; raw[j][i + 1] = v.y; }
+            else { raw[j][i] = ld_at<u64>(from + (u64)i * ldw, woff); raw[j][i + 1] = ld_at<u64>(from + (u64)(i + 1) * ldw, woff); }
         }
     };
     v4i acc[3][8];
@@ -406,15 +407,8 @@ __global__ __launch_bounds__(256) void k_mm_few(FewArgs a)
     for (int j = 0; j < 3; j++)
 #pragma unroll
         for (int u = 0; u < 8; u++) acc[j][u] = v4i{ 0, 0, 0, 0 };
-    if (cols)
-#pragma unroll
-        for (int j = 0; j < 3; j++) load(j, s0);
-    fetch(s0);
-    put(0);
-    __syncthreads();
-    for (u32 s = s0; s < s1; s++) {
-        const int buf = (s - s0) & 1;
-        if (s + 1 < s1) fetch(s + 1);
+    auto step = [&](u32 s, int buf, bool more) {
+        if (more && wave < 3) fetch(s + 1);
         if (cols) {
 #pragma unroll
             for (int j = 0; j < 3; j++) {
@@ -427,7 +421,7 @@ __global__ __launch_bounds__(256) void k_mm_few(FewArgs a)
 #pragma unroll
                     for (int i = 0; i < 8; i++) B[i] = v4i{ (int)(u32)y[i], (int)(u32)(y[i] >> 32), (int)(u32)z[i], (int)(u32)(z[i] >> 32) };
                 }
-                if (s + 1 < s1) load(j, s + 1);
+                if (more) load(j, s + 1);
 #pragma unroll
                 for (int h = 0; h < (ROWS == 8 ? 1 : 2); h++) {
                     // the sums' tile with w_j gives z_j; x_{j-1} with w_j gives z_{j-1}
@@ -442,9 +436,21 @@ __global__ __launch_bounds__(256) void k_mm_few(FewArgs a)
                 }
             }
         }
-        if (s + 1 < s1) put(buf ^ 1);
+        if (more && wave < 3) put(s + 1, buf ^ 1);
+    };
+    if (wave < 3) fetch(s0);
+    if (cols)
+#pragma unroll
+        for (int j = 0; j < 3; j++) load(j, s0);
+    if (wave < 3) put(s0, 0);
+    __syncthreads();
+    int buf = 0;
+    for (u32 s = s0; s + 1 < s1; s++) {
+        step(s, buf, true);
         __syncthreads();
+        buf ^= 1;
     }
+    step(s1 - 1, buf, false);
     if (!cols) return;
 #pragma unroll
     for (int v = 0; v < 4; v++) {
@@ -494,7 +500,12 @@ __global__ __launch_bounds__(256) void k_residues(ResArgs a)
 #pragma unroll
     for (int j = 0; j < 3; j++)
 #pragma unroll
-        for (int i = 0; i < 16; i++) x[j][i] = row < a.rows && k + i < a.K ? a.x.c[j][row * a.x.rs + (a.k0 + k + i) * a.x.ks] : 0;
+        for (int i = 0; i < 16; i++) x[j][i] = a.x.c[j][(row < a.rows ? row : a.rows - 1) * a.x.rs + (a.k0 + (k + i < a.K ? k + i : a.K - 1)) * a.x.ks];
+    // (words that exist were loaded where these do not)
+#pragma unroll
+    for (int j = 0; j < 3; j++)
+#pragma unroll
+        for (int i = 0; i < 16; i++) x[j][i] = row < a.rows && k + i < a.K ? x[j][i] : 0;
     unsigned char *out = a.out + ((u64)kb * a.nrb + rb) * 1024 + lane * 16;
 #pragma unroll
     for (int q = 0; q < 6; q++) {

@@ -117,7 +117,7 @@ static int do_dense(gt_ctx *c, MatView A, const MatView &B, u64 M, u64 N, u64 K,
 static int do_dense_w(gt_ctx *c, P6 x, u64 ldx, const WMat &W, bool transposed, u64 M, bool relu, const FinOut &o)
 {
     const u64 N = transposed ? W.K : W.N, K = transposed ? W.N : W.K;
-    if (M == 0 || M > GT_FEW_ROWS) return do_dense(c, view(x, ldx, 1), transposed ? wmat(W) : wmat_t(W), M, N, K, relu, o);
+    if (M == 0 || !few_rows(M, ldx)) return do_dense(c, view(x, ldx, 1), transposed ? wmat(W) : wmat_t(W), M, N, K, relu, o);
     GTCHK(grow_dacc(c, 3 * M * N));
     FewArgs a{};
     for (int j = 0; j < 3; j++) a.x[j] = x.o[j];

@@ -214,6 +214,7 @@ static inline InferShape infer_shape(u64 simds, u32 lgi, u64 ngrp, u32 ntrees, u
 // Product of few rows with a weight matrix (k_mm_few): rows of a tile, tiles, groups of 64 columns, splits of the long axis and steps of 64
 // terms a split.
 #define GT_FEW_ROWS 32                       // rows up to which the weights' words are read again for every tile of rows
+static inline bool few_rows(u64 M, u64 ldx) { return M <= GT_FEW_ROWS && ldx < (1u << 25); }       // a tile's words at 32-bit offsets
 struct FewShape { u32 rows; u64 ntile, ngrp; u32 nsplit, per; };
 static inline FewShape few_shape(u64 simds, u64 M, u64 N, u64 K)
 {
@@ -221,7 +222,7 @@ static inline FewShape few_shape(u64 simds, u64 M, u64 N, u64 K)
     s.rows = M <= 8 ? 8 : 16;
     s.ntile = (M + s.rows - 1) / s.rows;
     s.ngrp = (N + 63) / 64;
-    const u64 steps = (K + 63) / 64, want = std::max<u64>(1, simds / 2 / (s.ngrp * s.ntile));
+    const u64 steps = (K + 63) / 64, want = std::max<u64>(1, simds / 4 / (s.ngrp * s.ntile));
     // at most 64 steps: the int32 sums of a limb level stay below 2^31 (8 products of limbs of both factors, 2^14 each, 64 terms a step)
     s.per = (u32)std::min<u64>(64, std::max<u64>(1, (steps + want - 1) / want));
     s.nsplit = (u32)((steps + s.per - 1) / s.per);
