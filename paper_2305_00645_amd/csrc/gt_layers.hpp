@@ -193,12 +193,13 @@ constexpr RnsTable RNS = rns_make();
 static __device__ const RnsTable d_rns = rns_make();             // for a modulus that is not known when the kernel is compiled
 #define RNS_MAGIC 0x4b400000u                     // 1.5 * 2^23: this plus an integer is the float 1.5 * 2^23 plus it
 
-// an integer t, |t| < 2^21.1, given as RNS_MAGIC + t, to the balanced residue: in the low byte
-__device__ __forceinline__ u32 rns_reduce(u32 tm, float m, float inv)
+// An integer t, |t| < 2^21.1, given as RNS_MAGIC + t, to the balanced residue, in the low byte: t - round(t / m) m.  The low 24 bits of the
+// float RNS_MAGIC + q are 2^22 + q; the low byte knows neither the 2^22 nor the difference of -m and neg = 256 - m.
+__device__ __forceinline__ u32 rns_reduce(u32 tm, u32 neg, float inv)
 {
-    const float magic = __uint_as_float(RNS_MAGIC), x = __uint_as_float(tm);
-    const float q = __builtin_fmaf(x - magic, inv, magic) - magic;
-    return __float_as_uint(__builtin_fmaf(-q, m, x));
+    const float magic = __uint_as_float(RNS_MAGIC);
+    const float q = __builtin_fmaf(__uint_as_float(tm) - magic, inv, magic);
+    return (__float_as_uint(q) & 0xffffffu) * (neg & 0xffu) + tm;
 }
 __device__ __forceinline__ u32 low_bytes(u32 a, u32 b, u32 c, u32 d)
 {
@@ -484,52 +485,59 @@ __global__ __launch_bounds__(256, 1) void k_mm_few(FewArgs a)
 // lane l of an operand holds row l % 32 and the 16 terms from 16 (l / 32) on.  Matrices: the sums of adjacent components (0-2) and the components
 // (3-5), or the components alone (0-2).  Rows and terms beyond the matrix are zero.  A residue: two four-byte dot products of the word's
 // signed bytes with the powers of 256, a rounded quotient in floating point.  RIGHT: times (M / m_i)^-1.
-// A wavefront makes an operand of 32 x 32 words, all moduli.
-struct ResArgs { MatView x; unsigned char *out; u64 rows, K, k0; u32 nrb, nkb; int sums; };
-template <bool RIGHT>
+// A wavefront makes an operand of 32 x 32 words of one matrix for a range of moduli (blockIdx.y: matrix, blockIdx.z: range).  KC: terms contiguous
+// in memory; the words then go through LDS, so that loads are of whole rows.
+struct ResArgs { MatView x; unsigned char *out; u64 rows, K, k0; u32 nrb, nkb, per; int sums; };
+template <bool RIGHT, bool KC>
 __global__ __launch_bounds__(256) void k_residues(ResArgs a)
 {
-    const u32 lane = threadIdx.x & 63, lr = lane & 31, hi = lane >> 5;
+    __shared__ u64 s_t[KC ? 4 : 1][KC ? 32 * 33 : 1];
+    const u32 lane = threadIdx.x & 63, lr = lane & 31, hi = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = blockIdx.y;
     const u64 nfr = (u64)a.nrb * a.nkb, mat = nfr * 1024;
-    const u64 fr = (u64)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const u64 fr = (u64)blockIdx.x * 4 + wave;
     if (fr >= nfr) return;
     // neighbours along the axis that is contiguous in memory
-    const u32 rb = (u32)(a.x.ks == 1 ? fr / a.nkb : fr % a.nrb), kb = (u32)(a.x.ks == 1 ? fr % a.nkb : fr / a.nrb);
-    const u64 row = (u64)rb * 32 + lr, k = (u64)kb * 32 + hi * 16;
-    u64 x[3][16];
-#pragma unroll
-    for (int j = 0; j < 3; j++)
-#pragma unroll
-        for (int i = 0; i < 16; i++) x[j][i] = a.x.c[j][(row < a.rows ? row : a.rows - 1) * a.x.rs + (a.k0 + (k + i < a.K ? k + i : a.K - 1)) * a.x.ks];
-    // (words that exist were loaded where these do not)
-#pragma unroll
-    for (int j = 0; j < 3; j++)
-#pragma unroll
-        for (int i = 0; i < 16; i++) x[j][i] = row < a.rows && k + i < a.K ? x[j][i] : 0;
-    unsigned char *out = a.out + ((u64)kb * a.nrb + rb) * 1024 + lane * 16;
-#pragma unroll
-    for (int q = 0; q < 6; q++) {
-        if (q >= 3 && !a.sums) break;
-        u32 lo[16], hh[16];
+    const u32 rb = (u32)(KC ? fr / a.nkb : fr % a.nrb), kb = (u32)(KC ? fr % a.nkb : fr / a.nrb);
+    const bool sum = a.sums && q < 3;
+    const u64 *x0 = q % 3 == 0 ? a.x.c[0] : (q % 3 == 1 ? a.x.c[1] : a.x.c[2]), *x1 = q == 0 ? a.x.c[1] : (q == 1 ? a.x.c[2] : a.x.c[0]);
+    u64 x[16];
+    {
+        // (words that exist are loaded where these do not, and cleared)
+        u64 t[16];
 #pragma unroll
         for (int i = 0; i < 16; i++) {
-            const u64 w = q >= 3 ? x[q - 3][i] : a.sums ? x[q][i] + x[(q + 1) % 3][i] : x[q][i];
-            const u64 y = (w + GT_BIAS) ^ GT_BIAS;
-            lo[i] = (u32)y; hh[i] = (u32)(y >> 32);
+            const u64 r = (u64)rb * 32 + (KC ? 2 * i + hi : lr), k = (u64)kb * 32 + (KC ? lr : hi * 16 + i);
+            const u64 at = (r < a.rows ? r : a.rows - 1) * a.x.rs + (a.k0 + (k < a.K ? k : a.K - 1)) * a.x.ks;
+            x[i] = x0[at];
+            t[i] = sum ? x1[at] : 0;
         }
 #pragma unroll
-        for (int i = 0; i < RNS_N; i++) {
-            const int cl = (int)(RIGHT ? RNS.right[i][0] : RNS.left[i][0]), ch = (int)(RIGHT ? RNS.right[i][1] : RNS.left[i][1]);
-            u32 b[16];
-#pragma unroll
-            for (int e = 0; e < 16; e++)
-                b[e] = rns_reduce((u32)__builtin_amdgcn_sdot4((int)lo[e], cl, __builtin_amdgcn_sdot4((int)hh[e], ch, (int)RNS_MAGIC, false), false),
-                                  (float)RNS.m[i], RNS.inv[i]);
-            uint4 v;
-            v.x = low_bytes(b[0], b[1], b[2], b[3]); v.y = low_bytes(b[4], b[5], b[6], b[7]);
-            v.z = low_bytes(b[8], b[9], b[10], b[11]); v.w = low_bytes(b[12], b[13], b[14], b[15]);
-            *(uint4 *)(out + ((u64)q * RNS_N + i) * mat) = v;
+        for (int i = 0; i < 16; i++) {
+            const u64 r = (u64)rb * 32 + (KC ? 2 * i + hi : lr), k = (u64)kb * 32 + (KC ? lr : hi * 16 + i);
+            x[i] = ((x[i] + t[i] + GT_BIAS) ^ GT_BIAS) & (0 - (u64)(r < a.rows && k < a.K));
         }
+        if (KC) {
+#pragma unroll
+            for (int i = 0; i < 16; i++) s_t[wave][(2 * i + hi) * 33 + lr] = x[i];
+            wave_sync();
+#pragma unroll
+            for (int i = 0; i < 16; i++) x[i] = s_t[wave][lr * 33 + hi * 16 + i];
+        }
+    }
+    unsigned char *out = a.out + (u64)q * RNS_N * mat + ((u64)kb * a.nrb + rb) * 1024 + lane * 16;
+    const u32 i0 = blockIdx.z * a.per, i1 = i0 + a.per < RNS_N ? i0 + a.per : RNS_N;
+    for (u32 i = i0; i < i1; i++) {
+        const int cl = (int)(RIGHT ? d_rns.right[i][0] : d_rns.left[i][0]), ch = (int)(RIGHT ? d_rns.right[i][1] : d_rns.left[i][1]);
+        const u32 neg = 256 - (u32)d_rns.m[i];
+        const float inv = d_rns.inv[i];
+        u32 b[16];
+#pragma unroll
+        for (int e = 0; e < 16; e++)
+            b[e] = rns_reduce((u32)__builtin_amdgcn_sdot4((int)(u32)x[e], cl, __builtin_amdgcn_sdot4((int)(u32)(x[e] >> 32), ch, (int)RNS_MAGIC, false), false), neg, inv);
+        uint4 v;
+        v.x = low_bytes(b[0], b[1], b[2], b[3]); v.y = low_bytes(b[4], b[5], b[6], b[7]);
+        v.z = low_bytes(b[8], b[9], b[10], b[11]); v.w = low_bytes(b[12], b[13], b[14], b[15]);
+        *(uint4 *)(out + (u64)i * mat) = v;
     }
 }
 
@@ -603,7 +611,8 @@ __global__ __launch_bounds__(256, WM == 4 ? 2 : 4) void k_rns_mm(RmmArgs a)
         __syncthreads();
     }
     // |sum| < 2^28: low 13 bits and the rest times 2^13 mod m, below 2^21.1, then the balanced residue; through LDS to rows
-    const float m = (float)d_rns.m[mi], inv = d_rns.inv[mi];
+    const float inv = d_rns.inv[mi];
+    const u32 neg = 256 - (u32)d_rns.m[mi];
     const int c13 = d_rns.c13[mi];
 #pragma unroll
     for (int i = 0; i < WM; i++)
@@ -615,7 +624,7 @@ __global__ __launch_bounds__(256, WM == 4 ? 2 : 4) void k_rns_mm(RmmArgs a)
 #pragma unroll
                 for (int v = 0; v < 4; v++) {
                     const int z = acc[i][j][4 * g + v];
-                    b[v] = rns_reduce((u32)((z >> 13) * c13) + (((u32)z & 8191u) | RNS_MAGIC), m, inv);
+                    b[v] = rns_reduce((u32)((z >> 13) * c13) + (((u32)z & 8191u) | RNS_MAGIC), neg, inv);
                 }
                 *(u32 *)(s_buf + ((wm * WM + i) * 32 + (lane & 31)) * LD + (wn * WN + j) * 32 + 8 * g + 4 * (lane >> 5)) = low_bytes(b[0], b[1], b[2], b[3]);
             }
@@ -649,23 +658,29 @@ __global__ __launch_bounds__(256) void k_put(PutArgs a)
     }
 }
 
-// column sums of a shared matrix (local): a workgroup per 64 columns
-struct ColsumArgs { P6 x, out; u64 rows; u32 cols; };
+// Column sums of a shared matrix (local): a workgroup per 16 columns, component and, for many rows, range of rows; the ranges' sums meet by
+// atomic adds in words that were cleared (exact, order-free).
+struct ColsumArgs { P6 x, out; u64 rows, per; u32 cols; int add; };
 __global__ __launch_bounds__(256) void k_colsum(ColsumArgs a)
 {
-    __shared__ u64 s_sum[4][GT_LANES];
-    const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6, pl = blockIdx.y;
-    const u64 col = (u64)blockIdx.x * GT_LANES + lane;
+    __shared__ u64 s_sum[16][17];
+    const u32 c = threadIdx.x & 15, g = threadIdx.x >> 4, pl = blockIdx.y;
+    const u64 col = (u64)blockIdx.x * 16 + c, r0 = blockIdx.z * a.per, r1 = r0 + a.per < a.rows ? r0 + a.per : a.rows;
     const u64 *x = pl == 0 ? a.x.o[0] : (pl == 1 ? a.x.o[1] : a.x.o[2]);
     u64 s = 0;
-    if (col < a.cols) for (u64 r = wave; r < a.rows; r += 4) s += x[r * a.cols + col];
-    s_sum[wave][lane] = s;
+    if (col < a.cols) {
+#pragma unroll 4
+        for (u64 r = r0 + g; r < r1; r += 16) s += x[r * a.cols + col];
+    }
+    s_sum[g][c] = s;
     __syncthreads();
-    if (wave == 0 && col < a.cols) {
-        s += s_sum[1][lane] + s_sum[2][lane] + s_sum[3][lane];
+    if (g == 0 && col < a.cols) {
+#pragma unroll
+        for (int i = 1; i < 16; i++) s += s_sum[i][c];
         // component pl: party pl's own, its predecessor's next one
-        own_of(a.out, (int)pl)[col] = s;
-        nxt_of(a.out, pl == 0 ? 2 : (int)pl - 1)[col] = s;
+        u64 *o = &own_of(a.out, (int)pl)[col], *n = &nxt_of(a.out, pl == 0 ? 2 : (int)pl - 1)[col];
+        if (a.add) { atomicAdd((unsigned long long *)o, (unsigned long long)s); atomicAdd((unsigned long long *)n, (unsigned long long)s); }
+        else { *o = s; *n = s; }
     }
 }
 

@@ -73,7 +73,10 @@ static int residues(gt_ctx *c, const MatView &x, unsigned char *out, u64 rows, u
 {
     ResArgs a{};
     a.x = x; a.out = out; a.rows = rows; a.K = K; a.k0 = k0; a.nrb = nrb; a.nkb = nkb; a.sums = sums;
-    return launch(c, GT_KC_DENSE, k_residues<RIGHT>, dim3((unsigned)(((u64)nrb * nkb + 3) / 4)), B256, a);
+    const u64 nfr = (u64)nrb * nkb, mats = sums ? 6 : 3;
+    a.per = residue_range(c->simds, nfr * mats);
+    const dim3 g((unsigned)((nfr + 3) / 4), (unsigned)mats, (RNS_N + a.per - 1) / a.per);
+    return x.ks == 1 ? launch(c, GT_KC_DENSE, k_residues<RIGHT, true>, g, B256, a) : launch(c, GT_KC_DENSE, k_residues<RIGHT, false>, g, B256, a);
 }
 // completion of the product of A (M x K) and B (N x K), by residues: rows in blocks, the long axis in chunks of RNS_TERMS
 static int do_dense(gt_ctx *c, MatView A, const MatView &B, u64 M, u64 N, u64 K, bool relu, const FinOut &o)
@@ -217,7 +220,10 @@ extern "C" int gt_dense_backward(gt_ctx *c, const gt_dense *l, const gt_shares *
     }
     if (db) {
         ColsumArgs a{}; a.x = dz; a.out = to_p6(db); a.rows = rows; a.cols = l->dout;
-        GTCHK(launch(c, GT_KC_LOCAL, k_colsum, dim3((l->dout + GT_LANES - 1) / GT_LANES, 3), B256, a));
+        const u64 ngrp = (l->dout + 15) / 16, ranges = std::max<u64>(1, std::min<u64>((rows + 255) / 256, c->simds / (3 * ngrp)));
+        a.per = (rows + ranges - 1) / ranges; a.add = ranges > 1;
+        if (a.add) GTCHK(launch(c, GT_KC_LOCAL, k_fill_const, g1(l->dout), B256, a.out, (u64)0, (u64)l->dout, (u64)0));
+        GTCHK(launch(c, GT_KC_LOCAL, k_colsum, dim3((unsigned)ngrp, 3, (unsigned)ranges), B256, a));
     }
     return T.finish(GT_OK);
 }

@@ -242,3 +242,9 @@ static inline RmmShape rmm_shape(u64 simds, u64 M, u64 N)
     s.ntn = (N + 64 * s.wn - 1) / (64 * s.wn);
     return s;
 }
+// moduli of a wavefront of k_residues: all 18, fewer where few operands leave SIMDs without work
+static inline u32 residue_range(u64 simds, u64 operands)
+{
+    const u64 parts = std::min<u64>(6, std::max<u64>(1, 4 * simds / std::max<u64>(1, operands)));
+    return (u32)((18 + parts - 1) / parts);
+}
