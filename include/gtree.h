@@ -267,7 +267,7 @@ int gt_dense_destroy(gt_dense *layer);
 /* y = act(floor((x W + (b << tau) + 2^(tau-1)) / 2^tau)) + residual, x: rows x din, y, residual (NULL: none), gate: rows x dout.
  * Sums are added up modulo 2^64 and have to stay below 2^62 in absolute value, with GT_ACT_RELU below
  * 2^(tau+31) (results below 2^31).  gate (NULL: not wanted, GT_EINVAL without ReLU) receives ReLU's bit, 1 where the
- * value before the activation is at least 0.  y may be the residual's buffers, not those of x.  One operation id; rounds: 7, with ReLU 9.
+ * value before the activation is at least 0.  y may be the residual's buffers, not those of x.  One operation id; rounds: 6, with ReLU 8.
  * The context's workspace grows on first use or for larger calls (then the call waits for the stream and allocates). */
 int gt_dense_forward(gt_ctx *ctx, const gt_dense *layer, const gt_shares *x, size_t rows, int act, const gt_shares *residual,
                      const gt_shares *y, const gt_shares *gate);

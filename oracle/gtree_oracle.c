@@ -1535,12 +1535,14 @@ static void product_parts(const sh *X, int xt, const sh *W, int wt, size_t m, si
 }
 
 /* Block e of stream 5 under the dealer's key: the words of a completion beside the edaBit and daBit of stream 0: an arithmetic
- * sharing of r >> f and of r's top bit, and a second daBit. */
-typedef struct { u64 shift[3], top[3], bA[3], bB[3]; } finish_t;
+ * sharing of r >> f and of r's top bit, a second daBit, and Boolean sharings of the products of adjacent bits of r << (32 - f), product of bits 2b
+ * and 2b+1 at 2b (word 7: component 0 its even bits, component 1 its odd ones). */
+typedef struct { u64 shift[3], top[3], bA[3], bB[3], pr[3]; } finish_t;
+#define EVEN 0x5555555555555555ull
 static void dealer_finish(const orc_ctx *c, u32 op, u64 e, u64 r, u32 f, finish_t *G)
 {
     u32 out[16];
-    u64 w[8], beta;
+    u64 w[8], beta, win = r << (32 - f);
     orc_chacha_block(c->key[KEY_DEALER], (u32)e, (u32)(e >> 32), op, 5, PRF_ROUNDS, out);
     for (int i = 0; i < 8; i++) w[i] = (u64)out[2 * i] | ((u64)out[2 * i + 1] << 32);
     beta = w[6] & 1;
@@ -1548,39 +1550,46 @@ static void dealer_finish(const orc_ctx *c, u32 op, u64 e, u64 r, u32 f, finish_
     G->top[0] = w[2]; G->top[1] = w[3]; G->top[2] = (r >> 63) - w[2] - w[3];
     G->bA[0] = w[4]; G->bA[1] = w[5]; G->bA[2] = beta - w[4] - w[5];
     G->bB[0] = (w[6] >> 1) & 1; G->bB[1] = (w[6] >> 2) & 1; G->bB[2] = beta ^ G->bB[0] ^ G->bB[1];
+    G->pr[0] = w[7] & EVEN; G->pr[1] = (w[7] >> 1) & EVEN; G->pr[2] = (win & (win >> 1) & EVEN) ^ G->pr[0] ^ G->pr[1];
 }
 
-/* [c < r] for public c and bitwise shared r, on the low `width` bits of both: the prefix pairs of ge_el, levels up to
- * blocks of 64 or 32 bits.  low: the pair G of bits 0..31 (before the last level of 64). */
-static void less_el(const orc_ctx *c, u32 op, u64 e, u64 cw, const u64 rw[3], int levels, u64 low[3], u64 all[3])
+/* [c < r] for public c and bitwise shared r with the products of its adjacent bits, on the low 63 bits (halves = 2) or 32 (halves = 1): the prefix pairs
+ * of ge_el.  The pairs of two adjacent bits are local: with n = not c, G = n_h r_h xor n_l (r_h r_l xor n_h r_l), E = r_h r_l xor n_l r_h xor
+ * n_h r_l xor n_h n_l.  Then levels over the 16 blocks of each half, both halves side by side, and with two halves a last level that joins them.
+ * Gates are masked by bits of the Boolean zero sharing of stream 1: level v = 1..4, block b of half h: G at bit base_v + 4 * 2^(v-1) * b + 2 h, E one above, with
+ * base 0, 32, 36, 44; the last level's G at bit 60.  low: G of the low half (bits 0..31), all: of everything. */
+static void less_el(const orc_ctx *c, u32 op, u64 e, u64 cw, const u64 rw[3], const u64 pr[3], int halves, u64 low[3], u64 all[3])
 {
-    u64 AG[3], AE[3], G[64][3], E[64][3];
-    int n = 1 << levels;
-    for (int i = 0; i < n; i++) {
-        u64 nc = (~cw >> i) & 1;
-        for (int j = 0; j < 3; j++) { u64 rb = (rw[j] >> i) & 1; G[i][j] = nc & rb; E[i][j] = rb; }
-        E[i][0] ^= nc;
-        if (i == 63) for (int j = 0; j < 3; j++) { G[i][j] = 0; E[i][j] = j == 0; }
-    }
-    zero_b(c, op, 1, e, AG);
-    zero_b(c, op, 2, e, AE);
-    for (int k = 0; k < levels; k++) {
-        int s = 1 << k;
-        if (k == 5) memcpy(low, G[0], sizeof G[0]);
-        for (int i = 0; i < n; i += 2 * s) {
-            int hi = i + s, lo = i, bit = i + s - 1;
-            u64 al[3], p[3];
-            for (int j = 0; j < 3; j++) al[j] = (AG[j] >> bit) & 1;
-            and_el(E[hi], G[lo], al, 1, p);
-            for (int j = 0; j < 3; j++) G[lo][j] = G[hi][j] ^ p[j];
-            if (k < levels - 1) {
-                for (int j = 0; j < 3; j++) al[j] = (AE[j] >> bit) & 1;
-                and_el(E[hi], E[lo], al, 1, E[lo]);
-            }
+    static const int base[5] = { 0, 0, 32, 36, 44 };
+    u64 A[3], G[2][16][3], E[2][16][3];
+    for (int b = 0; b < 16 * halves; b++) {
+        const int top = b == 31;                      /* bit 63 does not count: (G, E) = (0, 1) */
+        const u64 nl = (~cw >> (2 * b)) & 1, nh = top ? 1 : (~cw >> (2 * b + 1)) & 1;
+        for (int j = 0; j < 3; j++) {
+            const u64 rl = (rw[j] >> (2 * b)) & 1, rh = top ? 0 : (rw[j] >> (2 * b + 1)) & 1, q = top ? 0 : (pr[j] >> (2 * b)) & 1;
+            G[b / 16][b % 16][j] = (nh & rh) ^ (nl & (q ^ (nh & rl)));
+            E[b / 16][b % 16][j] = q ^ (nl & rh) ^ (nh & rl) ^ (j == 0 ? nl & nh : 0);
         }
     }
-    if (levels == 5) memcpy(low, G[0], sizeof G[0]);
-    memcpy(all, G[0], sizeof G[0]);
+    zero_b(c, op, 1, e, A);
+    for (int v = 1; v <= 4; v++)
+        for (int h = 0; h < halves; h++)
+            for (int b = 0; b < 16 >> v; b++) {
+                u64 *Gh = G[h][2 * b + 1], *Gl = G[h][2 * b], *Eh = E[h][2 * b + 1], *El = E[h][2 * b], al[3], g[3], x[3];
+                const int bit = base[v] + (4 << (v - 1)) * b + 2 * h;
+                for (int j = 0; j < 3; j++) al[j] = A[j] >> bit;
+                and_el(Eh, Gl, al, 1, g);
+                for (int j = 0; j < 3; j++) al[j] = A[j] >> (bit + 1);
+                and_el(Eh, El, al, 1, x);
+                for (int j = 0; j < 3; j++) { G[h][b][j] = Gh[j] ^ g[j]; E[h][b][j] = x[j]; }
+            }
+    memcpy(low, G[0][0], sizeof G[0][0]);
+    if (halves == 2) {
+        u64 al[3], g[3];
+        for (int j = 0; j < 3; j++) al[j] = A[j] >> 60;
+        and_el(E[1][0], G[0][0], al, 1, g);
+        for (int j = 0; j < 3; j++) all[j] = G[1][0][j] ^ g[j];
+    }
 }
 
 /* Completion of sums v whose additive parts the parties hold: y = floor((v + 2^(f-1)) / 2^f), with ReLU times its sign bit (the gate),
@@ -1601,7 +1610,7 @@ static void finish(orc_ctx *c, u32 op, const sh *z, size_t n, int relu, const sh
         cw = ((u64)1 << (f - 1)) + off;
         for (int j = 0; j < 3; j++) cw += v[j] + al[j] + D.rA[j];          /* opened */
         for (int j = 0; j < 3; j++) rw[j] = D.rho[j] << (32 - f);
-        less_el(c, op, e, cw << (32 - f), rw, relu ? 6 : 5, low, all);
+        less_el(c, op, e, cw << (32 - f), rw, G.pr, relu ? 2 : 1, low, all);
         b2a_el(low, &D, b);
         for (int j = 0; j < 3; j++) {
             o[j] = (cw >> 63 ? 0 : G.top[j] << (64 - f)) - G.shift[j] - b[j];
@@ -1623,11 +1632,11 @@ static void finish(orc_ctx *c, u32 op, const sh *z, size_t n, int relu, const sh
         sh_set(y, e, o);
     }
     wire(c, +1, n, 64); wire(c, -1, n, 64);
-    for (int k = 0; k < (relu ? 5 : 4); k++) wire(c, -1, n, 2 * ((relu ? 32u : 16u) >> k));
-    wire(c, -1, n, 1);
+    for (int v = 1; v <= 4; v++) wire(c, -1, n, (relu ? 64u : 32u) >> v);    /* the last level's E of the low half is not used: it is sent all the same */
+    if (relu) wire(c, -1, n, 1);
     wire(c, +1, n, relu ? 2 : 1);
     if (relu) wire(c, -1, n, 64);
-    c->rounds += relu ? 9 : 7;
+    c->rounds += relu ? 8 : 6;
 }
 
 static sh sh_flat(const u64 *flat, size_t n) { sh v = sh_alloc(n); if (flat) sh_from_flat(&v, flat); return v; }

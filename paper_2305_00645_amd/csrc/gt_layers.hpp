@@ -7,16 +7,16 @@
 //   y = (c >> f) - (r >> f) + 2^(64-f) [c_63 = 0 and r_63 = 1] - [c mod 2^f < r mod 2^f] - (O >> f)
 // where r >> f and r_63 are dealer material and the last bit comes from a tree of ANDs.  With ReLU O = 2^(f+31): v + 2^(f-1) >= 0 iff bit
 // f+31 of c - r is set, and the borrow into that bit is the root of the tree whose lower half is the borrow of the rounding; so one
-// opening and one tree of 64 leaves (bits 0 .. f+31, shifted up to end at leaf 63) serve both.
+// opening and one tree (over bits 0 .. f+31, shifted up to end at bit 63; its lower half is bits 0 .. f-1) serve both.
 #pragma once
 #include "gt_kernels.hpp"
 
 #define GT_FIN_EL 16                              // elements of a wavefront's tile
-#define GT_FIN_ROWS 31                            // rows of material: 19 of the dealer's, 4 streams x 3 keys
+#define GT_FIN_ROWS 31                            // rows of material: 22 of the dealer's, 3 streams x 3 keys
 
 // The wavefront model with 16 lanes per party (lanes 48-63 repeat party 2's and neither store nor count): a tile starts at a multiple of
 // 8, so that its words under the three keys are whole blocks, and two dealer blocks per element, six blocks per stream make up one pass
-// of the block function (56 of 64 lanes with four streams).
+// of the block function (50 of 64 lanes with three streams).
 struct FWire : WWire {
     __device__ __forceinline__ void init(uint4 *region, u64 *s_cnt)
     {
@@ -41,7 +41,8 @@ struct FWire : WWire {
 };
 
 // Material of a tile: rows of GT_FIN_EL words.  0-2 r, 3-5 bits of r shifted up by 32 - f, 6-8 and 9 the daBit (arithmetic, both Boolean
-// ones), 10-12 r >> f, 13-15 r_63 << (64 - f), 16-18 the second daBit, then [stream][key].
+// ones), 10-12 r >> f, 13-15 r_63 << (64 - f), 16-18 the second daBit, 19-21 products of adjacent bits of the shifted r, then [stream][key]
+// of the streams 0 (opening), 1 (tree), 3 (product with ReLU's bit).
 template <int NS>
 struct FinTile {
     const u32 *keys;
@@ -57,7 +58,7 @@ struct FinTile {
 #pragma unroll
         for (int w = 0; w < 8; w++) kv.k[w] = from[w];
         u64 D[8];
-        chacha8<PRF_PAIR>(kv, dealer ? e0 + el : (e0 >> 3) + g, op, l < 16 ? 0u : (dealer ? 5u : i), D);
+        chacha8<PRF_PAIR>(kv, dealer ? e0 + el : (e0 >> 3) + g, op, l < 16 ? 0u : (dealer ? 5u : i + (i >> 1)), D);
         const u64 r = (u64)__shfl((unsigned long long)D[0], (int)el, GT_LANES);          // of the element's first block
         const u64 bits = dealer ? (l < 16 ? D[5] : D[6]) : 0, beta = bits & 1;
         const u32 b0 = (u32)(bits >> 1) & 1, b1 = (u32)(bits >> 2) & 1, bb = b0 | (b1 << 1) | ((((u32)beta ^ b0 ^ b1) & 1) << 2);
@@ -72,76 +73,118 @@ struct FinTile {
             to[160] = D[0]; to[176] = D[1]; to[192] = (r >> f) - D[0] - D[1];
             to[208] = D[2] << (64 - f); to[224] = D[3] << (64 - f); to[240] = ((r >> 63) - D[2] - D[3]) << (64 - f);
             to[256] = D[4]; to[272] = D[5]; to[288] = beta - D[4] - D[5];
+            const u64 EVEN = 0x5555555555555555ull, win = r << (32 - f), p0 = D[7] & EVEN, p1 = (D[7] >> 1) & EVEN;
+            to[304] = p0; to[320] = p1; to[336] = (win & (win >> 1) & EVEN) ^ p0 ^ p1;
         } else if (q < 6 * NS) {
 #pragma unroll
-            for (int w = 0; w < 8; w++) mat[(19 + q / 2) * GT_FIN_EL + g * 8 + w] = D[w];
+            for (int w = 0; w < 8; w++) mat[(22 + q / 2) * GT_FIN_EL + g * 8 + w] = D[w];
         }
         wave_sync();
     }
     __device__ __forceinline__ Sh pair(const WWire &W, int row) const { return Sh{ mat[(row + W.p) * GT_FIN_EL + W.t], mat[(row + W.pn) * GT_FIN_EL + W.t] }; }
-    __device__ __forceinline__ u64 za(const WWire &W, int i) const { const Sh w = pair(W, 19 + 3 * i); return w.o - w.n; }
-    __device__ __forceinline__ u64 zb(const WWire &W, int i) const { const Sh w = pair(W, 19 + 3 * i); return w.o ^ w.n; }
+    __device__ __forceinline__ u64 za(const WWire &W, int i) const { const Sh w = pair(W, 22 + 3 * i); return w.o - w.n; }
+    __device__ __forceinline__ u64 zb(const WWire &W, int i) const { const Sh w = pair(W, 22 + 3 * i); return w.o ^ w.n; }
 };
 
-// [c < r] on the low 63 bits (the prefix pairs of ge_bit_masks); low: on the low 32 bits
-__device__ __forceinline__ Sh less64(FWire &W, u64 c, Sh rho, u64 AG, u64 AE, bool act, Sh &low)
+// [c < r] of a public and a bitwise shared word on the low 63 bits (HALVES = 2) or 32, prefix pairs (G, E) as in ge_bit_masks: borrow and equality
+// of a block.  Pairs of two adjacent bits are local with the dealer's products of adjacent bits; they fill a dword for both halves: block b of a half
+// has G at bit 2b (low half) ... so that one AND on 32 bits serves G and E of all blocks of a level: a nibble holds G, E of the low
+// half's and G, E of the high half's block.  X' = (E_hi, E_hi) (G_lo, E_lo) xor (G_hi, 0).  low: the low half's borrow.
+template <int HALVES>
+__device__ __forceinline__ Sh less_tree(FWire &W, u64 c, Sh rho, Sh pr, u64 A, bool act, Sh &low)
 {
-    const u64 LOW63 = 0x7fffffffffffffffull, TOP = 0x8000000000000000ull, nc = ~c;
-    Sh G, E;
-    G.o = nc & rho.o & LOW63; G.n = nc & rho.n & LOW63;
-    E.o = rho.o & LOW63; E.n = rho.n & LOW63;
-    if (W.p == 0) E.o = ((rho.o ^ nc) & LOW63) | TOP;
-    if (W.p == 2) E.n = ((rho.n ^ nc) & LOW63) | TOP;
+    const u32 EV = 0x55555555u;
+    const u32 m0 = W.p == 0 ? ~0u : 0u, m2 = W.p == 2 ? ~0u : 0u;
+    u32 Xo[2], Xn[2];                              // G at even bits, E at odd ones, by half
 #pragma unroll
-    for (int k = 0; k < 6; k++) {
-        const int s = 1 << k;
-        const u64 sm = k == 0 ? 0x5555555555555555ull : k == 1 ? 0x1111111111111111ull
-                     : k == 2 ? 0x0101010101010101ull : k == 3 ? 0x0001000100010001ull
-                     : k == 4 ? 0x0000000100000001ull : 0x1ull;
-        Sh Eh, Gh;
-        Eh.o = E.o >> s; Eh.n = E.n >> s; Gh.o = G.o >> s; Gh.n = G.n >> s;
-        const u64 zg = (and3(Eh, G) ^ (AG >> (s - 1))) & sm;
-        if (k == 5) low = Sh{ G.o & 1, G.n & 1 };
-        if (k < 5) {
-            const u64 ze = (and3(Eh, E) ^ (AE >> (s - 1))) & sm;
-            u64 snd[2] = { zg, ze }, rcv[2];
-            W.template reshare<2>(snd, rcv, act ? 2u * (32u >> k) : 0u);
-            G.o = (Gh.o & sm) ^ zg; G.n = (Gh.n & sm) ^ rcv[0];
-            E.o = ze; E.n = rcv[1];
-        } else {
-            const u64 r = W.reshare1(zg, act ? 1u : 0u);
-            G.o = (Gh.o & sm) ^ zg; G.n = (Gh.n & sm) ^ r;
+    for (int h = 0; h < HALVES; h++) {
+        const u32 nc = ~(u32)(c >> (32 * h)), live = h == 1 ? 0x7fffffffu : ~0u;       // bit 63 does not count: (G, E) = (0, 1)
+        const u32 nl = nc & EV, nh = ((nc >> 1) | (h == 1 ? 0x40000000u : 0u)) & EV;
+        const u32 both = nl & nh;
+#pragma unroll
+        for (int w = 0; w < 2; w++) {
+            const u32 r = (u32)((w ? rho.n : rho.o) >> (32 * h)) & live, q = (u32)((w ? pr.n : pr.o) >> (32 * h)) & (h == 1 ? 0x15555555u : EV);
+            const u32 rh = (r >> 1) & EV;
+            const u32 u = nh & r, v = nl & rh;
+            const u32 G = (nh & rh) ^ (nl & (q ^ u)), E = q ^ u ^ v ^ (both & (w ? m2 : m0));
+            (w ? Xn[h] : Xo[h]) = G | (E << 1);
         }
     }
-    return G;
+    // level 1, from one or two dwords of 16 blocks into one: low half's results at bits 0, 1 of a nibble, high half's at 2, 3
+    u32 xo, xn, nresh = 0;
+    {
+        u32 l[2], e[2], g[2];
+#pragma unroll
+        for (int w = 0; w < 2; w++) {
+            const u32 a = w ? Xn[0] : Xo[0], b = HALVES == 2 ? (w ? Xn[1] : Xo[1]) : 0;
+            l[w] = (a & 0x33333333u) | (HALVES == 2 ? (b << 2) & 0xccccccccu : 0);
+            const u32 ee = ((a >> 3) & 0x11111111u) | (HALVES == 2 ? (b >> 1) & 0x44444444u : 0);
+            e[w] = ee | (ee << 1);
+            g[w] = ((a >> 2) & 0x11111111u) | (HALVES == 2 ? b & 0x44444444u : 0);
+        }
+        const u32 M = HALVES == 2 ? (u32)A : (u32)A & 0x33333333u;
+        u32 snd[1] = { and3l(e[0], e[1], l[0], l[1]) ^ M }, rcv[1];
+        W.template reshare<1>(snd, rcv);
+        xo = snd[0] ^ g[0]; xn = rcv[0] ^ g[1];
+        nresh += HALVES == 2 ? 32 : 16;
+    }
+    const u32 B = (u32)(A >> 32);
+#pragma unroll
+    for (int v = 2; v <= 4; v++) {
+        const int s = 2 << (v - 1);                // the neighbouring block's distance
+        const u32 EM = (HALVES == 2 ? 5u : 1u) * (v == 2 ? 0x01010101u : v == 3 ? 0x00010001u : 1u);
+        const u32 ho = xo >> s, hn = xn >> s;
+        const u32 eo = (ho >> 1) & EM, en = (hn >> 1) & EM;
+        const u32 M = (B >> (v == 2 ? 0 : v == 3 ? 4 : 12)) & (EM * 3);
+        u32 snd[1] = { and3l(eo | (eo << 1), en | (en << 1), xo, xn) ^ M }, rcv[1];
+        W.template reshare<1>(snd, rcv);
+        xo = snd[0] ^ (ho & EM); xn = rcv[0] ^ (hn & EM);
+        nresh += (HALVES == 2 ? 64 : 32) >> v;
+    }
+    low = Sh{ xo & 1, xn & 1 };
+    Sh all = { 0, 0 };
+    if (HALVES == 2) {
+        u32 snd[1] = { (and3l(xo >> 3, xn >> 3, xo, xn) ^ (B >> 28)) & 1 }, rcv[1];
+        W.template reshare<1>(snd, rcv);
+        all.o = snd[0] ^ ((xo >> 2) & 1); all.n = rcv[0] ^ ((xn >> 2) & 1);
+        nresh += 1;
+    }
+    W.nresh += act ? nresh : 0u;
+    return all;
 }
-// [c < r] of 32-bit words
-__device__ __forceinline__ Sh less32(FWire &W, u32 c, u32 ro, u32 rn, u32 AG, u32 AE, bool act)
+
+// Completion of a tile's elements: z the party's part of v, material dealt for the operation; returns y, with ReLU s y and the gate s.
+template <bool RELU, class TileT>
+__device__ __forceinline__ Sh finish_el(FWire &W, const TileT &T, u32 f, u64 z, bool act, Sh &gate)
 {
-    const u32 nc = ~c;
-    u32 Go = nc & ro, Gn = nc & rn, Eo = ro, En = rn;
-    if (W.p == 0) Eo ^= nc;
-    if (W.p == 2) En ^= nc;
-#pragma unroll
-    for (int k = 0; k < 5; k++) {
-        const int s = 1 << k;
-        const u32 sm = k == 0 ? 0x55555555u : k == 1 ? 0x11111111u : k == 2 ? 0x01010101u : k == 3 ? 0x00010001u : 1u;
-        const u32 eo = Eo >> s, en = En >> s;
-        const u32 zg = (and3l(eo, en, Go, Gn) ^ (AG >> (s - 1))) & sm;
-        if (k < 4) {
-            const u32 ze = (and3l(eo, en, Eo, En) ^ (AE >> (s - 1))) & sm;
-            u32 snd[2] = { zg, ze }, rcv[2];
-            W.template reshare<2>(snd, rcv);
-            Go = ((Go >> s) & sm) ^ zg; Gn = ((Gn >> s) & sm) ^ rcv[0];
-            Eo = ze; En = rcv[1];
-        } else {
-            u32 snd[1] = { zg }, rcv[1];
-            W.template reshare<1>(snd, rcv);
-            Go = ((Go >> s) & sm) ^ zg; Gn = ((Gn >> s) & sm) ^ rcv[0];
-        }
+    const int p = W.p;
+    const u64 off = RELU ? 1ull << (f + 31) : 1ull << 62;
+    const u64 c = W.open_both(z + T.za(W, 0) + T.pair(W, 0).o, act ? 64u : 0u) + ((1ull << (f - 1)) + off);
+    const u32 bits = (u32)T.mat[9 * GT_FIN_EL + W.t];
+    const Sh rho = T.pair(W, 3), d = T.pair(W, 6), one = pub(p, 1);
+    Sh low;
+    const Sh all = less_tree<RELU ? 2 : 1>(W, c << (32 - f), rho, T.pair(W, 19), T.zb(W, 1), act, low);
+    // the bits to arithmetic: one message
+    u32 fo[1] = { ((u32)low.o ^ (bits >> p)) & 1 }, fr[1];
+    u32 fn = ((u32)low.n ^ (bits >> W.pn)) & 1;
+    if (RELU) {
+        const u32 ct = (u32)(c >> (f + 31)) & 1;
+        const u32 so = (u32)(rho.o >> 63) ^ (u32)all.o ^ (p == 0 ? ct : 0), sn = (u32)(rho.n >> 63) ^ (u32)all.n ^ (p == 2 ? ct : 0);
+        fo[0] |= ((so ^ (bits >> (3 + p))) & 1) << 1;
+        fn |= ((sn ^ (bits >> (3 + W.pn))) & 1) << 1;
     }
-    W.nresh += act ? 61u : 0u;
-    return Sh{ Go, Gn };
+    W.template pass<1>(fo, fr, W.pv);
+    W.nopen += act ? (RELU ? 2u : 1u) : 0u;
+    const u32 ff = fo[0] ^ fn ^ fr[0];
+    const Sh b = ff & 1 ? one - d : d;
+    Sh y = pub(p, (c >> f) - (off >> f)) - T.pair(W, 10) - b;
+    if (!(c >> 63)) y = y + T.pair(W, 13);
+    if (RELU) {
+        const Sh d2 = T.pair(W, 16);
+        gate = ff & 2 ? one - d2 : d2;
+        y = mult_sh(W, gate, y, T.za(W, 2), act);
+    }
+    return y;
 }
 
 // ---------------------------------------------------------------------------------
@@ -245,11 +288,10 @@ __global__ __launch_bounds__(64) void k_finish(FinArgs a)
     __shared__ u64 s_cnt[6];
     __shared__ u64 s_z[SRC == FIN_RES ? 3 : 1][SRC == FIN_RES ? 8 * GT_FIN_EL + 8 : 1];
     FWire W; W.init(s_msg, s_cnt);
-    FinTile<RELU ? 4 : 3> T; T.keys = a.c.keys; T.mat = s_mat; T.f = a.f;
+    FinTile<RELU ? 3 : 2> T; T.keys = a.c.keys; T.mat = s_mat; T.f = a.f;
     const int p = W.p;
     const u32 f = a.f;
     const bool narrow = a.first + a.n <= 0xffffffffu;
-    const u64 off = RELU ? 1ull << (f + 31) : 1ull << 62;
     constexpr u32 PER = SRC == FIN_RES ? 8 : 1;                       // tiles at a time
     const u64 tiles = (a.n + GT_FIN_EL - 1) / GT_FIN_EL;
     for (u64 tile = (u64)blockIdx.x * PER, sub = 0; tile < tiles; sub++, tile += sub == PER ? (u64)(gridDim.x - 1) * PER + 1 : 1, sub = sub == PER ? 0 : sub) {
@@ -281,7 +323,6 @@ __global__ __launch_bounds__(64) void k_finish(FinArgs a)
         }
         const u64 e0 = a.first + tile * GT_FIN_EL, e = e0 + W.t;
         const bool act = tile * GT_FIN_EL + W.t < a.n;
-        const u32 on = act ? 1u : 0u;
         const u64 row = !act ? 0 : (narrow ? (u64)((u32)e / a.ncol) : e / a.ncol), col = act ? e - row * a.ncol : 0;
         u64 z = 0;
         if (act) {
@@ -291,33 +332,8 @@ __global__ __launch_bounds__(64) void k_finish(FinArgs a)
             if (a.has_bias) z += own_of(a.bias, p)[col] << f;
         }
         T.deal(a.c.op, e0);
-        z += T.za(W, 0) + T.pair(W, 0).o;
-        const u64 c = W.open_both(z, 64u * on) + ((1ull << (f - 1)) + off);
-        const u32 bits = (u32)T.mat[9 * GT_FIN_EL + W.t];
-        const Sh rho = T.pair(W, 3), d = T.pair(W, 6), one = pub(p, 1);
-        Sh low, s = { 0, 0 };
-        if (RELU) {
-            const Sh all = less64(W, c << (32 - f), rho, T.zb(W, 1), T.zb(W, 2), act, low);
-            s.o = ((rho.o >> 63) ^ all.o) & 1; s.n = ((rho.n >> 63) ^ all.n) & 1;
-            const u64 ct = (c >> (f + 31)) & 1;
-            if (p == 0) s.o ^= ct;
-            if (p == 2) s.n ^= ct;
-        } else low = less32(W, (u32)(c << (32 - f)), (u32)rho.o, (u32)rho.n, (u32)T.zb(W, 1), (u32)T.zb(W, 2), act);
-        // the bits to arithmetic: one message
-        u32 fo[1] = { ((u32)low.o ^ (bits >> p)) & 1 }, fr[1];
-        u32 fn = ((u32)low.n ^ (bits >> W.pn)) & 1;
-        if (RELU) { fo[0] |= (((u32)s.o ^ (bits >> (3 + p))) & 1) << 1; fn |= (((u32)s.n ^ (bits >> (3 + W.pn))) & 1) << 1; }
-        W.template pass<1>(fo, fr, W.pv);
-        W.nopen += (RELU ? 2u : 1u) * on;
-        const u32 ff = fo[0] ^ fn ^ fr[0];
-        const Sh b = ff & 1 ? one - d : d;
-        Sh y = Sh{ 0, 0 } - T.pair(W, 10) - b + pub(p, (c >> f) - (off >> f));
-        if (!(c >> 63)) y = y + T.pair(W, 13);
-        if (RELU) {
-            const Sh d2 = T.pair(W, 16), sa = ff & 2 ? one - d2 : d2;
-            y = mult_sh(W, sa, y, T.za(W, 3), act);
-            if (a.has_gate && act && W.real) st(a.gate, p, e, sa);
-        }
+        Sh gate, y = finish_el<RELU>(W, T, f, z, act, gate);
+        if (RELU && a.has_gate && act && W.real) st(a.gate, p, e, gate);
         if (act && W.real) {
             if (a.has_res) y = y + ld(a.res, p, e);
             st(a.y, p, e, y);

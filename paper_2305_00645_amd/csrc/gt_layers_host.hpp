@@ -37,11 +37,11 @@ struct gt_moe {
 static void acct_finish(gt_ctx *c, u64 n, bool relu)
 {
     wire_add(c, +1, n, 64); wire_add(c, -1, n, 64);
-    for (int k = 0; k < (relu ? 5 : 4); k++) wire_add(c, -1, n, 2 * ((relu ? 32u : 16u) >> k));
-    wire_add(c, -1, n, 1);
+    for (int v = 1; v <= 4; v++) wire_add(c, -1, n, (relu ? 64u : 32u) >> v);
+    if (relu) wire_add(c, -1, n, 1);
     wire_add(c, +1, n, relu ? 2 : 1);
     if (relu) wire_add(c, -1, n, 64);
-    c->acc.rounds += relu ? 9 : 7;
+    c->acc.rounds += relu ? 8 : 6;
 }
 
 struct FinOut { P6 y{}, gate{}, res{}, bias{}; bool has_res = false, has_gate = false, has_bias = false; };

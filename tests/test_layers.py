@@ -57,8 +57,8 @@ def test_dense_forward(seed, rows, din, dout, relu, bias, res):
     n = rows * dout
     bits = o.wire_bits()
     # opening to both others, the tree, the conversions, with ReLU the product
-    assert bits[0][1] == n * (64 + (2 if relu else 1)) and bits[0][2] == n * (64 + (125 + 64 if relu else 61))
-    assert o.stats()[0] == (9 if relu else 7)
+    assert bits[0][1] == n * (64 + (2 if relu else 1)) and bits[0][2] == n * (64 + (61 + 64 if relu else 30))
+    assert o.stats()[0] == (8 if relu else 6)
 
 
 @pytest.mark.parametrize("rows,din,dout,gated", [(1, 1, 1, True), (5, 3, 7, True), (4, 9, 2, False), (33, 6, 5, True)])
