@@ -12,11 +12,10 @@
 #include "gt_kernels.hpp"
 
 #define GT_FIN_EL 16                              // elements of a wavefront's tile
-#define GT_FIN_ROWS 31                            // rows of material: 22 of the dealer's, 3 streams x 3 keys
+#define GT_FIN_WORDS(NS) (22 * GT_FIN_EL + (NS) * 3 * 24)
 
-// The wavefront model with 16 lanes per party (lanes 48-63 repeat party 2's and neither store nor count): a tile starts at a multiple of
-// 8, so that its words under the three keys are whole blocks, and two dealer blocks per element, six blocks per stream make up one pass
-// of the block function (50 of 64 lanes with three streams).
+// The wavefront model with 16 lanes per party (lanes 48-63 repeat party 2's and neither store nor count): two dealer blocks per element and nine blocks
+// per stream (three groups of 8 elements that a tile can touch, three keys) make up one pass of the block function, 59 of 64 lanes with three streams.
 struct FWire : WWire {
     __device__ __forceinline__ void init(uint4 *region, u64 *s_cnt)
     {
@@ -41,22 +40,23 @@ struct FWire : WWire {
 };
 
 // Material of a tile: rows of GT_FIN_EL words.  0-2 r, 3-5 bits of r shifted up by 32 - f, 6-8 and 9 the daBit (arithmetic, both Boolean
-// ones), 10-12 r >> f, 13-15 r_63 << (64 - f), 16-18 the second daBit, 19-21 products of adjacent bits of the shifted r, then [stream][key]
-// of the streams 0 (opening), 1 (tree), 3 (product with ReLU's bit).
+// ones), 10-12 r >> f, 13-15 r_63 << (64 - f), 16-18 the second daBit, 19-21 products of adjacent bits of the shifted r, then rows of 24 words,
+// [stream][key], of the streams 0 (opening), 1 (tree), 3 (product with ReLU's bit).  A tile may start anywhere.
 template <int NS>
 struct FinTile {
     const u32 *keys;
     u64 *mat;
-    u32 f;
+    u32 f, w;                                     // w: the lane's word in the streams' rows
     __device__ __forceinline__ void deal(u32 op, u64 e0)
     {
-        const u32 l = threadIdx.x & (GT_LANES - 1), el = l & 15, q = l - 32, i = q / 6, j = (q % 6) / 2, g = q & 1;
+        const u32 l = threadIdx.x & (GT_LANES - 1), el = l & 15, q = l - 32, i = q / 9, j = (q % 9) / 3, g = q % 3;
         const bool dealer = l < 32;
+        w = ((u32)e0 & 7) + el;
         wave_sync();
         Key kv;
-        const u32 *from = keys + 8 * (dealer ? GT_KEY_DEALER : (int)(j < 3 ? j : 0));
+        const u32 *from = keys + 8 * (dealer ? GT_KEY_DEALER : (int)j);
 #pragma unroll
-        for (int w = 0; w < 8; w++) kv.k[w] = from[w];
+        for (int v = 0; v < 8; v++) kv.k[v] = from[v];
         u64 D[8];
         chacha8<PRF_PAIR>(kv, dealer ? e0 + el : (e0 >> 3) + g, op, l < 16 ? 0u : (dealer ? 5u : i + (i >> 1)), D);
         const u64 r = (u64)__shfl((unsigned long long)D[0], (int)el, GT_LANES);          // of the element's first block
@@ -75,15 +75,15 @@ struct FinTile {
             to[256] = D[4]; to[272] = D[5]; to[288] = beta - D[4] - D[5];
             const u64 EVEN = 0x5555555555555555ull, win = r << (32 - f), p0 = D[7] & EVEN, p1 = (D[7] >> 1) & EVEN;
             to[304] = p0; to[320] = p1; to[336] = (win & (win >> 1) & EVEN) ^ p0 ^ p1;
-        } else if (q < 6 * NS) {
+        } else if (q < 9 * NS) {
 #pragma unroll
-            for (int w = 0; w < 8; w++) mat[(22 + q / 2) * GT_FIN_EL + g * 8 + w] = D[w];
+            for (int v = 0; v < 8; v++) mat[22 * GT_FIN_EL + q * 8 + v] = D[v];
         }
         wave_sync();
     }
     __device__ __forceinline__ Sh pair(const WWire &W, int row) const { return Sh{ mat[(row + W.p) * GT_FIN_EL + W.t], mat[(row + W.pn) * GT_FIN_EL + W.t] }; }
-    __device__ __forceinline__ u64 za(const WWire &W, int i) const { const Sh w = pair(W, 22 + 3 * i); return w.o - w.n; }
-    __device__ __forceinline__ u64 zb(const WWire &W, int i) const { const Sh w = pair(W, 22 + 3 * i); return w.o ^ w.n; }
+    __device__ __forceinline__ u64 za(const WWire &W, int i) const { const u64 *m = mat + 22 * GT_FIN_EL + i * 72 + w; return m[W.p * 24] - m[W.pn * 24]; }
+    __device__ __forceinline__ u64 zb(const WWire &W, int i) const { const u64 *m = mat + 22 * GT_FIN_EL + i * 72 + w; return m[W.p * 24] ^ m[W.pn * 24]; }
 };
 
 // [c < r] of a public and a bitwise shared word on the low 63 bits (HALVES = 2) or 32, prefix pairs (G, E) as in ge_bit_masks: borrow and equality
@@ -284,7 +284,7 @@ template <int SRC, bool RELU>
 __global__ __launch_bounds__(64) void k_finish(FinArgs a)
 {
     __shared__ uint4 s_msg[GT_LANES];
-    __shared__ u64 s_mat[GT_FIN_ROWS * GT_FIN_EL];
+    __shared__ u64 s_mat[GT_FIN_WORDS(RELU ? 3 : 2)];
     __shared__ u64 s_cnt[6];
     __shared__ u64 s_z[SRC == FIN_RES ? 3 : 1][SRC == FIN_RES ? 8 * GT_FIN_EL + 8 : 1];
     FWire W; W.init(s_msg, s_cnt);
@@ -356,14 +356,36 @@ struct MatView { const u64 *c[3]; u64 rs, ks; };
 // turned into limbs in registers (byte permutes; a quarter of the time in which they arrive): one copy serves both passes, KC: k contiguous (the
 // transposed product of the backward pass).
 // Bound: the rate at which the weights arrive.
-struct FewArgs { const u64 *x[3]; const u64 *w; u64 *Z; u64 plane, ldx, ldw, M, N, K; u32 per, nsplit; };
+struct FewArgs { const u64 *x[3]; const u64 *w; u64 *Z; u64 plane, ldx, ldw, M, N, K; u32 per, nsplit, blocks; DivArgs div; };
+// division of a tile of elements by a workgroup of four wavefronts, as k_div<4>, in LDS that the caller has
+#define GT_DIV_BYTES (4 * GT_LANES * 16 + GT_DIV_STEPS * GT_EL_WORDS(3) * 8 + 4 * 6 * 8)
+__device__ __forceinline__ void div_block(const DivArgs &a, u64 tile, unsigned char *lds)
+{
+    uint4 (*s_msg)[GT_LANES] = (uint4 (*)[GT_LANES])lds;
+    u64 *s_mat = (u64 *)(lds + 4 * GT_LANES * 16);
+    u64 (*s_cnt)[6] = (u64 (*)[6])(lds + 4 * GT_LANES * 16 + GT_DIV_STEPS * GT_EL_WORDS(3) * 8);
+    const u32 wave = __builtin_amdgcn_readfirstlane(threadIdx.x / GT_LANES);
+    DWire W; W.init(s_msg[wave], s_cnt[wave]);
+    ElTile<3> T; T.init(a.c.keys, W, s_mat);
+    const u64 e0 = tile * GT_EL, e = e0 + W.t;
+    const bool act = W.t < GT_EL && e < a.n;
+    Sh r = { 0, 0 }, Q = { 0, 0 }, quo = { 0, 0 };
+    if (act) { Q = ld(a.Q, W.p, e); r = ld(a.S, W.p, e); }
+    div_steps_el<4>(W, T, s_mat, W.p, a.c.op, e0, el_live(e0, a.n), a.nsteps, Q, r, quo, act);
+    if (act && W.real && wave == 0) st(a.quo, W.p, e, quo);
+    W.flush(a.c.wire);
+}
 // a word at a wave-uniform address plus a lane's offset in bytes
 template <class T> __device__ __forceinline__ T ld_at(const void *base, u32 off) { return *(const T *)((const char *)base + off); }
-template <int ROWS, bool KC>
+// DIV: workgroups from `blocks` on divide (the gates of a mixture, which nothing waits for before the first product is done).
+template <int ROWS, bool KC, bool DIV>
 __global__ __launch_bounds__(256, 1) void k_mm_few(FewArgs a)
 {
     constexpr int SLOTS = ROWS == 8 ? 3 : 6, XP = ROWS / 8;           // tiles of the left factor: both factors in one, or three of each
-    __shared__ __align__(16) unsigned char s_a[2][SLOTS * 8 * 1024];  // [tile][limb][lane of the operand][16 bytes]
+    constexpr int ABYTES = SLOTS * 8 * 1024;                          // [tile][limb][lane of the operand][16 bytes], twice
+    __shared__ __align__(16) unsigned char s_lds[DIV && GT_DIV_BYTES > 2 * ABYTES ? GT_DIV_BYTES : 2 * ABYTES];
+    unsigned char (*s_a)[ABYTES] = (unsigned char (*)[ABYTES])s_lds;
+    if (DIV && blockIdx.x >= a.blocks) { if (blockIdx.y == 0) div_block(a.div, blockIdx.x - a.blocks, s_lds); return; }
     const u32 tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const u32 lr = lane & 15, kq = lane >> 4;
     const u32 split = blockIdx.x % a.nsplit;
@@ -701,88 +723,106 @@ __global__ __launch_bounds__(256) void k_colsum(ColsumArgs a)
 }
 
 // ---------------------------------------------------------------------------------
-// Mixture of experts: choice of the experts of a few tokens.
-// w[t * P + q] = [s_a >= s_b] of the q-th pair a < b (a beats b: ties go to the lower index)
+// Mixture of experts.  Operation ids from c.op on: scores, pairs, choice, chosen scores, tau + 1 of the division, inputs, hidden values, their scaling,
+// weighted hidden values, result.
 __device__ __forceinline__ void pair_of(u32 q, u32 E, u32 &a, u32 &b)
 {
     a = 0;
     while (q >= E - 1 - a) { q -= E - 1 - a; a++; }
     b = a + 1 + q;
 }
-__device__ __forceinline__ u32 pair_at(u32 a, u32 b, u32 E) { return a * (2 * E - a - 1) / 2 + b - a - 1; }      // a < b
-struct MoeArgs { KCommon c; P6 s, w, o, S, Q, g, x, xe, hg, he; u64 rows; u32 E, k, d, ff, f; };
-__global__ __launch_bounds__(64) void k_moe_pairs(MoeArgs a)
+struct MoeArgs { KCommon c; u64 *Z; P6 s, bias, o, S, Q, g, x, xe, hg, he; u64 rows; u32 E, k, d, ff, f; int parts, has_bias; };
+// The choice for a row, a workgroup: completion of the scores (parts: from the router's parts, which are left at zero, else they are there), all pairs
+// [s_a >= s_b], a < b (a beats b: ties go to the lower index), ranks (how many others beat an expert: local sums of the bits), o_j[a] = [rank of a = j] and the
+// same times 2^f behind the row's inputs, S_j = sum_a o_j[a] s_a, Q = 1 + sum_a s_a.  Bound: the chain of its rounds.
+__global__ __launch_bounds__(256) void k_moe_choose(MoeArgs a)
 {
-    GT_EL_SHARED(2, PRF_ALONE)
-    const u32 P = a.E * (a.E - 1) / 2;
-    const u64 n = a.rows * P;
-    GT_FOR_EL(n) {
-        const u64 e0 = tile_ * GT_EL, e = e0 + W.t;
-        const bool act = W.t < GT_EL && e < n;
-        Sh v = { 0, 0 };
-        if (act) {
-            u32 x, y;
-            pair_of((u32)(e % P), a.E, x, y);
-            v = ld(a.s, p, e / P * a.E + x) - ld(a.s, p, e / P * a.E + y);
-        }
-        const u32 st2[2] = { 1, 2 }, w = (u32)(e0 & 7) + W.t;
-        T.deal(W, a.c.op, e0, st2, el_live(e0, n));
-        const Dealer D = T.dealer(W);
-        const Sh b = b2a(W, p, ge_bit_masks(W, p, v, D, T.zb(W, 0, w), T.zb(W, 1, w), act), D, act);
-        if (act && W.real) st(a.w, p, e, b);
-        W.drain();
+    __shared__ uint4 s_msg[4][GT_LANES];
+    __shared__ u64 s_mat[4][GT_FIN_WORDS(3)];
+    __shared__ u64 s_cnt[4][6];
+    __shared__ u64 s_s[6][GT_MAX_EXPERTS], s_rank[6][GT_MAX_EXPERTS], s_sum[3][GT_MAX_EXPERTS];      // 2 p: own, 2 p + 1: next
+    const u32 tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), E = a.E, k = a.k;
+    const u64 t = blockIdx.x;
+    for (u32 i = tid; i < GT_MAX_EXPERTS; i += 256) {
+#pragma unroll
+        for (int q = 0; q < 6; q++) s_rank[q][i] = 0;
+#pragma unroll
+        for (int q = 0; q < 3; q++) s_sum[q][i] = 0;
     }
-    W.flush(a.c.wire);
-}
-// o[(t * k + j) * E + a] = [rank of a = j], the rank: how many others beat it; and the same times 2^f behind the row's inputs
-__global__ __launch_bounds__(64) void k_moe_hot(MoeArgs a)
-{
-    GT_EL_SHARED(1, PRF_ALONE)
-    const u64 n = a.rows * a.k * a.E, P = a.E * (a.E - 1) / 2;
-    GT_FOR_EL(n) {
-        const u64 e0 = tile_ * GT_EL, e = e0 + W.t;
-        const bool act = W.t < GT_EL && e < n;
-        Sh v = { 0, 0 };
-        const u32 x = (u32)(e % a.E);
-        if (act) {
-            const u64 t = e / ((u64)a.E * a.k);
-            for (u32 y = 0; y < a.E; y++)
-                if (y < x) v = v + ld(a.w, p, t * P + pair_at(y, x, a.E));
-                else if (y > x) v = v + pub(p, 1) - ld(a.w, p, t * P + pair_at(x, y, a.E));
-            v = v - pub(p, e / a.E % a.k);
+    {
+        FWire W; W.init(s_msg[wave], s_cnt[wave]);
+        FinTile<3> T; T.keys = a.c.keys; T.mat = s_mat[wave]; T.f = a.f;
+        for (u32 i0 = wave * GT_FIN_EL; i0 < E; i0 += 4 * GT_FIN_EL) {
+            const u32 i = i0 + W.t;
+            const bool act = i < E;
+            const u64 e = t * E + i;
+            Sh y = { 0, 0 }, gate;
+            if (a.parts) {
+                u64 z = 0;
+                if (act) {
+                    u64 *from = &a.Z[(u64)W.p * a.rows * E + e];
+                    z = *from;
+                    if (a.has_bias) z += own_of(a.bias, W.p)[i] << a.f;
+                    if (W.real) *from = 0;
+                }
+                T.deal(a.c.op, t * E + i0);
+                y = finish_el<true>(W, T, a.f, z, act, gate);
+            } else if (act) y = ld(a.s, W.p, e);
+            if (act && W.real) { s_s[2 * W.p][i] = y.o; s_s[2 * W.p + 1][i] = y.n; }
         }
-        T.deal_mask(W, a.c.op, e0, 1, el_live(e0, n));
+        W.flush(a.c.wire);
+    }
+    __syncthreads();
+    DWire W; W.init(s_msg[wave], s_cnt[wave]);
+    const int p = W.p;
+    ElTile<2> T; T.init(a.c.keys, W, s_mat[wave]);
+    const u32 P = E * (E - 1) / 2;
+    for (u32 q0 = wave * GT_EL; q0 < P; q0 += 4 * GT_EL) {
+        const u32 q = q0 + W.t;
+        const bool act = W.t < GT_EL && q < P;
+        u32 x = 0, y = 0;
+        Sh v = { 0, 0 };
+        if (act) {
+            pair_of(q, E, x, y);
+            v = Sh{ s_s[2 * p][x] - s_s[2 * p][y], s_s[2 * p + 1][x] - s_s[2 * p + 1][y] };
+        }
+        const u64 e0 = t * P + q0;
+        const u32 st2[2] = { 1, 2 }, w = (u32)(e0 & 7) + W.t;
+        T.deal(W, a.c.op + 1, e0, st2, el_live(q0, P));
+        const Dealer D = T.dealer(W);
+        const Sh b = b2a(W, p, ge_bit_masks(W, p, v, D, T.zb(W, 0, w), T.zb(W, 1, w), act), D, act), nb = pub(p, 1) - b;
+        if (act && W.real) {
+            atomicAdd((unsigned long long *)&s_rank[2 * p][y], (unsigned long long)b.o); atomicAdd((unsigned long long *)&s_rank[2 * p + 1][y], (unsigned long long)b.n);
+            atomicAdd((unsigned long long *)&s_rank[2 * p][x], (unsigned long long)nb.o); atomicAdd((unsigned long long *)&s_rank[2 * p + 1][x], (unsigned long long)nb.n);
+        }
+    }
+    __syncthreads();
+    for (u32 q0 = wave * GT_EL; q0 < k * E; q0 += 4 * GT_EL) {
+        const u32 q = q0 + W.t, x = q % E, j = q / E;
+        const bool act = W.t < GT_EL && q < k * E;
+        Sh v = { 0, 0 };
+        if (act) v = Sh{ s_rank[2 * p][x], s_rank[2 * p + 1][x] } - pub(p, j);
+        const u64 e0 = t * k * E + q0;
+        T.deal_mask(W, a.c.op + 2, e0, 1, el_live(q0, k * E));
         const Dealer D = T.dealer(W);
         const Sh b = b2a(W, p, eq_bit_mask(W, p, v, D, T.zb(W, 0, (u32)(e0 & 7) + W.t), act), D, act);
         if (act && W.real) {
-            st(a.o, p, e, b);
-            st(a.xe, p, e / a.E * ((u64)a.E * (a.d + 1)) + (u64)a.E * a.d + x, scale(b, 1ull << a.f));
+            st(a.o, p, e0 + W.t, b);
+            st(a.xe, p, (t * k + j) * ((u64)E * (a.d + 1)) + (u64)E * a.d + x, scale(b, 1ull << a.f));
+            atomicAdd((unsigned long long *)&s_sum[p][j], (unsigned long long)prod3(b, Sh{ s_s[2 * p][x], s_s[2 * p + 1][x] }));
         }
-        W.drain();
     }
-    W.flush(a.c.wire);
-}
-// S = sum_a o[a] s[a] (one reshare), Q = 1 + sum_a s[a]
-__global__ __launch_bounds__(64) void k_moe_pick(MoeArgs a)
-{
-    GT_EL_SHARED(1, PRF_ALONE)
-    const u64 n = a.rows * a.k;
-    GT_FOR_EL(n) {
-        const u64 e0 = tile_ * GT_EL, e = e0 + W.t;
-        const bool act = W.t < GT_EL && e < n;
-        Sh q = pub(p, 1), z;
-        u64 s = 0;
-        if (act)
-            for (u32 x = 0; x < a.E; x++) {
-                const Sh v = ld(a.s, p, e / a.k * a.E + x);
-                s += prod3(ld(a.o, p, e * a.E + x), v);
-                q = q + v;
-            }
-        T.deal_mask(W, a.c.op, e0, 0, 0);
-        z.o = s + T.za(W, 0, (u32)(e0 & 7) + W.t);
+    __syncthreads();
+    for (u32 q0 = wave * GT_EL; q0 < k; q0 += 4 * GT_EL) {
+        const u32 j = q0 + W.t;
+        const bool act = W.t < GT_EL && j < k;
+        const u64 e0 = t * k + q0;
+        T.deal_mask(W, a.c.op + 3, e0, 0, 0);
+        Sh Q = pub(p, 1), z;
+        for (u32 x = 0; x < E; x++) Q = Q + Sh{ s_s[2 * p][x], s_s[2 * p + 1][x] };
+        z.o = (act ? s_sum[p][j] : 0) + T.za(W, 0, (u32)(e0 & 7) + W.t);
         z.n = W.reshare1(z.o, act ? 64u : 0u);
-        if (act && W.real) { st(a.S, p, e, z); st(a.Q, p, e, q); }
-        W.drain();
+        if (act && W.real) { st(a.S, p, e0 + W.t, z); st(a.Q, p, e0 + W.t, Q); }
     }
     W.flush(a.c.wire);
 }
@@ -803,6 +843,80 @@ __global__ __launch_bounds__(64) void k_moe_spread(MoeArgs a)
         z.n = W.reshare1(z.o, act ? 64u : 0u);
         if (act && W.real) st(a.xe, p, r * (Ed + a.E) + q, z);
         W.drain();
+    }
+    W.flush(a.c.wire);
+}
+// The hidden values of a row's 16 columns, a wavefront: h_j = ReLU of the first product's parts (left at zero; operation op), hg_j = g_j h_j rounded (op + 1), and
+// he[a * ff + i] = sum_j o_j[a] hg_j[i] (op + 2, one reshare each); the row's last wavefront does sum_j o_j[a] g_j, behind them.  hg is kept in memory
+// between the steps by the lane that reads it again.
+__global__ __launch_bounds__(64) void k_moe_hidden(MoeArgs a)
+{
+    __shared__ uint4 s_msg[GT_LANES];
+    __shared__ u64 s_mat[GT_FIN_WORDS(3)];
+    __shared__ u64 s_cnt[6];
+    FWire W; W.init(s_msg, s_cnt);
+    const int p = W.p;
+    const u32 lane = threadIdx.x, k = a.k, E = a.E, ff = a.ff, ntile = (ff + GT_FIN_EL - 1) / GT_FIN_EL;
+    const u64 t = blockIdx.x / (ntile + 1), n = a.rows * k * ff, len = (u64)E * (ff + 1);
+    const u32 ft = blockIdx.x % (ntile + 1);
+    const bool tail = ft == ntile;
+    const u32 i0 = ft * GT_FIN_EL, i = i0 + W.t;
+    const bool act = !tail && i < ff;
+    if (!tail)
+        for (u32 j = 0; j < k; j++) {
+            const u64 r = t * k + j, e0 = r * ff + i0, e = e0 + W.t;
+            u64 z = 0;
+            Sh g = { 0, 0 }, gate, y;
+            if (act) {
+                u64 *from = &a.Z[(u64)p * n + e];
+                z = *from;
+                if (W.real) *from = 0;
+                g = ld(a.g, p, r);
+            }
+            {
+                FinTile<3> T; T.keys = a.c.keys; T.mat = s_mat; T.f = a.f;
+                T.deal(a.c.op, e0);
+                y = finish_el<true>(W, T, a.f, z, act, gate);
+            }
+            {
+                FinTile<2> T; T.keys = a.c.keys; T.mat = s_mat; T.f = a.f;
+                T.deal(a.c.op + 1, e0);
+                y = finish_el<false>(W, T, a.f, prod3(g, y), act, gate);
+            }
+            if (act && W.real) st(a.hg, p, e, y);
+        }
+    // words of the zero sharing: nine blocks for 16 adjacent outputs, seven such runs a pass
+    const u32 runs = tail ? (E + 15) / 16 : E, run = lane / 9, key = (lane % 9) / 3, grp = lane % 3;
+    for (u32 x0 = 0; x0 < runs; x0 += 7) {
+        const u32 x = x0 + run;
+        const u64 first = t * len + (tail ? (u64)E * ff + x * 16 : (u64)x * ff + i0);
+        wave_sync();
+        if (run < 7 && x < runs) {
+            Key kv;
+#pragma unroll
+            for (int v = 0; v < 8; v++) kv.k[v] = a.c.keys[8 * key + v];
+            u64 D[8];
+            chacha8<PRF_PAIR>(kv, (first >> 3) + grp, a.c.op + 2, 0, D);
+#pragma unroll
+            for (int v = 0; v < 8; v++) s_mat[lane * 8 + v] = D[v];
+        }
+        wave_sync();
+        const u32 most = runs - x0 < 7 ? runs - x0 : 7;
+        for (u32 q = 0; q < most; q++) {
+            const u32 y = x0 + q, ex = tail ? y * 16 + W.t : y;           // expert
+            const u64 at = t * len + (tail ? (u64)E * ff + y * 16 : (u64)y * ff + i0) + W.t;
+            const bool on = tail ? ex < E : act;
+            u64 z = 0;
+            if (on)
+                for (u32 j = 0; j < k; j++) {
+                    const u64 r = t * k + j;
+                    z += prod3(ld(a.o, p, r * E + ex), tail ? ld(a.g, p, r) : ld(a.hg, p, r * ff + i));
+                }
+            const u64 *m = s_mat + q * 72 + ((at - W.t) & 7) + W.t;
+            Sh v = { z + (m[p * 24] - m[W.pn * 24]), 0 };
+            v.n = W.reshare1(v.o, on ? 64u : 0u);
+            if (on && W.real) st(a.he, p, at, v);
+        }
     }
     W.flush(a.c.wire);
 }

@@ -31,7 +31,7 @@ struct gt_moe {
     u32 d, ff, E, k, max_rows;
     bool has_br;
     WMat Wr, W1, W2;             // biases of the experts' layers as further rows
-    DSh br, s, w, o, S, Q, g, xe, h, hg, he;
+    DSh br, s, o, S, Q, g, xe, h, hg, he;
 };
 
 static void acct_finish(gt_ctx *c, u64 n, bool relu)
@@ -116,20 +116,29 @@ static int do_dense(gt_ctx *c, MatView A, const MatView &B, u64 M, u64 N, u64 K,
     acct_finish(c, M * N, relu);
     return GT_OK;
 }
-// the same for few rows of x and weights: x (M rows of K words), W or, transposed, its rows as columns
-static int do_dense_w(gt_ctx *c, P6 x, u64 ldx, const WMat &W, bool transposed, u64 M, bool relu, const FinOut &o)
+// Parts of the product of few rows x (M rows of K words) and weights, or, transposed, the weights' rows as columns, in the workspace of
+// partial inner products; div: a division that may run beside it.
+static int few_parts(gt_ctx *c, P6 x, u64 ldx, const WMat &W, bool transposed, u64 M, const DivArgs *div = nullptr)
 {
     const u64 N = transposed ? W.K : W.N, K = transposed ? W.N : W.K;
-    if (M == 0 || !few_rows(M, ldx)) return do_dense(c, view(x, ldx, 1), transposed ? wmat(W) : wmat_t(W), M, N, K, relu, o);
     GTCHK(grow_dacc(c, 3 * M * N));
     FewArgs a{};
     for (int j = 0; j < 3; j++) a.x[j] = x.o[j];
     a.w = W.base; a.Z = c->dacc; a.plane = W.plane(); a.ldx = ldx; a.ldw = W.Np; a.M = M; a.N = N; a.K = K;
     const FewShape s = few_shape(c->simds, M, N, K);
-    a.per = s.per; a.nsplit = s.nsplit;
-    const dim3 g((unsigned)(s.ngrp * s.nsplit), (unsigned)s.ntile);
-    GTCHK(s.rows == 8 ? (transposed ? launch(c, GT_KC_DENSE, k_mm_few<8, true>, g, B256, a) : launch(c, GT_KC_DENSE, k_mm_few<8, false>, g, B256, a))
-          : (transposed ? launch(c, GT_KC_DENSE, k_mm_few<16, true>, g, B256, a) : launch(c, GT_KC_DENSE, k_mm_few<16, false>, g, B256, a)));
+    a.per = s.per; a.nsplit = s.nsplit; a.blocks = (u32)(s.ngrp * s.nsplit);
+    if (div) a.div = *div;
+    const dim3 g(a.blocks + (div ? gE(div->n).x : 0), (unsigned)s.ntile);
+    if (div) return s.rows == 8 ? launch(c, GT_KC_DENSE, k_mm_few<8, false, true>, g, B256, a) : launch(c, GT_KC_DENSE, k_mm_few<16, false, true>, g, B256, a);
+    return s.rows == 8 ? (transposed ? launch(c, GT_KC_DENSE, k_mm_few<8, true, false>, g, B256, a) : launch(c, GT_KC_DENSE, k_mm_few<8, false, false>, g, B256, a))
+           : (transposed ? launch(c, GT_KC_DENSE, k_mm_few<16, true, false>, g, B256, a) : launch(c, GT_KC_DENSE, k_mm_few<16, false, false>, g, B256, a));
+}
+// the product of x and weights, completed
+static int do_dense_w(gt_ctx *c, P6 x, u64 ldx, const WMat &W, bool transposed, u64 M, bool relu, const FinOut &o)
+{
+    const u64 N = transposed ? W.K : W.N, K = transposed ? W.N : W.K;
+    if (M == 0 || !few_rows(M, ldx)) return do_dense(c, view(x, ldx, 1), transposed ? wmat(W) : wmat_t(W), M, N, K, relu, o);
+    GTCHK(few_parts(c, x, ldx, W, transposed, M));
     return do_finish(c, FIN_PARTS, relu, M * N, (u32)N, o);
 }
 
@@ -231,14 +240,14 @@ extern "C" int gt_dense_backward(gt_ctx *c, const gt_dense *l, const gt_shares *
 static void moe_free(gt_moe *m)
 {
     for (WMat *w : { &m->Wr, &m->W1, &m->W2 }) if (w->base) (void)hipFree(w->base);
-    DSh *all[] = { &m->br, &m->s, &m->w, &m->o, &m->S, &m->Q, &m->g, &m->xe, &m->h, &m->hg, &m->he };
+    DSh *all[] = { &m->br, &m->s, &m->o, &m->S, &m->Q, &m->g, &m->xe, &m->h, &m->hg, &m->he };
     for (DSh *s : all) dsh_free(*s);
     delete m;
 }
 static int moe_init(gt_ctx *c, gt_moe *m, const gt_shares *Wr, const gt_shares *br, const gt_shares *W1, const gt_shares *b1, const gt_shares *W2,
                     const gt_shares *b2)
 {
-    const u64 E = m->E, d = m->d, ff = m->ff, rows = m->max_rows, rk = rows * m->k, P = E * (E - 1) / 2;
+    const u64 E = m->E, d = m->d, ff = m->ff, rows = m->max_rows, rk = rows * m->k;
     GTCHK(wmat_alloc(m->Wr, d, E, c->stream));
     GTCHK(wmat_alloc(m->W1, E * (d + 1), ff, c->stream));
     GTCHK(wmat_alloc(m->W2, E * (ff + 1), d, c->stream));
@@ -248,7 +257,7 @@ static int moe_init(gt_ctx *c, gt_moe *m, const gt_shares *Wr, const gt_shares *
     if (b1) GTCHK(wmat_put(c, m->W1, b1, E * d, E));
     if (b2) GTCHK(wmat_put(c, m->W2, b2, E * ff, E));
     if (br) { GTCHK(dsh_alloc(m->br, E, c->stream)); GTCHK(copy6(c, m->br.v, 0, to_p6(br), 0, E)); }
-    GTCHK(dsh_alloc(m->s, rows * E, c->stream)); GTCHK(dsh_alloc(m->w, rows * P, c->stream)); GTCHK(dsh_alloc(m->o, rk * E, c->stream));
+    GTCHK(dsh_alloc(m->s, rows * E, c->stream)); GTCHK(dsh_alloc(m->o, rk * E, c->stream));
     for (DSh *s : { &m->S, &m->Q, &m->g }) GTCHK(dsh_alloc(*s, rk, c->stream));
     GTCHK(dsh_alloc(m->xe, rk * E * (d + 1), c->stream));
     GTCHK(dsh_alloc(m->h, rk * ff, c->stream)); GTCHK(dsh_alloc(m->hg, rk * ff, c->stream));
@@ -282,37 +291,46 @@ extern "C" int gt_moe_forward(gt_ctx *c, gt_moe *m, const gt_shares *x, size_t r
     const u64 E = m->E, d = m->d, ff = m->ff, rk = rows * m->k, P = E * (E - 1) / 2;
     if (!shares_ok(x, rows * d) || !shares_ok(y, rows * d) || (res && !shares_ok(res, rows * d))) return GT_EINVAL;
     Timed T(c);
+    const bool few = rk && few_rows(rk, E * (d + 1)) && few_rows(rows, E * (ff + 1));     // parts of the products by k_mm_few, else results
     MoeArgs a{};
-    a.s = m->s.v; a.w = m->w.v; a.o = m->o.v; a.S = m->S.v; a.Q = m->Q.v; a.g = m->g.v; a.x = to_p6(x); a.xe = m->xe.v; a.hg = m->hg.v; a.he = m->he.v;
-    a.rows = rows; a.E = (u32)E; a.k = m->k; a.d = m->d; a.ff = m->ff; a.f = c->tau;
+    a.s = m->s.v; a.bias = m->br.v; a.o = m->o.v; a.S = m->S.v; a.Q = m->Q.v; a.g = m->g.v; a.x = to_p6(x); a.xe = m->xe.v; a.hg = m->hg.v; a.he = m->he.v;
+    a.rows = rows; a.E = (u32)E; a.k = m->k; a.d = m->d; a.ff = m->ff; a.f = c->tau; a.parts = few; a.has_bias = m->has_br;
     FinOut o;
     o.y = m->s.v;
     if (m->has_br) { o.has_bias = true; o.bias = m->br.v; }
-    GTCHK(do_dense_w(c, a.x, d, m->Wr, false, rows, true, o));
-    a.c = kc(c, c->op++);
-    if (rows * P) GTCHK(launch(c, GT_KC_SMALL, k_moe_pairs, gE(rows * P), B64, a));
+    a.c = kc(c, c->op);
+    if (few) { GTCHK(few_parts(c, a.x, d, m->Wr, false, rows)); acct_finish(c, rows * E, true); c->op++; }
+    else GTCHK(do_dense_w(c, a.x, d, m->Wr, false, rows, true, o));
+    a.Z = c->dacc;
+    if (rk) GTCHK(launch(c, GT_KC_SMALL, k_moe_choose, dim3((unsigned)rows), B256, a));
     acct_ge(c, rows * P); acct_b2a(c, rows * P);
-    a.c = kc(c, c->op++);
-    if (rk) GTCHK(launch(c, GT_KC_SMALL, k_moe_hot, gE(rk * E), B64, a));
     acct_eq(c, rk * E); acct_b2a(c, rk * E);
-    a.c = kc(c, c->op++);
-    if (rk) GTCHK(launch(c, GT_KC_SMALL, k_moe_pick, gE(rk), B64, a));
     acct_reshare(c, rk, 1);
+    c->op += 3;
     DivArgs q{}; q.c = kc(c, c->op); q.S = m->S.v; q.Q = m->Q.v; q.quo = m->g.v; q.n = rk; q.nsteps = c->tau + 1;
     c->op += c->tau + 1;
-    if (rk) GTCHK(few_elements(c, rk) ? launch(c, GT_KC_SMALL, k_div<4>, gE(rk), dim3(4 * GT_LANES), q) : launch(c, GT_KC_SMALL, k_div<1>, gE(rk), B64, q));
     acct_div(c, rk);
     a.c = kc(c, c->op++);
     if (rk) GTCHK(launch(c, GT_KC_MULT, k_moe_spread, gE(rk * E * d), B64, a));
     acct_reshare(c, rk * E * d, 1);
-    FinOut oh;
-    oh.y = m->h.v;
-    GTCHK(do_dense_w(c, m->xe.v, E * (d + 1), m->W1, false, rk, true, oh));
-    FinOut og;
-    og.y = m->hg.v;
-    GTCHK(do_finish(c, FIN_SCALE, false, rk * ff, m->ff, og, m->g.v, m->h.v));
-    a.c = kc(c, c->op++);
-    if (rk) GTCHK(launch(c, GT_KC_MULT, k_moe_gather, gE(rows * E * (ff + 1)), B64, a));
+    if (few) {
+        GTCHK(few_parts(c, m->xe.v, E * (d + 1), m->W1, false, rk, &q));
+        a.c = kc(c, c->op); a.Z = c->dacc;
+        const u64 blocks = rows * ((ff + GT_FIN_EL - 1) / GT_FIN_EL + 1);
+        GTCHK(launch(c, GT_KC_FINISH, k_moe_hidden, dim3((unsigned)blocks), B64, a));
+        acct_finish(c, rk * ff, true); acct_finish(c, rk * ff, false);
+        c->op += 3;
+    } else {
+        if (rk) GTCHK(few_elements(c, rk) ? launch(c, GT_KC_SMALL, k_div<4>, gE(rk), dim3(4 * GT_LANES), q) : launch(c, GT_KC_SMALL, k_div<1>, gE(rk), B64, q));
+        FinOut oh;
+        oh.y = m->h.v;
+        GTCHK(do_dense_w(c, m->xe.v, E * (d + 1), m->W1, false, rk, true, oh));
+        FinOut og;
+        og.y = m->hg.v;
+        GTCHK(do_finish(c, FIN_SCALE, false, rk * ff, m->ff, og, m->g.v, m->h.v));
+        a.c = kc(c, c->op++);
+        if (rk) GTCHK(launch(c, GT_KC_MULT, k_moe_gather, gE(rows * E * (ff + 1)), B64, a));
+    }
     acct_reshare(c, rows * E * (ff + 1), 1);
     FinOut oy;
     oy.y = to_p6(y);
