@@ -344,19 +344,31 @@ __global__ __launch_bounds__(64) void k_finish(FinArgs a)
 }
 
 // ---------------------------------------------------------------------------------
-// A matrix of shared words by component, element (row, k) at c[j][row * rs + k * ks].
-struct MatView { const u64 *c[3]; u64 rs, ks; };
+// A matrix of shared words by component, element (row, k) at c[j][row * rs + k * ks], or weights (tiled): 1: rows are their columns, 2: their rows.
+// Weights lie in tiles of 64 rows x 16 columns in the order in which a wavefront of k_mm_few takes them, [block of 16 columns][64 rows]
+// [component][8][64 lanes][2 words]: lane n % 16 + 16 (k % 64 / 16) has the 16 words of its column in pairs, so that a step of a wavefront is 24 KB on end (with
+// rows of words, 128 bytes at a time, 2.8-3.4 TB/s).
+#define GT_WTILE 1024
+struct MatView { const u64 *c[3]; u64 rs, ks; u32 tiled, nst; };
+__device__ __host__ __forceinline__ u64 wtile_at(u64 k, u64 n, u32 nst)
+{
+    return ((n >> 4) * nst + (k >> 6)) * (3 * GT_WTILE) + ((k & 15) >> 1) * 128 + ((n & 15) + (k & 48)) * 2 + (k & 1);
+}
+__device__ __forceinline__ u64 mat_at(const MatView &m, u64 r, u64 k)
+{
+    return m.tiled == 0 ? r * m.rs + k * m.ks : m.tiled == 1 ? wtile_at(k, r, m.nst) : wtile_at(r, k, m.nst);
+}
 
 // Parts of the product of a few rows with a weight matrix, on the matrix cores in signed 8-bit limbs (36 products of
 // limbs per ring product, as in k_count).  A wavefront owns 16 columns, a workgroup 64 and `per` steps of 64 terms of the long axis;
 // the splits' parts meet by atomic adds of 64-bit words (exact, order-free).  z_p = (x_p + x_{p+1}) w_p + x_p w_{p+1}: the sum is made of
 // the few rows' words, so each component of the weights is read once and meets both factors.  Up to 8 rows both factors share a 16-row tile:
 //   rows 0-7: x_j + x_{j+1} -> z_j     rows 8-15: x_{j-1} -> z_{j-1}      (times w_j)
-// so that a term costs 36 instructions a component and not 72.  The weights stay words in memory, 24 bytes each, and are
+// so that a term costs 36 instructions a component and not 72.  The weights stay words in memory, 24 bytes each (tiles, see MatView), and are
 // turned into limbs in registers (byte permutes; a quarter of the time in which they arrive): one copy serves both passes, KC: k contiguous (the
 // transposed product of the backward pass).
 // Bound: the rate at which the weights arrive.
-struct FewArgs { const u64 *x[3]; const u64 *w; u64 *Z; u64 plane, ldx, ldw, M, N, K; u32 per, nsplit, blocks; DivArgs div; };
+struct FewArgs { const u64 *x[3]; const u64 *w; u64 *Z; u64 ldx, M, N, K; u32 nst, per, nsplit, blocks; DivArgs div; };
 // division of a tile of elements by a workgroup of four wavefronts, as k_div<4>, in LDS that the caller has
 #define GT_DIV_BYTES (4 * GT_LANES * 16 + GT_DIV_STEPS * GT_EL_WORDS(3) * 8 + 4 * 6 * 8)
 __device__ __forceinline__ void div_block(const DivArgs &a, u64 tile, unsigned char *lds)
@@ -431,14 +443,15 @@ __global__ __launch_bounds__(256, 1) void k_mm_few(FewArgs a)
         }
     };
     u64 raw[3][16];
-    const u32 ldw = (u32)a.ldw, woff = (KC ? lr * ldw + kq * 16 : kq * 16 * ldw + lr) * 8;
-    const u64 *w0 = a.w + (KC ? c0 * ldw : c0);
+    // transposed: column c0 + lr is row c0 + lr of the weights, the 16 terms from 16 kq on lie in one tile
+    const u32 woff = KC ? (kq * a.nst * 3 * GT_WTILE + (lr >> 1) * 128 + (lr & 1)) * 8 : lane * 16;
+    const u64 *w0 = a.w + (KC ? (c0 >> 6) * (3 * GT_WTILE) + (c0 & 48) * 2 : (c0 >> 4) * a.nst * (3 * GT_WTILE));
     auto load = [&](int j, u32 s) {
-        const u64 *from = w0 + (u64)j * a.plane + (KC ? (u64)s * 64 : (u64)s * 64 * ldw);
+        const u64 *from = w0 + (u64)j * GT_WTILE + (KC ? (u64)s * 4 * a.nst : (u64)s) * (3 * GT_WTILE);
 #pragma unroll
         for (int i = 0; i < 16; i += 2) {
-            if (KC) { const ulonglong2 v = ld_at<ulonglong2>(from + i, woff); raw[j][i] = v.x; raw[j][i + 1] = v.y; }
-            else { raw[j][i] = ld_at<u64>(from + (u64)i * ldw, woff); raw[j][i + 1] = ld_at<u64>(from + (u64)(i + 1) * ldw, woff); }
+            if (KC) { raw[j][i] = ld_at<u64>(from, woff + i * 16); raw[j][i + 1] = ld_at<u64>(from, woff + i * 16 + 16); }
+            else { const ulonglong2 v = ld_at<ulonglong2>(from, woff + i * 512); raw[j][i] = v.x; raw[j][i + 1] = v.y; }
         }
     };
     v4i acc[3][8];
@@ -545,7 +558,7 @@ __global__ __launch_bounds__(256) void k_residues(ResArgs a)
 #pragma unroll
         for (int i = 0; i < 16; i++) {
             const u64 r = (u64)rb * 32 + (KC ? 2 * i + hi : lr), k = (u64)kb * 32 + (KC ? lr : hi * 16 + i);
-            const u64 at = (r < a.rows ? r : a.rows - 1) * a.x.rs + (a.k0 + (k < a.K ? k : a.K - 1)) * a.x.ks;
+            const u64 at = mat_at(a.x, r < a.rows ? r : a.rows - 1, a.k0 + (k < a.K ? k : a.K - 1));
             x[i] = x0[at];
             t[i] = sum ? x1[at] : 0;
         }
@@ -684,15 +697,15 @@ __global__ __launch_bounds__(256, WM == 4 ? 2 : 4) void k_rns_mm(RmmArgs a)
     }
 }
 
-// components (own planes) of a rows x cols matrix into a padded one, rows from row0 on; padding stays at zero
-struct PutArgs { P6 src; u64 *dst; u64 plane, ld, row0, rows, cols; };
+// components (own planes) of a rows x cols matrix into the tiles of weights, rows from row0 on; padding stays at zero
+struct PutArgs { P6 src; u64 *dst; u64 row0, rows, cols; u32 nst; };
 __global__ __launch_bounds__(256) void k_put(PutArgs a)
 {
     const u64 n = a.rows * a.cols;
     for (u64 e = (u64)blockIdx.x * blockDim.x + threadIdx.x; e < n; e += (u64)gridDim.x * blockDim.x) {
-        const u64 r = e / a.cols, to = (a.row0 + r) * a.ld + (e - r * a.cols);
+        const u64 r = e / a.cols, to = wtile_at(a.row0 + r, e - r * a.cols, a.nst);
 #pragma unroll
-        for (int j = 0; j < 3; j++) a.dst[j * a.plane + to] = a.src.o[j][e];
+        for (int j = 0; j < 3; j++) a.dst[(u64)j * GT_WTILE + to] = a.src.o[j][e];
     }
 }
 
@@ -846,24 +859,26 @@ __global__ __launch_bounds__(64) void k_moe_spread(MoeArgs a)
     }
     W.flush(a.c.wire);
 }
-// The hidden values of a row's 16 columns, a wavefront: h_j = ReLU of the first product's parts (left at zero; operation op), hg_j = g_j h_j rounded (op + 1), and
-// he[a * ff + i] = sum_j o_j[a] hg_j[i] (op + 2, one reshare each); the row's last wavefront does sum_j o_j[a] g_j, behind them.  hg is kept in memory
-// between the steps by the lane that reads it again.
-__global__ __launch_bounds__(64) void k_moe_hidden(MoeArgs a)
+// The hidden values of 16 columns of a row, a workgroup: h_j = ReLU of the first product's parts (left at zero; operation op), hg_j = g_j h_j rounded (op + 1), a
+// wavefront per choice j, then he[a * ff + i] = sum_j o_j[a] hg_j[i] (op + 2, one reshare each), a wavefront per seven experts; the row's last workgroup does
+// sum_j o_j[a] g_j, behind them.
+__global__ __launch_bounds__(256) void k_moe_hidden(MoeArgs a)
 {
-    __shared__ uint4 s_msg[GT_LANES];
-    __shared__ u64 s_mat[GT_FIN_WORDS(3)];
-    __shared__ u64 s_cnt[6];
-    FWire W; W.init(s_msg, s_cnt);
+    __shared__ uint4 s_msg[4][GT_LANES];
+    __shared__ u64 s_all[4][GT_FIN_WORDS(3)];
+    __shared__ u64 s_cnt[4][6];
+    const u32 wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    u64 *s_mat = s_all[wave];
+    FWire W; W.init(s_msg[wave], s_cnt[wave]);
     const int p = W.p;
-    const u32 lane = threadIdx.x, k = a.k, E = a.E, ff = a.ff, ntile = (ff + GT_FIN_EL - 1) / GT_FIN_EL;
+    const u32 k = a.k, E = a.E, ff = a.ff, ntile = (ff + GT_FIN_EL - 1) / GT_FIN_EL;
     const u64 t = blockIdx.x / (ntile + 1), n = a.rows * k * ff, len = (u64)E * (ff + 1);
     const u32 ft = blockIdx.x % (ntile + 1);
     const bool tail = ft == ntile;
     const u32 i0 = ft * GT_FIN_EL, i = i0 + W.t;
     const bool act = !tail && i < ff;
     if (!tail)
-        for (u32 j = 0; j < k; j++) {
+        for (u32 j = wave; j < k; j += 4) {
             const u64 r = t * k + j, e0 = r * ff + i0, e = e0 + W.t;
             u64 z = 0;
             Sh g = { 0, 0 }, gate, y;
@@ -885,13 +900,15 @@ __global__ __launch_bounds__(64) void k_moe_hidden(MoeArgs a)
             }
             if (act && W.real) st(a.hg, p, e, y);
         }
+    __syncthreads();
     // words of the zero sharing: nine blocks for 16 adjacent outputs, seven such runs a pass
     const u32 runs = tail ? (E + 15) / 16 : E, run = lane / 9, key = (lane % 9) / 3, grp = lane % 3;
-    for (u32 x0 = 0; x0 < runs; x0 += 7) {
+    const u32 per = runs <= 28 ? (runs + 3) / 4 : 7;                       // runs of a wavefront at a time
+    for (u32 x0 = wave * per; x0 < runs; x0 += 4 * per) {
         const u32 x = x0 + run;
         const u64 first = t * len + (tail ? (u64)E * ff + x * 16 : (u64)x * ff + i0);
         wave_sync();
-        if (run < 7 && x < runs) {
+        if (run < per && x < runs) {
             Key kv;
 #pragma unroll
             for (int v = 0; v < 8; v++) kv.k[v] = a.c.keys[8 * key + v];
@@ -901,7 +918,7 @@ __global__ __launch_bounds__(64) void k_moe_hidden(MoeArgs a)
             for (int v = 0; v < 8; v++) s_mat[lane * 8 + v] = D[v];
         }
         wave_sync();
-        const u32 most = runs - x0 < 7 ? runs - x0 : 7;
+        const u32 most = runs - x0 < per ? runs - x0 : per;
         for (u32 q = 0; q < most; q++) {
             const u32 y = x0 + q, ex = tail ? y * 16 + W.t : y;           // expert
             const u64 at = t * len + (tail ? (u64)E * ff + y * 16 : (u64)y * ff + i0) + W.t;

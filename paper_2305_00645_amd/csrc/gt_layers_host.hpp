@@ -1,16 +1,16 @@
 // Host side of the layers: argument checks, the operation schedule, message accounting, launches (part of gtree.hip).
 #pragma once
 
-// Words of a weight matrix by component, rows padded to a multiple of 64, columns to one of 16, zero there.
+// Words of a weight matrix in tiles (see MatView), rows and columns padded to multiples of 64, zero there.
 struct WMat {
     u64 *base = nullptr;
-    u64 K = 0, N = 0, Kp = 0, Np = 0;
-    u64 plane() const { return Kp * Np; }
+    u64 K = 0, N = 0;
+    u32 nst = 0;                 // tiles of 64 rows
 };
 static int wmat_alloc(WMat &w, u64 K, u64 N, hipStream_t st)
 {
-    w.K = K; w.N = N; w.Kp = (K + 63) & ~(u64)63; w.Np = (N + 15) & ~(u64)15;
-    const u64 words = 3 * w.plane() + 64;                  // a step of the transposed product reads up to 48 words past a row
+    w.K = K; w.N = N; w.nst = (u32)((K + 63) / 64);
+    const u64 words = (N + 63) / 64 * 4 * w.nst * 3 * GT_WTILE;
     if (hipMalloc(&w.base, words * 8) != hipSuccess) { w.base = nullptr; return GT_ENOMEM; }
     HIPCHK(hipMemsetAsync(w.base, 0, words * 8, st));
     return GT_OK;
@@ -18,13 +18,14 @@ static int wmat_alloc(WMat &w, u64 K, u64 N, hipStream_t st)
 static int wmat_put(gt_ctx *c, const WMat &w, const gt_shares *src, u64 row0, u64 rows)
 {
     PutArgs a{};
-    a.src = to_p6(src); a.dst = w.base; a.plane = w.plane(); a.ld = w.Np; a.row0 = row0; a.rows = rows; a.cols = w.N;
+    a.src = to_p6(src); a.dst = w.base; a.row0 = row0; a.rows = rows; a.cols = w.N; a.nst = w.nst;
     return launch(c, GT_KC_LOCAL, k_put, g1(rows * w.N), B256, a);
 }
+static MatView wview(const WMat &w, u32 tiled) { MatView v{}; for (int j = 0; j < 3; j++) v.c[j] = w.base + (u64)j * GT_WTILE; v.tiled = tiled; v.nst = w.nst; return v; }
 // rows: the matrix's columns (outputs), k: its rows
-static MatView wmat_t(const WMat &w) { MatView v; for (int j = 0; j < 3; j++) v.c[j] = w.base + j * w.plane(); v.rs = 1; v.ks = w.Np; return v; }
-static MatView wmat(const WMat &w) { MatView v; for (int j = 0; j < 3; j++) v.c[j] = w.base + j * w.plane(); v.rs = w.Np; v.ks = 1; return v; }
-static MatView view(P6 a, u64 rs, u64 ks) { MatView v; for (int j = 0; j < 3; j++) v.c[j] = a.o[j]; v.rs = rs; v.ks = ks; return v; }
+static MatView wmat_t(const WMat &w) { return wview(w, 1); }
+static MatView wmat(const WMat &w) { return wview(w, 2); }
+static MatView view(P6 a, u64 rs, u64 ks) { MatView v{}; for (int j = 0; j < 3; j++) v.c[j] = a.o[j]; v.rs = rs; v.ks = ks; return v; }
 
 struct gt_dense { u32 din, dout; bool has_b; WMat W; DSh b; };
 struct gt_moe {
@@ -96,7 +97,7 @@ static int do_dense(gt_ctx *c, MatView A, const MatView &B, u64 M, u64 N, u64 K,
         const u64 abytes = (asums ? 6 : 3) * RNS_N * amat, bbytes = (asums ? 3 : 6) * RNS_N * bmat, rbytes = 3 * RNS_N * plane;
         GTCHK(grow_res(c, abytes + bbytes + nchunk * rbytes));
         MatView Ar = A;
-        for (int j = 0; j < 3; j++) Ar.c[j] += r0 * A.rs;
+        for (int j = 0; j < 3; j++) Ar.c[j] += r0 * A.rs;          // (A is no tiled matrix)
         for (u32 ch = 0; ch < nchunk; ch++) {
             const u64 k0 = (u64)ch * RNS_TERMS, k = std::min<u64>(K - k0, RNS_TERMS);
             const u32 kb = (u32)((k + 63) / 64 * 2);
@@ -124,7 +125,7 @@ static int few_parts(gt_ctx *c, P6 x, u64 ldx, const WMat &W, bool transposed, u
     GTCHK(grow_dacc(c, 3 * M * N));
     FewArgs a{};
     for (int j = 0; j < 3; j++) a.x[j] = x.o[j];
-    a.w = W.base; a.Z = c->dacc; a.plane = W.plane(); a.ldx = ldx; a.ldw = W.Np; a.M = M; a.N = N; a.K = K;
+    a.w = W.base; a.Z = c->dacc; a.nst = W.nst; a.ldx = ldx; a.M = M; a.N = N; a.K = K;
     const FewShape s = few_shape(c->simds, M, N, K);
     a.per = s.per; a.nsplit = s.nsplit; a.blocks = (u32)(s.ngrp * s.nsplit);
     if (div) a.div = *div;
@@ -317,7 +318,7 @@ extern "C" int gt_moe_forward(gt_ctx *c, gt_moe *m, const gt_shares *x, size_t r
         GTCHK(few_parts(c, m->xe.v, E * (d + 1), m->W1, false, rk, &q));
         a.c = kc(c, c->op); a.Z = c->dacc;
         const u64 blocks = rows * ((ff + GT_FIN_EL - 1) / GT_FIN_EL + 1);
-        GTCHK(launch(c, GT_KC_FINISH, k_moe_hidden, dim3((unsigned)blocks), B64, a));
+        GTCHK(launch(c, GT_KC_FINISH, k_moe_hidden, dim3((unsigned)blocks), B256, a));
         acct_finish(c, rk * ff, true); acct_finish(c, rk * ff, false);
         c->op += 3;
     } else {
