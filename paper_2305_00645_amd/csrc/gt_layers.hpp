@@ -460,7 +460,9 @@ __global__ __launch_bounds__(256, 1) void k_mm_few(FewArgs a)
 #pragma unroll
         for (int u = 0; u < 8; u++) acc[j][u] = v4i{ 0, 0, 0, 0 };
     auto step = [&](u32 s, int buf, bool more) {
+        // (the fences keep the loads of the next step where they are: the compiler moves them to the end of the step to save registers)
         if (more && wave < 3) fetch(s + 1);
+        __builtin_amdgcn_sched_barrier(0);
         if (cols) {
 #pragma unroll
             for (int j = 0; j < 3; j++) {
@@ -474,6 +476,7 @@ __global__ __launch_bounds__(256, 1) void k_mm_few(FewArgs a)
                     for (int i = 0; i < 8; i++) B[i] = v4i{ (int)(u32)y[i], (int)(u32)(y[i] >> 32), (int)(u32)z[i], (int)(u32)(z[i] >> 32) };
                 }
                 if (more) load(j, s + 1);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int h = 0; h < (ROWS == 8 ? 1 : 2); h++) {
                     // the sums' tile with w_j gives z_j; x_{j-1} with w_j gives z_{j-1}
@@ -486,6 +489,7 @@ __global__ __launch_bounds__(256, 1) void k_mm_few(FewArgs a)
                         for (int t = 0; t < 8 - sl; t++) acc[to][sl + t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(A, B[t], acc[to][sl + t], 0, 0, 0);
                     }
                 }
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
         if (more && wave < 3) put(s + 1, buf ^ 1);
