@@ -9,6 +9,7 @@
 // f+31 of c - r is set, and the borrow into that bit is the root of the tree whose lower half is the borrow of the rounding; so one
 // opening and one tree (over bits 0 .. f+31, shifted up to end at bit 63; its lower half is bits 0 .. f-1) serve both.
 #pragma once
+#include <type_traits>
 #include "gt_kernels.hpp"
 
 #define GT_FIN_EL 16                              // elements of a wavefront's tile
@@ -347,7 +348,7 @@ __global__ __launch_bounds__(64) void k_finish(FinArgs a)
 // A matrix of shared words by component, element (row, k) at c[j][row * rs + k * ks], or weights (tiled): 1: rows are their columns, 2: their rows.
 // Weights lie in tiles of 64 rows x 16 columns in the order in which a wavefront of k_mm_few takes them, [block of 16 columns][64 rows]
 // [component][8][64 lanes][2 words]: lane n % 16 + 16 (k % 64 / 16) has the 16 words of its column in pairs, so that a step of a wavefront is 24 KB on end (with
-// rows of words, 128 bytes at a time, 2.8-3.4 TB/s).
+// rows of words, 128 bytes at a time, 2.8-3.4 TB/s).  A word is kept as its eight signed bytes d_s, sum of d_s 256^s.
 #define GT_WTILE 1024
 struct MatView { const u64 *c[3]; u64 rs, ks; u32 tiled, nst; };
 __device__ __host__ __forceinline__ u64 wtile_at(u64 k, u64 n, u32 nst)
@@ -369,6 +370,7 @@ __device__ __forceinline__ u64 mat_at(const MatView &m, u64 r, u64 k)
 // transposed product of the backward pass).
 // Bound: the rate at which the weights arrive.
 struct FewArgs { const u64 *x[3]; const u64 *w; u64 *Z; u64 ldx, M, N, K; u32 nst, per, nsplit, blocks; DivArgs div; };
+#define GT_FEW_PAD 66                             // words between the rows of the staging area
 // division of a tile of elements by a workgroup of four wavefronts, as k_div<4>, in LDS that the caller has
 #define GT_DIV_BYTES (4 * GT_LANES * 16 + GT_DIV_STEPS * GT_EL_WORDS(3) * 8 + 4 * 6 * 8)
 __device__ __forceinline__ void div_block(const DivArgs &a, u64 tile, unsigned char *lds)
@@ -395,7 +397,8 @@ __global__ __launch_bounds__(256, 1) void k_mm_few(FewArgs a)
 {
     constexpr int SLOTS = ROWS == 8 ? 3 : 6, XP = ROWS / 8;           // tiles of the left factor: both factors in one, or three of each
     constexpr int ABYTES = SLOTS * 8 * 1024;                          // [tile][limb][lane of the operand][16 bytes], twice
-    __shared__ __align__(16) unsigned char s_lds[DIV && GT_DIV_BYTES > 2 * ABYTES ? GT_DIV_BYTES : 2 * ABYTES];
+    constexpr int BYTES = 2 * ABYTES + 3 * 2 * 8 * GT_FEW_PAD * 8;
+    __shared__ __align__(16) unsigned char s_lds[DIV && GT_DIV_BYTES > BYTES ? GT_DIV_BYTES : BYTES];
     unsigned char (*s_a)[ABYTES] = (unsigned char (*)[ABYTES])s_lds;
     if (DIV && blockIdx.x >= a.blocks) { if (blockIdx.y == 0) div_block(a.div, blockIdx.x - a.blocks, s_lds); return; }
     const u32 tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -405,34 +408,37 @@ __global__ __launch_bounds__(256, 1) void k_mm_few(FewArgs a)
     const u32 nsteps = (u32)((a.K + 63) / 64), s0 = split * a.per, s1 = s0 + a.per < nsteps ? s0 + a.per : nsteps;
     const bool cols = c0 < a.N;                                      // whole wavefront; it takes part in the barriers
     const u32 nrow = a.M - r0 < (u64)ROWS ? (u32)(a.M - r0) : ROWS, K = (u32)a.K, ldx = (u32)a.ldx;
-    // The left factor: wavefront j < 3 makes x_j + x_{j+1} (tile j) and x_j (meets w_{j+1}), a lane eight terms of a row.
+    // The left factor: wavefront j < 3 makes x_j + x_{j+1} (tile j) and x_j (meets w_{j+1}).  A lane loads one term of every row (whole lines; with eight
+    // terms of a row per lane the 64 lines of every load took longer than the weights), and takes eight of a row through LDS.
     const u64 *xa = (wave == 0 ? a.x[0] : wave == 1 ? a.x[1] : a.x[2]) + r0 * a.ldx, *xb = (wave == 0 ? a.x[1] : wave == 1 ? a.x[2] : a.x[0]) + r0 * a.ldx;
-    const u32 xr = lane >> 3, xg = lane & 7;
-    u64 va[XP][8], vb[XP][8];
+    u64 *stage = (u64 *)(s_lds + 2 * ABYTES) + (wave < 3 ? wave : 0) * (2 * 8 * GT_FEW_PAD);
+    u64 va[ROWS], vb[ROWS];
     auto fetch = [&](u32 s) {
+        const u32 k = s * 64 + lane, at = (k < K ? k : K - 1) * 8;
 #pragma unroll
-        for (int q = 0; q < XP; q++) {
-            const u32 r = xr + 8 * q, base = (r < nrow ? r : 0) * ldx, k0 = s * 64 + xg * 8;
-#pragma unroll
-            for (int i = 0; i < 8; i++) {                             // (words that exist where these do not: loads without branches)
-                const u32 at = (base + (k0 + i < K ? k0 + i : K - 1)) * 8;
-                va[q][i] = ld_at<u64>(xa, at); vb[q][i] = ld_at<u64>(xb, at);
-            }
+        for (int r = 0; r < ROWS; r++) {                              // (words that exist where these do not: loads without branches)
+            const u64 row = (u64)((u32)r < nrow ? r : 0) * ldx;
+            va[r] = ld_at<u64>(xa + row, at); vb[r] = ld_at<u64>(xb + row, at);
         }
     };
     auto put = [&](u32 s, int buf) {
+        const u32 xr = lane >> 3, xg = lane & 7;
+        // (rows that do not exist make sums that nobody stores; terms that do not exist meet weights that are zero)
 #pragma unroll
         for (int q = 0; q < XP; q++) {
-            const u32 r = xr + 8 * q, k0 = s * 64 + xg * 8;
-            const bool on = r < nrow;
-            u64 ys[8], yp[8];
+            wave_sync();
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const u64 live = 0 - (u64)(on && k0 + i < K);
-                ys[i] = (((va[q][i] + vb[q][i]) + GT_BIAS) ^ GT_BIAS) & live;
-                yp[i] = ((va[q][i] + GT_BIAS) ^ GT_BIAS) & live;
+            for (int r = 0; r < 8; r++) {
+                const u64 x = va[r + 8 * q], y = x + vb[r + 8 * q];
+                stage[r * GT_FEW_PAD + lane] = (y + GT_BIAS) ^ GT_BIAS;
+                stage[(8 + r) * GT_FEW_PAD + lane] = (x + GT_BIAS) ^ GT_BIAS;
             }
+            wave_sync();
+            u64 ys[8], yp[8];
+            ld8_whole(stage + xr * GT_FEW_PAD + xg * 8, ys);
+            ld8_whole(stage + (8 + xr) * GT_FEW_PAD + xg * 8, yp);
             transpose8x8(ys); transpose8x8(yp);
+            const u32 r = xr + 8 * q;
             const u32 slot = ROWS == 8 ? (wave == 2 ? 0 : wave + 1) : 3 + wave, row = ROWS == 8 ? 8 + r : r;     // of the component
             unsigned char *to = s_a[buf] + 256 * (xg >> 1) + 8 * (xg & 1);
 #pragma unroll
@@ -459,24 +465,29 @@ __global__ __launch_bounds__(256, 1) void k_mm_few(FewArgs a)
     for (int j = 0; j < 3; j++)
 #pragma unroll
         for (int u = 0; u < 8; u++) acc[j][u] = v4i{ 0, 0, 0, 0 };
-    auto step = [&](u32 s, int buf, bool more) {
+    v4i B[2][8];
+    // limbs of a component's words: byte permutes, between the matrix instructions of the component before
+    auto limbs = [&](int to, int j) {
+        u64 y[8], z[8];
+#pragma unroll
+        for (int i = 0; i < 8; i++) { y[i] = raw[j][i]; z[i] = raw[j][8 + i]; }
+        transpose8x8(y); transpose8x8(z);
+#pragma unroll
+        for (int i = 0; i < 8; i++) B[to][i] = v4i{ (int)(u32)y[i], (int)(u32)(y[i] >> 32), (int)(u32)z[i], (int)(u32)(z[i] >> 32) };
+    };
+    // par: parity of the step's first component (its limbs are in B[par])
+    auto step = [&](auto PAR, u32 s, int buf, bool more) {
         // (the fences keep the loads of the next step where they are: the compiler moves them to the end of the step to save registers)
+        constexpr int P0 = decltype(PAR)::value;
         if (more && wave < 3) fetch(s + 1);
         __builtin_amdgcn_sched_barrier(0);
         if (cols) {
 #pragma unroll
             for (int j = 0; j < 3; j++) {
-                v4i B[8];
-                {
-                    u64 y[8], z[8];
-#pragma unroll
-                    for (int i = 0; i < 8; i++) { y[i] = (raw[j][i] + GT_BIAS) ^ GT_BIAS; z[i] = (raw[j][8 + i] + GT_BIAS) ^ GT_BIAS; }
-                    transpose8x8(y); transpose8x8(z);
-#pragma unroll
-                    for (int i = 0; i < 8; i++) B[i] = v4i{ (int)(u32)y[i], (int)(u32)(y[i] >> 32), (int)(u32)z[i], (int)(u32)(z[i] >> 32) };
-                }
+                const int b = (P0 + j) & 1;
                 if (more) load(j, s + 1);
                 __builtin_amdgcn_sched_barrier(0);
+                if (j < 2 || more) limbs(b ^ 1, (j + 1) % 3);
 #pragma unroll
                 for (int h = 0; h < (ROWS == 8 ? 1 : 2); h++) {
                     // the sums' tile with w_j gives z_j; x_{j-1} with w_j gives z_{j-1}
@@ -486,8 +497,15 @@ __global__ __launch_bounds__(256, 1) void k_mm_few(FewArgs a)
                     for (int sl = 0; sl < 8; sl++) {
                         const v4i A = *(const v4i *)(A0 + sl * 1024);
 #pragma unroll
-                        for (int t = 0; t < 8 - sl; t++) acc[to][sl + t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(A, B[t], acc[to][sl + t], 0, 0, 0);
+                        for (int t = 0; t < 8 - sl; t++) acc[to][sl + t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(A, B[b][t], acc[to][sl + t], 0, 0, 0);
                     }
+                }
+                __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
+#pragma unroll
+                for (int q = 0; q < (ROWS == 8 ? 36 : 72); q++) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x002, ROWS == 8 ? 4 : 2, 0);
+                    if (q % 4 == 0) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -500,13 +518,21 @@ __global__ __launch_bounds__(256, 1) void k_mm_few(FewArgs a)
         for (int j = 0; j < 3; j++) load(j, s0);
     if (wave < 3) put(s0, 0);
     __syncthreads();
-    int buf = 0;
-    for (u32 s = s0; s + 1 < s1; s++) {
-        step(s, buf, true);
+    if (cols) limbs(0, 0);
+    std::integral_constant<int, 0> even;
+    std::integral_constant<int, 1> odd;
+    u32 s = s0;
+    for (; s + 2 < s1; s += 2) {
+        step(even, s, 0, true);
         __syncthreads();
-        buf ^= 1;
+        step(odd, s + 1, 1, true);
+        __syncthreads();
     }
-    step(s1 - 1, buf, false);
+    if (s + 1 < s1) {
+        step(even, s, 0, true);
+        __syncthreads();
+        step(odd, s + 1, 1, false);
+    } else step(even, s, 0, false);
     if (!cols) return;
 #pragma unroll
     for (int v = 0; v < 4; v++) {
@@ -569,6 +595,7 @@ __global__ __launch_bounds__(256) void k_residues(ResArgs a)
 #pragma unroll
         for (int i = 0; i < 16; i++) {
             const u64 r = (u64)rb * 32 + (KC ? 2 * i + hi : lr), k = (u64)kb * 32 + (KC ? lr : hi * 16 + i);
+            if (a.x.tiled) { x[i] = (x[i] ^ GT_BIAS) - GT_BIAS; t[i] = sum ? (t[i] ^ GT_BIAS) - GT_BIAS : 0; }
             x[i] = ((x[i] + t[i] + GT_BIAS) ^ GT_BIAS) & (0 - (u64)(r < a.rows && k < a.K));
         }
         if (KC) {
@@ -709,7 +736,7 @@ __global__ __launch_bounds__(256) void k_put(PutArgs a)
     for (u64 e = (u64)blockIdx.x * blockDim.x + threadIdx.x; e < n; e += (u64)gridDim.x * blockDim.x) {
         const u64 r = e / a.cols, to = wtile_at(a.row0 + r, e - r * a.cols, a.nst);
 #pragma unroll
-        for (int j = 0; j < 3; j++) a.dst[(u64)j * GT_WTILE + to] = a.src.o[j][e];
+        for (int j = 0; j < 3; j++) a.dst[(u64)j * GT_WTILE + to] = (a.src.o[j][e] + GT_BIAS) ^ GT_BIAS;
     }
 }
 
