@@ -278,9 +278,34 @@ __device__ __forceinline__ u64 rns_join(const u32 (&r)[5])
 
 // Completion.  Z: the parties' parts, [3][n] words, left at zero for the next product; bias: ncol words or none.
 // FIN_RES: R: residues of the elements from `first` on, planes [chunk][party][modulus] of `plane` bytes, chunks added up; a workgroup takes
-// 128 elements at a time: a lane of a party turns the residues of eight adjacent ones into words and leaves them in LDS.
+// `per` tiles at a time, at most 8: a lane of a party turns the residues of eight adjacent ones into words and leaves them in LDS.
 enum { FIN_PARTS = 0, FIN_SCALE = 1, FIN_RES = 2 };   // parts in memory; z = row factor S[e / ncol] times x (experts' gates); residues
-struct FinArgs { KCommon c; u64 *Z; P6 bias, res, y, gate, S, x; u64 n; u32 ncol, f; int has_bias, has_res, has_gate; const unsigned char *R; u64 first, plane; u32 nchunk; };
+struct FinArgs { KCommon c; u64 *Z; P6 bias, res, y, gate, S, x; u64 n; u32 ncol, f; int has_bias, has_res, has_gate; const unsigned char *R; u64 first, plane; u32 nchunk, per; };
+// a party's parts of eight adjacent elements (of the launch's, from i0, a multiple of 8) from their residues
+__device__ __forceinline__ void rns_words(const FinArgs &a, int p, u64 i0, u64 (&zw)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; i++) zw[i] = 0;
+    for (u32 ch = 0; ch < a.nchunk; ch++) {
+        const unsigned char *R = a.R + (u64)(ch * 3 + p) * RNS_N * a.plane + i0;
+        u32 r[2][20];
+#pragma unroll
+        for (int i = 0; i < RNS_N; i++) { const uint2 v = *(const uint2 *)(R + (u64)i * a.plane); r[0][i] = v.x; r[1][i] = v.y; }
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            r[h][18] = 0; r[h][19] = 0;
+            u32 q[5][4];
+#pragma unroll
+            for (int g = 0; g < 5; g++) {
+#pragma unroll
+                for (int i = 0; i < 4; i++) q[g][i] = r[h][4 * g + i];
+                transpose4x4(q[g]);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; i++) { const u32 w[5] = { q[0][i], q[1][i], q[2][i], q[3][i], q[4][i] }; zw[4 * h + i] += rns_join(w); }
+        }
+    }
+}
 template <int SRC, bool RELU>
 __global__ __launch_bounds__(64) void k_finish(FinArgs a)
 {
@@ -293,33 +318,16 @@ __global__ __launch_bounds__(64) void k_finish(FinArgs a)
     const int p = W.p;
     const u32 f = a.f;
     const bool narrow = a.first + a.n <= 0xffffffffu;
-    constexpr u32 PER = SRC == FIN_RES ? 8 : 1;                       // tiles at a time
+    const u32 PER = SRC == FIN_RES ? a.per : 1;                       // tiles at a time
     const u64 tiles = (a.n + GT_FIN_EL - 1) / GT_FIN_EL;
     for (u64 tile = (u64)blockIdx.x * PER, sub = 0; tile < tiles; sub++, tile += sub == PER ? (u64)(gridDim.x - 1) * PER + 1 : 1, sub = sub == PER ? 0 : sub) {
         if (SRC == FIN_RES && sub == 0) {
-            u64 zw[8] = { 0, 0, 0, 0, 0, 0, 0, 0 };
-            for (u32 ch = 0; ch < a.nchunk; ch++) {
-                const unsigned char *R = a.R + (u64)(ch * 3 + p) * RNS_N * a.plane + tile * GT_FIN_EL + 8 * W.t;
-                u32 r[2][20];
-#pragma unroll
-                for (int i = 0; i < RNS_N; i++) { const uint2 v = *(const uint2 *)(R + (u64)i * a.plane); r[0][i] = v.x; r[1][i] = v.y; }
-#pragma unroll
-                for (int h = 0; h < 2; h++) {
-                    r[h][18] = 0; r[h][19] = 0;
-                    u32 q[5][4];
-#pragma unroll
-                    for (int g = 0; g < 5; g++) {
-#pragma unroll
-                        for (int i = 0; i < 4; i++) q[g][i] = r[h][4 * g + i];
-                        transpose4x4(q[g]);
-                    }
-#pragma unroll
-                    for (int i = 0; i < 4; i++) { const u32 w[5] = { q[0][i], q[1][i], q[2][i], q[3][i], q[4][i] }; zw[4 * h + i] += rns_join(w); }
-                }
-            }
+            u64 zw[8];
+            const u32 t8 = W.t < 2 * PER ? W.t : 2 * PER - 1;
+            rns_words(a, p, tile * GT_FIN_EL + 8 * t8, zw);
             wave_sync();
 #pragma unroll
-            for (int i = 0; i < 8; i++) s_z[p][8 * W.t + i] = zw[i];
+            for (int i = 0; i < 8; i++) s_z[p][8 * t8 + i] = zw[i];
             wave_sync();
         }
         const u64 e0 = a.first + tile * GT_FIN_EL, e = e0 + W.t;
@@ -340,6 +348,242 @@ __global__ __launch_bounds__(64) void k_finish(FinArgs a)
             st(a.y, p, e, y);
         }
         W.drain();
+    }
+    W.flush(a.c.wire);
+}
+
+// ---------------------------------------------------------------------------------
+// The completion of many elements: tiles of 40, two per lane of a party (lanes 0-19 of its 21), so that two passes of the block function (80 dealer
+// blocks and 45 blocks of three streams on 2 x 63 lanes) and a chain of messages serve 40 elements where k_finish spends a pass and a chain on 16.
+#define GT_FP_EL 40
+#define GT_FP_ROW 40                              // words of a row of material; rows as in FinTile, streams' rows from 22 on
+#define GT_FP_CHUNK 160                           // elements whose residues a party's 20 lanes join at a time, eight adjacent ones each
+template <int NS>
+struct FinPair {
+    const u32 *keys;
+    u64 *mat;
+    u32 f;
+    __device__ __forceinline__ void deal(const WWire &W, u32 op, u64 e0)
+    {
+        const u32 m = W.m;
+        const bool dealer = m < GT_FP_EL;
+        u64 r = 0;
+        u32 bits = 0;
+        wave_sync();
+#pragma unroll
+        for (int pass = 0; pass < 2; pass++) {
+            const u32 q = m - GT_FP_EL + 23 * pass, i = q / 15, j = (q % 15) / 5, g = q % 5;
+            Key kv;
+            const u32 *from = keys + 8 * (dealer ? GT_KEY_DEALER : (int)j);
+#pragma unroll
+            for (int v = 0; v < 8; v++) kv.k[v] = from[v];
+            u64 D[8];
+            chacha8<PRF_PAIR>(kv, dealer ? e0 + m : (e0 >> 3) + g, op, dealer ? 5u * (u32)pass : i + (i >> 1), D);
+            if (dealer) {
+                u64 *to = mat + m;
+                const u64 w = pass == 0 ? D[5] : D[6], beta = w & 1;
+                const u32 b0 = (u32)(w >> 1) & 1, b1 = (u32)(w >> 2) & 1, bb = b0 | (b1 << 1) | ((((u32)beta ^ b0 ^ b1) & 1) << 2);
+                if (pass == 0) {
+                    r = D[0];
+                    bits = bb;
+                    to[0] = D[1]; to[GT_FP_ROW] = D[2]; to[2 * GT_FP_ROW] = r - D[1] - D[2];
+                    to[3 * GT_FP_ROW] = D[3] << (32 - f); to[4 * GT_FP_ROW] = D[4] << (32 - f); to[5 * GT_FP_ROW] = (r ^ D[3] ^ D[4]) << (32 - f);
+                    to[6 * GT_FP_ROW] = D[6]; to[7 * GT_FP_ROW] = D[7]; to[8 * GT_FP_ROW] = beta - D[6] - D[7];
+                } else {
+                    to[9 * GT_FP_ROW] = bits | (bb << 3);
+                    to[10 * GT_FP_ROW] = D[0]; to[11 * GT_FP_ROW] = D[1]; to[12 * GT_FP_ROW] = (r >> f) - D[0] - D[1];
+                    to[13 * GT_FP_ROW] = D[2] << (64 - f); to[14 * GT_FP_ROW] = D[3] << (64 - f); to[15 * GT_FP_ROW] = ((r >> 63) - D[2] - D[3]) << (64 - f);
+                    if (NS == 3) { to[16 * GT_FP_ROW] = D[4]; to[17 * GT_FP_ROW] = D[5]; to[18 * GT_FP_ROW] = beta - D[4] - D[5]; }
+                    const u64 EVEN = 0x5555555555555555ull, win = r << (32 - f), p0 = D[7] & EVEN, p1 = (D[7] >> 1) & EVEN;
+                    to[19 * GT_FP_ROW] = p0; to[20 * GT_FP_ROW] = p1; to[21 * GT_FP_ROW] = (win & (win >> 1) & EVEN) ^ p0 ^ p1;
+                }
+            } else if (q < 15 * NS) {
+#pragma unroll
+                for (int v = 0; v < 8; v++) mat[(22 + q / 5) * GT_FP_ROW + g * 8 + v] = D[v];
+            }
+        }
+        wave_sync();
+    }
+    __device__ __forceinline__ Sh pair(const WWire &W, int row, u32 e) const { return Sh{ mat[(row + W.p) * GT_FP_ROW + e], mat[(row + W.pn) * GT_FP_ROW + e] }; }
+    __device__ __forceinline__ u64 za(const WWire &W, int i, u32 e) const { const Sh w = pair(W, 22 + 3 * i, e); return w.o - w.n; }
+    __device__ __forceinline__ u64 zb(const WWire &W, int i, u32 e) const { const Sh w = pair(W, 22 + 3 * i, e); return w.o ^ w.n; }
+};
+// less_tree of two elements, a message for both; on: bits 0, 1: which of them exist
+template <int HALVES>
+__device__ __forceinline__ void less_pair(WWire &W, const u64 (&c)[2], const Sh (&rho)[2], const Sh (&pr)[2], const u64 (&A)[2], u32 live2, u32 (&lo)[2], u32 (&ln)[2],
+                                          u32 (&ao)[2], u32 (&an)[2])
+{
+    const u32 EV = 0x55555555u;
+    const u32 m0 = W.p == 0 ? ~0u : 0u, m2 = W.p == 2 ? ~0u : 0u;
+    u32 x[2], y[2], g0[2], g1[2], snd[2], rcv[2], nresh = HALVES == 2 ? 32 : 16;
+#pragma unroll
+    for (int q = 0; q < 2; q++) {
+        u32 Xo[2], Xn[2];
+#pragma unroll
+        for (int h = 0; h < HALVES; h++) {
+            const u32 nc = ~(u32)(c[q] >> (32 * h)), live = h == 1 ? 0x7fffffffu : ~0u;
+            const u32 nl = nc & EV, nh = ((nc >> 1) | (h == 1 ? 0x40000000u : 0u)) & EV;
+            const u32 both = nl & nh;
+#pragma unroll
+            for (int w = 0; w < 2; w++) {
+                const u32 r = (u32)((w ? rho[q].n : rho[q].o) >> (32 * h)) & live, d = (u32)((w ? pr[q].n : pr[q].o) >> (32 * h)) & (h == 1 ? 0x15555555u : EV);
+                const u32 rh = (r >> 1) & EV;
+                const u32 u = nh & r, v = nl & rh;
+                const u32 G = (nh & rh) ^ (nl & (d ^ u)), E = d ^ u ^ v ^ (both & (w ? m2 : m0));
+                (w ? Xn[h] : Xo[h]) = G | (E << 1);
+            }
+        }
+        u32 l[2], e[2], g[2];
+#pragma unroll
+        for (int w = 0; w < 2; w++) {
+            const u32 a = w ? Xn[0] : Xo[0], b = HALVES == 2 ? (w ? Xn[1] : Xo[1]) : 0;
+            l[w] = (a & 0x33333333u) | (HALVES == 2 ? (b << 2) & 0xccccccccu : 0);
+            const u32 ee = ((a >> 3) & 0x11111111u) | (HALVES == 2 ? (b >> 1) & 0x44444444u : 0);
+            e[w] = ee | (ee << 1);
+            g[w] = ((a >> 2) & 0x11111111u) | (HALVES == 2 ? b & 0x44444444u : 0);
+        }
+        snd[q] = and3l(e[0], e[1], l[0], l[1]) ^ (HALVES == 2 ? (u32)A[q] : (u32)A[q] & 0x33333333u);
+        g0[q] = g[0]; g1[q] = g[1];
+    }
+    W.reshare<2>(snd, rcv);
+#pragma unroll
+    for (int q = 0; q < 2; q++) { x[q] = snd[q] ^ g0[q]; y[q] = rcv[q] ^ g1[q]; }
+#pragma unroll
+    for (int v = 2; v <= 4; v++) {
+        const int s = 2 << (v - 1);
+        const u32 EM = (HALVES == 2 ? 5u : 1u) * (v == 2 ? 0x01010101u : v == 3 ? 0x00010001u : 1u);
+#pragma unroll
+        for (int q = 0; q < 2; q++) {
+            const u32 ho = x[q] >> s, hn = y[q] >> s, eo = (ho >> 1) & EM, en = (hn >> 1) & EM;
+            const u32 M = ((u32)(A[q] >> 32) >> (v == 2 ? 0 : v == 3 ? 4 : 12)) & (EM * 3);
+            snd[q] = and3l(eo | (eo << 1), en | (en << 1), x[q], y[q]) ^ M;
+            g0[q] = ho & EM; g1[q] = hn & EM;
+        }
+        W.reshare<2>(snd, rcv);
+#pragma unroll
+        for (int q = 0; q < 2; q++) { x[q] = snd[q] ^ g0[q]; y[q] = rcv[q] ^ g1[q]; }
+        nresh += (HALVES == 2 ? 64 : 32) >> v;
+    }
+#pragma unroll
+    for (int q = 0; q < 2; q++) { lo[q] = x[q] & 1; ln[q] = y[q] & 1; ao[q] = 0; an[q] = 0; }
+    if (HALVES == 2) {
+#pragma unroll
+        for (int q = 0; q < 2; q++) snd[q] = (and3l(x[q] >> 3, y[q] >> 3, x[q], y[q]) ^ ((u32)(A[q] >> 32) >> 28)) & 1;
+        W.reshare<2>(snd, rcv);
+#pragma unroll
+        for (int q = 0; q < 2; q++) { ao[q] = snd[q] ^ ((x[q] >> 2) & 1); an[q] = rcv[q] ^ ((y[q] >> 2) & 1); }
+        nresh += 1;
+    }
+    W.nresh += nresh * live2;
+}
+
+template <bool RELU>
+__global__ __launch_bounds__(64) void k_finish_pair(FinArgs a)
+{
+    constexpr int NS = RELU ? 3 : 2;
+    __shared__ uint4 s_msg[GT_LANES];
+    __shared__ u64 s_mat[(22 + 3 * NS) * GT_FP_ROW];
+    __shared__ u64 s_cnt[6];
+    __shared__ u64 s_z[3][GT_FP_CHUNK];
+    WWire W; W.init(s_msg, s_cnt);
+    FinPair<NS> T; T.keys = a.c.keys; T.mat = s_mat; T.f = a.f;
+    const int p = W.p;
+    const u32 f = a.f, t = W.t < 20 ? W.t : 19;
+    const bool mine = W.real && W.t < 20, narrow = a.first + a.n <= 0xffffffffu;
+    const u64 off = RELU ? 1ull << (f + 31) : 1ull << 62;
+    const Sh one = pub(p, 1);
+    for (u64 c0 = (u64)blockIdx.x * GT_FP_CHUNK; c0 < a.n; c0 += (u64)gridDim.x * GT_FP_CHUNK) {
+        {
+            u64 zw[8];
+            rns_words(a, p, c0 + 8 * t, zw);
+            wave_sync();
+#pragma unroll
+            for (int i = 0; i < 8; i++) s_z[p][8 * t + i] = zw[i];
+            wave_sync();
+        }
+        for (u32 k0 = 0; k0 < GT_FP_CHUNK && c0 + k0 < a.n; k0 += GT_FP_EL) {
+            const u64 e0 = a.first + c0 + k0;
+            const u32 el[2] = { t, t + 20 };
+            bool act[2];
+            u64 z[2], col[2];
+#pragma unroll
+            for (int q = 0; q < 2; q++) {
+                act[q] = W.t < 20 && c0 + k0 + el[q] < a.n;
+                z[q] = s_z[p][k0 + el[q]];
+                if (a.has_bias) {
+                    const u64 e = e0 + el[q];
+                    col[q] = act[q] ? (narrow ? (u64)((u32)e % a.ncol) : e % a.ncol) : 0;
+                    z[q] += own_of(a.bias, p)[col[q]] << f;
+                }
+            }
+            const u32 na = (u32)act[0] + (u32)act[1];
+            Sh res[2];
+            if (a.has_res)
+#pragma unroll
+                for (int q = 0; q < 2; q++) res[q] = act[q] ? ld(a.res, p, e0 + el[q]) : Sh{ 0, 0 };
+            T.deal(W, a.c.op, e0);
+            u64 m[2], c[2];
+            {
+#pragma unroll
+                for (int q = 0; q < 2; q++) m[q] = z[q] + T.za(W, 0, el[q]) + T.mat[p * GT_FP_ROW + el[q]];
+                wave_sync();
+                s_msg[W.m] = make_uint4((u32)m[0], (u32)(m[0] >> 32), (u32)m[1], (u32)(m[1] >> 32));
+                wave_sync();
+                const uint4 x = s_msg[W.nx], y = s_msg[W.pv];
+                c[0] = m[0] + ((u64)x.x | ((u64)x.y << 32)) + ((u64)y.x | ((u64)y.y << 32)) + ((1ull << (f - 1)) + off);
+                c[1] = m[1] + ((u64)x.z | ((u64)x.w << 32)) + ((u64)y.z | ((u64)y.w << 32)) + ((1ull << (f - 1)) + off);
+                W.nopen += 64u * na; W.nresh += 64u * na;
+            }
+            const Sh rho[2] = { T.pair(W, 3, el[0]), T.pair(W, 3, el[1]) }, pr[2] = { T.pair(W, 19, el[0]), T.pair(W, 19, el[1]) };
+            const u64 A[2] = { T.zb(W, 1, el[0]), T.zb(W, 1, el[1]) }, cw[2] = { c[0] << (32 - f), c[1] << (32 - f) };
+            u32 lo[2], ln[2], ao[2], an[2];
+            less_pair<RELU ? 2 : 1>(W, cw, rho, pr, A, na, lo, ln, ao, an);
+            u32 fo[1] = { 0 }, fr[1], fn = 0;
+#pragma unroll
+            for (int q = 0; q < 2; q++) {
+                const u32 bits = (u32)T.mat[9 * GT_FP_ROW + el[q]];
+                u32 o = (lo[q] ^ (bits >> p)) & 1, n = (ln[q] ^ (bits >> W.pn)) & 1;
+                if (RELU) {
+                    const u32 ct = (u32)(c[q] >> (f + 31)) & 1;
+                    const u32 so = (u32)(rho[q].o >> 63) ^ ao[q] ^ (p == 0 ? ct : 0), sn = (u32)(rho[q].n >> 63) ^ an[q] ^ (p == 2 ? ct : 0);
+                    o |= ((so ^ (bits >> (3 + p))) & 1) << 1;
+                    n |= ((sn ^ (bits >> (3 + W.pn))) & 1) << 1;
+                }
+                fo[0] |= o << (2 * q); fn |= n << (2 * q);
+            }
+            W.pass<1>(fo, fr, W.pv);
+            W.nopen += (RELU ? 2u : 1u) * na;
+            const u32 ff = fo[0] ^ fn ^ fr[0];
+            Sh y[2], gate[2];
+#pragma unroll
+            for (int q = 0; q < 2; q++) {
+                const Sh d = T.pair(W, 6, el[q]), b = (ff >> (2 * q)) & 1 ? one - d : d;
+                y[q] = pub(p, (c[q] >> f) - (off >> f)) - T.pair(W, 10, el[q]) - b;
+                const Sh top = T.pair(W, 13, el[q]);
+                const u64 wrap = 0 - (u64)!(c[q] >> 63);
+                y[q].o += top.o & wrap; y[q].n += top.n & wrap;
+                if (RELU) {
+                    const Sh d2 = T.pair(W, 16, el[q]);
+                    gate[q] = (ff >> (2 * q)) & 2 ? one - d2 : d2;
+                    m[q] = prod3(gate[q], y[q]) + T.za(W, 2, el[q]);
+                }
+            }
+            if (RELU) {
+                u64 rcv[2];
+                W.reshare64<2>(m, rcv);
+                W.nresh += 64u * na;
+#pragma unroll
+                for (int q = 0; q < 2; q++) y[q] = Sh{ m[q], rcv[q] };
+            }
+#pragma unroll
+            for (int q = 0; q < 2; q++)
+                if (act[q] && mine) {
+                    if (RELU && a.has_gate) st(a.gate, p, e0 + el[q], gate[q]);
+                    if (a.has_res) y[q] = y[q] + res[q];
+                    st(a.y, p, e0 + el[q], y[q]);
+                }
+            W.drain();
+        }
     }
     W.flush(a.c.wire);
 }

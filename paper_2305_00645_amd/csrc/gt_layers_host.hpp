@@ -93,7 +93,7 @@ static int do_dense(gt_ctx *c, MatView A, const MatView &B, u64 M, u64 N, u64 K,
         const u32 narb = (u32)(s.ntm * 2 * s.wm), nbrb = (u32)(s.ntn * 2 * s.wn);
         const bool asums = m <= N;                                       // the factor with fewer rows is converted twice
         const u32 nkb = (u32)((std::min<u64>(K, RNS_TERMS) + 63) / 64 * 2);
-        const u64 amat = (u64)narb * nkb * 1024, bmat = (u64)nbrb * nkb * 1024, plane = (m * N + 127) & ~(u64)127;
+        const u64 amat = (u64)narb * nkb * 1024, bmat = (u64)nbrb * nkb * 1024, plane = (m * N + 1279) / 1280 * 1280;        // whole tiles of both completions
         const u64 abytes = (asums ? 6 : 3) * RNS_N * amat, bbytes = (asums ? 3 : 6) * RNS_N * bmat, rbytes = 3 * RNS_N * plane;
         GTCHK(grow_res(c, abytes + bbytes + nchunk * rbytes));
         MatView Ar = A;
@@ -111,8 +111,16 @@ static int do_dense(gt_ctx *c, MatView A, const MatView &B, u64 M, u64 N, u64 K,
             GTCHK(s.wm == 4 ? launch(c, GT_KC_DENSE, k_rns_mm<4, 2>, g, B256, a) : launch(c, GT_KC_DENSE, k_rns_mm<1, 1>, g, B256, a));
         }
         f.R = c->res + abytes + bbytes; f.first = r0 * N; f.plane = plane; f.nchunk = nchunk; f.n = m * N;
-        const dim3 g((unsigned)std::min<u64>((f.n + 127) / 128, 1u << 16));
-        GTCHK(relu ? launch(c, GT_KC_FINISH, k_finish<FIN_RES, true>, g, B64, f) : launch(c, GT_KC_FINISH, k_finish<FIN_RES, false>, g, B64, f));
+        const FinShape fs = fin_shape(c->simds, f.n);
+        f.per = fs.per;
+        if (fs.pairs) {
+            const dim3 g((unsigned)std::min<u64>((f.n + GT_FP_CHUNK - 1) / GT_FP_CHUNK, 1u << 16));
+            GTCHK(relu ? launch(c, GT_KC_FINISH, k_finish_pair<true>, g, B64, f) : launch(c, GT_KC_FINISH, k_finish_pair<false>, g, B64, f));
+        } else {
+            const u64 tiles = (f.n + GT_FIN_EL - 1) / GT_FIN_EL;
+            const dim3 g((unsigned)std::min<u64>((tiles + f.per - 1) / f.per, 1u << 16));
+            GTCHK(relu ? launch(c, GT_KC_FINISH, k_finish<FIN_RES, true>, g, B64, f) : launch(c, GT_KC_FINISH, k_finish<FIN_RES, false>, g, B64, f));
+        }
     }
     acct_finish(c, M * N, relu);
     return GT_OK;

@@ -248,3 +248,11 @@ static inline u32 residue_range(u64 simds, u64 operands)
     const u64 parts = std::min<u64>(6, std::max<u64>(1, 4 * simds / std::max<u64>(1, operands)));
     return (u32)((18 + parts - 1) / parts);
 }
+// completion of residues: two elements per lane, or tiles of 16, `per` of them joined at a time
+struct FinShape { bool pairs; u32 per; };
+static inline FinShape fin_shape(u64 simds, u64 n)
+{
+    FinShape s = { n >= 160 * simds, 8 };
+    while (s.per > 1 && n < 16 * s.per * 2 * simds) s.per /= 2;
+    return s;
+}
