@@ -892,16 +892,24 @@ __global__ __launch_bounds__(256, WM == 4 ? 2 : 4) void k_rns_mm(RmmArgs a)
     const unsigned char *A0 = a.A + ((u64)p * RNS_N + mi) * a.amat, *A1 = a.A + ((u64)(a.asums ? 3 + p : pn) * RNS_N + mi) * a.amat;
     const unsigned char *B0 = a.B + ((u64)p * RNS_N + mi) * a.bmat, *B1 = a.B + ((u64)(a.asums ? pn : 3 + p) * RNS_N + mi) * a.bmat;
     const u32 half = a.nstep / 2;                                              // steps of a product
-    v4i st[LOADS];
-    auto fetch = [&](u32 s) {
-        const u32 k = s >= half ? s - half : s;
-        const unsigned char *A = (s >= half ? A1 : A0) + ((u64)k * 2 * a.narb + tm * FA) * 1024, *B = (s >= half ? B1 : B0) + ((u64)k * 2 * a.nbrb + tn * FB) * 1024;
+    // a wavefront's loads of a step: operands q * 4 + wave of [2 blocks of terms][FA] of the left factor, then of the right one
+    const unsigned char *at[LOADS];
+    auto start = [&](const unsigned char *A, const unsigned char *B) {
 #pragma unroll
         for (int q = 0; q < LOADS; q++) {
-            const u32 o = q * 4 + wave;                                        // operand: [2 blocks of terms][FA] of A, then of B
+            const u32 o = q * 4 + wave;
             const bool isA = o < 2 * FA;
             const u32 w = isA ? o : o - 2 * FA, kb = isA ? w / FA : w / FB, r = isA ? w % FA : w % FB;
-            st[q] = *(const v4i *)((isA ? A + ((u64)kb * a.narb + r) * 1024 : B + ((u64)kb * a.nbrb + r) * 1024) + lane * 16);
+            at[q] = isA ? A + ((u64)kb * a.narb + tm * FA + r) * 1024 : B + ((u64)kb * a.nbrb + tn * FB + r) * 1024;
+        }
+    };
+    v4i st[LOADS];
+    auto fetch = [&](u32 s) {
+        if (s == half) start(A1, B1);
+#pragma unroll
+        for (int q = 0; q < LOADS; q++) {
+            st[q] = *(const v4i *)(at[q] + lane * 16);
+            at[q] += (u64)(q * 4 + (int)wave < 2 * FA ? a.narb : a.nbrb) * 2048;
         }
     };
     auto put = [&](u32 buf) {
@@ -915,24 +923,29 @@ __global__ __launch_bounds__(256, WM == 4 ? 2 : 4) void k_rns_mm(RmmArgs a)
         for (int j = 0; j < WN; j++)
 #pragma unroll
             for (int v = 0; v < 16; v++) acc[i][j][v] = 0;
+    start(A0, B0);
     fetch(0);
     put(0);
     __syncthreads();
     for (u32 s = 0; s < a.nstep; s++) {
         if (s + 1 < a.nstep) fetch(s + 1);
         const unsigned char *buf = s_buf + (s & 1) * STEP + lane * 16;
+        v4i x[2][WM], w[2][WN];
 #pragma unroll
         for (int kb = 0; kb < 2; kb++) {
-            v4i x[WM], w[WN];
 #pragma unroll
-            for (int i = 0; i < WM; i++) x[i] = *(const v4i *)(buf + (kb * FA + wm * WM + i) * 1024);
+            for (int j = 0; j < WN; j++) w[kb][j] = *(const v4i *)(buf + (2 * FA + kb * FB + wn * WN + j) * 1024);
 #pragma unroll
-            for (int j = 0; j < WN; j++) w[j] = *(const v4i *)(buf + (2 * FA + kb * FB + wn * WN + j) * 1024);
+            for (int i = 0; i < WM; i++) x[kb][i] = *(const v4i *)(buf + (kb * FA + wm * WM + i) * 1024);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int kb = 0; kb < 2; kb++)
 #pragma unroll
             for (int i = 0; i < WM; i++)
 #pragma unroll
-                for (int j = 0; j < WN; j++) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[j], x[i], acc[i][j], 0, 0, 0);
-        }
+                for (int j = 0; j < WN; j++) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[kb][j], x[kb][i], acc[i][j], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
         if (s + 1 < a.nstep) put((s + 1) & 1);
         __syncthreads();
     }
