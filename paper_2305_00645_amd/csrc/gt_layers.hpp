@@ -492,6 +492,9 @@ __global__ __launch_bounds__(64) void k_finish_pair(FinArgs a)
     const bool mine = W.real && W.t < 20, narrow = a.first + a.n <= 0xffffffffu;
     const u64 off = RELU ? 1ull << (f + 31) : 1ull << 62;
     const Sh one = pub(p, 1);
+    // the party's planes, chosen once
+    u64 *const yo = own_of(a.y, p), *const yn = nxt_of(a.y, p), *const go = own_of(a.gate, p), *const gn = nxt_of(a.gate, p);
+    const u64 *const ro = own_of(a.res, p), *const rn = nxt_of(a.res, p), *const bo = own_of(a.bias, p);
     for (u64 c0 = (u64)blockIdx.x * GT_FP_CHUNK; c0 < a.n; c0 += (u64)gridDim.x * GT_FP_CHUNK) {
         {
             u64 zw[8];
@@ -505,22 +508,21 @@ __global__ __launch_bounds__(64) void k_finish_pair(FinArgs a)
             const u64 e0 = a.first + c0 + k0;
             const u32 el[2] = { t, t + 20 };
             bool act[2];
-            u64 z[2], col[2];
+            u64 z[2], e[2];
+            Sh res[2];
 #pragma unroll
             for (int q = 0; q < 2; q++) {
                 act[q] = W.t < 20 && c0 + k0 + el[q] < a.n;
+                e[q] = a.first + (c0 + k0 + el[q] < a.n ? c0 + k0 + el[q] : a.n - 1);         // (a last tile loads its last element where none exists)
                 z[q] = s_z[p][k0 + el[q]];
-                if (a.has_bias) {
-                    const u64 e = e0 + el[q];
-                    col[q] = act[q] ? (narrow ? (u64)((u32)e % a.ncol) : e % a.ncol) : 0;
-                    z[q] += own_of(a.bias, p)[col[q]] << f;
-                }
             }
             const u32 na = (u32)act[0] + (u32)act[1];
-            Sh res[2];
+            if (a.has_bias)
+#pragma unroll
+                for (int q = 0; q < 2; q++) z[q] += bo[narrow ? (u64)((u32)e[q] % a.ncol) : e[q] % a.ncol] << f;
             if (a.has_res)
 #pragma unroll
-                for (int q = 0; q < 2; q++) res[q] = act[q] ? ld(a.res, p, e0 + el[q]) : Sh{ 0, 0 };
+                for (int q = 0; q < 2; q++) res[q] = Sh{ ro[e[q]], rn[e[q]] };
             T.deal(W, a.c.op, e0);
             u64 m[2], c[2];
             {
@@ -575,13 +577,17 @@ __global__ __launch_bounds__(64) void k_finish_pair(FinArgs a)
 #pragma unroll
                 for (int q = 0; q < 2; q++) y[q] = Sh{ m[q], rcv[q] };
             }
+            if (a.has_res)
 #pragma unroll
-            for (int q = 0; q < 2; q++)
-                if (act[q] && mine) {
-                    if (RELU && a.has_gate) st(a.gate, p, e0 + el[q], gate[q]);
-                    if (a.has_res) y[q] = y[q] + res[q];
-                    st(a.y, p, e0 + el[q], y[q]);
-                }
+                for (int q = 0; q < 2; q++) y[q] = y[q] + res[q];
+            if (mine && act[0]) {
+                yo[e[0]] = y[0].o; yn[e[0]] = y[0].n;
+                if (RELU && a.has_gate) { go[e[0]] = gate[0].o; gn[e[0]] = gate[0].n; }
+            }
+            if (mine && act[1]) {
+                yo[e[1]] = y[1].o; yn[e[1]] = y[1].n;
+                if (RELU && a.has_gate) { go[e[1]] = gate[1].o; gn[e[1]] = gate[1].n; }
+            }
             W.drain();
         }
     }
