@@ -816,20 +816,21 @@ __global__ __launch_bounds__(256, 1) void k_mm_few(FewArgs a)
 // lane l of an operand holds row l % 32 and the 16 terms from 16 (l / 32) on.  Matrices: the sums of adjacent components (0-2) and the components
 // (3-5), or the components alone (0-2).  Rows and terms beyond the matrix are zero.  A residue: two four-byte dot products of the word's
 // signed bytes with the powers of 256, a rounded quotient in floating point.  RIGHT: times (M / m_i)^-1.
-// A wavefront makes an operand of 32 x 32 words of one matrix for a range of moduli (blockIdx.y: matrix, blockIdx.z: range).  KC: terms contiguous
-// in memory; the words then go through LDS, so that loads are of whole rows.
-struct ResArgs { MatView x; unsigned char *out; u64 rows, K, k0; u32 nrb, nkb, per; int sums; };
+// A wavefront makes an operand of 32 x 32 words of one matrix for `per` moduli; a launch makes both factors' (blocks below na: the left one's).
+// KC: terms contiguous in memory; the words then go through LDS, so that loads are of whole rows.  Bound: what it writes, 18 bytes a word, and reads (2048 x 1024
+// words in six matrices 36 us, 5 TB/s; with a lane's terms from memory, all moduli and matrices by one wavefront, 95).
+struct ResArgs { MatView x; unsigned char *out; u64 rows, K, k0; u32 nrb, nkb, per, mats; };
 template <bool RIGHT, bool KC>
-__global__ __launch_bounds__(256) void k_residues(ResArgs a)
+__device__ __forceinline__ void residue_block(const ResArgs &a, u32 block, u64 (*s_t)[32 * 33])
 {
-    __shared__ u64 s_t[KC ? 4 : 1][KC ? 32 * 33 : 1];
-    const u32 lane = threadIdx.x & 63, lr = lane & 31, hi = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = blockIdx.y;
+    const u32 lane = threadIdx.x & 63, lr = lane & 31, hi = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const u32 nfb = (u32)(((u64)a.nrb * a.nkb + 3) / 4), q = block / nfb % a.mats, range = block / nfb / a.mats;
     const u64 nfr = (u64)a.nrb * a.nkb, mat = nfr * 1024;
-    const u64 fr = (u64)blockIdx.x * 4 + wave;
+    const u64 fr = (u64)(block % nfb) * 4 + wave;
     if (fr >= nfr) return;
     // neighbours along the axis that is contiguous in memory
     const u32 rb = (u32)(KC ? fr / a.nkb : fr % a.nrb), kb = (u32)(KC ? fr % a.nkb : fr / a.nrb);
-    const bool sum = a.sums && q < 3;
+    const bool sum = a.mats == 6 && q < 3;
     const u64 *x0 = q % 3 == 0 ? a.x.c[0] : (q % 3 == 1 ? a.x.c[1] : a.x.c[2]), *x1 = q == 0 ? a.x.c[1] : (q == 1 ? a.x.c[2] : a.x.c[0]);
     u64 x[16];
     {
@@ -857,7 +858,7 @@ __global__ __launch_bounds__(256) void k_residues(ResArgs a)
         }
     }
     unsigned char *out = a.out + (u64)q * RNS_N * mat + ((u64)kb * a.nrb + rb) * 1024 + lane * 16;
-    const u32 i0 = blockIdx.z * a.per, i1 = i0 + a.per < RNS_N ? i0 + a.per : RNS_N;
+    const u32 i0 = range * a.per, i1 = i0 + a.per < RNS_N ? i0 + a.per : RNS_N;
     for (u32 i = i0; i < i1; i++) {
         const int cl = (int)(RIGHT ? d_rns.right[i][0] : d_rns.left[i][0]), ch = (int)(RIGHT ? d_rns.right[i][1] : d_rns.left[i][1]);
         const u32 neg = 256 - (u32)d_rns.m[i];
@@ -873,6 +874,15 @@ __global__ __launch_bounds__(256) void k_residues(ResArgs a)
     }
 }
 
+__global__ __launch_bounds__(256) void k_residues(ResArgs a, ResArgs b, u32 na)
+{
+    __shared__ u64 s_t[4][32 * 33];
+    if (blockIdx.x < na) {
+        if (a.x.ks == 1) residue_block<false, true>(a, blockIdx.x, s_t); else residue_block<false, false>(a, blockIdx.x, s_t);
+    } else if (b.x.ks == 1) residue_block<true, true>(b, blockIdx.x - na, s_t);
+    else residue_block<true, false>(b, blockIdx.x - na, s_t);
+}
+
 // The products of residues: for every party and modulus the sum of two products, party p's
 //   (a_p + a_{p+1}) b_p + a_p b_{p+1}      or      a_p (b_p + b_{p+1}) + a_{p+1} b_p
 // (sums in the left or the right factor), reduced to balanced residues, [party][modulus] planes of bytes, row-major M x N.
@@ -881,7 +891,7 @@ __global__ __launch_bounds__(256) void k_residues(ResArgs a)
 // that a lane holds four adjacent columns of a result.  Consecutive workgroups of an XCD take the tiles of one product.
 struct RmmArgs { const unsigned char *A, *B; unsigned char *R; u64 amat, bmat, plane; u32 M, N, narb, nbrb, nstep, ntm, ntn, total; int asums; };   // amat, bmat: bytes of a modulus's matrix; narb: blocks of 32 rows
 template <int WM, int WN>
-__global__ __launch_bounds__(256, WM == 4 ? 2 : 4) void k_rns_mm(RmmArgs a)
+__global__ __launch_bounds__(256, WM == 4 ? 2 : WM == 2 ? 3 : 4) void k_rns_mm(RmmArgs a)
 {
     constexpr int FA = 2 * WM, FB = 2 * WN, STEP = 2 * (FA + FB) * 1024;       // operands of 32 rows a workgroup, bytes of a step
     constexpr int LD = 64 * WN + 16, OUT = 64 * WM * LD;

@@ -69,15 +69,15 @@ static int grow_res(gt_ctx *c, size_t need)
     c->res_bytes = need;
     return GT_OK;
 }
-template <bool RIGHT>
-static int residues(gt_ctx *c, const MatView &x, unsigned char *out, u64 rows, u64 K, u64 k0, u32 nrb, u32 nkb, bool sums)
+// arguments of a factor's conversion, and its workgroups
+static ResArgs residues(gt_ctx *c, const MatView &x, unsigned char *out, u64 rows, u64 K, u64 k0, u32 nrb, u32 nkb, bool sums, u32 *blocks)
 {
     ResArgs a{};
-    a.x = x; a.out = out; a.rows = rows; a.K = K; a.k0 = k0; a.nrb = nrb; a.nkb = nkb; a.sums = sums;
-    const u64 nfr = (u64)nrb * nkb, mats = sums ? 6 : 3;
-    a.per = residue_range(c->simds, nfr * mats);
-    const dim3 g((unsigned)((nfr + 3) / 4), (unsigned)mats, (RNS_N + a.per - 1) / a.per);
-    return x.ks == 1 ? launch(c, GT_KC_DENSE, k_residues<RIGHT, true>, g, B256, a) : launch(c, GT_KC_DENSE, k_residues<RIGHT, false>, g, B256, a);
+    a.x = x; a.out = out; a.rows = rows; a.K = K; a.k0 = k0; a.nrb = nrb; a.nkb = nkb; a.mats = sums ? 6 : 3;
+    const u64 nfr = (u64)nrb * nkb;
+    a.per = residue_range(c->simds, nfr * a.mats);
+    *blocks = (u32)((nfr + 3) / 4) * a.mats * ((RNS_N + a.per - 1) / a.per);
+    return a;
 }
 // completion of the product of A (M x K) and B (N x K), by residues: rows in blocks, the long axis in chunks of RNS_TERMS
 static int do_dense(gt_ctx *c, MatView A, const MatView &B, u64 M, u64 N, u64 K, bool relu, const FinOut &o)
@@ -101,14 +101,15 @@ static int do_dense(gt_ctx *c, MatView A, const MatView &B, u64 M, u64 N, u64 K,
         for (u32 ch = 0; ch < nchunk; ch++) {
             const u64 k0 = (u64)ch * RNS_TERMS, k = std::min<u64>(K - k0, RNS_TERMS);
             const u32 kb = (u32)((k + 63) / 64 * 2);
-            GTCHK(residues<false>(c, Ar, c->res, m, k, k0, narb, kb, asums));
-            GTCHK(residues<true>(c, B, c->res + abytes, N, k, k0, nbrb, kb, !asums));
+            u32 na, nb;
+            const ResArgs ra = residues(c, Ar, c->res, m, k, k0, narb, kb, asums, &na), rb = residues(c, B, c->res + abytes, N, k, k0, nbrb, kb, !asums, &nb);
+            GTCHK(launch(c, GT_KC_DENSE, k_residues, dim3(na + nb), B256, ra, rb, na));
             RmmArgs a{};
             a.A = c->res; a.B = c->res + abytes; a.R = c->res + abytes + bbytes + ch * rbytes; a.amat = (u64)narb * kb * 1024; a.bmat = (u64)nbrb * kb * 1024;
             a.plane = plane; a.M = (u32)m; a.N = (u32)N; a.narb = narb; a.nbrb = nbrb; a.nstep = kb; a.ntm = (u32)s.ntm; a.ntn = (u32)s.ntn; a.asums = asums;
             a.total = (u32)(3 * RNS_N * s.ntm * s.ntn);
             const dim3 g((a.total + 7) / 8 * 8);
-            GTCHK(s.wm == 4 ? launch(c, GT_KC_DENSE, k_rns_mm<4, 2>, g, B256, a) : launch(c, GT_KC_DENSE, k_rns_mm<1, 1>, g, B256, a));
+            GTCHK(s.wm == 4 ? launch(c, GT_KC_DENSE, k_rns_mm<4, 2>, g, B256, a) : s.wm == 2 ? launch(c, GT_KC_DENSE, k_rns_mm<2, 2>, g, B256, a) : launch(c, GT_KC_DENSE, k_rns_mm<1, 1>, g, B256, a));
         }
         f.R = c->res + abytes + bbytes; f.first = r0 * N; f.plane = plane; f.nchunk = nchunk; f.n = m * N;
         const FinShape fs = fin_shape(c->simds, f.n);
