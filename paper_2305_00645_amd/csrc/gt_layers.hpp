@@ -306,9 +306,14 @@ __device__ __forceinline__ void rns_words(const FinArgs &a, int p, u64 i0, u64 (
         }
     }
 }
+// One or two completions in a launch: workgroups below na are the first one's.
+struct FinSet { FinArgs f[2]; u32 na; };
 template <int SRC, bool RELU>
-__global__ __launch_bounds__(64) void k_finish(FinArgs a)
+__global__ __launch_bounds__(64) void k_finish(FinSet set)
 {
+    const bool second = blockIdx.x >= set.na;
+    const FinArgs &a = set.f[second ? 1 : 0];
+    const u32 block = second ? blockIdx.x - set.na : blockIdx.x, blocks = second ? gridDim.x - set.na : set.na;
     __shared__ uint4 s_msg[GT_LANES];
     __shared__ u64 s_mat[GT_FIN_WORDS(RELU ? 3 : 2)];
     __shared__ u64 s_cnt[6];
@@ -320,7 +325,7 @@ __global__ __launch_bounds__(64) void k_finish(FinArgs a)
     const bool narrow = a.first + a.n <= 0xffffffffu;
     const u32 PER = SRC == FIN_RES ? a.per : 1;                       // tiles at a time
     const u64 tiles = (a.n + GT_FIN_EL - 1) / GT_FIN_EL;
-    for (u64 tile = (u64)blockIdx.x * PER, sub = 0; tile < tiles; sub++, tile += sub == PER ? (u64)(gridDim.x - 1) * PER + 1 : 1, sub = sub == PER ? 0 : sub) {
+    for (u64 tile = (u64)block * PER, sub = 0; tile < tiles; sub++, tile += sub == PER ? (u64)(blocks - 1) * PER + 1 : 1, sub = sub == PER ? 0 : sub) {
         if (SRC == FIN_RES && sub == 0) {
             u64 zw[8];
             const u32 t8 = W.t < 2 * PER ? W.t : 2 * PER - 1;
@@ -874,13 +879,17 @@ __device__ __forceinline__ void residue_block(const ResArgs &a, u32 block, u64 (
     }
 }
 
-__global__ __launch_bounds__(256) void k_residues(ResArgs a, ResArgs b, u32 na)
+// the factors of one or two products: left, right, left, right; end: their workgroups, added up
+struct ResSet { ResArgs r[4]; u32 end[4]; };
+__global__ __launch_bounds__(256) void k_residues(ResSet set)
 {
     __shared__ u64 s_t[4][32 * 33];
-    if (blockIdx.x < na) {
-        if (a.x.ks == 1) residue_block<false, true>(a, blockIdx.x, s_t); else residue_block<false, false>(a, blockIdx.x, s_t);
-    } else if (b.x.ks == 1) residue_block<true, true>(b, blockIdx.x - na, s_t);
-    else residue_block<true, false>(b, blockIdx.x - na, s_t);
+    const u32 b = blockIdx.x, i = (b >= set.end[0] ? 1u : 0u) + (b >= set.end[1] ? 1u : 0u) + (b >= set.end[2] ? 1u : 0u);
+    const ResArgs &a = set.r[i];
+    const u32 block = b - (i ? set.end[i - 1] : 0);
+    if (i & 1) { if (a.x.ks == 1) residue_block<true, true>(a, block, s_t); else residue_block<true, false>(a, block, s_t); }
+    else if (a.x.ks == 1) residue_block<false, true>(a, block, s_t);
+    else residue_block<false, false>(a, block, s_t);
 }
 
 // The products of residues: for every party and modulus the sum of two products, party p's
@@ -890,17 +899,22 @@ __global__ __launch_bounds__(256) void k_residues(ResArgs a, ResArgs b, u32 na)
 // flight during the step before), where an operand lies as it is loaded: no bank conflicts.  The right factor takes the role of rows, so
 // that a lane holds four adjacent columns of a result.  Consecutive workgroups of an XCD take the tiles of one product.
 struct RmmArgs { const unsigned char *A, *B; unsigned char *R; u64 amat, bmat, plane; u32 M, N, narb, nbrb, nstep, ntm, ntn, total; int asums; };   // amat, bmat: bytes of a modulus's matrix; narb: blocks of 32 rows
+// One or two products in a launch: workgroups below na are the first one's.
+struct RmmSet { RmmArgs m[2]; u32 na; };
 template <int WM, int WN>
-__global__ __launch_bounds__(256, WM == 4 ? 2 : WM == 2 ? 3 : 4) void k_rns_mm(RmmArgs a)
+__global__ __launch_bounds__(256, WM == 4 ? 2 : WM == 2 ? 3 : 4) void k_rns_mm(RmmSet set)
 {
+    const bool second = blockIdx.x >= set.na;
+    const RmmArgs &a = set.m[second ? 1 : 0];
+    const u32 block = second ? blockIdx.x - set.na : blockIdx.x;
     constexpr int FA = 2 * WM, FB = 2 * WN, STEP = 2 * (FA + FB) * 1024;       // operands of 32 rows a workgroup, bytes of a step
     constexpr int LD = 64 * WN + 16, OUT = 64 * WM * LD;
     constexpr int LOADS = STEP / 4096;                                         // of 16 bytes a lane
     __shared__ __align__(16) unsigned char s_buf[2 * STEP > OUT ? 2 * STEP : OUT];
     const u32 tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave & 1, wn = wave >> 1;
     // blocks go to the XCDs in turn: XCD x takes the x-th eighth of the work
-    const u32 per = (a.total + 7) / 8, id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-    if ((blockIdx.x >> 3) >= per || id >= a.total) return;
+    const u32 per = (a.total + 7) / 8, id = (block & 7) * per + (block >> 3);
+    if ((block >> 3) >= per || id >= a.total) return;
     const u32 tiles = a.ntm * a.ntn, batch = id / tiles, tile = id % tiles, p = batch / RNS_N, mi = batch % RNS_N;
     // groups of 8 row tiles, column tiles one after the other
     const u32 grp = tile / (8 * a.ntn), gm = a.ntm - grp * 8 < 8 ? a.ntm - grp * 8 : 8, in = tile - grp * 8 * a.ntn;

@@ -52,9 +52,11 @@ static int do_finish(gt_ctx *c, int src, bool relu, u64 n, u32 ncol, const FinOu
     FinArgs a{};
     a.c = kc(c, c->op++); a.Z = c->dacc; a.n = n; a.ncol = ncol; a.f = c->tau; a.S = S; a.x = x;
     a.y = o.y; a.gate = o.gate; a.res = o.res; a.bias = o.bias; a.has_res = o.has_res; a.has_gate = o.has_gate; a.has_bias = o.has_bias;
-    if (n) GTCHK(src == FIN_SCALE ? launch(c, GT_KC_FINISH, k_finish<FIN_SCALE, false>, gF(n), B64, a)
-                 : relu ? launch(c, GT_KC_FINISH, k_finish<FIN_PARTS, true>, gF(n), B64, a)
-                 : launch(c, GT_KC_FINISH, k_finish<FIN_PARTS, false>, gF(n), B64, a));
+    FinSet set{};
+    set.f[0] = a; set.na = gF(n).x;
+    if (n) GTCHK(src == FIN_SCALE ? launch(c, GT_KC_FINISH, k_finish<FIN_SCALE, false>, gF(n), B64, set)
+                 : relu ? launch(c, GT_KC_FINISH, k_finish<FIN_PARTS, true>, gF(n), B64, set)
+                 : launch(c, GT_KC_FINISH, k_finish<FIN_PARTS, false>, gF(n), B64, set));
     acct_finish(c, n, relu);
     return GT_OK;
 }
@@ -69,6 +71,11 @@ static int grow_res(gt_ctx *c, size_t need)
     c->res_bytes = need;
     return GT_OK;
 }
+static u32 fin_blocks(const FinShape &s, u64 n)
+{
+    const u64 per = s.pairs ? GT_FP_CHUNK : (u64)GT_FIN_EL * s.per;
+    return (u32)std::min<u64>((n + per - 1) / per, 1u << 16);
+}
 // arguments of a factor's conversion, and its workgroups
 static ResArgs residues(gt_ctx *c, const MatView &x, unsigned char *out, u64 rows, u64 K, u64 k0, u32 nrb, u32 nkb, bool sums, u32 *blocks)
 {
@@ -79,51 +86,125 @@ static ResArgs residues(gt_ctx *c, const MatView &x, unsigned char *out, u64 row
     *blocks = (u32)((nfr + 3) / 4) * a.mats * ((RNS_N + a.per - 1) / a.per);
     return a;
 }
-// completion of the product of A (M x K) and B (N x K), by residues: rows in blocks, the long axis in chunks of RNS_TERMS
-static int do_dense(gt_ctx *c, MatView A, const MatView &B, u64 M, u64 N, u64 K, bool relu, const FinOut &o)
-{
-    FinArgs f{};
-    f.c = kc(c, c->op++); f.ncol = (u32)N; f.f = c->tau;
-    f.y = o.y; f.gate = o.gate; f.res = o.res; f.bias = o.bias; f.has_res = o.has_res; f.has_gate = o.has_gate; f.has_bias = o.has_bias;
-    const u32 nchunk = (u32)((K + RNS_TERMS - 1) / RNS_TERMS);
-    const u64 step = rns_rows(N);
-    for (u64 r0 = 0; r0 < M; r0 += step) {
-        const u64 m = std::min<u64>(M - r0, step);
-        const RmmShape s = rmm_shape(c->simds, m, N);
-        const u32 narb = (u32)(s.ntm * 2 * s.wm), nbrb = (u32)(s.ntn * 2 * s.wn);
-        const bool asums = m <= N;                                       // the factor with fewer rows is converted twice
-        const u32 nkb = (u32)((std::min<u64>(K, RNS_TERMS) + 63) / 64 * 2);
-        const u64 amat = (u64)narb * nkb * 1024, bmat = (u64)nbrb * nkb * 1024, plane = (m * N + 1279) / 1280 * 1280;        // whole tiles of both completions
-        const u64 abytes = (asums ? 6 : 3) * RNS_N * amat, bbytes = (asums ? 3 : 6) * RNS_N * bmat, rbytes = 3 * RNS_N * plane;
-        GTCHK(grow_res(c, abytes + bbytes + nchunk * rbytes));
-        MatView Ar = A;
-        for (int j = 0; j < 3; j++) Ar.c[j] += r0 * A.rs;          // (A is no tiled matrix)
-        for (u32 ch = 0; ch < nchunk; ch++) {
-            const u64 k0 = (u64)ch * RNS_TERMS, k = std::min<u64>(K - k0, RNS_TERMS);
-            const u32 kb = (u32)((k + 63) / 64 * 2);
-            u32 na, nb;
-            const ResArgs ra = residues(c, Ar, c->res, m, k, k0, narb, kb, asums, &na), rb = residues(c, B, c->res + abytes, N, k, k0, nbrb, kb, !asums, &nb);
-            GTCHK(launch(c, GT_KC_DENSE, k_residues, dim3(na + nb), B256, ra, rb, na));
-            RmmArgs a{};
-            a.A = c->res; a.B = c->res + abytes; a.R = c->res + abytes + bbytes + ch * rbytes; a.amat = (u64)narb * kb * 1024; a.bmat = (u64)nbrb * kb * 1024;
-            a.plane = plane; a.M = (u32)m; a.N = (u32)N; a.narb = narb; a.nbrb = nbrb; a.nstep = kb; a.ntm = (u32)s.ntm; a.ntn = (u32)s.ntn; a.asums = asums;
-            a.total = (u32)(3 * RNS_N * s.ntm * s.ntn);
-            const dim3 g((a.total + 7) / 8 * 8);
-            GTCHK(s.wm == 4 ? launch(c, GT_KC_DENSE, k_rns_mm<4, 2>, g, B256, a) : s.wm == 2 ? launch(c, GT_KC_DENSE, k_rns_mm<2, 2>, g, B256, a) : launch(c, GT_KC_DENSE, k_rns_mm<1, 1>, g, B256, a));
-        }
-        f.R = c->res + abytes + bbytes; f.first = r0 * N; f.plane = plane; f.nchunk = nchunk; f.n = m * N;
-        const FinShape fs = fin_shape(c->simds, f.n);
-        f.per = fs.per;
-        if (fs.pairs) {
-            const dim3 g((unsigned)std::min<u64>((f.n + GT_FP_CHUNK - 1) / GT_FP_CHUNK, 1u << 16));
-            GTCHK(relu ? launch(c, GT_KC_FINISH, k_finish_pair<true>, g, B64, f) : launch(c, GT_KC_FINISH, k_finish_pair<false>, g, B64, f));
-        } else {
-            const u64 tiles = (f.n + GT_FIN_EL - 1) / GT_FIN_EL;
-            const dim3 g((unsigned)std::min<u64>((tiles + f.per - 1) / f.per, 1u << 16));
-            GTCHK(relu ? launch(c, GT_KC_FINISH, k_finish<FIN_RES, true>, g, B64, f) : launch(c, GT_KC_FINISH, k_finish<FIN_RES, false>, g, B64, f));
-        }
+// A product of A (M x K) and B (N x K) by residues with its completion: what a pass over some rows and all of the long axis needs.
+struct RnsJob {
+    MatView A, B;
+    u64 M, N, K;
+    bool relu;
+    FinArgs f;
+    RmmShape s;
+    bool asums;
+    u32 nchunk, narb, nbrb;
+    u64 plane, abytes, bbytes, rbytes;
+    unsigned char *at;
+    RnsJob() {}
+    RnsJob(gt_ctx *c, const MatView &A_, const MatView &B_, u64 M_, u64 N_, u64 K_, bool relu_, const FinOut &o) : A(A_), B(B_), M(M_), N(N_), K(K_), relu(relu_), f{}
+    {
+        f.c = kc(c, c->op++); f.ncol = (u32)N; f.f = c->tau;
+        f.y = o.y; f.gate = o.gate; f.res = o.res; f.bias = o.bias; f.has_res = o.has_res; f.has_gate = o.has_gate; f.has_bias = o.has_bias;
+        acct_finish(c, M * N, relu);
+        shape(c);
     }
-    acct_finish(c, M * N, relu);
+    void shape(gt_ctx *c)
+    {
+        s = rmm_shape(c->simds, M, N);
+        asums = M <= N;                                                  // the factor with fewer rows is converted twice
+        nchunk = (u32)((K + RNS_TERMS - 1) / RNS_TERMS);
+        narb = (u32)(s.ntm * 2 * s.wm); nbrb = (u32)(s.ntn * 2 * s.wn);
+        const u64 nkb = (std::min<u64>(K, RNS_TERMS) + 63) / 64 * 2;
+        plane = (M * N + 1279) / 1280 * 1280;                            // whole tiles of both completions
+        abytes = (asums ? 6 : 3) * RNS_N * narb * nkb * 1024; bbytes = (asums ? 3 : 6) * RNS_N * nbrb * nkb * 1024; rbytes = 3 * RNS_N * plane;
+    }
+    u64 bytes() const { return abytes + bbytes + nchunk * rbytes; }
+    u32 nkb(u32 ch) const { return (u32)((std::min<u64>(K - (u64)ch * RNS_TERMS, RNS_TERMS) + 63) / 64 * 2); }
+    ResArgs left(gt_ctx *c, u32 ch, u32 *blocks) const
+    { const u64 k0 = (u64)ch * RNS_TERMS; return residues(c, A, at, M, std::min<u64>(K - k0, RNS_TERMS), k0, narb, nkb(ch), asums, blocks); }
+    ResArgs right(gt_ctx *c, u32 ch, u32 *blocks) const
+    { const u64 k0 = (u64)ch * RNS_TERMS; return residues(c, B, at + abytes, N, std::min<u64>(K - k0, RNS_TERMS), k0, nbrb, nkb(ch), !asums, blocks); }
+    RmmArgs product(u32 ch) const
+    {
+        RmmArgs a{};
+        a.A = at; a.B = at + abytes; a.R = at + abytes + bbytes + ch * rbytes; a.amat = (u64)narb * nkb(ch) * 1024; a.bmat = (u64)nbrb * nkb(ch) * 1024;
+        a.plane = plane; a.M = (u32)M; a.N = (u32)N; a.narb = narb; a.nbrb = nbrb; a.nstep = nkb(ch); a.ntm = (u32)s.ntm; a.ntn = (u32)s.ntn; a.asums = asums;
+        a.total = (u32)(3 * RNS_N * s.ntm * s.ntn);
+        return a;
+    }
+};
+static u32 rmm_blocks(const RmmArgs &a) { return (a.total + 7) / 8 * 8; }
+static int rmm_launch(gt_ctx *c, u32 wm, const RmmSet &m, u32 blocks)
+{
+    return wm == 4 ? launch(c, GT_KC_DENSE, k_rns_mm<4, 2>, dim3(blocks), B256, m) : wm == 2 ? launch(c, GT_KC_DENSE, k_rns_mm<2, 2>, dim3(blocks), B256, m)
+           : launch(c, GT_KC_DENSE, k_rns_mm<1, 1>, dim3(blocks), B256, m);
+}
+// rows in blocks, the long axis in chunks of RNS_TERMS
+static int run_job(gt_ctx *c, const RnsJob &all)
+{
+    const u64 step = rns_rows(all.N);
+    for (u64 r0 = 0; r0 < all.M; r0 += step) {
+        RnsJob j = all;
+        j.M = std::min<u64>(all.M - r0, step);
+        for (int p = 0; p < 3; p++) j.A.c[p] += r0 * j.A.rs;             // (the left factor is no matrix of weights)
+        if (j.M != all.M) j.shape(c);
+        GTCHK(grow_res(c, j.bytes()));
+        j.at = c->res;
+        for (u32 ch = 0; ch < j.nchunk; ch++) {
+            ResSet r{};
+            u32 na, nb;
+            r.r[0] = j.left(c, ch, &na); r.r[1] = j.right(c, ch, &nb);
+            r.end[0] = na; r.end[1] = r.end[2] = r.end[3] = na + nb;
+            GTCHK(launch(c, GT_KC_DENSE, k_residues, dim3(na + nb), B256, r));
+            RmmSet m{};
+            m.m[0] = j.product(ch); m.na = rmm_blocks(m.m[0]);
+            GTCHK(rmm_launch(c, j.s.wm, m, m.na));
+        }
+        FinSet f{};
+        f.f[0] = j.f;
+        f.f[0].R = j.at + j.abytes + j.bbytes; f.f[0].first = r0 * j.N; f.f[0].plane = j.plane; f.f[0].nchunk = j.nchunk; f.f[0].n = j.M * j.N;
+        const FinShape fs = fin_shape(c->simds, j.M * j.N);
+        f.f[0].per = fs.per;
+        f.na = fin_blocks(fs, j.M * j.N);
+        const dim3 g(f.na);
+        if (fs.pairs) GTCHK(j.relu ? launch(c, GT_KC_FINISH, k_finish_pair<true>, g, B64, f.f[0]) : launch(c, GT_KC_FINISH, k_finish_pair<false>, g, B64, f.f[0]));
+        else GTCHK(j.relu ? launch(c, GT_KC_FINISH, k_finish<FIN_RES, true>, g, B64, f) : launch(c, GT_KC_FINISH, k_finish<FIN_RES, false>, g, B64, f));
+    }
+    return GT_OK;
+}
+// Two products that do not wait for each other, without activation: side by side in the same three launches where neither fills the chip alone (267 x 22 -> 16:
+// 12 launches of a backward pass, 66 us, where the host's calls count, to 9).
+static int run_jobs(gt_ctx *c, const RnsJob &x, const RnsJob &y)
+{
+    if (x.nchunk != 1 || y.nchunk != 1 || x.M > rns_rows(x.N) || y.M > rns_rows(y.N) || x.s.wm != y.s.wm || x.s.wm == 4) {
+        GTCHK(run_job(c, x));
+        return run_job(c, y);
+    }
+    RnsJob j[2] = { x, y };
+    FinShape fs[2];
+    GTCHK(grow_res(c, x.bytes() + y.bytes()));
+    j[0].at = c->res; j[1].at = c->res + x.bytes();
+    ResSet r{};
+    RmmSet m{};
+    FinSet f{};
+    u32 rblocks = 0, mblocks = 0, fblocks = 0;
+    for (int i = 0; i < 2; i++) {
+        u32 na, nb;
+        r.r[2 * i] = j[i].left(c, 0, &na); r.r[2 * i + 1] = j[i].right(c, 0, &nb);
+        r.end[2 * i] = rblocks + na; r.end[2 * i + 1] = rblocks += na + nb;
+        m.m[i] = j[i].product(0);
+        mblocks += rmm_blocks(m.m[i]);
+        f.f[i] = j[i].f;
+        fs[i] = fin_shape(c->simds, j[i].M * j[i].N);
+        f.f[i].R = j[i].at + j[i].abytes + j[i].bbytes; f.f[i].plane = j[i].plane; f.f[i].nchunk = 1; f.f[i].n = j[i].M * j[i].N; f.f[i].per = fs[i].per;
+        fblocks += fin_blocks(fs[i], f.f[i].n);
+        if (i == 0) { m.na = mblocks; f.na = fblocks; }
+    }
+    GTCHK(launch(c, GT_KC_DENSE, k_residues, dim3(rblocks), B256, r));
+    GTCHK(rmm_launch(c, x.s.wm, m, mblocks));
+    if (!fs[0].pairs && !fs[1].pairs) return launch(c, GT_KC_FINISH, k_finish<FIN_RES, false>, dim3(fblocks), B64, f);
+    for (int i = 0; i < 2; i++) {
+        FinSet one{};
+        one.f[0] = f.f[i]; one.na = fin_blocks(fs[i], f.f[i].n);
+        GTCHK(fs[i].pairs ? launch(c, GT_KC_FINISH, k_finish_pair<false>, dim3(one.na), B64, one.f[0]) : launch(c, GT_KC_FINISH, k_finish<FIN_RES, false>, dim3(one.na), B64, one));
+    }
     return GT_OK;
 }
 // Parts of the product of few rows x (M rows of K words) and weights, or, transposed, the weights' rows as columns, in the workspace of
@@ -147,7 +228,7 @@ static int few_parts(gt_ctx *c, P6 x, u64 ldx, const WMat &W, bool transposed, u
 static int do_dense_w(gt_ctx *c, P6 x, u64 ldx, const WMat &W, bool transposed, u64 M, bool relu, const FinOut &o)
 {
     const u64 N = transposed ? W.K : W.N, K = transposed ? W.N : W.K;
-    if (M == 0 || !few_rows(M, ldx)) return do_dense(c, view(x, ldx, 1), transposed ? wmat(W) : wmat_t(W), M, N, K, relu, o);
+    if (M == 0 || !few_rows(M, ldx)) return run_job(c, RnsJob(c, view(x, ldx, 1), transposed ? wmat(W) : wmat_t(W), M, N, K, relu, o));
     GTCHK(few_parts(c, x, ldx, W, transposed, M));
     return do_finish(c, FIN_PARTS, relu, M * N, (u32)N, o);
 }
@@ -227,16 +308,16 @@ extern "C" int gt_dense_backward(gt_ctx *c, const gt_dense *l, const gt_shares *
         if (n) GTCHK(launch(c, GT_KC_MULT, k_mult, dim3(tiles8(n)), GT_BLOCK, m));
         acct_reshare(c, n, 1);
     }
-    if (dx) {
-        FinOut o;
-        o.y = to_p6(dx);
-        GTCHK(do_dense_w(c, dz, l->dout, l->W, true, rows, false, o));
+    FinOut ox, ow;
+    if (dx) ox.y = to_p6(dx);
+    if (dW) ow.y = to_p6(dW);
+    if (dx && (rows == 0 || few_rows(rows, l->dout) || !dW)) GTCHK(do_dense_w(c, dz, l->dout, l->W, true, rows, false, ox));
+    else if (dx) {
+        const RnsJob jx(c, view(dz, l->dout, 1), wmat(l->W), rows, l->din, l->dout, false, ox), jw(c, view(to_p6(x), 1, l->din), view(dz, 1, l->dout), l->din, l->dout, rows, false, ow);
+        GTCHK(run_jobs(c, jx, jw));
+        dW = nullptr;
     }
-    if (dW) {
-        FinOut o;
-        o.y = to_p6(dW);
-        GTCHK(do_dense(c, view(to_p6(x), 1, l->din), view(dz, 1, l->dout), l->din, l->dout, rows, false, o));
-    }
+    if (dW) GTCHK(run_job(c, RnsJob(c, view(to_p6(x), 1, l->din), view(dz, 1, l->dout), l->din, l->dout, rows, false, ow)));
     if (db) {
         ColsumArgs a{}; a.x = dz; a.out = to_p6(db); a.rows = rows; a.cols = l->dout;
         const u64 ngrp = (l->dout + 15) / 16, ranges = std::max<u64>(1, std::min<u64>((rows + 255) / 256, c->simds / (3 * ngrp)));

@@ -7,6 +7,7 @@ fallback: if the library is missing, loading fails loudly.
 import ctypes as C
 import os
 import re
+import struct
 
 import numpy as np
 
@@ -30,6 +31,9 @@ class _Plane2(C.Structure):
 
 class _Shares(C.Structure):
     _fields_ = [("party", _Plane2 * 3), ("n", C.c_size_t)]
+
+
+_SHARES_WORDS = struct.Struct("=7Q").pack               # the same as raw words, filled in one call
 
 
 class _Stats(C.Structure):
@@ -146,14 +150,8 @@ class Shares:
         self.t = t if t is not None else torch.zeros((3, 2, max(self.n, 1)), dtype=torch.int64, device=device)
 
     def c_struct(self):
-        s = _Shares()
-        stride = self.t.stride(1) * 8
-        base = self.t.data_ptr()
-        for p in range(3):
-            s.party[p].own = base + (2 * p) * stride
-            s.party[p].next = base + (2 * p + 1) * stride
-        s.n = self.n
-        return s
+        a, b = self.t.data_ptr(), self.t.stride(1) * 8
+        return _Shares.from_buffer_copy(_SHARES_WORDS(a, a + b, a + 2 * b, a + 3 * b, a + 4 * b, a + 5 * b, self.n))
 
     def planes(self):
         """numpy uint64 array (3, 2, n)."""
