@@ -924,27 +924,28 @@ __global__ __launch_bounds__(256, WM == 4 ? 2 : WM == 2 ? 3 : 4) void k_rns_mm(R
     const u32 half = a.nstep / 2;                                              // steps of a product
     // a wavefront's loads of a step: operands q * 4 + wave of [2 blocks of terms][FA] of the left factor, then of the right one
     const unsigned char *at[LOADS];
-    auto start = [&](const unsigned char *A, const unsigned char *B) {
+#pragma unroll
+    for (int q = 0; q < LOADS; q++) {
+        const u32 o = q * 4 + wave;
+        const bool isA = o < 2 * FA;
+        const u32 w = isA ? o : o - 2 * FA, kb = isA ? w / FA : w / FB, r = isA ? w % FA : w % FB;
+        at[q] = isA ? A0 + ((u64)kb * a.narb + tm * FA + r) * 1024 : B0 + ((u64)kb * a.nbrb + tn * FB + r) * 1024;
+    }
+    const u64 nextA = (u64)a.narb * 2048, nextB = (u64)a.nbrb * 2048;          // to the next step, or to the second product
+    const u64 jumpA = (u64)(A1 - A0) - (half - 1) * nextA, jumpB = (u64)(B1 - B0) - (half - 1) * nextB;
+    v4i st[2][LOADS];
+    auto fetch = [&](u32 s, int to) {
+        const bool jump = s + 1 == half;
+        const u64 da = jump ? jumpA : nextA, db = jump ? jumpB : nextB;
 #pragma unroll
         for (int q = 0; q < LOADS; q++) {
-            const u32 o = q * 4 + wave;
-            const bool isA = o < 2 * FA;
-            const u32 w = isA ? o : o - 2 * FA, kb = isA ? w / FA : w / FB, r = isA ? w % FA : w % FB;
-            at[q] = isA ? A + ((u64)kb * a.narb + tm * FA + r) * 1024 : B + ((u64)kb * a.nbrb + tn * FB + r) * 1024;
+            st[to][q] = *(const v4i *)(at[q] + lane * 16);
+            at[q] += q * 4 + (int)wave < 2 * FA ? da : db;
         }
     };
-    v4i st[LOADS];
-    auto fetch = [&](u32 s) {
-        if (s == half) start(A1, B1);
+    auto put = [&](int buf) {
 #pragma unroll
-        for (int q = 0; q < LOADS; q++) {
-            st[q] = *(const v4i *)(at[q] + lane * 16);
-            at[q] += (u64)(q * 4 + (int)wave < 2 * FA ? a.narb : a.nbrb) * 2048;
-        }
-    };
-    auto put = [&](u32 buf) {
-#pragma unroll
-        for (int q = 0; q < LOADS; q++) *(v4i *)(s_buf + buf * STEP + (q * 4 + wave) * 1024 + lane * 16) = st[q];
+        for (int q = 0; q < LOADS; q++) *(v4i *)(s_buf + buf * STEP + (q * 4 + wave) * 1024 + lane * 16) = st[buf][q];
     };
     v16i acc[WM][WN];
 #pragma unroll
@@ -953,13 +954,10 @@ __global__ __launch_bounds__(256, WM == 4 ? 2 : WM == 2 ? 3 : 4) void k_rns_mm(R
         for (int j = 0; j < WN; j++)
 #pragma unroll
             for (int v = 0; v < 16; v++) acc[i][j][v] = 0;
-    start(A0, B0);
-    fetch(0);
-    put(0);
-    __syncthreads();
-    for (u32 s = 0; s < a.nstep; s++) {
-        if (s + 1 < a.nstep) fetch(s + 1);
-        const unsigned char *buf = s_buf + (s & 1) * STEP + lane * 16;
+    // Step s, of parity par: its matrix instructions, between them the words of step s + 1 (loaded during step s - 2) go to LDS, whose half was last read
+    // in step s - 1, and the loads of step s + 3 start.
+    auto step = [&](u32 s, int par, auto NEXT, auto MORE) {
+        const unsigned char *buf = s_buf + par * STEP + lane * 16;
         v4i x[2][WM], w[2][WN];
 #pragma unroll
         for (int kb = 0; kb < 2; kb++) {
@@ -969,16 +967,39 @@ __global__ __launch_bounds__(256, WM == 4 ? 2 : WM == 2 ? 3 : 4) void k_rns_mm(R
             for (int i = 0; i < WM; i++) x[kb][i] = *(const v4i *)(buf + (kb * FA + wm * WM + i) * 1024);
         }
         __builtin_amdgcn_sched_barrier(0);
+        if (decltype(NEXT)::value) put(par ^ 1);
+        if (decltype(MORE)::value) fetch(s + 3, par ^ 1);
 #pragma unroll
         for (int kb = 0; kb < 2; kb++)
 #pragma unroll
             for (int i = 0; i < WM; i++)
 #pragma unroll
                 for (int j = 0; j < WN; j++) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[kb][j], x[kb][i], acc[i][j], 0, 0, 0);
+#pragma unroll
+        for (int q = 0; q < 2 * WM * WN; q++) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            if (decltype(NEXT)::value && q < LOADS) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
+            if (decltype(MORE)::value && q < LOADS) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+        }
         __builtin_amdgcn_sched_barrier(0);
-        if (s + 1 < a.nstep) put((s + 1) & 1);
         __syncthreads();
-    }
+    };
+    const std::integral_constant<bool, true> yes;
+    const std::integral_constant<bool, false> no;
+    fetch(0, 0);
+    fetch(1, 1);
+    put(0);
+    u32 s = 0;                                                                 // (steps are even in number)
+    if (a.nstep > 2) {
+        fetch(2, 0);
+        __syncthreads();
+        for (; s + 4 < a.nstep; s += 2) { step(s, 0, yes, yes); step(s + 1, 1, yes, yes); }
+        step(s, 0, yes, yes);
+        step(s + 1, 1, yes, no);
+        s += 2;
+    } else __syncthreads();
+    step(s, 0, yes, no);
+    step(s + 1, 1, no, no);
     // |sum| < 2^28: low 13 bits and the rest times 2^13 mod m, below 2^21.1, then the balanced residue; through LDS to rows
     const float inv = d_rns.inv[mi];
     const u32 neg = 256 - (u32)d_rns.m[mi];
