@@ -277,9 +277,8 @@ __device__ __forceinline__ u64 rns_join(const u32 (&r)[5])
 }
 
 // Completion.  Z: the parties' parts, [3][n] words, left at zero for the next product; bias: ncol words or none.
-// FIN_RES: R: residues of the elements from `first` on, planes [chunk][party][modulus] of `plane` bytes, chunks added up; a workgroup takes
-// `per` tiles at a time, at most 8: a lane of a party turns the residues of eight adjacent ones into words and leaves them in LDS.
-enum { FIN_PARTS = 0, FIN_SCALE = 1, FIN_RES = 2 };   // parts in memory; z = row factor S[e / ncol] times x (experts' gates); residues
+// k_finish_pair: R: residues of the elements from `first` on, planes [chunk][party][modulus] of `plane` bytes, chunks added up; per: see there.
+enum { FIN_PARTS = 0, FIN_SCALE = 1 };                // parts in memory; z = row factor S[e / ncol] times x (experts' gates)
 struct FinArgs { KCommon c; u64 *Z; P6 bias, res, y, gate, S, x; u64 n; u32 ncol, f; int has_bias, has_res, has_gate; const unsigned char *R; u64 first, plane; u32 nchunk, per; };
 // a party's parts of eight adjacent elements (of the launch's, from i0, a multiple of 8) from their residues
 __device__ __forceinline__ void rns_words(const FinArgs &a, int p, u64 i0, u64 (&zw)[8])
@@ -306,43 +305,26 @@ __device__ __forceinline__ void rns_words(const FinArgs &a, int p, u64 i0, u64 (
         }
     }
 }
-// One or two completions in a launch: workgroups below na are the first one's.
-struct FinSet { FinArgs f[2]; u32 na; };
 template <int SRC, bool RELU>
-__global__ __launch_bounds__(64) void k_finish(FinSet set)
+__global__ __launch_bounds__(64) void k_finish(FinArgs a)
 {
-    const bool second = blockIdx.x >= set.na;
-    const FinArgs &a = set.f[second ? 1 : 0];
-    const u32 block = second ? blockIdx.x - set.na : blockIdx.x, blocks = second ? gridDim.x - set.na : set.na;
     __shared__ uint4 s_msg[GT_LANES];
     __shared__ u64 s_mat[GT_FIN_WORDS(RELU ? 3 : 2)];
     __shared__ u64 s_cnt[6];
-    __shared__ u64 s_z[SRC == FIN_RES ? 3 : 1][SRC == FIN_RES ? 8 * GT_FIN_EL + 8 : 1];
     FWire W; W.init(s_msg, s_cnt);
     FinTile<RELU ? 3 : 2> T; T.keys = a.c.keys; T.mat = s_mat; T.f = a.f;
     const int p = W.p;
     const u32 f = a.f;
-    const bool narrow = a.first + a.n <= 0xffffffffu;
-    const u32 PER = SRC == FIN_RES ? a.per : 1;                       // tiles at a time
+    const bool narrow = a.n <= 0xffffffffu;
     const u64 tiles = (a.n + GT_FIN_EL - 1) / GT_FIN_EL;
-    for (u64 tile = (u64)block * PER, sub = 0; tile < tiles; sub++, tile += sub == PER ? (u64)(blocks - 1) * PER + 1 : 1, sub = sub == PER ? 0 : sub) {
-        if (SRC == FIN_RES && sub == 0) {
-            u64 zw[8];
-            const u32 t8 = W.t < 2 * PER ? W.t : 2 * PER - 1;
-            rns_words(a, p, tile * GT_FIN_EL + 8 * t8, zw);
-            wave_sync();
-#pragma unroll
-            for (int i = 0; i < 8; i++) s_z[p][8 * t8 + i] = zw[i];
-            wave_sync();
-        }
-        const u64 e0 = a.first + tile * GT_FIN_EL, e = e0 + W.t;
-        const bool act = tile * GT_FIN_EL + W.t < a.n;
+    for (u64 tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const u64 e0 = tile * GT_FIN_EL, e = e0 + W.t;
+        const bool act = e < a.n;
         const u64 row = !act ? 0 : (narrow ? (u64)((u32)e / a.ncol) : e / a.ncol), col = act ? e - row * a.ncol : 0;
         u64 z = 0;
         if (act) {
             if (SRC == FIN_PARTS) { z = a.Z[(u64)p * a.n + e]; if (W.real) a.Z[(u64)p * a.n + e] = 0; }
-            else if (SRC == FIN_SCALE) z = prod3(ld(a.S, p, row), ld(a.x, p, e));
-            else z = s_z[p][sub * GT_FIN_EL + W.t];
+            else z = prod3(ld(a.S, p, row), ld(a.x, p, e));
             if (a.has_bias) z += own_of(a.bias, p)[col] << f;
         }
         T.deal(a.c.op, e0);
@@ -358,11 +340,11 @@ __global__ __launch_bounds__(64) void k_finish(FinSet set)
 }
 
 // ---------------------------------------------------------------------------------
-// The completion of many elements: tiles of 40, two per lane of a party (lanes 0-19 of its 21), so that two passes of the block function (80 dealer
+// The completion of residues: tiles of 40, two per lane of a party (lanes 0-19 of its 21), so that two passes of the block function (80 dealer
 // blocks and 45 blocks of three streams on 2 x 63 lanes) and a chain of messages serve 40 elements where k_finish spends a pass and a chain on 16.
 #define GT_FP_EL 40
 #define GT_FP_ROW 40                              // words of a row of material; rows as in FinTile, streams' rows from 22 on
-#define GT_FP_CHUNK 160                           // elements whose residues a party's 20 lanes join at a time, eight adjacent ones each
+#define GT_FP_CHUNK 160                           // elements whose residues a party's 20 lanes join at a time at most, eight adjacent ones each: `per` tiles
 template <int NS>
 struct FinPair {
     const u32 *keys;
@@ -482,14 +464,18 @@ __device__ __forceinline__ void less_pair(WWire &W, const u64 (&c)[2], const Sh 
     W.nresh += nresh * live2;
 }
 
+// One or two completions in a launch: workgroups below na are the first one's.
+struct FinSet { FinArgs f[2]; u32 na; };
 template <bool RELU>
-__global__ __launch_bounds__(64) void k_finish_pair(FinArgs a)
+__global__ __launch_bounds__(64) void k_finish_pair(FinSet set)
 {
+    const bool second = blockIdx.x >= set.na;
+    const FinArgs &a = set.f[second ? 1 : 0];
+    const u32 block = second ? blockIdx.x - set.na : blockIdx.x, blocks = second ? gridDim.x - set.na : set.na;
     constexpr int NS = RELU ? 3 : 2;
     __shared__ uint4 s_msg[GT_LANES];
     __shared__ u64 s_mat[(22 + 3 * NS) * GT_FP_ROW];
     __shared__ u64 s_cnt[6];
-    __shared__ u64 s_z[3][GT_FP_CHUNK];
     WWire W; W.init(s_msg, s_cnt);
     FinPair<NS> T; T.keys = a.c.keys; T.mat = s_mat; T.f = a.f;
     const int p = W.p;
@@ -500,16 +486,11 @@ __global__ __launch_bounds__(64) void k_finish_pair(FinArgs a)
     // the party's planes, chosen once
     u64 *const yo = own_of(a.y, p), *const yn = nxt_of(a.y, p), *const go = own_of(a.gate, p), *const gn = nxt_of(a.gate, p);
     const u64 *const ro = own_of(a.res, p), *const rn = nxt_of(a.res, p), *const bo = own_of(a.bias, p);
-    for (u64 c0 = (u64)blockIdx.x * GT_FP_CHUNK; c0 < a.n; c0 += (u64)gridDim.x * GT_FP_CHUNK) {
-        {
-            u64 zw[8];
-            rns_words(a, p, c0 + 8 * t, zw);
-            wave_sync();
-#pragma unroll
-            for (int i = 0; i < 8; i++) s_z[p][8 * t + i] = zw[i];
-            wave_sync();
-        }
-        for (u32 k0 = 0; k0 < GT_FP_CHUNK && c0 + k0 < a.n; k0 += GT_FP_EL) {
+    const u32 chunk = a.per * GT_FP_EL, t8 = t < 5 * a.per ? t : 5 * a.per - 1;
+    for (u64 c0 = (u64)block * chunk; c0 < a.n; c0 += (u64)blocks * chunk) {
+        u64 zw[8];
+        rns_words(a, p, c0 + 8 * t8, zw);
+        for (u32 k0 = 0; k0 < chunk && c0 + k0 < a.n; k0 += GT_FP_EL) {
             const u64 e0 = a.first + c0 + k0;
             const u32 el[2] = { t, t + 20 };
             bool act[2];
@@ -519,7 +500,17 @@ __global__ __launch_bounds__(64) void k_finish_pair(FinArgs a)
             for (int q = 0; q < 2; q++) {
                 act[q] = W.t < 20 && c0 + k0 + el[q] < a.n;
                 e[q] = a.first + (c0 + k0 + el[q] < a.n ? c0 + k0 + el[q] : a.n - 1);         // (a last tile loads its last element where none exists)
-                z[q] = s_z[p][k0 + el[q]];
+            }
+            // the tile's words from the five lanes that joined them, through the message region
+            {
+                u64 *words = (u64 *)s_msg + GT_FP_EL * p;
+                const u32 from = 8 * t8 - k0;                        // (wraps for the lanes of tiles before)
+                wave_sync();
+                if (from < GT_FP_EL)
+#pragma unroll
+                    for (int i = 0; i < 8; i++) words[from + i] = zw[i];
+                wave_sync();
+                z[0] = words[t]; z[1] = words[t + 20];
             }
             const u32 na = (u32)act[0] + (u32)act[1];
             if (a.has_bias)

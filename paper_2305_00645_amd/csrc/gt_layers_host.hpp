@@ -52,11 +52,9 @@ static int do_finish(gt_ctx *c, int src, bool relu, u64 n, u32 ncol, const FinOu
     FinArgs a{};
     a.c = kc(c, c->op++); a.Z = c->dacc; a.n = n; a.ncol = ncol; a.f = c->tau; a.S = S; a.x = x;
     a.y = o.y; a.gate = o.gate; a.res = o.res; a.bias = o.bias; a.has_res = o.has_res; a.has_gate = o.has_gate; a.has_bias = o.has_bias;
-    FinSet set{};
-    set.f[0] = a; set.na = gF(n).x;
-    if (n) GTCHK(src == FIN_SCALE ? launch(c, GT_KC_FINISH, k_finish<FIN_SCALE, false>, gF(n), B64, set)
-                 : relu ? launch(c, GT_KC_FINISH, k_finish<FIN_PARTS, true>, gF(n), B64, set)
-                 : launch(c, GT_KC_FINISH, k_finish<FIN_PARTS, false>, gF(n), B64, set));
+    if (n) GTCHK(src == FIN_SCALE ? launch(c, GT_KC_FINISH, k_finish<FIN_SCALE, false>, gF(n), B64, a)
+                 : relu ? launch(c, GT_KC_FINISH, k_finish<FIN_PARTS, true>, gF(n), B64, a)
+                 : launch(c, GT_KC_FINISH, k_finish<FIN_PARTS, false>, gF(n), B64, a));
     acct_finish(c, n, relu);
     return GT_OK;
 }
@@ -71,10 +69,13 @@ static int grow_res(gt_ctx *c, size_t need)
     c->res_bytes = need;
     return GT_OK;
 }
-static u32 fin_blocks(const FinShape &s, u64 n)
+// a completion of residues, and its workgroups
+static u32 fin_residues(gt_ctx *c, FinArgs &f, const unsigned char *R, u64 first, u64 n, u64 plane, u32 nchunk)
 {
-    const u64 per = s.pairs ? GT_FP_CHUNK : (u64)GT_FIN_EL * s.per;
-    return (u32)std::min<u64>((n + per - 1) / per, 1u << 16);
+    f.R = R; f.first = first; f.n = n; f.plane = plane; f.nchunk = nchunk;
+    f.per = fin_tiles(c->simds, n);
+    const u64 chunk = (u64)f.per * GT_FP_EL;
+    return (u32)std::min<u64>((n + chunk - 1) / chunk, 1u << 16);
 }
 // arguments of a factor's conversion, and its workgroups
 static ResArgs residues(gt_ctx *c, const MatView &x, unsigned char *out, u64 rows, u64 K, u64 k0, u32 nrb, u32 nkb, bool sums, u32 *blocks)
@@ -159,13 +160,8 @@ static int run_job(gt_ctx *c, const RnsJob &all)
         }
         FinSet f{};
         f.f[0] = j.f;
-        f.f[0].R = j.at + j.abytes + j.bbytes; f.f[0].first = r0 * j.N; f.f[0].plane = j.plane; f.f[0].nchunk = j.nchunk; f.f[0].n = j.M * j.N;
-        const FinShape fs = fin_shape(c->simds, j.M * j.N);
-        f.f[0].per = fs.per;
-        f.na = fin_blocks(fs, j.M * j.N);
-        const dim3 g(f.na);
-        if (fs.pairs) GTCHK(j.relu ? launch(c, GT_KC_FINISH, k_finish_pair<true>, g, B64, f.f[0]) : launch(c, GT_KC_FINISH, k_finish_pair<false>, g, B64, f.f[0]));
-        else GTCHK(j.relu ? launch(c, GT_KC_FINISH, k_finish<FIN_RES, true>, g, B64, f) : launch(c, GT_KC_FINISH, k_finish<FIN_RES, false>, g, B64, f));
+        f.na = fin_residues(c, f.f[0], j.at + j.abytes + j.bbytes, r0 * j.N, j.M * j.N, j.plane, j.nchunk);
+        GTCHK(j.relu ? launch(c, GT_KC_FINISH, k_finish_pair<true>, dim3(f.na), B64, f) : launch(c, GT_KC_FINISH, k_finish_pair<false>, dim3(f.na), B64, f));
     }
     return GT_OK;
 }
@@ -178,7 +174,6 @@ static int run_jobs(gt_ctx *c, const RnsJob &x, const RnsJob &y)
         return run_job(c, y);
     }
     RnsJob j[2] = { x, y };
-    FinShape fs[2];
     GTCHK(grow_res(c, x.bytes() + y.bytes()));
     j[0].at = c->res; j[1].at = c->res + x.bytes();
     ResSet r{};
@@ -192,20 +187,12 @@ static int run_jobs(gt_ctx *c, const RnsJob &x, const RnsJob &y)
         m.m[i] = j[i].product(0);
         mblocks += rmm_blocks(m.m[i]);
         f.f[i] = j[i].f;
-        fs[i] = fin_shape(c->simds, j[i].M * j[i].N);
-        f.f[i].R = j[i].at + j[i].abytes + j[i].bbytes; f.f[i].plane = j[i].plane; f.f[i].nchunk = 1; f.f[i].n = j[i].M * j[i].N; f.f[i].per = fs[i].per;
-        fblocks += fin_blocks(fs[i], f.f[i].n);
+        fblocks += fin_residues(c, f.f[i], j[i].at + j[i].abytes + j[i].bbytes, 0, j[i].M * j[i].N, j[i].plane, 1);
         if (i == 0) { m.na = mblocks; f.na = fblocks; }
     }
     GTCHK(launch(c, GT_KC_DENSE, k_residues, dim3(rblocks), B256, r));
     GTCHK(rmm_launch(c, x.s.wm, m, mblocks));
-    if (!fs[0].pairs && !fs[1].pairs) return launch(c, GT_KC_FINISH, k_finish<FIN_RES, false>, dim3(fblocks), B64, f);
-    for (int i = 0; i < 2; i++) {
-        FinSet one{};
-        one.f[0] = f.f[i]; one.na = fin_blocks(fs[i], f.f[i].n);
-        GTCHK(fs[i].pairs ? launch(c, GT_KC_FINISH, k_finish_pair<false>, dim3(one.na), B64, one.f[0]) : launch(c, GT_KC_FINISH, k_finish<FIN_RES, false>, dim3(one.na), B64, one));
-    }
-    return GT_OK;
+    return launch(c, GT_KC_FINISH, k_finish_pair<false>, dim3(fblocks), B64, f);
 }
 // Parts of the product of few rows x (M rows of K words) and weights, or, transposed, the weights' rows as columns, in the workspace of
 // partial inner products; div: a division that may run beside it.

@@ -251,11 +251,17 @@ static inline u32 residue_range(u64 simds, u64 operands)
     const u64 parts = std::min<u64>(6, std::max<u64>(1, 4 * simds / std::max<u64>(1, operands)));
     return (u32)((18 + parts - 1) / parts);
 }
-// completion of residues: two elements per lane, or tiles of 16, `per` of them joined at a time
-struct FinShape { bool pairs; u32 per; };
-static inline FinShape fin_shape(u64 simds, u64 n)
+// completion of residues (k_finish_pair): tiles of 40 whose residues a wavefront joins together, at most 4: what leaves the fewest rounds of three wavefronts
+// per SIMD, a join priced as 0.45 of a tile
+static inline u32 fin_tiles(u64 simds, u64 n)
 {
-    FinShape s = { n >= 160 * simds, 8 };
-    while (s.per > 1 && n < 16 * s.per * 2 * simds) s.per /= 2;
-    return s;
+    const u64 tiles = (n + 39) / 40;
+    u32 best = 4;
+    double least = 0;
+    for (u32 per = 4; per >= 1; per--) {
+        const u64 waves = (tiles + per - 1) / per, rounds = (waves + 3 * simds - 1) / (3 * simds);
+        const double cost = (double)rounds * (per + 0.45);
+        if (per == 4 || cost < least) { best = per; least = cost; }
+    }
+    return best;
 }
