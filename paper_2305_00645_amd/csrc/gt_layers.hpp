@@ -279,7 +279,7 @@ __device__ __forceinline__ u64 rns_join(const u32 (&r)[5])
 // Completion.  Z: the parties' parts, [3][n] words, left at zero for the next product; bias: ncol words or none.
 // k_finish_pair: R: residues of the elements from `first` on, planes [chunk][party][modulus] of `plane` bytes, chunks added up; per: see there.
 enum { FIN_PARTS = 0, FIN_SCALE = 1 };                // parts in memory; z = row factor S[e / ncol] times x (experts' gates)
-struct FinArgs { KCommon c; u64 *Z; P6 bias, res, y, gate, S, x; u64 n; u32 ncol, f; int has_bias, has_res, has_gate; const unsigned char *R; u64 first, plane; u32 nchunk, per; };
+struct FinArgs { KCommon c; u64 *Z; P6 bias, res, y, gate, S, x; u64 n; u32 ncol, f; int has_bias, has_res, has_gate; const unsigned char *R; u64 first, plane; u32 nchunk, per, nbig; };
 // a party's parts of eight adjacent elements (of the launch's, from i0, a multiple of 8) from their residues
 __device__ __forceinline__ void rns_words(const FinArgs &a, int p, u64 i0, u64 (&zw)[8])
 {
@@ -342,9 +342,9 @@ __global__ __launch_bounds__(64) void k_finish(FinArgs a)
 // ---------------------------------------------------------------------------------
 // The completion of residues: tiles of 40, two per lane of a party (lanes 0-19 of its 21), so that two passes of the block function (80 dealer
 // blocks and 45 blocks of three streams on 2 x 63 lanes) and a chain of messages serve 40 elements where k_finish spends a pass and a chain on 16.
+// The first nbig wavefronts take `per` tiles (at most 4), whose residues a party's 20 lanes join together, eight adjacent elements each, the others one.
 #define GT_FP_EL 40
 #define GT_FP_ROW 40                              // words of a row of material; rows as in FinTile, streams' rows from 22 on
-#define GT_FP_CHUNK 160                           // elements whose residues a party's 20 lanes join at a time at most, eight adjacent ones each: `per` tiles
 template <int NS>
 struct FinPair {
     const u32 *keys;
@@ -471,7 +471,7 @@ __global__ __launch_bounds__(64) void k_finish_pair(FinSet set)
 {
     const bool second = blockIdx.x >= set.na;
     const FinArgs &a = set.f[second ? 1 : 0];
-    const u32 block = second ? blockIdx.x - set.na : blockIdx.x, blocks = second ? gridDim.x - set.na : set.na;
+    const u32 block = second ? blockIdx.x - set.na : blockIdx.x;
     constexpr int NS = RELU ? 3 : 2;
     __shared__ uint4 s_msg[GT_LANES];
     __shared__ u64 s_mat[(22 + 3 * NS) * GT_FP_ROW];
@@ -486,8 +486,9 @@ __global__ __launch_bounds__(64) void k_finish_pair(FinSet set)
     // the party's planes, chosen once
     u64 *const yo = own_of(a.y, p), *const yn = nxt_of(a.y, p), *const go = own_of(a.gate, p), *const gn = nxt_of(a.gate, p);
     const u64 *const ro = own_of(a.res, p), *const rn = nxt_of(a.res, p), *const bo = own_of(a.bias, p);
-    const u32 chunk = a.per * GT_FP_EL, t8 = t < 5 * a.per ? t : 5 * a.per - 1;
-    for (u64 c0 = (u64)block * chunk; c0 < a.n; c0 += (u64)blocks * chunk) {
+    const u32 per = block < a.nbig ? a.per : 1, chunk = per * GT_FP_EL, t8 = t < 5 * per ? t : 5 * per - 1;
+    {
+        const u64 c0 = (block < a.nbig ? (u64)block * a.per : (u64)a.nbig * (a.per - 1) + block) * GT_FP_EL;
         u64 zw[8];
         rns_words(a, p, c0 + 8 * t8, zw);
         for (u32 k0 = 0; k0 < chunk && c0 + k0 < a.n; k0 += GT_FP_EL) {

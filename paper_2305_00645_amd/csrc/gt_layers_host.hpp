@@ -73,9 +73,9 @@ static int grow_res(gt_ctx *c, size_t need)
 static u32 fin_residues(gt_ctx *c, FinArgs &f, const unsigned char *R, u64 first, u64 n, u64 plane, u32 nchunk)
 {
     f.R = R; f.first = first; f.n = n; f.plane = plane; f.nchunk = nchunk;
-    f.per = fin_tiles(c->simds, n);
-    const u64 chunk = (u64)f.per * GT_FP_EL;
-    return (u32)std::min<u64>((n + chunk - 1) / chunk, 1u << 16);
+    const FinShape s = fin_shape(c->simds, n);
+    f.per = s.per; f.nbig = s.nbig;
+    return s.waves;
 }
 // arguments of a factor's conversion, and its workgroups
 static ResArgs residues(gt_ctx *c, const MatView &x, unsigned char *out, u64 rows, u64 K, u64 k0, u32 nrb, u32 nkb, bool sums, u32 *blocks)

@@ -251,17 +251,14 @@ static inline u32 residue_range(u64 simds, u64 operands)
     const u64 parts = std::min<u64>(6, std::max<u64>(1, 4 * simds / std::max<u64>(1, operands)));
     return (u32)((18 + parts - 1) / parts);
 }
-// completion of residues (k_finish_pair): tiles of 40 whose residues a wavefront joins together, at most 4: what leaves the fewest rounds of three wavefronts
-// per SIMD, a join priced as 0.45 of a tile
-static inline u32 fin_tiles(u64 simds, u64 n)
+// Completion of residues (k_finish_pair): the first nbig wavefronts take `per` tiles of 40, whose residues they join together (a join costs as much as 0.45 of
+// a tile, however many), the others one, so that three wavefronts of every SIMD end together.  At most 2^27 elements and a row are completed at a time.
+struct FinShape { u32 per, nbig, waves; };
+static inline FinShape fin_shape(u64 simds, u64 n)
 {
-    const u64 tiles = (n + 39) / 40;
-    u32 best = 4;
-    double least = 0;
-    for (u32 per = 4; per >= 1; per--) {
-        const u64 waves = (tiles + per - 1) / per, rounds = (waves + 3 * simds - 1) / (3 * simds);
-        const double cost = (double)rounds * (per + 0.45);
-        if (per == 4 || cost < least) { best = per; least = cost; }
-    }
-    return best;
+    const u64 tiles = (n + 39) / 40, slots = 3 * simds;
+    FinShape s = { tiles >= 2 * slots ? 4u : tiles >= slots ? 2u : 1u, 0, 0 };
+    if (s.per > 1) s.nbig = (u32)((tiles - slots / 2) / s.per);
+    s.waves = (u32)(tiles - (u64)s.nbig * (s.per - 1));
+    return s;
 }
