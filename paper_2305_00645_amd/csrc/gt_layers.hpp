@@ -592,19 +592,17 @@ __global__ __launch_bounds__(64) void k_finish_pair(FinSet set)
 }
 
 // ---------------------------------------------------------------------------------
-// A matrix of shared words by component, element (row, k) at c[j][row * rs + k * ks], or weights (tiled): 1: rows are their columns, 2: their rows.
+// A matrix of shared words by component. MAT_ROWS: element (row, k) at c[j][row * ld + k], MAT_COLS: at c[j][row + k * ld]; or weights in tiles, MAT_W: rows are
+// theirs, MAT_WT: rows are their columns.
 // Weights lie in tiles of 64 rows x 16 columns in the order in which a wavefront of k_mm_few takes them, [block of 16 columns][64 rows]
 // [component][8][64 lanes][2 words]: lane n % 16 + 16 (k % 64 / 16) has the 16 words of its column in pairs, so that a step of a wavefront is 24 KB on end (with
 // rows of words, 128 bytes at a time, 2.8-3.4 TB/s).  A word is kept as its eight signed bytes d_s, sum of d_s 256^s.
 #define GT_WTILE 1024
-struct MatView { const u64 *c[3]; u64 rs, ks; u32 tiled, nst; };
-__device__ __host__ __forceinline__ u64 wtile_at(u64 k, u64 n, u32 nst)
+enum { MAT_ROWS = 0, MAT_COLS = 1, MAT_W = 2, MAT_WT = 3 };
+struct MatView { const u64 *c[3]; u64 ld; u32 kind, nst; };
+__device__ __forceinline__ u64 wtile_at(u64 k, u64 n, u32 nst)
 {
     return ((n >> 4) * nst + (k >> 6)) * (3 * GT_WTILE) + ((k & 15) >> 1) * 128 + ((n & 15) + (k & 48)) * 2 + (k & 1);
-}
-__device__ __forceinline__ u64 mat_at(const MatView &m, u64 r, u64 k)
-{
-    return m.tiled == 0 ? r * m.rs + k * m.ks : m.tiled == 1 ? wtile_at(k, r, m.nst) : wtile_at(r, k, m.nst);
 }
 
 // Parts of the product of a few rows with a weight matrix, on the matrix cores in signed 8-bit limbs (36 products of
@@ -814,45 +812,81 @@ __global__ __launch_bounds__(256, 1) void k_mm_few(FewArgs a)
 // (3-5), or the components alone (0-2).  Rows and terms beyond the matrix are zero.  A residue: two four-byte dot products of the word's
 // signed bytes with the powers of 256, a rounded quotient in floating point.  RIGHT: times (M / m_i)^-1.
 // A wavefront makes an operand of 32 x 32 words of one matrix for `per` moduli; a launch makes both factors' (blocks below na: the left one's).
-// KC: terms contiguous in memory; the words then go through LDS, so that loads are of whole rows.  Bound: what it writes, 18 bytes a word, and reads (2048 x 1024
+// MAT_ROWS: the words go through LDS, so that loads are of whole rows.  Bound: what it writes, 18 bytes a word, and reads (2048 x 1024
 // words in six matrices 36 us, 5 TB/s; with a lane's terms from memory, all moduli and matrices by one wavefront, 95).
 struct ResArgs { MatView x; unsigned char *out; u64 rows, K, k0; u32 nrb, nkb, per, mats; };
-template <bool RIGHT, bool KC>
+// an operand's words, a lane's 16 terms (MAT_ROWS: of rows 2 i + hi its term lr): component x0, or with x1 its sum with that one, as signed bytes
+template <int KIND>
+__device__ __forceinline__ void residue_words(const ResArgs &a, const u64 *x0, const u64 *x1, bool sum, u32 rb, u32 kb, u32 lr, u32 hi, u64 (&x)[16])
+{
+    const u64 r0 = (u64)rb * 32, k0 = (u64)kb * 32;
+    u64 t[16];
+    if (KIND == MAT_W || KIND == MAT_WT) {
+        // zero where the padded matrix has none
+        const bool in = r0 < (a.rows + 63) / 64 * 64 && k0 < (a.K + 63) / 64 * 64;
+        const u64 n = KIND == MAT_W ? a.k0 + k0 + 16 * hi : r0 + lr, k = KIND == MAT_W ? r0 + lr : a.k0 + k0 + 16 * hi;
+        const u64 at = in ? wtile_at(k, n, a.x.nst) : 0;
+#pragma unroll
+        for (int i = 0; i < 16; i++) {                                // (MAT_W: the next column, MAT_WT: the next row)
+            const u32 d = KIND == MAT_W ? 2 * i : (i >> 1) * 128 + (i & 1);
+            x[i] = x0[at + d];
+            t[i] = sum ? x1[at + d] : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+            if (sum) x[i] = ((((x[i] ^ GT_BIAS) - GT_BIAS) + ((t[i] ^ GT_BIAS) - GT_BIAS)) + GT_BIAS) ^ GT_BIAS;
+            if (!in) x[i] = 0;
+        }
+        return;
+    }
+    const u64 ld = a.x.ld;
+    if (r0 + 32 <= a.rows && k0 + 32 <= a.K) {                        // a whole operand: uniform addresses and a lane's offset
+        const u64 first = KIND == MAT_ROWS ? r0 * ld + a.k0 + k0 : r0 + (a.k0 + k0) * ld, step = KIND == MAT_ROWS ? 2 * ld : ld;
+        const u32 off = (KIND == MAT_ROWS ? hi * (u32)ld + lr : hi * 16 * (u32)ld + lr) * 8;
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+            x[i] = ld_at<u64>(x0 + first + i * step, off);
+            t[i] = sum ? ld_at<u64>(x1 + first + i * step, off) : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; i++) x[i] = (x[i] + t[i] + GT_BIAS) ^ GT_BIAS;
+        return;
+    }
+    // (words that exist are loaded where these do not, and cleared)
+#pragma unroll
+    for (int i = 0; i < 16; i++) {
+        const u64 r = r0 + (KIND == MAT_ROWS ? 2 * i + hi : lr), k = k0 + (KIND == MAT_ROWS ? lr : hi * 16 + i);
+        const u64 re = r < a.rows ? r : a.rows - 1, ke = a.k0 + (k < a.K ? k : a.K - 1), at = KIND == MAT_ROWS ? re * ld + ke : re + ke * ld;
+        x[i] = x0[at];
+        t[i] = sum ? x1[at] : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; i++) {
+        const u64 r = r0 + (KIND == MAT_ROWS ? 2 * i + hi : lr), k = k0 + (KIND == MAT_ROWS ? lr : hi * 16 + i);
+        x[i] = ((x[i] + t[i] + GT_BIAS) ^ GT_BIAS) & (0 - (u64)(r < a.rows && k < a.K));
+    }
+}
+template <bool RIGHT, int KIND>
 __device__ __forceinline__ void residue_block(const ResArgs &a, u32 block, u64 (*s_t)[32 * 33])
 {
+    constexpr bool KC = KIND == MAT_ROWS || KIND == MAT_W;
     const u32 lane = threadIdx.x & 63, lr = lane & 31, hi = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const u32 nfb = (u32)(((u64)a.nrb * a.nkb + 3) / 4), q = block / nfb % a.mats, range = block / nfb / a.mats;
     const u64 nfr = (u64)a.nrb * a.nkb, mat = nfr * 1024;
-    const u64 fr = (u64)(block % nfb) * 4 + wave;
+    const u32 fr = block % nfb * 4 + wave;
     if (fr >= nfr) return;
     // neighbours along the axis that is contiguous in memory
-    const u32 rb = (u32)(KC ? fr / a.nkb : fr % a.nrb), kb = (u32)(KC ? fr % a.nkb : fr / a.nrb);
+    const u32 rb = KC ? fr / a.nkb : fr % a.nrb, kb = KC ? fr % a.nkb : fr / a.nrb;
     const bool sum = a.mats == 6 && q < 3;
     const u64 *x0 = q % 3 == 0 ? a.x.c[0] : (q % 3 == 1 ? a.x.c[1] : a.x.c[2]), *x1 = q == 0 ? a.x.c[1] : (q == 1 ? a.x.c[2] : a.x.c[0]);
     u64 x[16];
-    {
-        // (words that exist are loaded where these do not, and cleared)
-        u64 t[16];
+    residue_words<KIND>(a, x0, x1, sum, rb, kb, lr, hi, x);
+    if (KIND == MAT_ROWS) {
 #pragma unroll
-        for (int i = 0; i < 16; i++) {
-            const u64 r = (u64)rb * 32 + (KC ? 2 * i + hi : lr), k = (u64)kb * 32 + (KC ? lr : hi * 16 + i);
-            const u64 at = mat_at(a.x, r < a.rows ? r : a.rows - 1, a.k0 + (k < a.K ? k : a.K - 1));
-            x[i] = x0[at];
-            t[i] = sum ? x1[at] : 0;
-        }
+        for (int i = 0; i < 16; i++) s_t[wave][(2 * i + hi) * 33 + lr] = x[i];
+        wave_sync();
 #pragma unroll
-        for (int i = 0; i < 16; i++) {
-            const u64 r = (u64)rb * 32 + (KC ? 2 * i + hi : lr), k = (u64)kb * 32 + (KC ? lr : hi * 16 + i);
-            if (a.x.tiled) { x[i] = (x[i] ^ GT_BIAS) - GT_BIAS; t[i] = sum ? (t[i] ^ GT_BIAS) - GT_BIAS : 0; }
-            x[i] = ((x[i] + t[i] + GT_BIAS) ^ GT_BIAS) & (0 - (u64)(r < a.rows && k < a.K));
-        }
-        if (KC) {
-#pragma unroll
-            for (int i = 0; i < 16; i++) s_t[wave][(2 * i + hi) * 33 + lr] = x[i];
-            wave_sync();
-#pragma unroll
-            for (int i = 0; i < 16; i++) x[i] = s_t[wave][lr * 33 + hi * 16 + i];
-        }
+        for (int i = 0; i < 16; i++) x[i] = s_t[wave][lr * 33 + hi * 16 + i];
     }
     unsigned char *out = a.out + (u64)q * RNS_N * mat + ((u64)kb * a.nrb + rb) * 1024 + lane * 16;
     const u32 i0 = range * a.per, i1 = i0 + a.per < RNS_N ? i0 + a.per : RNS_N;
@@ -879,9 +913,10 @@ __global__ __launch_bounds__(256) void k_residues(ResSet set)
     const u32 b = blockIdx.x, i = (b >= set.end[0] ? 1u : 0u) + (b >= set.end[1] ? 1u : 0u) + (b >= set.end[2] ? 1u : 0u);
     const ResArgs &a = set.r[i];
     const u32 block = b - (i ? set.end[i - 1] : 0);
-    if (i & 1) { if (a.x.ks == 1) residue_block<true, true>(a, block, s_t); else residue_block<true, false>(a, block, s_t); }
-    else if (a.x.ks == 1) residue_block<false, true>(a, block, s_t);
-    else residue_block<false, false>(a, block, s_t);
+    if (!(i & 1)) { if (a.x.kind == MAT_ROWS) residue_block<false, MAT_ROWS>(a, block, s_t); else residue_block<false, MAT_COLS>(a, block, s_t); }
+    else if (a.x.kind == MAT_COLS) residue_block<true, MAT_COLS>(a, block, s_t);
+    else if (a.x.kind == MAT_W) residue_block<true, MAT_W>(a, block, s_t);
+    else residue_block<true, MAT_WT>(a, block, s_t);
 }
 
 // The products of residues: for every party and modulus the sum of two products, party p's

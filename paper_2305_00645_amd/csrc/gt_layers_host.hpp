@@ -21,11 +21,9 @@ static int wmat_put(gt_ctx *c, const WMat &w, const gt_shares *src, u64 row0, u6
     a.src = to_p6(src); a.dst = w.base; a.row0 = row0; a.rows = rows; a.cols = w.N; a.nst = w.nst;
     return launch(c, GT_KC_LOCAL, k_put, g1(rows * w.N), B256, a);
 }
-static MatView wview(const WMat &w, u32 tiled) { MatView v{}; for (int j = 0; j < 3; j++) v.c[j] = w.base + (u64)j * GT_WTILE; v.tiled = tiled; v.nst = w.nst; return v; }
-// rows: the matrix's columns (outputs), k: its rows
-static MatView wmat_t(const WMat &w) { return wview(w, 1); }
-static MatView wmat(const WMat &w) { return wview(w, 2); }
-static MatView view(P6 a, u64 rs, u64 ks) { MatView v{}; for (int j = 0; j < 3; j++) v.c[j] = a.o[j]; v.rs = rs; v.ks = ks; return v; }
+static MatView wmat(const WMat &w, u32 kind)
+{ MatView v{}; for (int j = 0; j < 3; j++) v.c[j] = w.base + (u64)j * GT_WTILE; v.kind = kind; v.nst = w.nst; return v; }
+static MatView view(P6 a, u64 ld, u32 kind) { MatView v{}; for (int j = 0; j < 3; j++) v.c[j] = a.o[j]; v.ld = ld; v.kind = kind; return v; }
 
 struct gt_dense { u32 din, dout; bool has_b; WMat W; DSh b; };
 struct gt_moe {
@@ -87,7 +85,7 @@ static ResArgs residues(gt_ctx *c, const MatView &x, unsigned char *out, u64 row
     *blocks = (u32)((nfr + 3) / 4) * a.mats * ((RNS_N + a.per - 1) / a.per);
     return a;
 }
-// A product of A (M x K) and B (N x K) by residues with its completion: what a pass over some rows and all of the long axis needs.
+// A product of A (M x K, MAT_ROWS or MAT_COLS) and B (N x K, MAT_COLS or weights) by residues with its completion: what a pass over some rows and all of the long axis needs.
 struct RnsJob {
     MatView A, B;
     u64 M, N, K;
@@ -144,7 +142,7 @@ static int run_job(gt_ctx *c, const RnsJob &all)
     for (u64 r0 = 0; r0 < all.M; r0 += step) {
         RnsJob j = all;
         j.M = std::min<u64>(all.M - r0, step);
-        for (int p = 0; p < 3; p++) j.A.c[p] += r0 * j.A.rs;             // (the left factor is no matrix of weights)
+        for (int p = 0; p < 3; p++) j.A.c[p] += j.A.kind == MAT_ROWS ? r0 * j.A.ld : r0;
         if (j.M != all.M) j.shape(c);
         GTCHK(grow_res(c, j.bytes()));
         j.at = c->res;
@@ -215,7 +213,7 @@ static int few_parts(gt_ctx *c, P6 x, u64 ldx, const WMat &W, bool transposed, u
 static int do_dense_w(gt_ctx *c, P6 x, u64 ldx, const WMat &W, bool transposed, u64 M, bool relu, const FinOut &o)
 {
     const u64 N = transposed ? W.K : W.N, K = transposed ? W.N : W.K;
-    if (M == 0 || !few_rows(M, ldx)) return run_job(c, RnsJob(c, view(x, ldx, 1), transposed ? wmat(W) : wmat_t(W), M, N, K, relu, o));
+    if (M == 0 || !few_rows(M, ldx)) return run_job(c, RnsJob(c, view(x, ldx, MAT_ROWS), wmat(W, transposed ? MAT_W : MAT_WT), M, N, K, relu, o));
     GTCHK(few_parts(c, x, ldx, W, transposed, M));
     return do_finish(c, FIN_PARTS, relu, M * N, (u32)N, o);
 }
@@ -300,11 +298,11 @@ extern "C" int gt_dense_backward(gt_ctx *c, const gt_dense *l, const gt_shares *
     if (dW) ow.y = to_p6(dW);
     if (dx && (rows == 0 || few_rows(rows, l->dout) || !dW)) GTCHK(do_dense_w(c, dz, l->dout, l->W, true, rows, false, ox));
     else if (dx) {
-        const RnsJob jx(c, view(dz, l->dout, 1), wmat(l->W), rows, l->din, l->dout, false, ox), jw(c, view(to_p6(x), 1, l->din), view(dz, 1, l->dout), l->din, l->dout, rows, false, ow);
+        const RnsJob jx(c, view(dz, l->dout, MAT_ROWS), wmat(l->W, MAT_W), rows, l->din, l->dout, false, ox), jw(c, view(to_p6(x), l->din, MAT_COLS), view(dz, l->dout, MAT_COLS), l->din, l->dout, rows, false, ow);
         GTCHK(run_jobs(c, jx, jw));
         dW = nullptr;
     }
-    if (dW) GTCHK(run_job(c, RnsJob(c, view(to_p6(x), 1, l->din), view(dz, 1, l->dout), l->din, l->dout, rows, false, ow)));
+    if (dW) GTCHK(run_job(c, RnsJob(c, view(to_p6(x), l->din, MAT_COLS), view(dz, l->dout, MAT_COLS), l->din, l->dout, rows, false, ow)));
     if (db) {
         ColsumArgs a{}; a.x = dz; a.out = to_p6(db); a.rows = rows; a.cols = l->dout;
         const u64 ngrp = (l->dout + 15) / 16, ranges = std::max<u64>(1, std::min<u64>((rows + 255) / 256, c->simds / (3 * ngrp)));
