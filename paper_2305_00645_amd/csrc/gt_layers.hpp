@@ -816,55 +816,55 @@ __global__ __launch_bounds__(256, 1) void k_mm_few(FewArgs a)
 // words in six matrices 36 us, 5 TB/s; with a lane's terms from memory, all moduli and matrices by one wavefront, 95).
 struct ResArgs { MatView x; unsigned char *out; u64 rows, K, k0; u32 nrb, nkb, per, mats; };
 // an operand's words, a lane's 16 terms (MAT_ROWS: of rows 2 i + hi its term lr): component x0, or with x1 its sum with that one, as signed bytes
+// (a sum's second words are loaded in a loop of their own: with a condition at each, every load is waited for)
 template <int KIND>
 __device__ __forceinline__ void residue_words(const ResArgs &a, const u64 *x0, const u64 *x1, bool sum, u32 rb, u32 kb, u32 lr, u32 hi, u64 (&x)[16])
 {
-    const u64 r0 = (u64)rb * 32, k0 = (u64)kb * 32;
+    const u64 r0 = (u64)rb * 32, k0 = (u64)kb * 32, ld = a.x.ld;
     u64 t[16];
+    auto both = [&](auto at) {
+#pragma unroll
+        for (int i = 0; i < 16; i++) x[i] = at(x0, i);
+        if (sum) {
+#pragma unroll
+            for (int i = 0; i < 16; i++) t[i] = at(x1, i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; i++) t[i] = 0;
+        }
+    };
     if (KIND == MAT_W || KIND == MAT_WT) {
         // zero where the padded matrix has none
         const bool in = r0 < (a.rows + 63) / 64 * 64 && k0 < (a.K + 63) / 64 * 64;
         const u64 n = KIND == MAT_W ? a.k0 + k0 + 16 * hi : r0 + lr, k = KIND == MAT_W ? r0 + lr : a.k0 + k0 + 16 * hi;
-        const u64 at = in ? wtile_at(k, n, a.x.nst) : 0;
+        const u64 first = in ? wtile_at(k, n, a.x.nst) : 0;
+        // (MAT_W: the next column, MAT_WT: the next row)
+        both([&](const u64 *c, int i) { return c[first + (KIND == MAT_W ? 2 * i : (i >> 1) * 128 + (i & 1))]; });
+        if (sum)
 #pragma unroll
-        for (int i = 0; i < 16; i++) {                                // (MAT_W: the next column, MAT_WT: the next row)
-            const u32 d = KIND == MAT_W ? 2 * i : (i >> 1) * 128 + (i & 1);
-            x[i] = x0[at + d];
-            t[i] = sum ? x1[at + d] : 0;
-        }
+            for (int i = 0; i < 16; i++) x[i] = ((((x[i] ^ GT_BIAS) - GT_BIAS) + ((t[i] ^ GT_BIAS) - GT_BIAS)) + GT_BIAS) ^ GT_BIAS;
+        if (!in)
 #pragma unroll
-        for (int i = 0; i < 16; i++) {
-            if (sum) x[i] = ((((x[i] ^ GT_BIAS) - GT_BIAS) + ((t[i] ^ GT_BIAS) - GT_BIAS)) + GT_BIAS) ^ GT_BIAS;
-            if (!in) x[i] = 0;
-        }
+            for (int i = 0; i < 16; i++) x[i] = 0;
         return;
     }
-    const u64 ld = a.x.ld;
     if (r0 + 32 <= a.rows && k0 + 32 <= a.K) {                        // a whole operand: uniform addresses and a lane's offset
         const u64 first = KIND == MAT_ROWS ? r0 * ld + a.k0 + k0 : r0 + (a.k0 + k0) * ld, step = KIND == MAT_ROWS ? 2 * ld : ld;
         const u32 off = (KIND == MAT_ROWS ? hi * (u32)ld + lr : hi * 16 * (u32)ld + lr) * 8;
-#pragma unroll
-        for (int i = 0; i < 16; i++) {
-            x[i] = ld_at<u64>(x0 + first + i * step, off);
-            t[i] = sum ? ld_at<u64>(x1 + first + i * step, off) : 0;
-        }
+        both([&](const u64 *c, int i) { return ld_at<u64>(c + first + i * step, off); });
 #pragma unroll
         for (int i = 0; i < 16; i++) x[i] = (x[i] + t[i] + GT_BIAS) ^ GT_BIAS;
         return;
     }
     // (words that exist are loaded where these do not, and cleared)
+    auto row = [&](int i) { return r0 + (KIND == MAT_ROWS ? 2 * i + hi : lr); };
+    auto term = [&](int i) { return k0 + (KIND == MAT_ROWS ? lr : hi * 16 + i); };
+    both([&](const u64 *c, int i) {
+        const u64 r = row(i) < a.rows ? row(i) : a.rows - 1, k = a.k0 + (term(i) < a.K ? term(i) : a.K - 1);
+        return c[KIND == MAT_ROWS ? r * ld + k : r + k * ld];
+    });
 #pragma unroll
-    for (int i = 0; i < 16; i++) {
-        const u64 r = r0 + (KIND == MAT_ROWS ? 2 * i + hi : lr), k = k0 + (KIND == MAT_ROWS ? lr : hi * 16 + i);
-        const u64 re = r < a.rows ? r : a.rows - 1, ke = a.k0 + (k < a.K ? k : a.K - 1), at = KIND == MAT_ROWS ? re * ld + ke : re + ke * ld;
-        x[i] = x0[at];
-        t[i] = sum ? x1[at] : 0;
-    }
-#pragma unroll
-    for (int i = 0; i < 16; i++) {
-        const u64 r = r0 + (KIND == MAT_ROWS ? 2 * i + hi : lr), k = k0 + (KIND == MAT_ROWS ? lr : hi * 16 + i);
-        x[i] = ((x[i] + t[i] + GT_BIAS) ^ GT_BIAS) & (0 - (u64)(r < a.rows && k < a.K));
-    }
+    for (int i = 0; i < 16; i++) x[i] = ((x[i] + t[i] + GT_BIAS) ^ GT_BIAS) & (0 - (u64)(row(i) < a.rows && term(i) < a.K));
 }
 template <bool RIGHT, int KIND>
 __device__ __forceinline__ void residue_block(const ResArgs &a, u32 block, u64 (*s_t)[32 * 33])
