@@ -213,7 +213,7 @@ static int few_parts(gt_ctx *c, P6 x, u64 ldx, const WMat &W, bool transposed, u
 static int do_dense_w(gt_ctx *c, P6 x, u64 ldx, const WMat &W, bool transposed, u64 M, bool relu, const FinOut &o)
 {
     const u64 N = transposed ? W.K : W.N, K = transposed ? W.N : W.K;
-    if (M == 0 || !few_rows(M, ldx)) return run_job(c, RnsJob(c, view(x, ldx, MAT_ROWS), wmat(W, transposed ? MAT_W : MAT_WT), M, N, K, relu, o));
+    if (M == 0 || !few_rows(c->simds, M, N, K, ldx)) return run_job(c, RnsJob(c, view(x, ldx, MAT_ROWS), wmat(W, transposed ? MAT_W : MAT_WT), M, N, K, relu, o));
     GTCHK(few_parts(c, x, ldx, W, transposed, M));
     return do_finish(c, FIN_PARTS, relu, M * N, (u32)N, o);
 }
@@ -296,7 +296,7 @@ extern "C" int gt_dense_backward(gt_ctx *c, const gt_dense *l, const gt_shares *
     FinOut ox, ow;
     if (dx) ox.y = to_p6(dx);
     if (dW) ow.y = to_p6(dW);
-    if (dx && (rows == 0 || few_rows(rows, l->dout) || !dW)) GTCHK(do_dense_w(c, dz, l->dout, l->W, true, rows, false, ox));
+    if (dx && (rows == 0 || !dW || few_rows_apart(rows, l->din, l->dout))) GTCHK(do_dense_w(c, dz, l->dout, l->W, true, rows, false, ox));
     else if (dx) {
         const RnsJob jx(c, view(dz, l->dout, MAT_ROWS), wmat(l->W, MAT_W), rows, l->din, l->dout, false, ox), jw(c, view(to_p6(x), l->din, MAT_COLS), view(dz, l->dout, MAT_COLS), l->din, l->dout, rows, false, ow);
         GTCHK(run_jobs(c, jx, jw));
@@ -367,7 +367,7 @@ extern "C" int gt_moe_forward(gt_ctx *c, gt_moe *m, const gt_shares *x, size_t r
     const u64 E = m->E, d = m->d, ff = m->ff, rk = rows * m->k, P = E * (E - 1) / 2;
     if (!shares_ok(x, rows * d) || !shares_ok(y, rows * d) || (res && !shares_ok(res, rows * d))) return GT_EINVAL;
     Timed T(c);
-    const bool few = rk && few_rows(rk, E * (d + 1)) && few_rows(rows, E * (ff + 1));     // parts of the products by k_mm_few, else results
+    const bool few = rk && few_rows(c->simds, rk, ff, E * (d + 1), E * (d + 1)) && few_rows(c->simds, rows, d, E * (ff + 1), E * (ff + 1));     // parts of the products by k_mm_few, else results
     MoeArgs a{};
     a.s = m->s.v; a.bias = m->br.v; a.o = m->o.v; a.S = m->S.v; a.Q = m->Q.v; a.g = m->g.v; a.x = to_p6(x); a.xe = m->xe.v; a.hg = m->hg.v; a.he = m->he.v;
     a.rows = rows; a.E = (u32)E; a.k = m->k; a.d = m->d; a.ff = m->ff; a.f = c->tau; a.parts = few; a.has_bias = m->has_br;

@@ -213,8 +213,19 @@ static inline InferShape infer_shape(u64 simds, u32 lgi, u64 ngrp, u32 ntrees, u
 
 // Product of few rows with a weight matrix (k_mm_few): rows of a tile, tiles, groups of 64 columns, splits of the long axis and steps of 64
 // terms a split.
-#define GT_FEW_ROWS 32                       // rows up to which the weights' words are read again for every tile of rows
-static inline bool few_rows(u64 M, u64 ldx) { return M <= GT_FEW_ROWS && ldx < (1u << 25); }       // a tile's words at 32-bit offsets
+// Such a product, with its completion of words, or one by residues (k_residues, k_rns_mm, k_finish_pair)?  The first reads the weights' words again for every 16
+// rows and takes 36 products of limbs where the second takes 18 of residues, whose conversion costs more than the product where rows are few.  In us, with
+// ReLU, few and residues: 64 rows, 1024 x 4096 99, 173; 128 203, 203; 192 281, 280; 256 369, 307.  256 rows, 600 x 600 62, 64; 512 118, 90.  512 rows, 300 x 300
+// 43, 50; 64 x 1024 61, 66; 2048 rows, 100 x 200 60, 72, 22 x 16 15, 28.
+#define GT_FEW_ROWS 192
+static inline bool few_rows(u64 simds, u64 M, u64 N, u64 K, u64 ldx)
+{
+    if (ldx >= (1u << 25)) return false;                              // a row's words at 32-bit offsets
+    return M <= GT_FEW_ROWS || (M + 15) / 16 * ((N + 63) / 64) * ((K + 63) / 64) <= simds;        // four steps a compute unit
+}
+// dx of a backward pass that computes dW too, whose product by residues dx's can join: apart from it only where the conversion of the weights is much (both
+// gradients, us, apart and joined: 33 rows, 32 x 32 32, 23, 64 x 1024 45, 39, 600 x 600 80, 94, 1024 x 1024 133, 155; 128 rows 178, 162)
+static inline bool few_rows_apart(u64 rows, u64 din, u64 dout) { return rows <= 64 && din * dout >= (1u << 17); }
 struct FewShape { u32 rows; u64 ntile, ngrp; u32 nsplit, per; };
 static inline FewShape few_shape(u64 simds, u64 M, u64 N, u64 K)
 {
