@@ -278,7 +278,7 @@ __device__ __forceinline__ u64 rns_join(const u32 (&r)[5])
 
 // Completion.  Z: the parties' parts, [3][n] words, left at zero for the next product; bias: ncol words or none.
 // k_finish_pair: R: residues of the elements from `first` on, planes [chunk][party][modulus] of `plane` bytes, chunks added up; per: see there.
-enum { FIN_PARTS = 0, FIN_SCALE = 1 };                // parts in memory; z = row factor S[e / ncol] times x (experts' gates)
+enum { FIN_PARTS = 0, FIN_SCALE = 1, FIN_RES = 2 };   // parts in memory; z = row factor S[e / ncol] times x (experts' gates); residues
 struct FinArgs { KCommon c; u64 *Z; P6 bias, res, y, gate, S, x; u64 n; u32 ncol, f; int has_bias, has_res, has_gate; const unsigned char *R; u64 first, plane; u32 nchunk, per, nbig; };
 // a party's parts of eight adjacent elements (of the launch's, from i0, a multiple of 8) from their residues
 __device__ __forceinline__ void rns_words(const FinArgs &a, int p, u64 i0, u64 (&zw)[8])
@@ -340,9 +340,9 @@ __global__ __launch_bounds__(64) void k_finish(FinArgs a)
 }
 
 // ---------------------------------------------------------------------------------
-// The completion of residues: tiles of 40, two per lane of a party (lanes 0-19 of its 21), so that two passes of the block function (80 dealer
+// The completion of residues, and of many parts: tiles of 40, two per lane of a party (lanes 0-19 of its 21), so that two passes of the block function (80 dealer
 // blocks and 45 blocks of three streams on 2 x 63 lanes) and a chain of messages serve 40 elements where k_finish spends a pass and a chain on 16.
-// The first nbig wavefronts take `per` tiles (at most 4), whose residues a party's 20 lanes join together, eight adjacent elements each, the others one.
+// Residues: the first nbig wavefronts take `per` tiles (at most 4), whose residues a party's 20 lanes join together, eight adjacent elements each, the others one.
 #define GT_FP_EL 40
 #define GT_FP_ROW 40                              // words of a row of material; rows as in FinTile, streams' rows from 22 on
 template <int NS>
@@ -466,7 +466,7 @@ __device__ __forceinline__ void less_pair(WWire &W, const u64 (&c)[2], const Sh 
 
 // One or two completions in a launch: workgroups below na are the first one's.
 struct FinSet { FinArgs f[2]; u32 na; };
-template <bool RELU>
+template <int SRC, bool RELU>
 __global__ __launch_bounds__(64) void k_finish_pair(FinSet set)
 {
     const bool second = blockIdx.x >= set.na;
@@ -486,11 +486,11 @@ __global__ __launch_bounds__(64) void k_finish_pair(FinSet set)
     // the party's planes, chosen once
     u64 *const yo = own_of(a.y, p), *const yn = nxt_of(a.y, p), *const go = own_of(a.gate, p), *const gn = nxt_of(a.gate, p);
     const u64 *const ro = own_of(a.res, p), *const rn = nxt_of(a.res, p), *const bo = own_of(a.bias, p);
-    const u32 per = block < a.nbig ? a.per : 1, chunk = per * GT_FP_EL, t8 = t < 5 * per ? t : 5 * per - 1;
+    const u32 per = SRC == FIN_RES && block < a.nbig ? a.per : 1, chunk = per * GT_FP_EL, t8 = t < 5 * per ? t : 5 * per - 1;
     {
         const u64 c0 = (block < a.nbig ? (u64)block * a.per : (u64)a.nbig * (a.per - 1) + block) * GT_FP_EL;
         u64 zw[8];
-        rns_words(a, p, c0 + 8 * t8, zw);
+        if (SRC == FIN_RES) rns_words(a, p, c0 + 8 * t8, zw);
         for (u32 k0 = 0; k0 < chunk && c0 + k0 < a.n; k0 += GT_FP_EL) {
             const u64 e0 = a.first + c0 + k0;
             const u32 el[2] = { t, t + 20 };
@@ -502,6 +502,13 @@ __global__ __launch_bounds__(64) void k_finish_pair(FinSet set)
                 act[q] = W.t < 20 && c0 + k0 + el[q] < a.n;
                 e[q] = a.first + (c0 + k0 + el[q] < a.n ? c0 + k0 + el[q] : a.n - 1);         // (a last tile loads its last element where none exists)
             }
+            if (SRC == FIN_PARTS) {
+                u64 *from = a.Z + (u64)p * a.n;
+#pragma unroll
+                for (int q = 0; q < 2; q++) z[q] = from[e[q]];
+#pragma unroll
+                for (int q = 0; q < 2; q++) if (mine && act[q]) from[e[q]] = 0;
+            } else
             // the tile's words from the five lanes that joined them, through the message region
             {
                 u64 *words = (u64 *)s_msg + GT_FP_EL * p;
@@ -1075,29 +1082,32 @@ __global__ __launch_bounds__(256) void k_put(PutArgs a)
     }
 }
 
-// Column sums of a shared matrix (local): a workgroup per 16 columns, component and, for many rows, range of rows; the ranges' sums meet by
-// atomic adds in words that were cleared (exact, order-free).
-struct ColsumArgs { P6 x, out; u64 rows, per; u32 cols; int add; };
-__global__ __launch_bounds__(256) void k_colsum(ColsumArgs a)
+// Column sums of a shared matrix (local): a workgroup per 16 columns and component, 64 rows at a time.  Bound: reading the matrix (2048 x 1024, 50 MB).
+struct ColsumArgs { P6 x, out; u64 rows; u32 cols; };
+__global__ __launch_bounds__(1024) void k_colsum(ColsumArgs a)
 {
-    __shared__ u64 s_sum[16][17];
+    __shared__ u64 s_sum[64][17];
     const u32 c = threadIdx.x & 15, g = threadIdx.x >> 4, pl = blockIdx.y;
-    const u64 col = (u64)blockIdx.x * 16 + c, r0 = blockIdx.z * a.per, r1 = r0 + a.per < a.rows ? r0 + a.per : a.rows;
+    const u64 col = (u64)blockIdx.x * 16 + c;
     const u64 *x = pl == 0 ? a.x.o[0] : (pl == 1 ? a.x.o[1] : a.x.o[2]);
     u64 s = 0;
     if (col < a.cols) {
-#pragma unroll 4
-        for (u64 r = r0 + g; r < r1; r += 16) s += x[r * a.cols + col];
+#pragma unroll 8
+        for (u64 r = g; r < a.rows; r += 64) s += x[r * a.cols + col];
     }
     s_sum[g][c] = s;
     __syncthreads();
+    if (g < 8) {
+#pragma unroll
+        for (u32 i = 1; i < 8; i++) s += s_sum[g + 8 * i][c];
+        s_sum[g][c] = s;
+    }
+    __syncthreads();
     if (g == 0 && col < a.cols) {
 #pragma unroll
-        for (int i = 1; i < 16; i++) s += s_sum[i][c];
+        for (int i = 1; i < 8; i++) s += s_sum[i][c];
         // component pl: party pl's own, its predecessor's next one
-        u64 *o = &own_of(a.out, (int)pl)[col], *n = &nxt_of(a.out, pl == 0 ? 2 : (int)pl - 1)[col];
-        if (a.add) { atomicAdd((unsigned long long *)o, (unsigned long long)s); atomicAdd((unsigned long long *)n, (unsigned long long)s); }
-        else { *o = s; *n = s; }
+        own_of(a.out, (int)pl)[col] = s; nxt_of(a.out, pl == 0 ? 2 : (int)pl - 1)[col] = s;
     }
 }
 

@@ -50,7 +50,11 @@ static int do_finish(gt_ctx *c, int src, bool relu, u64 n, u32 ncol, const FinOu
     FinArgs a{};
     a.c = kc(c, c->op++); a.Z = c->dacc; a.n = n; a.ncol = ncol; a.f = c->tau; a.S = S; a.x = x;
     a.y = o.y; a.gate = o.gate; a.res = o.res; a.bias = o.bias; a.has_res = o.has_res; a.has_gate = o.has_gate; a.has_bias = o.has_bias;
-    if (n) GTCHK(src == FIN_SCALE ? launch(c, GT_KC_FINISH, k_finish<FIN_SCALE, false>, gF(n), B64, a)
+    if (src == FIN_PARTS && fin_pairs(c->simds, n)) {
+        FinSet set{};
+        set.f[0] = a; set.na = (u32)((n + GT_FP_EL - 1) / GT_FP_EL);
+        GTCHK(relu ? launch(c, GT_KC_FINISH, k_finish_pair<FIN_PARTS, true>, dim3(set.na), B64, set) : launch(c, GT_KC_FINISH, k_finish_pair<FIN_PARTS, false>, dim3(set.na), B64, set));
+    } else if (n) GTCHK(src == FIN_SCALE ? launch(c, GT_KC_FINISH, k_finish<FIN_SCALE, false>, gF(n), B64, a)
                  : relu ? launch(c, GT_KC_FINISH, k_finish<FIN_PARTS, true>, gF(n), B64, a)
                  : launch(c, GT_KC_FINISH, k_finish<FIN_PARTS, false>, gF(n), B64, a));
     acct_finish(c, n, relu);
@@ -159,7 +163,7 @@ static int run_job(gt_ctx *c, const RnsJob &all)
         FinSet f{};
         f.f[0] = j.f;
         f.na = fin_residues(c, f.f[0], j.at + j.abytes + j.bbytes, r0 * j.N, j.M * j.N, j.plane, j.nchunk);
-        GTCHK(j.relu ? launch(c, GT_KC_FINISH, k_finish_pair<true>, dim3(f.na), B64, f) : launch(c, GT_KC_FINISH, k_finish_pair<false>, dim3(f.na), B64, f));
+        GTCHK(j.relu ? launch(c, GT_KC_FINISH, k_finish_pair<FIN_RES, true>, dim3(f.na), B64, f) : launch(c, GT_KC_FINISH, k_finish_pair<FIN_RES, false>, dim3(f.na), B64, f));
     }
     return GT_OK;
 }
@@ -190,7 +194,7 @@ static int run_jobs(gt_ctx *c, const RnsJob &x, const RnsJob &y)
     }
     GTCHK(launch(c, GT_KC_DENSE, k_residues, dim3(rblocks), B256, r));
     GTCHK(rmm_launch(c, x.s.wm, m, mblocks));
-    return launch(c, GT_KC_FINISH, k_finish_pair<false>, dim3(fblocks), B64, f);
+    return launch(c, GT_KC_FINISH, k_finish_pair<FIN_RES, false>, dim3(fblocks), B64, f);
 }
 // Parts of the product of few rows x (M rows of K words) and weights, or, transposed, the weights' rows as columns, in the workspace of
 // partial inner products; div: a division that may run beside it.
@@ -305,10 +309,7 @@ extern "C" int gt_dense_backward(gt_ctx *c, const gt_dense *l, const gt_shares *
     if (dW) GTCHK(run_job(c, RnsJob(c, view(to_p6(x), l->din, MAT_COLS), view(dz, l->dout, MAT_COLS), l->din, l->dout, rows, false, ow)));
     if (db) {
         ColsumArgs a{}; a.x = dz; a.out = to_p6(db); a.rows = rows; a.cols = l->dout;
-        const u64 ngrp = (l->dout + 15) / 16, ranges = std::max<u64>(1, std::min<u64>((rows + 255) / 256, c->simds / (3 * ngrp)));
-        a.per = (rows + ranges - 1) / ranges; a.add = ranges > 1;
-        if (a.add) GTCHK(launch(c, GT_KC_LOCAL, k_fill_const, g1(l->dout), B256, a.out, (u64)0, (u64)l->dout, (u64)0));
-        GTCHK(launch(c, GT_KC_LOCAL, k_colsum, dim3((unsigned)ngrp, 3, (unsigned)ranges), B256, a));
+        GTCHK(launch(c, GT_KC_LOCAL, k_colsum, dim3((l->dout + 15) / 16, 3), dim3(1024), a));
     }
     return T.finish(GT_OK);
 }

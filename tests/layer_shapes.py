@@ -26,6 +26,7 @@ extern "C" void fin(u64 simds, u64 n, u64 *out)
     const FinShape s = fin_shape(simds, n);
     out[0] = s.per; out[1] = s.nbig; out[2] = s.waves;
 }
+extern "C" int parts_pairs(u64 simds, u64 n) { return fin_pairs(simds, n); }
 extern "C" u64 rows_of_pass(u64 N) { return rns_rows(N); }
 """
 
@@ -44,6 +45,7 @@ def _lib():
     L.few_split.argtypes, L.few_split.restype = [u64] * 4 + [vp], None
     L.rmm.argtypes, L.rmm.restype = [u64] * 3 + [vp], None
     L.fin.argtypes, L.fin.restype = [u64, u64, vp], None
+    L.parts_pairs.argtypes = [u64] * 2
     L.rows_of_pass.argtypes, L.rows_of_pass.restype = [u64], u64
     return L
 
@@ -75,6 +77,11 @@ def rmm(M, N):
 def fin(n):
     """(tiles of a first wavefront, such wavefronts, wavefronts)"""
     return _array(_lib().fin, 3, n)
+
+
+def parts_pairs(n):
+    """Are n parts completed by two elements a lane?"""
+    return bool(_lib().parts_pairs(SIMDS, n))
 
 
 def rows_of_pass(N):

@@ -19,6 +19,16 @@ def test_dense_forward(mods, seed, rows, din, dout, relu, bias, res):
     check_dense(mods, seed, rows, din, dout, relu, bias, res, calls=2)
 
 
+# few rows with many outputs
+FEW_MANY = [(150, 64, 700), (129, 33, 641), (2, 40, 50000)]
+
+
+@pytest.mark.parametrize("rows,din,dout", FEW_MANY)
+@pytest.mark.parametrize("relu,bias,res", [(False, True, True), (True, True, False), (True, False, True)])
+def test_few_rows_with_many_outputs(mods, seed, rows, din, dout, relu, bias, res):
+    check_dense(mods, seed, rows, din, dout, relu, bias, res, calls=2)
+
+
 @pytest.mark.parametrize("f", [1, 8, 20])
 @pytest.mark.parametrize("relu", [False, True])
 def test_fraction_widths(mods, seed, f, relu):

@@ -3,7 +3,7 @@ import pytest
 
 import test_gpu_layers as gl
 import test_gpu_layers_variants as gv
-from layer_shapes import apart, few, few_split, fin, rmm, rows_of_pass
+from layer_shapes import apart, few, few_split, fin, parts_pairs, rmm, rows_of_pass
 
 SIZES = [1, 2, 15, 16, 17, 63, 64, 65, 127, 128, 129, 192, 193, 255, 257, 600, 1000, 4097, 30000, 1 << 20]
 
@@ -34,7 +34,8 @@ def kinds(sizes):
 
 def test_calls_take_the_variants_that_they_name():
     assert kinds(gl.SIZES) == {True}
-    assert kinds(gv.RESIDUES) == {False}
+    assert kinds(gv.RESIDUES) == {False} and kinds(gv.FEW_MANY) == {True}
+    assert {parts_pairs(M * N) for M, K, N in gv.FEW_MANY} == {True} and {parts_pairs(M * N) for M, K, N in gl.SIZES} == {False}
     assert {rmm(M, N)[:2] for M, K, N in gv.RESIDUES} == {(1, 1), (2, 2), (4, 2)}
     assert {fin(M * N)[0] for M, K, N in gv.RESIDUES} == {1, 2, 4}
     assert any(M > rows_of_pass(N) for M, K, N in gv.RESIDUES) and any(K > 4096 for M, K, N in gv.RESIDUES)
