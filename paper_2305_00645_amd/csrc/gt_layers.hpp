@@ -257,17 +257,20 @@ __device__ __forceinline__ void transpose4x4(u32 (&x)[4])
     x[0] = __builtin_amdgcn_perm(c, a, 0x05040100u); x[1] = __builtin_amdgcn_perm(d, b, 0x05040100u);
     x[2] = __builtin_amdgcn_perm(c, a, 0x07060302u); x[3] = __builtin_amdgcn_perm(d, b, 0x07060302u);
 }
+// The first of a chain of dot products.  It saturates, which no sum here comes near: the form that does takes any register as its third operand, the
+// other one overwrites it and costs a move.
+__device__ __forceinline__ int dot_first(u64 a, int b, int c) { return __builtin_amdgcn_sdot4((int)(u32)a, b, c, true); }
 // the word that 18 residues (bytes of five words, four a word, the last two bytes zero) stand for
 __device__ __forceinline__ u64 rns_join(const u32 (&r)[5])
 {
-    int qs = 1 << 13;
+    int qs = dot_first(r[0], (int)RNS.quot[0], 1 << 13);
 #pragma unroll
-    for (int g = 0; g < 5; g++) qs = __builtin_amdgcn_sdot4((int)r[g], (int)RNS.quot[g], qs, false);
+    for (int g = 1; g < 5; g++) qs = __builtin_amdgcn_sdot4((int)r[g], (int)RNS.quot[g], qs, false);
     const u32 last = r[4] | (((u32)-(qs >> 14) & 0xffu) << 16);
     int D[8];
 #pragma unroll
     for (int b = 0; b < 8; b++) {
-        int d = __builtin_amdgcn_sdot4((int)last, (int)RNS.join[b][4], 0, false);
+        int d = dot_first(last, (int)RNS.join[b][4], 0);
 #pragma unroll
         for (int g = 0; g < 4; g++) d = __builtin_amdgcn_sdot4((int)r[g], (int)RNS.join[b][g], d, false);
         D[b] = d;
@@ -904,7 +907,7 @@ __device__ __forceinline__ void residue_block(const ResArgs &a, u32 block, u64 (
         u32 b[16];
 #pragma unroll
         for (int e = 0; e < 16; e++)
-            b[e] = rns_reduce((u32)__builtin_amdgcn_sdot4((int)(u32)x[e], cl, __builtin_amdgcn_sdot4((int)(u32)(x[e] >> 32), ch, (int)RNS_MAGIC, false), false), neg, inv);
+            b[e] = rns_reduce((u32)__builtin_amdgcn_sdot4((int)(u32)x[e], cl, dot_first(x[e] >> 32, ch, (int)RNS_MAGIC), false), neg, inv);
         uint4 v;
         v.x = low_bytes(b[0], b[1], b[2], b[3]); v.y = low_bytes(b[4], b[5], b[6], b[7]);
         v.z = low_bytes(b[8], b[9], b[10], b[11]); v.w = low_bytes(b[12], b[13], b[14], b[15]);
