@@ -254,7 +254,8 @@ int gt_infer_forest(gt_ctx *ctx, const gt_forest *forest, const gt_shares *I, si
 
 /* ---- layers in fixed point: tau fraction bits (no part of the paper: the layers of a small network on
  * the same shares, for users who keep such a model beside trees).  All values are
- * signed words x = round(real * 2^tau); all matrices row-major without gaps; results are exact. */
+ * signed words x = round(real * 2^tau); all matrices row-major without gaps; results are exact.  Outputs share no memory with inputs but where it
+ * is said.  Operation ids, rounds and bytes do not depend on which kernels a call takes. */
 #define GT_ACT_NONE 0
 #define GT_ACT_RELU 1
 typedef struct gt_dense gt_dense; /* weights din x dout, bias */

@@ -345,6 +345,7 @@ __global__ __launch_bounds__(64) void k_finish(FinArgs a)
 // ---------------------------------------------------------------------------------
 // The completion of residues, and of many parts: tiles of 40, two per lane of a party (lanes 0-19 of its 21), so that two passes of the block function (80 dealer
 // blocks and 45 blocks of three streams on 2 x 63 lanes) and a chain of messages serve 40 elements where k_finish spends a pass and a chain on 16.
+// Bound: the vector units, 1,590 instructions a tile with ReLU, half of them the block function's (2048 x 4096: 0.60 ms); three wavefronts per SIMD.
 // Residues: the first nbig wavefronts take `per` tiles (at most 4), whose residues a party's 20 lanes join together, eight adjacent elements each, the others one.
 #define GT_FP_EL 40
 #define GT_FP_ROW 40                              // words of a row of material; rows as in FinTile, streams' rows from 22 on
@@ -623,7 +624,8 @@ __device__ __forceinline__ u64 wtile_at(u64 k, u64 n, u32 nst)
 // so that a term costs 36 instructions a component and not 72.  The weights stay words in memory, 24 bytes each (tiles, see MatView), and are
 // turned into limbs in registers (byte permutes; a quarter of the time in which they arrive): one copy serves both passes, KC: k contiguous (the
 // transposed product of the backward pass).
-// Bound: the rate at which the weights arrive.
+// Bound: the rate at which the weights arrive (1 x 1024 x 4096, 101 MB: 20 us, 5 TB/s; 8 x 32784 x 512, 403 MB: 86 us, 4.7 TB/s; 16 x 8208 x 2048, 403 MB: 117 us,
+// 3.4 TB/s, where the left factor's conversion in three of the four wavefronts holds up every step).
 struct FewArgs { const u64 *x[3]; const u64 *w; u64 *Z; u64 ldx, M, N, K; u32 nst, per, nsplit, blocks; DivArgs div; };
 #define GT_FEW_PAD 66                             // words between the rows of the staging area
 // division of a tile of elements by a workgroup of four wavefronts, as k_div<4>, in LDS that the caller has
@@ -822,8 +824,9 @@ __global__ __launch_bounds__(256, 1) void k_mm_few(FewArgs a)
 // (3-5), or the components alone (0-2).  Rows and terms beyond the matrix are zero.  A residue: two four-byte dot products of the word's
 // signed bytes with the powers of 256, a rounded quotient in floating point.  RIGHT: times (M / m_i)^-1.
 // A wavefront makes an operand of 32 x 32 words of one matrix for `per` moduli; a launch makes both factors' (blocks below na: the left one's).
-// MAT_ROWS: the words go through LDS, so that loads are of whole rows.  Bound: what it writes, 18 bytes a word, and reads (2048 x 1024
-// words in six matrices 36 us, 5 TB/s; with a lane's terms from memory, all moduli and matrices by one wavefront, 95).
+// MAT_ROWS: the words go through LDS, so that loads are of whole rows.  Bound: what it writes, 18 bytes a word, and reads, for large matrices (both factors of
+// 2048 x 1024 x 4096, 453 MB written and 151 MB read, 122 us, 5 TB/s), else the vector units' 110 instructions per operand and modulus (1000 x 294 x 257
+// backward: 95 MB written, 32 us).
 struct ResArgs { MatView x; unsigned char *out; u64 rows, K, k0; u32 nrb, nkb, per, mats; };
 // an operand's words, a lane's 16 terms (MAT_ROWS: of rows 2 i + hi its term lr): component x0, or with x1 its sum with that one, as signed bytes
 // (a sum's second words are loaded in a loop of their own: with a condition at each, every load is waited for)
@@ -932,9 +935,12 @@ __global__ __launch_bounds__(256) void k_residues(ResSet set)
 // The products of residues: for every party and modulus the sum of two products, party p's
 //   (a_p + a_{p+1}) b_p + a_p b_{p+1}      or      a_p (b_p + b_{p+1}) + a_{p+1} b_p
 // (sums in the left or the right factor), reduced to balanced residues, [party][modulus] planes of bytes, row-major M x N.
-// A workgroup of 2 x 2 wavefronts owns 64 WM x 64 WN outputs, a wavefront 32 WM x 32 WN; a step of 64 terms of both operands goes through LDS (its loads are in
-// flight during the step before), where an operand lies as it is loaded: no bank conflicts.  The right factor takes the role of rows, so
+// A workgroup of 2 x 2 wavefronts owns 64 WM x 64 WN outputs, a wavefront 32 WM x 32 WN; a step of 64 terms of both operands goes through LDS,
+// where an operand lies as it is loaded: no bank conflicts.  The right factor takes the role of rows, so
 // that a lane holds four adjacent columns of a result.  Consecutive workgroups of an XCD take the tiles of one product.
+// Bound: the matrix cores at the clock that the card's power leaves: 2048 x 1024 x 4096, 1.86e15 operations in 0.96 ms, 1.94 POP/s (a large int8 product
+// of the vendor's library 2.4-2.5; these matrix instructions alone on random registers 3.3, with this LDS traffic and a barrier a step 2.5; zeros 4.5).
+// With the words to LDS behind the matrix instructions and loads a step ahead 1.09 ms; 256 x 256 outputs by eight wavefronts 0.97.
 struct RmmArgs { const unsigned char *A, *B; unsigned char *R; u64 amat, bmat, plane; u32 M, N, narb, nbrb, nstep, ntm, ntn, total; int asums; };   // amat, bmat: bytes of a modulus's matrix; narb: blocks of 32 rows
 // One or two products in a launch: workgroups below na are the first one's.
 struct RmmSet { RmmArgs m[2]; u32 na; };

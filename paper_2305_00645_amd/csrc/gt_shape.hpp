@@ -240,9 +240,10 @@ static inline FewShape few_shape(u64 simds, u64 M, u64 N, u64 K)
     return s;
 }
 
-// Product by residues (k_rns_mm): tiles of 64 wm x 64 wn outputs, the largest that leave every compute unit four rounds of its two
-// workgroups; 64 x 64 for few tiles or a narrow side.  256 x 128, 128 x 128, 64 x 64 (us): 2048 x 4096, 1024 terms, in all 1799, 1831; 1000 x 512, 294 terms 35, 30, 38;
-// 300 x 300, 1000 terms 40, 26, 29; 100 x 100 10, 7, 4.5; 64 x 2048, 2048 terms 140, 86, 75; 2048 x 64, 512 terms 25, 25, 20.
+// Product by residues (k_rns_mm): tiles of 64 wm x 64 wn outputs, the largest that leave every compute unit three rounds of its two
+// workgroups; 64 x 64 for few tiles or a narrow side.  256 x 128, 128 x 128, 64 x 64, the whole layer without ReLU, us: 2048 x 4096, 1024 terms 1547, 1585, 2059;
+// 1024 x 1024, 2048 terms 401, 420, 540; 1000 x 512, 294 terms 85, 82, 85; 300 x 300, 1000 terms 76, 59, 58; 100 x 100, 300 terms 30, 25, 22; 2048 x 64,
+// 512 terms 64, 62, 58.
 // rows of a pass, a multiple of 128: its outputs' residues, 54 bytes each, stay below 7 GB (more for over 2^20 columns)
 static inline u64 rns_rows(u64 N) { return std::max<u64>(128, std::min<u64>(16384, ((u64)1 << 27) / N / 128 * 128)); }
 struct RmmShape { u32 wm, wn; u64 ntm, ntn; };
@@ -250,7 +251,7 @@ static inline RmmShape rmm_shape(u64 simds, u64 M, u64 N)
 {
     const u64 cus = simds / 4;
     RmmShape s = { 2, 2, 0, 0 };
-    if ((M + 255) / 256 * ((N + 127) / 128) * 54 >= 8 * cus) s.wm = 4;
+    if ((M + 255) / 256 * ((N + 127) / 128) * 54 >= 6 * cus) s.wm = 4;
     else if (M <= 64 || N <= 64 || (M + 127) / 128 * ((N + 127) / 128) * 54 < cus) s.wm = s.wn = 1;
     s.ntm = (M + 64 * s.wm - 1) / (64 * s.wm);
     s.ntn = (N + 64 * s.wn - 1) / (64 * s.wn);
