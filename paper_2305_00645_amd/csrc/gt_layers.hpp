@@ -625,8 +625,8 @@ __device__ __forceinline__ u64 wtile_at(u64 k, u64 n, u32 nst)
 // turned into limbs in registers (byte permutes; a quarter of the time in which they arrive): one copy serves both passes, KC: k contiguous (the
 // transposed product of the backward pass).
 // Bound: the rate at which the weights arrive (1 x 1024 x 4096, 101 MB: 20 us, 5 TB/s; 8 x 32784 x 512, 403 MB: 86 us, 4.7 TB/s; 16 x 8208 x 2048, 403 MB: 117 us,
-// 3.4 TB/s, where the left factor's conversion in three of the four wavefronts holds up every step).
-struct FewArgs { const u64 *x[3]; const u64 *w; u64 *Z; u64 ldx, M, N, K; u32 nst, per, nsplit, blocks; DivArgs div; };
+// 3.4 TB/s, with the left factor's conversion in three of the four wavefronts; see k_few_left).
+struct FewArgs { const u64 *x[3]; const u64 *w; unsigned char *left; u64 *Z; u64 ldx, M, N, K; u32 nst, per, nsplit, blocks; DivArgs div; };
 #define GT_FEW_PAD 66                             // words between the rows of the staging area
 // division of a tile of elements by a workgroup of four wavefronts, as k_div<4>, in LDS that the caller has
 #define GT_DIV_BYTES (4 * GT_LANES * 16 + GT_DIV_STEPS * GT_EL_WORDS(3) * 8 + 4 * 6 * 8)
@@ -648,13 +648,51 @@ __device__ __forceinline__ void div_block(const DivArgs &a, u64 tile, unsigned c
 }
 // a word at a wave-uniform address plus a lane's offset in bytes
 template <class T> __device__ __forceinline__ T ld_at(const void *base, u32 off) { return *(const T *)((const char *)base + off); }
-// DIV: workgroups from `blocks` on divide (the gates of a mixture, which nothing waits for before the first product is done).
-template <int ROWS, bool KC, bool DIV>
+// The left factor's limbs, as k_mm_few wants them in LDS: [tile of 16 rows][step][x_j + x_{j+1}, x_j by component][limb][lane of the operand][16 bytes].
+// A launch of its own where so many workgroups take the same rows that converting them in each costs more (16 rows, 8208 x 2048: 116 -> 102 us).
+#define GT_FEW_LEFT (6 * 8 * 1024)
+__global__ __launch_bounds__(192) void k_few_left(FewArgs a)
+{
+    __shared__ __align__(16) u64 s_stage[3][2 * 8 * GT_FEW_PAD];
+    const u32 lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), xr = lane >> 3, xg = lane & 7;
+    const u64 r0 = (u64)blockIdx.y * 16, k = (u64)blockIdx.x * 64 + lane, at = k < a.K ? k : a.K - 1;
+    const u64 *xa = wave == 0 ? a.x[0] : wave == 1 ? a.x[1] : a.x[2], *xb = wave == 0 ? a.x[1] : wave == 1 ? a.x[2] : a.x[0];
+    u64 *stage = s_stage[wave], va[16], vb[16];
+    // (rows and terms that exist where these do not, as in k_mm_few)
+#pragma unroll
+    for (int r = 0; r < 16; r++) {
+        const u64 row = (r0 + r < a.M ? r0 + r : r0) * a.ldx + at;
+        va[r] = xa[row]; vb[r] = xb[row];
+    }
+    unsigned char *out = a.left + ((u64)blockIdx.y * gridDim.x + blockIdx.x) * GT_FEW_LEFT + 256 * (xg >> 1) + 8 * (xg & 1) + xr * 16;
+#pragma unroll
+    for (int q = 0; q < 2; q++) {
+        wave_sync();
+#pragma unroll
+        for (int r = 0; r < 8; r++) {
+            const u64 x = va[r + 8 * q], y = x + vb[r + 8 * q];
+            stage[r * GT_FEW_PAD + lane] = (y + GT_BIAS) ^ GT_BIAS;
+            stage[(8 + r) * GT_FEW_PAD + lane] = (x + GT_BIAS) ^ GT_BIAS;
+        }
+        wave_sync();
+        u64 ys[8], yp[8];
+        ld8_whole(stage + xr * GT_FEW_PAD + xg * 8, ys);
+        ld8_whole(stage + (8 + xr) * GT_FEW_PAD + xg * 8, yp);
+        transpose8x8(ys); transpose8x8(yp);
+#pragma unroll
+        for (int sl = 0; sl < 8; sl++) {
+            *(u64 *)(out + wave * 8192 + q * 128 + sl * 1024) = ys[sl];
+            *(u64 *)(out + (3 + wave) * 8192 + q * 128 + sl * 1024) = yp[sl];
+        }
+    }
+}
+// DIV: workgroups from `blocks` on divide (the gates of a mixture, which nothing waits for before the first product is done). LEFT: the left factor's limbs are there.
+template <int ROWS, bool KC, bool DIV, bool LEFT>
 __global__ __launch_bounds__(256, 1) void k_mm_few(FewArgs a)
 {
     constexpr int SLOTS = ROWS == 8 ? 3 : 6, XP = ROWS / 8;           // tiles of the left factor: both factors in one, or three of each
     constexpr int ABYTES = SLOTS * 8 * 1024;                          // [tile][limb][lane of the operand][16 bytes], twice
-    constexpr int BYTES = 2 * ABYTES + 3 * 2 * 8 * GT_FEW_PAD * 8;
+    constexpr int BYTES = 2 * ABYTES + (LEFT ? 0 : 3 * 2 * 8 * GT_FEW_PAD * 8);
     __shared__ __align__(16) unsigned char s_lds[DIV && GT_DIV_BYTES > BYTES ? GT_DIV_BYTES : BYTES];
     unsigned char (*s_a)[ABYTES] = (unsigned char (*)[ABYTES])s_lds;
     if (DIV && blockIdx.x >= a.blocks) { if (blockIdx.y == 0) div_block(a.div, blockIdx.x - a.blocks, s_lds); return; }
@@ -669,8 +707,16 @@ __global__ __launch_bounds__(256, 1) void k_mm_few(FewArgs a)
     // terms of a row per lane the 64 lines of every load took longer than the weights), and takes eight of a row through LDS.
     const u64 *xa = (wave == 0 ? a.x[0] : wave == 1 ? a.x[1] : a.x[2]) + r0 * a.ldx, *xb = (wave == 0 ? a.x[1] : wave == 1 ? a.x[2] : a.x[0]) + r0 * a.ldx;
     u64 *stage = (u64 *)(s_lds + 2 * ABYTES) + (wave < 3 ? wave : 0) * (2 * 8 * GT_FEW_PAD);
+    const bool converts = LEFT || wave < 3;
     u64 va[ROWS], vb[ROWS];
+    v4i ready[ABYTES / 4096];
     auto fetch = [&](u32 s) {
+        if (LEFT) {
+            const unsigned char *from = a.left + ((u64)blockIdx.y * nsteps + s) * ABYTES;
+#pragma unroll
+            for (int q = 0; q < ABYTES / 4096; q++) ready[q] = ld_at<v4i>(from + q * 4096, tid * 16);
+            return;
+        }
         const u32 k = s * 64 + lane, at = (k < K ? k : K - 1) * 8;
 #pragma unroll
         for (int r = 0; r < ROWS; r++) {                              // (words that exist where these do not: loads without branches)
@@ -679,6 +725,11 @@ __global__ __launch_bounds__(256, 1) void k_mm_few(FewArgs a)
         }
     };
     auto put = [&](u32 s, int buf) {
+        if (LEFT) {
+#pragma unroll
+            for (int q = 0; q < ABYTES / 4096; q++) *(v4i *)(s_a[buf] + q * 4096 + tid * 16) = ready[q];
+            return;
+        }
         const u32 xr = lane >> 3, xg = lane & 7;
         // (rows that do not exist make sums that nobody stores; terms that do not exist meet weights that are zero)
 #pragma unroll
@@ -736,7 +787,7 @@ __global__ __launch_bounds__(256, 1) void k_mm_few(FewArgs a)
     auto step = [&](auto PAR, u32 s, int buf, bool more) {
         // (the fences keep the loads of the next step where they are: the compiler moves them to the end of the step to save registers)
         constexpr int P0 = decltype(PAR)::value;
-        if (more && wave < 3) fetch(s + 1);
+        if (more && converts) fetch(s + 1);
         __builtin_amdgcn_sched_barrier(0);
         if (cols) {
 #pragma unroll
@@ -767,13 +818,13 @@ __global__ __launch_bounds__(256, 1) void k_mm_few(FewArgs a)
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
-        if (more && wave < 3) put(s + 1, buf ^ 1);
+        if (more && converts) put(s + 1, buf ^ 1);
     };
-    if (wave < 3) fetch(s0);
+    if (converts) fetch(s0);
     if (cols)
 #pragma unroll
         for (int j = 0; j < 3; j++) load(j, s0);
-    if (wave < 3) put(s0, 0);
+    if (converts) put(s0, 0);
     __syncthreads();
     if (cols) limbs(0, 0);
     std::integral_constant<int, 0> even;

@@ -208,10 +208,22 @@ static int few_parts(gt_ctx *c, P6 x, u64 ldx, const WMat &W, bool transposed, u
     const FewShape s = few_shape(c->simds, M, N, K);
     a.per = s.per; a.nsplit = s.nsplit; a.blocks = (u32)(s.ngrp * s.nsplit);
     if (div) a.div = *div;
+    const u64 steps = (K + 63) / 64;
+    const bool left = s.rows == 16 && few_left(c->simds, s.ntile, s.ngrp, steps);
+    if (left) {
+        GTCHK(grow_res(c, s.ntile * steps * GT_FEW_LEFT));
+        a.left = c->res;
+        GTCHK(launch(c, GT_KC_DENSE, k_few_left, dim3((unsigned)steps, (unsigned)s.ntile), dim3(192), a));
+    }
     const dim3 g(a.blocks + (div ? gE(div->n).x : 0), (unsigned)s.ntile);
-    if (div) return s.rows == 8 ? launch(c, GT_KC_DENSE, k_mm_few<8, false, true>, g, B256, a) : launch(c, GT_KC_DENSE, k_mm_few<16, false, true>, g, B256, a);
-    return s.rows == 8 ? (transposed ? launch(c, GT_KC_DENSE, k_mm_few<8, true, false>, g, B256, a) : launch(c, GT_KC_DENSE, k_mm_few<8, false, false>, g, B256, a))
-           : (transposed ? launch(c, GT_KC_DENSE, k_mm_few<16, true, false>, g, B256, a) : launch(c, GT_KC_DENSE, k_mm_few<16, false, false>, g, B256, a));
+    const auto go = [&](auto LEFT) {
+        constexpr bool L = decltype(LEFT)::value;
+        return div ? launch(c, GT_KC_DENSE, k_mm_few<16, false, true, L>, g, B256, a) : transposed ? launch(c, GT_KC_DENSE, k_mm_few<16, true, false, L>, g, B256, a)
+               : launch(c, GT_KC_DENSE, k_mm_few<16, false, false, L>, g, B256, a);
+    };
+    if (s.rows == 16) return left ? go(std::integral_constant<bool, true>()) : go(std::integral_constant<bool, false>());
+    return div ? launch(c, GT_KC_DENSE, k_mm_few<8, false, true, false>, g, B256, a) : transposed ? launch(c, GT_KC_DENSE, k_mm_few<8, true, false, false>, g, B256, a)
+           : launch(c, GT_KC_DENSE, k_mm_few<8, false, false, false>, g, B256, a);
 }
 // the product of x and weights, completed
 static int do_dense_w(gt_ctx *c, P6 x, u64 ldx, const WMat &W, bool transposed, u64 M, bool relu, const FinOut &o)

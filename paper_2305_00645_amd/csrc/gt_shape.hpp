@@ -240,6 +240,11 @@ static inline FewShape few_shape(u64 simds, u64 M, u64 N, u64 K)
     return s;
 }
 
+// The left factor's limbs by a launch of their own (k_few_left, 48 KB a tile and step, at most 1 GB) rather than in every workgroup?  Where at least 16 groups of
+// columns take them, and eight steps a compute unit.  With and without, the whole layer, us: 16 rows, 8208 x 2048 102, 116; 64, 1024 x 4096 82, 100;
+// 192, 1024 x 1024 75, 90; but 16, 32784 x 512 (eight groups) 111, 108.
+static inline bool few_left(u64 simds, u64 ntile, u64 ngrp, u64 steps) { return ngrp >= 16 && ntile * steps <= 21845 && ntile * ngrp * steps >= 2 * simds; }
+
 // Product by residues (k_rns_mm): tiles of 64 wm x 64 wn outputs, the largest that leave every compute unit three rounds of its two
 // workgroups; 64 x 64 for few tiles or a narrow side.  256 x 128, 128 x 128, 64 x 64, the whole layer without ReLU, us: 2048 x 4096, 1024 terms 1547, 1585, 2059;
 // 1024 x 1024, 2048 terms 401, 420, 540; 1000 x 512, 294 terms 85, 82, 85; 300 x 300, 1000 terms 76, 59, 58; 100 x 100, 300 terms 30, 25, 22; 2048 x 64,

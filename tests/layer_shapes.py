@@ -27,6 +27,11 @@ extern "C" void fin(u64 simds, u64 n, u64 *out)
     out[0] = s.per; out[1] = s.nbig; out[2] = s.waves;
 }
 extern "C" int parts_pairs(u64 simds, u64 n) { return fin_pairs(simds, n); }
+extern "C" int left(u64 simds, u64 M, u64 N, u64 K)
+{
+    const FewShape s = few_shape(simds, M, N, K);
+    return s.rows == 16 && few_left(simds, s.ntile, s.ngrp, (K + 63) / 64);
+}
 extern "C" u64 rows_of_pass(u64 N) { return rns_rows(N); }
 """
 
@@ -46,6 +51,7 @@ def _lib():
     L.rmm.argtypes, L.rmm.restype = [u64] * 3 + [vp], None
     L.fin.argtypes, L.fin.restype = [u64, u64, vp], None
     L.parts_pairs.argtypes = [u64] * 2
+    L.left.argtypes = [u64] * 4
     L.rows_of_pass.argtypes, L.rows_of_pass.restype = [u64], u64
     return L
 
@@ -82,6 +88,11 @@ def fin(n):
 def parts_pairs(n):
     """Are n parts completed by two elements a lane?"""
     return bool(_lib().parts_pairs(SIMDS, n))
+
+
+def left(M, N, K):
+    """Are the few rows converted by a launch of their own?"""
+    return bool(_lib().left(SIMDS, M, N, K))
 
 
 def rows_of_pass(N):

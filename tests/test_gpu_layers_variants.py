@@ -29,6 +29,24 @@ def test_few_rows_with_many_outputs(mods, seed, rows, din, dout, relu, bias, res
     check_dense(mods, seed, rows, din, dout, relu, bias, res, calls=2)
 
 
+# few rows, converted by a launch of their own
+LEFT = [(180, 700, 1100), (65, 1030, 2045)]
+
+
+@pytest.mark.parametrize("rows,din,dout", LEFT)
+@pytest.mark.parametrize("relu,bias,res", [(False, False, True), (True, True, False)])
+def test_rows_converted_ahead(mods, seed, rows, din, dout, relu, bias, res):
+    check_dense(mods, seed, rows, din, dout, relu, bias, res, calls=2)
+
+
+LEFT_BACKWARD = [(190, 1100, 700), (177, 1030, 1025)]
+
+
+@pytest.mark.parametrize("rows,din,dout", LEFT_BACKWARD)
+def test_gradient_rows_converted_ahead(mods, seed, rows, din, dout):
+    check_backward(mods, seed, rows, din, dout, True, want=(True, False, True))
+
+
 @pytest.mark.parametrize("f", [1, 8, 20])
 @pytest.mark.parametrize("relu", [False, True])
 def test_fraction_widths(mods, seed, f, relu):
@@ -112,9 +130,11 @@ def test_gradient_of_the_input_alone(mods, seed, rows, din, dout):
 
 # rows, d, ff, experts, top: products by residues at the first layer, at both
 MIXTURES = [(200, 40, 450, 8, 2), (400, 130, 300, 4, 1)]
+# rows converted by a launch of their own, the division beside the product
+LEFT_MIXTURES = [(24, 340, 1024, 8, 2)]
 
 
-@pytest.mark.parametrize("rows,d,ff,E,top", MIXTURES)
+@pytest.mark.parametrize("rows,d,ff,E,top", MIXTURES + LEFT_MIXTURES)
 @pytest.mark.parametrize("bias", [False, True])
 def test_mixture_of_many_rows(mods, seed, rows, d, ff, E, top, bias):
     o, g = pair(mods, seed)

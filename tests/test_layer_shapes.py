@@ -3,7 +3,7 @@ import pytest
 
 import test_gpu_layers as gl
 import test_gpu_layers_variants as gv
-from layer_shapes import apart, few, few_split, fin, parts_pairs, rmm, rows_of_pass
+from layer_shapes import apart, few, few_split, fin, left, parts_pairs, rmm, rows_of_pass
 
 SIZES = [1, 2, 15, 16, 17, 63, 64, 65, 127, 128, 129, 192, 193, 255, 257, 600, 1000, 4097, 30000, 1 << 20]
 
@@ -41,6 +41,9 @@ def test_calls_take_the_variants_that_they_name():
     assert any(M > rows_of_pass(N) for M, K, N in gv.RESIDUES) and any(K > 4096 for M, K, N in gv.RESIDUES)
     assert {few_split(M, N, K)[0] for M, K, N in gl.SIZES} == {8, 16}
     assert [few(M, N, K) for M, K, N in gv.LARGEST] == [True, True, True, False, False]
+    assert {left(M, N, K) for M, K, N in gv.LEFT} == {True} and kinds(gv.LEFT) == {True} and {left(M, N, K) for M, K, N in gl.SIZES} == {False}
+    assert all(left(rows, din, dout) for rows, din, dout in gv.LEFT_BACKWARD)
+    assert all(left(rows * k, ff, E * (d + 1)) and few(rows, d, E * (ff + 1)) for rows, d, ff, E, k in gv.LEFT_MIXTURES)
     assert {apart(*s) for s in gv.BACKWARD} == {False, True}
     for rows, d, ff, E, k in gv.MIXTURES:
         assert not (few(rows * k, ff, E * (d + 1)) and few(rows, d, E * (ff + 1)))
