@@ -269,7 +269,8 @@ int gt_dense_destroy(gt_dense *layer);
  * Sums are added up modulo 2^64 and have to stay below 2^62 in absolute value, with GT_ACT_RELU below
  * 2^(tau+31) (results below 2^31).  gate (NULL: not wanted, GT_EINVAL without ReLU) receives ReLU's bit, 1 where the
  * value before the activation is at least 0.  y may be the residual's buffers, not those of x.  One operation id; rounds: 6, with ReLU 8.
- * The context's workspace grows on first use or for larger calls (then the call waits for the stream and allocates). */
+ * The context's workspace grows on first use or for larger calls (then the call waits for the stream and allocates): a caller that captures
+ * these calls into a graph makes the largest one eagerly first, and no larger one while the graph is in use. */
 int gt_dense_forward(gt_ctx *ctx, const gt_dense *layer, const gt_shares *x, size_t rows, int act, const gt_shares *residual,
                      const gt_shares *y, const gt_shares *gate);
 /* dz = gate dy (gate NULL: dz = dy), dx = floor((dz W^T + 2^(tau-1)) / 2^tau), dW = the same of x^T dz, db = column sums of dz; outputs

@@ -624,8 +624,8 @@ __device__ __forceinline__ u64 wtile_at(u64 k, u64 n, u32 nst)
 // so that a term costs 36 instructions a component and not 72.  The weights stay words in memory, 24 bytes each (tiles, see MatView), and are
 // turned into limbs in registers (byte permutes; a quarter of the time in which they arrive): one copy serves both passes, KC: k contiguous (the
 // transposed product of the backward pass).
-// Bound: the rate at which the weights arrive (1 x 1024 x 4096, 101 MB: 20 us, 5 TB/s; 8 x 32784 x 512, 403 MB: 86 us, 4.7 TB/s; 16 x 8208 x 2048, 403 MB: 117 us,
-// 3.4 TB/s, with the left factor's conversion in three of the four wavefronts; see k_few_left).
+// Bound: the rate at which the weights arrive (1 x 1024 x 4096, 101 MB: 20 us, 5 TB/s; 8 x 32784 x 512, 403 MB: 86 us, 4.7 TB/s; 16 x 8208 x 2048, 403 MB: 103 us,
+// 3.9 TB/s with the left factor's limbs made ahead, 117 with its conversion in three of the four wavefronts).
 struct FewArgs { const u64 *x[3]; const u64 *w; unsigned char *left; u64 *Z; u64 ldx, M, N, K; u32 nst, per, nsplit, blocks; DivArgs div; };
 #define GT_FEW_PAD 66                             // words between the rows of the staging area
 // division of a tile of elements by a workgroup of four wavefronts, as k_div<4>, in LDS that the caller has
