@@ -1130,15 +1130,24 @@ __global__ __launch_bounds__(256, WM == 4 ? 2 : WM == 2 ? 3 : 4) void k_rns_mm(R
     }
 }
 
-// components (own planes) of a rows x cols matrix into the tiles of weights, rows from row0 on; padding stays at zero
+// Components (own planes) of a rows x cols matrix into the tiles of weights, rows from row0 on; padding stays at zero.  A thread takes a pair of rows, whose words
+// are adjacent there, so that 16 columns are 256 bytes on end (1024 x 4096: 30 us; a word at a time 188).
 struct PutArgs { P6 src; u64 *dst; u64 row0, rows, cols; u32 nst; };
 __global__ __launch_bounds__(256) void k_put(PutArgs a)
 {
-    const u64 n = a.rows * a.cols;
+    const u64 first = a.row0 / 2, n = ((a.row0 + a.rows + 1) / 2 - first) * a.cols;
     for (u64 e = (u64)blockIdx.x * blockDim.x + threadIdx.x; e < n; e += (u64)gridDim.x * blockDim.x) {
-        const u64 r = e / a.cols, to = wtile_at(a.row0 + r, e - r * a.cols, a.nst);
+        const u64 pair = e / a.cols, c = e - pair * a.cols, k = 2 * (first + pair), to = wtile_at(k, c, a.nst);
+        const bool low = k >= a.row0, high = k + 1 < a.row0 + a.rows;
+        const u64 from = (k - a.row0) * a.cols + c;                   // (wraps where the pair's first row is the one before; not read then)
 #pragma unroll
-        for (int j = 0; j < 3; j++) a.dst[(u64)j * GT_WTILE + to] = (a.src.o[j][e] + GT_BIAS) ^ GT_BIAS;
+        for (int j = 0; j < 3; j++) {
+            u64 *out = a.dst + (u64)j * GT_WTILE + to;
+            const u64 x = low ? (a.src.o[j][from] + GT_BIAS) ^ GT_BIAS : 0, y = high ? (a.src.o[j][from + a.cols] + GT_BIAS) ^ GT_BIAS : 0;
+            if (low && high) { ulonglong2 v; v.x = x; v.y = y; *(ulonglong2 *)out = v; }
+            else if (low) out[0] = x;
+            else out[1] = y;
+        }
     }
 }
 

@@ -19,7 +19,7 @@ static int wmat_put(gt_ctx *c, const WMat &w, const gt_shares *src, u64 row0, u6
 {
     PutArgs a{};
     a.src = to_p6(src); a.dst = w.base; a.row0 = row0; a.rows = rows; a.cols = w.N; a.nst = w.nst;
-    return launch(c, GT_KC_LOCAL, k_put, g1(rows * w.N), B256, a);
+    return launch(c, GT_KC_LOCAL, k_put, g1(((row0 + rows + 1) / 2 - row0 / 2) * w.N), B256, a);
 }
 static MatView wmat(const WMat &w, u32 kind)
 { MatView v{}; for (int j = 0; j < 3; j++) v.c[j] = w.base + (u64)j * GT_WTILE; v.kind = kind; v.nst = w.nst; return v; }
