@@ -215,8 +215,8 @@ static inline InferShape infer_shape(u64 simds, u32 lgi, u64 ngrp, u32 ntrees, u
 // terms a split.
 // Such a product, with its completion of words, or one by residues (k_residues, k_rns_mm, k_finish_pair)?  The first reads the weights' words again for every 16
 // rows and takes 36 products of limbs where the second takes 18 of residues, whose conversion costs more than the product where rows are few.  In us, with
-// ReLU, few and residues: 64 rows, 1024 x 4096 99, 173; 128 203, 203; 192 281, 280; 256 369, 307.  256 rows, 600 x 600 62, 64; 512 118, 90.  512 rows, 300 x 300
-// 43, 50; 64 x 1024 61, 66; 2048 rows, 100 x 200 60, 72, 22 x 16 15, 28.
+// ReLU, few and residues: 64 rows, 1024 x 4096 78, 173; 128 145, 203; 192 214, 280; 256 369 (rows not converted ahead), 293.  256 rows, 600 x 600 62, 62; 512 118,
+// 88.  512 rows, 300 x 300 42, 50; 64 x 1024 54, 66; 2048 rows, 100 x 200 60, 72, 22 x 16 15, 28.
 #define GT_FEW_ROWS 192
 static inline bool few_rows(u64 simds, u64 M, u64 N, u64 K, u64 ldx)
 {
