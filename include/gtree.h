@@ -32,6 +32,11 @@
  *    counter; shares are a pure function of (keys, operation id, element index),
  *    so results do not depend on launch shapes.  Two contexts created with the
  *    same parameters and driven with the same calls produce identical shares.
+ *  - Calls that are captured into a HIP graph (gt_oaa_static, the layers) have their operation ids fixed
+ *    then: every replay masks what it opens with the same words.  That is private
+ *    only while the inputs stay the same; with new ones the difference of two replays' opened
+ *    words is the difference of the secrets.  A graph that is replayed on new inputs
+ *    starts with a captured gt_rekey, which gives every replay keys of its own.
  *  - Public values (leaked by design, Sec. I): all sizes, depths, tau, K.
  */
 #ifndef GTREE_H
@@ -125,6 +130,10 @@ int gt_ctx_destroy(gt_ctx *ctx);
 int gt_stats_get(gt_ctx *ctx, gt_stats *out);
 int gt_stats_reset(gt_ctx *ctx);
 uint32_t gt_op_counter(const gt_ctx *ctx);
+/* New keys on the context's stream: every call enqueued behind it, and every call behind it in a graph at each replay, draws from keys
+ * derived of those before: words 0-7 of block 0 of operation 0, stream 0xffffffff, under the old key, for
+ * each of the five (the holders of a key derive its successor without a message).  No message, no operation id, no allocation. */
+int gt_rekey(gt_ctx *ctx);
 const char *gt_strerror(int code);
 
 /* ---- sharing (Sec. II-B, Share^A / Rec^A; the data owner's and query user's role) */
@@ -151,7 +160,7 @@ int gt_oaa(gt_ctx *ctx, const gt_shares *W, size_t w, const gt_shares *u, size_t
  * (6 * GT_STATIC_MAX_N words = 12 MiB per GPU, held until the process ends) instead of
  * the context's workspace, the array is cleared by a fill kernel, and no allocating call
  * of any kind is made.  n > GT_STATIC_MAX_N returns GT_EINVAL.  All contexts on one GPU
- * share the array: calls that overlap on one GPU race. */
+ * share the array: calls that overlap on one GPU race.  Captured for new inputs: gt_rekey first. */
 int gt_oaa_static(gt_ctx *ctx, const gt_shares *W, size_t w, const gt_shares *u, size_t n, const gt_shares *z);
 /* gt_oaa run as the paper prints it (Sec. V-A, Alg. "Oblivious Array Access"): every one of
  * the N = w*n array elements goes through a SelectShare of its own (conversion with the
@@ -270,7 +279,8 @@ int gt_dense_destroy(gt_dense *layer);
  * 2^(tau+31) (results below 2^31).  gate (NULL: not wanted, GT_EINVAL without ReLU) receives ReLU's bit, 1 where the
  * value before the activation is at least 0.  y may be the residual's buffers, not those of x.  One operation id; rounds: 6, with ReLU 8.
  * The context's workspace grows on first use or for larger calls (then the call waits for the stream and allocates): a caller that captures
- * these calls into a graph makes the largest one eagerly first, and no larger one while the graph is in use. */
+ * these calls into a graph makes the largest one eagerly first, and no larger one while the graph is in use; the captured part starts with gt_rekey
+ * where replays see new inputs. */
 int gt_dense_forward(gt_ctx *ctx, const gt_dense *layer, const gt_shares *x, size_t rows, int act, const gt_shares *residual,
                      const gt_shares *y, const gt_shares *gate);
 /* dz = gate dy (gate NULL: dz = dy), dx = floor((dz W^T + 2^(tau-1)) / 2^tau), dW = the same of x^T dz, db = column sums of dz; outputs

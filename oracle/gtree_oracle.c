@@ -373,6 +373,16 @@ void orc_stats_reset(orc_ctx *c)
     memset(c->scorer, 0, sizeof c->scorer);
 }
 uint32_t orc_op_counter(const orc_ctx *c) { return c->op; }
+void orc_rekey(orc_ctx *c)
+{
+    for (int k = 0; k < 5; k++) {
+        u32 out[16];
+        orc_chacha_block(c->key[k], 0, 0, 0, 0xffffffffu, PRF_ROUNDS, out);
+        memcpy(c->key[k], out, sizeof c->key[k]);
+    }
+}
+/* calls recorded at an operation id run again with that id */
+void orc_set_op(orc_ctx *c, uint32_t op) { c->op = op; }
 void orc_set_threads(int n)
 {
 #ifdef _OPENMP

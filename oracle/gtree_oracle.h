@@ -61,6 +61,10 @@ void orc_stats_bits(const orc_ctx *c, uint64_t wire_bits[9]);
 void orc_stats_scorer(const orc_ctx *c, uint64_t bytes[2]);
 void orc_stats_reset(orc_ctx *);
 uint32_t orc_op_counter(const orc_ctx *);
+/* every key to its successor: words 0-7 of block 0 of operation 0, stream 0xffffffff, under it */
+void orc_rekey(orc_ctx *);
+/* the counter to an id that was taken before, as a replay of recorded calls uses it */
+void orc_set_op(orc_ctx *, uint32_t op);
 void orc_set_threads(int n); /* OpenMP threads for the element loops; 0 = default */
 int orc_get_threads(void);
 

@@ -56,6 +56,8 @@ def _load():
         "orc_oaa_literal": (None, [vp, _u64p, sz, _u64p, sz, _u64p]),
         "orc_stats_reset": (None, [vp]),
         "orc_op_counter": (u32, [vp]),
+        "orc_rekey": (None, [vp]),
+        "orc_set_op": (None, [vp, u32]),
         "orc_set_threads": (None, [i]),
         "orc_get_threads": (i, []),
         "orc_chacha_block": (None, [_u32p, u32, u32, u32, u32, i, _u32p]),
@@ -165,6 +167,13 @@ class Oracle:
 
     def op_counter(self):
         return int(self.L.orc_op_counter(self.ctx))
+
+    def rekey(self):
+        self.L.orc_rekey(self.ctx)
+
+    def set_op(self, op):
+        """As a replay of calls that were recorded when the counter stood at op."""
+        self.L.orc_set_op(self.ctx, op)
 
     # -- randomness --------------------------------------------------------
     def prf_word(self, key_index, op, stream, j):

@@ -69,6 +69,20 @@ __global__ __launch_bounds__(256) void k_share(const u32 *keys, u32 op, const u6
     share_tiles(keys, GT_KEY_OWNER, op, plain, n, s_tr[wave][0], s_tr[wave][1], [&](u64 e, u64 a, u64 b, u64 x3) { put_share(out, e, a, b, x3); });
 }
 
+// The keys' successors (gt_rekey), in place: a lane per key.  The stream is one that no protocol has.
+__global__ __launch_bounds__(64) void k_rekey(u32 *keys)
+{
+    if (threadIdx.x >= 5) return;
+    u32 *key = keys + 8 * threadIdx.x;
+    Key k;
+#pragma unroll
+    for (int i = 0; i < 8; i++) k.k[i] = key[i];
+    u64 w[8];
+    chacha8(k, 0, 0, 0xffffffffu, w);
+#pragma unroll
+    for (int i = 0; i < 4; i++) { key[2 * i] = (u32)w[i]; key[2 * i + 1] = (u32)(w[i] >> 32); }
+}
+
 // The six sharings that the scorer of the heuristic by reconstruction hands back, one launch:
 // blockIdx.y = which (operation op + which), under the dealer's key; `off` the first element of
 // `out`.  The fourth, the children's node type, goes to both children of a node.  (Six launches and a

@@ -345,6 +345,12 @@ extern "C" int gt_prof_get(gt_ctx *c, gt_prof *out)
     return GT_OK;
 }
 extern "C" uint32_t gt_op_counter(const gt_ctx *c) { return c ? c->op : 0; }
+extern "C" int gt_rekey(gt_ctx *c)
+{
+    if (!c) return GT_EINVAL;
+    Timed T(c);
+    return T.finish(launch(c, GT_KC_LOCAL, k_rekey, dim3(1), B64, c->keys_d));
+}
 
 // ---------------------------------------------------------------------------------
 extern "C" int gt_share_a(gt_ctx *c, const uint64_t *plain, size_t n, const gt_shares *out)

@@ -85,6 +85,7 @@ def load():
         "gt_prof_get": (i, [vp, C.POINTER(_Prof)]),
         "gt_train_reset": (i, [vp, vp, S, S]),
         "gt_op_counter": (u32, [vp]),
+        "gt_rekey": (i, [vp]),
         "gt_strerror": (C.c_char_p, [i]),
         "gt_share_a": (i, [vp, vp, sz, S]),
         "gt_reconstruct_a": (i, [vp, S, vp, sz]),
@@ -247,6 +248,10 @@ class GTree:
 
     def op_counter(self):
         return int(self.L.gt_op_counter(self.ctx))
+
+    def rekey(self):
+        """Keys of their own for all that follows; first in a captured graph, for every replay (see gtree.h: without it replays repeat their masks)."""
+        _chk(self.L.gt_rekey(self.ctx), "gt_rekey")
 
     # -- sharing -----------------------------------------------------------
     def share_a(self, plain):
