@@ -99,6 +99,9 @@ typedef struct {
  * per level with the node index in device memory) instead of one launch that carries every
  * instance through all levels; same shares, kept for comparison. */
 #define GT_FLAG_LEVELWISE_INFER 2u
+/* GT_FLAG_SMALL_WORKSPACE: the products of layers by residues keep 128 MB of the card instead of up to 17 GB (beside 24 bytes an output
+ * of a pass, see gt_dense_forward) and take more passes; same shares.  For layers beside data that fill the card. */
+#define GT_FLAG_SMALL_WORKSPACE 4u
 /* tuning knob of the one-launch inference: instances per workgroup 16 / 32 / 64 instead of
  * the choice made from the batch size (flags |= GT_FLAG_INFER_TILE(16)) */
 #define GT_FLAG_INFER_TILE_MASK 0x300u
@@ -278,7 +281,8 @@ int gt_dense_destroy(gt_dense *layer);
  * Sums are added up modulo 2^64 and have to stay below 2^62 in absolute value, with GT_ACT_RELU below
  * 2^(tau+31) (results below 2^31).  gate (NULL: not wanted, GT_EINVAL without ReLU) receives ReLU's bit, 1 where the
  * value before the activation is at least 0.  y may be the residual's buffers, not those of x.  One operation id; rounds: 6, with ReLU 8.
- * The context's workspace grows on first use or for larger calls (then the call waits for the stream and allocates): a caller that captures
+ * The context's workspace: up to 17 GB of residues, and 24 bytes an output of few rows or, where not all residues fit, of a pass (2^27 outputs,
+ * at least 128 rows).  It grows on first use or for larger calls (then the call waits for the stream and allocates): a caller that captures
  * these calls into a graph makes the largest one eagerly first, and no larger one while the graph is in use; the captured part starts with gt_rekey
  * where replays see new inputs. */
 int gt_dense_forward(gt_ctx *ctx, const gt_dense *layer, const gt_shares *x, size_t rows, int act, const gt_shares *residual,

@@ -191,12 +191,11 @@ __device__ __forceinline__ Sh finish_el(FWire &W, const TileT &T, u32 f, u64 z, 
 // ---------------------------------------------------------------------------------
 // Residues.  Products of many rows run as products of small residues: words are taken as signed numbers, their products
 // added up exactly, |S| <= 2 * RNS_TERMS * 2^126, from 18 coprime moduli whose product M is 2^140.4 > 2 |S| / 0.74, and only then
-// reduced modulo 2^64.  A modulus costs one int8 product per term, so a ring product costs 18 of them where signed limbs cost 36.
+// reduced modulo 2^64 (RNS_TERMS terms at a time, two products of words each).  A modulus costs one int8 product per term, so a ring product costs 18 of them where signed limbs cost 36.
 //   r_i = (sum of the products of residues, the right factor's times (M / m_i)^-1) mod m_i, balanced
 //   S = sum_i r_i M / m_i - q M,  q = round(sum_i r_i / m_i)
 // q is exact: |S / M| <= 0.367 and the fixed-point sum below is off by at most 18 * 128 / 2^15 = 0.071 < 0.5 - 0.367.
 #define RNS_N 18
-#define RNS_TERMS 4096                            // terms of the long axis in a product (two products of words each)
 struct RnsTable {
     int m[RNS_N];                                 // moduli
     float inv[RNS_N];
@@ -280,11 +279,12 @@ __device__ __forceinline__ u64 rns_join(const u32 (&r)[5])
 }
 
 // Completion.  Z: the parties' parts, [3][n] words, left at zero for the next product; bias: ncol words or none.
-// k_finish_pair: R: residues of the elements from `first` on, planes [chunk][party][modulus] of `plane` bytes, chunks added up; per: see there.
+// k_finish_pair: of the elements from `first` on the parts, or R: residues, planes [chunk][party][modulus] of `plane` bytes, chunks added up; per: see there.
 enum { FIN_PARTS = 0, FIN_SCALE = 1, FIN_RES = 2 };   // parts in memory; z = row factor S[e / ncol] times x (experts' gates); residues
 struct FinArgs { KCommon c; u64 *Z; P6 bias, res, y, gate, S, x; u64 n; u32 ncol, f; int has_bias, has_res, has_gate; const unsigned char *R; u64 first, plane; u32 nchunk, per, nbig; };
 // a party's parts of eight adjacent elements (of the launch's, from i0, a multiple of 8) from their residues
-__device__ __forceinline__ void rns_words(const FinArgs &a, int p, u64 i0, u64 (&zw)[8])
+template <class Args>
+__device__ __forceinline__ void rns_words(const Args &a, int p, u64 i0, u64 (&zw)[8])
 {
 #pragma unroll
     for (int i = 0; i < 8; i++) zw[i] = 0;
@@ -306,6 +306,24 @@ __device__ __forceinline__ void rns_words(const FinArgs &a, int p, u64 i0, u64 (
 #pragma unroll
             for (int i = 0; i < 4; i++) { const u32 w[5] = { q[0][i], q[1][i], q[2][i], q[3][i], q[4][i] }; zw[4 * h + i] += rns_join(w); }
         }
+    }
+}
+// The words of some chunks' residues, n elements of a block of `cols` columns, added to the parts: [3][parts] words, rows of `ld`, the block's first column at c0.  For products whose
+// residues are not kept until the completion.  Bound: what it reads and writes, 54 + 48 bytes an element.
+struct JoinArgs { const unsigned char *R; u64 *Z; u64 plane, n, parts, ld, c0, cols; u32 nchunk; };
+__global__ __launch_bounds__(256) void k_join(JoinArgs a)
+{
+    const int p = (int)blockIdx.y;
+    const u64 i0 = ((u64)blockIdx.x * 256 + threadIdx.x) * 8;
+    if (i0 >= a.n) return;
+    u64 zw[8];
+    rns_words(a, p, i0, zw);
+    u64 row = i0 / a.cols, col = i0 - row * a.cols;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        if (i0 + i >= a.n) return;
+        a.Z[(u64)p * a.parts + row * a.ld + a.c0 + col] += zw[i];
+        if (++col == a.cols) { col = 0; row++; }
     }
 }
 template <int SRC, bool RELU>
@@ -509,9 +527,9 @@ __global__ __launch_bounds__(64) void k_finish_pair(FinSet set)
             if (SRC == FIN_PARTS) {
                 u64 *from = a.Z + (u64)p * a.n;
 #pragma unroll
-                for (int q = 0; q < 2; q++) z[q] = from[e[q]];
+                for (int q = 0; q < 2; q++) z[q] = from[e[q] - a.first];
 #pragma unroll
-                for (int q = 0; q < 2; q++) if (mine && act[q]) from[e[q]] = 0;
+                for (int q = 0; q < 2; q++) if (mine && act[q]) from[e[q] - a.first] = 0;
             } else
             // the tile's words from the five lanes that joined them, through the message region
             {

@@ -96,6 +96,7 @@ struct RnsJob {
     bool relu;
     FinArgs f;
     RmmShape s;
+    RnsPlan plan;
     bool asums;
     u32 nchunk, narb, nbrb;
     u64 plane, abytes, bbytes, rbytes;
@@ -106,19 +107,28 @@ struct RnsJob {
         f.c = kc(c, c->op++); f.ncol = (u32)N; f.f = c->tau;
         f.y = o.y; f.gate = o.gate; f.res = o.res; f.bias = o.bias; f.has_res = o.has_res; f.has_gate = o.has_gate; f.has_bias = o.has_bias;
         acct_finish(c, M * N, relu);
+        plan = rns_plan(M, N, K, c->rns_limit);
         shape(c);
+    }
+    // rows from r0 and columns from c0 (multiples of 128 and 256) on
+    RnsJob part(gt_ctx *c, u64 r0, u64 rows, u64 c0, u64 cols) const
+    {
+        RnsJob j = *this;
+        for (int p = 0; p < 3; p++) {
+            j.A.c[p] += A.kind == MAT_ROWS ? r0 * A.ld : r0;
+            j.B.c[p] += B.kind == MAT_COLS ? c0 : (B.kind == MAT_W ? c0 >> 6 : (c0 >> 4) * B.nst) * (3 * GT_WTILE);
+        }
+        j.M = rows; j.N = cols;
+        if (rows != M || cols != N) j.shape(c);
+        return j;
     }
     void shape(gt_ctx *c)
     {
-        s = rmm_shape(c->simds, M, N);
-        asums = M <= N;                                                  // the factor with fewer rows is converted twice
+        const RnsSizes z = rns_sizes(c->simds, M, N, K);
+        s = z.s; asums = z.asums; narb = z.narb; nbrb = z.nbrb; plane = z.plane; abytes = z.abytes; bbytes = z.bbytes; rbytes = z.rbytes;
         nchunk = (u32)((K + RNS_TERMS - 1) / RNS_TERMS);
-        narb = (u32)(s.ntm * 2 * s.wm); nbrb = (u32)(s.ntn * 2 * s.wn);
-        const u64 nkb = (std::min<u64>(K, RNS_TERMS) + 63) / 64 * 2;
-        plane = (M * N + 1279) / 1280 * 1280;                            // whole tiles of both completions
-        abytes = (asums ? 6 : 3) * RNS_N * narb * nkb * 1024; bbytes = (asums ? 3 : 6) * RNS_N * nbrb * nkb * 1024; rbytes = 3 * RNS_N * plane;
     }
-    u64 bytes() const { return abytes + bbytes + nchunk * rbytes; }
+    u64 bytes() const { return abytes + bbytes + plan.keep * rbytes; }
     u32 nkb(u32 ch) const { return (u32)((std::min<u64>(K - (u64)ch * RNS_TERMS, RNS_TERMS) + 63) / 64 * 2); }
     ResArgs left(gt_ctx *c, u32 ch, u32 *blocks) const
     { const u64 k0 = (u64)ch * RNS_TERMS; return residues(c, A, at, M, std::min<u64>(K - k0, RNS_TERMS), k0, narb, nkb(ch), asums, blocks); }
@@ -127,7 +137,7 @@ struct RnsJob {
     RmmArgs product(u32 ch) const
     {
         RmmArgs a{};
-        a.A = at; a.B = at + abytes; a.R = at + abytes + bbytes + ch * rbytes; a.amat = (u64)narb * nkb(ch) * 1024; a.bmat = (u64)nbrb * nkb(ch) * 1024;
+        a.A = at; a.B = at + abytes; a.R = at + abytes + bbytes + ch % plan.keep * rbytes; a.amat = (u64)narb * nkb(ch) * 1024; a.bmat = (u64)nbrb * nkb(ch) * 1024;
         a.plane = plane; a.M = (u32)M; a.N = (u32)N; a.narb = narb; a.nbrb = nbrb; a.nstep = nkb(ch); a.ntm = (u32)s.ntm; a.ntn = (u32)s.ntn; a.asums = asums;
         a.total = (u32)(3 * RNS_N * s.ntm * s.ntn);
         return a;
@@ -139,31 +149,42 @@ static int rmm_launch(gt_ctx *c, u32 wm, const RmmSet &m, u32 blocks)
     return wm == 4 ? launch(c, GT_KC_DENSE, k_rns_mm<4, 2>, dim3(blocks), B256, m) : wm == 2 ? launch(c, GT_KC_DENSE, k_rns_mm<2, 2>, dim3(blocks), B256, m)
            : launch(c, GT_KC_DENSE, k_rns_mm<1, 1>, dim3(blocks), B256, m);
 }
-// rows in blocks, the long axis in chunks of RNS_TERMS
+// rows and columns in blocks, the long axis in chunks of RNS_TERMS (see rns_plan)
 static int run_job(gt_ctx *c, const RnsJob &all)
 {
-    const u64 step = rns_rows(all.N);
-    for (u64 r0 = 0; r0 < all.M; r0 += step) {
-        RnsJob j = all;
-        j.M = std::min<u64>(all.M - r0, step);
-        for (int p = 0; p < 3; p++) j.A.c[p] += j.A.kind == MAT_ROWS ? r0 * j.A.ld : r0;
-        if (j.M != all.M) j.shape(c);
-        GTCHK(grow_res(c, j.bytes()));
-        j.at = c->res;
-        for (u32 ch = 0; ch < j.nchunk; ch++) {
-            ResSet r{};
-            u32 na, nb;
-            r.r[0] = j.left(c, ch, &na); r.r[1] = j.right(c, ch, &nb);
-            r.end[0] = na; r.end[1] = r.end[2] = r.end[3] = na + nb;
-            GTCHK(launch(c, GT_KC_DENSE, k_residues, dim3(na + nb), B256, r));
-            RmmSet m{};
-            m.m[0] = j.product(ch); m.na = rmm_blocks(m.m[0]);
-            GTCHK(rmm_launch(c, j.s.wm, m, m.na));
-        }
+    const RnsPlan &plan = all.plan;
+    for (u64 r0 = 0; r0 < all.M; r0 += plan.rows) {
+        const u64 rows = std::min<u64>(all.M - r0, plan.rows), n = rows * all.N;
         FinSet f{};
-        f.f[0] = j.f;
-        f.na = fin_residues(c, f.f[0], j.at + j.abytes + j.bbytes, r0 * j.N, j.M * j.N, j.plane, j.nchunk);
-        GTCHK(j.relu ? launch(c, GT_KC_FINISH, k_finish_pair<FIN_RES, true>, dim3(f.na), B64, f) : launch(c, GT_KC_FINISH, k_finish_pair<FIN_RES, false>, dim3(f.na), B64, f));
+        f.f[0] = all.f;
+        if (!plan.whole) GTCHK(grow_dacc(c, 3 * n));
+        for (u64 c0 = 0; c0 < all.N; c0 += plan.cols) {
+            RnsJob j = all.part(c, r0, rows, c0, std::min<u64>(all.N - c0, plan.cols));
+            GTCHK(grow_res(c, j.bytes()));
+            j.at = c->res;
+            for (u32 ch = 0; ch < j.nchunk; ch++) {
+                ResSet r{};
+                u32 na, nb;
+                r.r[0] = j.left(c, ch, &na); r.r[1] = j.right(c, ch, &nb);
+                r.end[0] = na; r.end[1] = r.end[2] = r.end[3] = na + nb;
+                GTCHK(launch(c, GT_KC_DENSE, k_residues, dim3(na + nb), B256, r));
+                RmmSet m{};
+                m.m[0] = j.product(ch); m.na = rmm_blocks(m.m[0]);
+                GTCHK(rmm_launch(c, j.s.wm, m, m.na));
+                if (plan.whole || (ch % plan.keep != plan.keep - 1 && ch != j.nchunk - 1)) continue;
+                JoinArgs a{};
+                a.R = j.at + j.abytes + j.bbytes; a.Z = c->dacc; a.plane = j.plane; a.n = rows * j.N; a.parts = n; a.ld = all.N; a.c0 = c0; a.cols = j.N; a.nchunk = ch % plan.keep + 1;
+                GTCHK(launch(c, GT_KC_DENSE, k_join, dim3((unsigned)((a.n + 2047) / 2048), 3), B256, a));
+            }
+            if (plan.whole) f.na = fin_residues(c, f.f[0], j.at + j.abytes + j.bbytes, r0 * all.N, n, j.plane, j.nchunk);
+        }
+        if (plan.whole) {
+            GTCHK(all.relu ? launch(c, GT_KC_FINISH, k_finish_pair<FIN_RES, true>, dim3(f.na), B64, f) : launch(c, GT_KC_FINISH, k_finish_pair<FIN_RES, false>, dim3(f.na), B64, f));
+            continue;
+        }
+        f.f[0].Z = c->dacc; f.f[0].first = r0 * all.N; f.f[0].n = n;
+        f.na = (u32)((n + GT_FP_EL - 1) / GT_FP_EL);
+        GTCHK(all.relu ? launch(c, GT_KC_FINISH, k_finish_pair<FIN_PARTS, true>, dim3(f.na), B64, f) : launch(c, GT_KC_FINISH, k_finish_pair<FIN_PARTS, false>, dim3(f.na), B64, f));
     }
     return GT_OK;
 }
@@ -171,7 +192,8 @@ static int run_job(gt_ctx *c, const RnsJob &all)
 // 12 launches of a backward pass, 66 us, where the host's calls count, to 9).
 static int run_jobs(gt_ctx *c, const RnsJob &x, const RnsJob &y)
 {
-    if (x.nchunk != 1 || y.nchunk != 1 || x.M > rns_rows(x.N) || y.M > rns_rows(y.N) || x.s.wm != y.s.wm || x.s.wm == 4) {
+    const auto once = [](const RnsJob &j) { return j.nchunk == 1 && j.M <= j.plan.rows && j.plan.whole; };
+    if (!once(x) || !once(y) || x.s.wm != y.s.wm || x.s.wm == 4) {
         GTCHK(run_job(c, x));
         return run_job(c, y);
     }

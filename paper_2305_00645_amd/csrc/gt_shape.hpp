@@ -245,12 +245,33 @@ static inline FewShape few_shape(u64 simds, u64 M, u64 N, u64 K)
 // 192, 1024 x 1024 75, 90; but 16, 32784 x 512 (eight groups) 111, 108.
 static inline bool few_left(u64 simds, u64 ntile, u64 ngrp, u64 steps) { return ngrp >= 16 && ntile * steps <= 21845 && ntile * ngrp * steps >= 2 * simds; }
 
+// Terms of a chunk of the long axis, whose products are summed in 32 bits.
+#define RNS_TERMS 4096
+// What a product by residues does at a time, so that its workspace does not grow with its sizes.  A residue is 54 bytes an output and chunk (three parties, 18 moduli) and 54
+// bytes a word of a factor, twice that of the one whose sums are converted, too.  `limit` outputs and words of the right factor (2^27) make up to 7.3 GB each; with
+// the left factor's 16384 rows of 4096 words below 17 GB.  rows: of a pass, a multiple of 128; cols: columns, a multiple of 256; keep: chunks whose residues are kept.
+// whole: all chunks of all columns, which the completion joins (54 bytes read an output and chunk); else k_join adds them to the parts' words first, 24
+// bytes an output of a pass (at the copy's rate a twentieth of the time of a chunk's product).
+#define RNS_LIMIT ((u64)1 << 27)
+#define RNS_LIMIT_SMALL ((u64)1 << 15)            // below 128 MB, beside the words of 128 rows: GT_FLAG_SMALL_WORKSPACE
+static inline u64 rns_rows(u64 N, u64 limit = RNS_LIMIT) { return std::max<u64>(128, std::min<u64>(16384, limit / N / 128 * 128)); }
+struct RnsPlan { u64 rows, cols; u32 keep; bool whole; };
+static inline RnsPlan rns_plan(u64 M, u64 N, u64 K, u64 limit)
+{
+    const u64 terms = std::min<u64>(std::max<u64>(128, K), RNS_TERMS), chunks = (K + RNS_TERMS - 1) / RNS_TERMS;
+    RnsPlan p;
+    p.rows = std::min(rns_rows(N, limit), rns_rows(terms, limit));
+    p.cols = N * terms <= limit ? N : std::max<u64>(256, limit / terms / 256 * 256);
+    const u64 outputs = std::max<u64>(1280, std::min(M, p.rows) * std::min(N, p.cols));            // (planes of whole tiles)
+    p.keep = (u32)std::min<u64>(chunks, std::max<u64>(1, limit / outputs));
+    p.whole = p.cols >= N && p.keep == chunks;
+    return p;
+}
+
 // Product by residues (k_rns_mm): tiles of 64 wm x 64 wn outputs, the largest that leave every compute unit three rounds of its two
 // workgroups; 64 x 64 for few tiles or a narrow side.  256 x 128, 128 x 128, 64 x 64, the whole layer without ReLU, us: 2048 x 4096, 1024 terms 1547, 1585, 2059;
 // 1024 x 1024, 2048 terms 401, 420, 540; 1000 x 512, 294 terms 85, 82, 85; 300 x 300, 1000 terms 76, 59, 58; 100 x 100, 300 terms 30, 25, 22; 2048 x 64,
 // 512 terms 64, 62, 58.
-// rows of a pass, a multiple of 128: its outputs' residues, 54 bytes each, stay below 7 GB (more for over 2^20 columns)
-static inline u64 rns_rows(u64 N) { return std::max<u64>(128, std::min<u64>(16384, ((u64)1 << 27) / N / 128 * 128)); }
 struct RmmShape { u32 wm, wn; u64 ntm, ntn; };
 static inline RmmShape rmm_shape(u64 simds, u64 M, u64 N)
 {
@@ -261,6 +282,19 @@ static inline RmmShape rmm_shape(u64 simds, u64 M, u64 N)
     s.ntm = (M + 64 * s.wm - 1) / (64 * s.wm);
     s.ntn = (N + 64 * s.wn - 1) / (64 * s.wn);
     return s;
+}
+// Bytes of such a product: residues of the left factor, of the right one (sums: the one with fewer rows is converted twice) and, of a chunk, of the outputs.
+struct RnsSizes { RmmShape s; bool asums; u32 narb, nbrb; u64 plane, abytes, bbytes, rbytes; };
+static inline RnsSizes rns_sizes(u64 simds, u64 M, u64 N, u64 K)
+{
+    RnsSizes z;
+    z.s = rmm_shape(simds, M, N);
+    z.asums = M <= N;
+    z.narb = (u32)(z.s.ntm * 2 * z.s.wm); z.nbrb = (u32)(z.s.ntn * 2 * z.s.wn);
+    const u64 nkb = (std::min<u64>(K, RNS_TERMS) + 63) / 64 * 2;
+    z.plane = (M * N + 1279) / 1280 * 1280;                              // whole tiles of both completions
+    z.abytes = (z.asums ? 6 : 3) * 18 * z.narb * nkb * 1024; z.bbytes = (z.asums ? 3 : 6) * 18 * z.nbrb * nkb * 1024; z.rbytes = 3 * 18 * z.plane;
+    return z;
 }
 // moduli of a wavefront of k_residues: all 18, fewer where few operands leave SIMDs without work
 static inline u32 residue_range(u64 simds, u64 operands)

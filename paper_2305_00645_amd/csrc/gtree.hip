@@ -54,6 +54,7 @@ struct gt_ctx {
     DSh ws[5];                // inference workspace, grown on demand, kept between calls
     unsigned char *res;       // residues of a layer's product, likewise
     size_t res_bytes;
+    u64 rns_limit;            // bounds that workspace (rns_plan)
     DSh ws_dz;                // a layer's gradient behind its activation, likewise
     u64 *dacc;                // partial inner products of split equality grids
     size_t dacc_words;
@@ -271,6 +272,7 @@ extern "C" int gt_ctx_create(gt_ctx **out, const gt_params *prm)
     memset(&c->acc, 0, sizeof c->acc); memset(&c->prof, 0, sizeof c->prof);
     c->profile = (prm->flags & GT_FLAG_PROFILE) != 0;
     c->levelwise_infer = (prm->flags & GT_FLAG_LEVELWISE_INFER) != 0;
+    c->rns_limit = prm->flags & GT_FLAG_SMALL_WORKSPACE ? RNS_LIMIT_SMALL : RNS_LIMIT;
     c->infer_lgi = 0;
     if (prm->flags & GT_FLAG_INFER_TILE_MASK) c->infer_lgi = 3 + (int)((prm->flags & GT_FLAG_INFER_TILE_MASK) >> 8);
     c->tau = prm->tau; c->K = prm->K; c->stream = (hipStream_t)prm->hip_stream;

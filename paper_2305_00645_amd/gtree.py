@@ -43,6 +43,7 @@ class _Stats(C.Structure):
 
 GT_FLAG_PROFILE = 1
 GT_FLAG_LEVELWISE_INFER = 2
+GT_FLAG_SMALL_WORKSPACE = 4
 GT_FLAG_INFER_TILE = {16: 0x100, 32: 0x200, 64: 0x300}
 KC_NAMES = ("share", "mult", "eqgrid", "count", "small", "local", "eqgrid_rows", "eqgrid_store", "infer", "partmm", "dense",
             "finish")
