@@ -71,6 +71,38 @@ static int grow_res(gt_ctx *c, size_t need)
     c->res_bytes = need;
     return GT_OK;
 }
+// What a call needs of the context's workspaces: words of parts, bytes of residues.  It is reserved before the call takes operation ids, counts or launches
+// anything, so that one that does not get it (GT_ENOMEM) leaves no trace; nothing below grows a workspace by itself.
+struct Need {
+    u64 words = 0, res = 0;
+    void also(const Need &o) { words = std::max(words, o.words); res = std::max(res, o.res); }
+};
+static int reserve(gt_ctx *c, const Need &n)
+{
+    GTCHK(grow_dacc(c, n.words));
+    return grow_res(c, n.res);
+}
+static Need job_need(gt_ctx *c, u64 M, u64 N, u64 K)
+{
+    const RnsPlan p = rns_plan(M, N, K, c->rns_limit);
+    Need n;
+    n.res = rns_bytes(c->simds, M, N, K, p);
+    if (!p.whole) n.words = 3 * std::min(M, p.rows) * N;
+    return n;
+}
+static bool few_ahead(gt_ctx *c, const FewShape &s, u64 steps) { return s.rows == 16 && few_left(c->simds, s.ntile, s.ngrp, steps); }
+static Need few_need(gt_ctx *c, u64 M, u64 N, u64 K)
+{
+    const FewShape s = few_shape(c->simds, M, N, K);
+    const u64 steps = (K + 63) / 64;
+    Need n;
+    n.words = 3 * M * N;
+    if (few_ahead(c, s, steps)) n.res = s.ntile * steps * GT_FEW_LEFT;
+    return n;
+}
+// a product with weights by either (do_dense_w)
+static bool takes_few(gt_ctx *c, u64 M, u64 N, u64 K, u64 ldx) { return M != 0 && few_rows(c->simds, M, N, K, ldx); }
+static Need dense_need(gt_ctx *c, u64 M, u64 N, u64 K, u64 ldx) { return takes_few(c, M, N, K, ldx) ? few_need(c, M, N, K) : job_need(c, M, N, K); }
 // a completion of residues, and its workgroups
 static u32 fin_residues(gt_ctx *c, FinArgs &f, const unsigned char *R, u64 first, u64 n, u64 plane, u32 nchunk)
 {
@@ -104,12 +136,13 @@ struct RnsJob {
     RnsJob() {}
     RnsJob(gt_ctx *c, const MatView &A_, const MatView &B_, u64 M_, u64 N_, u64 K_, bool relu_, const FinOut &o) : A(A_), B(B_), M(M_), N(N_), K(K_), relu(relu_), f{}
     {
-        f.c = kc(c, c->op++); f.ncol = (u32)N; f.f = c->tau;
+        f.ncol = (u32)N; f.f = c->tau;
         f.y = o.y; f.gate = o.gate; f.res = o.res; f.bias = o.bias; f.has_res = o.has_res; f.has_gate = o.has_gate; f.has_bias = o.has_bias;
-        acct_finish(c, M * N, relu);
         plan = rns_plan(M, N, K, c->rns_limit);
         shape(c);
     }
+    // the operation id and the messages
+    void take(gt_ctx *c) { f.c = kc(c, c->op++); acct_finish(c, M * N, relu); }
     // rows from r0 and columns from c0 (multiples of 128 and 256) on
     RnsJob part(gt_ctx *c, u64 r0, u64 rows, u64 c0, u64 cols) const
     {
@@ -149,18 +182,16 @@ static int rmm_launch(gt_ctx *c, u32 wm, const RmmSet &m, u32 blocks)
     return wm == 4 ? launch(c, GT_KC_DENSE, k_rns_mm<4, 2>, dim3(blocks), B256, m) : wm == 2 ? launch(c, GT_KC_DENSE, k_rns_mm<2, 2>, dim3(blocks), B256, m)
            : launch(c, GT_KC_DENSE, k_rns_mm<1, 1>, dim3(blocks), B256, m);
 }
-// rows and columns in blocks, the long axis in chunks of RNS_TERMS (see rns_plan)
-static int run_job(gt_ctx *c, const RnsJob &all)
+// rows and columns in blocks, the long axis in chunks of RNS_TERMS (see rns_plan); its workspace is there
+static int run_taken(gt_ctx *c, const RnsJob &all)
 {
     const RnsPlan &plan = all.plan;
     for (u64 r0 = 0; r0 < all.M; r0 += plan.rows) {
         const u64 rows = std::min<u64>(all.M - r0, plan.rows), n = rows * all.N;
         FinSet f{};
         f.f[0] = all.f;
-        if (!plan.whole) GTCHK(grow_dacc(c, 3 * n));
         for (u64 c0 = 0; c0 < all.N; c0 += plan.cols) {
             RnsJob j = all.part(c, r0, rows, c0, std::min<u64>(all.N - c0, plan.cols));
-            GTCHK(grow_res(c, j.bytes()));
             j.at = c->res;
             for (u32 ch = 0; ch < j.nchunk; ch++) {
                 ResSet r{};
@@ -188,17 +219,33 @@ static int run_job(gt_ctx *c, const RnsJob &all)
     }
     return GT_OK;
 }
+static int run_job(gt_ctx *c, RnsJob j)
+{
+    j.take(c);
+    return run_taken(c, j);
+}
 // Two products that do not wait for each other, without activation: side by side in the same three launches where neither fills the chip alone (267 x 22 -> 16:
 // 12 launches of a backward pass, 66 us, where the host's calls count, to 9).
-static int run_jobs(gt_ctx *c, const RnsJob &x, const RnsJob &y)
+static bool joined(const RnsJob &x, const RnsJob &y)
 {
     const auto once = [](const RnsJob &j) { return j.nchunk == 1 && j.M <= j.plan.rows && j.plan.whole; };
-    if (!once(x) || !once(y) || x.s.wm != y.s.wm || x.s.wm == 4) {
-        GTCHK(run_job(c, x));
-        return run_job(c, y);
+    return once(x) && once(y) && x.s.wm == y.s.wm && x.s.wm != 4;
+}
+static Need jobs_need(gt_ctx *c, const RnsJob &x, const RnsJob &y)
+{
+    Need n;
+    if (joined(x, y)) n.res = x.bytes() + y.bytes();
+    else { n = job_need(c, x.M, x.N, x.K); n.also(job_need(c, y.M, y.N, y.K)); }
+    return n;
+}
+static int run_jobs(gt_ctx *c, RnsJob x, RnsJob y)
+{
+    x.take(c); y.take(c);
+    if (!joined(x, y)) {
+        GTCHK(run_taken(c, x));
+        return run_taken(c, y);
     }
     RnsJob j[2] = { x, y };
-    GTCHK(grow_res(c, x.bytes() + y.bytes()));
     j[0].at = c->res; j[1].at = c->res + x.bytes();
     ResSet r{};
     RmmSet m{};
@@ -223,7 +270,6 @@ static int run_jobs(gt_ctx *c, const RnsJob &x, const RnsJob &y)
 static int few_parts(gt_ctx *c, P6 x, u64 ldx, const WMat &W, bool transposed, u64 M, const DivArgs *div = nullptr)
 {
     const u64 N = transposed ? W.K : W.N, K = transposed ? W.N : W.K;
-    GTCHK(grow_dacc(c, 3 * M * N));
     FewArgs a{};
     for (int j = 0; j < 3; j++) a.x[j] = x.o[j];
     a.w = W.base; a.Z = c->dacc; a.nst = W.nst; a.ldx = ldx; a.M = M; a.N = N; a.K = K;
@@ -231,9 +277,8 @@ static int few_parts(gt_ctx *c, P6 x, u64 ldx, const WMat &W, bool transposed, u
     a.per = s.per; a.nsplit = s.nsplit; a.blocks = (u32)(s.ngrp * s.nsplit);
     if (div) a.div = *div;
     const u64 steps = (K + 63) / 64;
-    const bool left = s.rows == 16 && few_left(c->simds, s.ntile, s.ngrp, steps);
+    const bool left = few_ahead(c, s, steps);
     if (left) {
-        GTCHK(grow_res(c, s.ntile * steps * GT_FEW_LEFT));
         a.left = c->res;
         GTCHK(launch(c, GT_KC_DENSE, k_few_left, dim3((unsigned)steps, (unsigned)s.ntile), dim3(192), a));
     }
@@ -251,7 +296,7 @@ static int few_parts(gt_ctx *c, P6 x, u64 ldx, const WMat &W, bool transposed, u
 static int do_dense_w(gt_ctx *c, P6 x, u64 ldx, const WMat &W, bool transposed, u64 M, bool relu, const FinOut &o)
 {
     const u64 N = transposed ? W.K : W.N, K = transposed ? W.N : W.K;
-    if (M == 0 || !few_rows(c->simds, M, N, K, ldx)) return run_job(c, RnsJob(c, view(x, ldx, MAT_ROWS), wmat(W, transposed ? MAT_W : MAT_WT), M, N, K, relu, o));
+    if (!takes_few(c, M, N, K, ldx)) return run_job(c, RnsJob(c, view(x, ldx, MAT_ROWS), wmat(W, transposed ? MAT_W : MAT_WT), M, N, K, relu, o));
     GTCHK(few_parts(c, x, ldx, W, transposed, M));
     return do_finish(c, FIN_PARTS, relu, M * N, (u32)N, o);
 }
@@ -298,6 +343,7 @@ extern "C" int gt_dense_forward(gt_ctx *c, const gt_dense *l, const gt_shares *x
     const size_t n = rows * l->dout;
     if (!shares_ok(x, rows * l->din) || !shares_ok(y, n) || (res && !shares_ok(res, n)) || (gate && (act != GT_ACT_RELU || !shares_ok(gate, n)))) return GT_EINVAL;
     Timed T(c);
+    GTCHK(reserve(c, dense_need(c, rows, l->dout, l->din, l->din)));
     FinOut o;
     o.y = to_p6(y);
     if (res) { o.has_res = true; o.res = to_p6(res); }
@@ -321,26 +367,28 @@ extern "C" int gt_dense_backward(gt_ctx *c, const gt_dense *l, const gt_shares *
     if (!shares_ok(dy, n) || (gate && !shares_ok(gate, n)) || (dW && !shares_ok(x, nx)) || (dx && !shares_ok(dx, nx)) || (dW && !shares_ok(dW, nw)) ||
         (db && !shares_ok(db, l->dout))) return GT_EINVAL;
     Timed T(c);
-    P6 dz = to_p6(dy);
+    if (gate) GTCHK(ws_grow(c, c->ws_dz, n));
+    const P6 dz = gate ? c->ws_dz.v : to_p6(dy);
+    FinOut ox, ow;
+    if (dx) ox.y = to_p6(dx);
+    if (dW) ow.y = to_p6(dW);
+    const bool apart = dx && (rows == 0 || !dW || few_rows_apart(rows, l->din, l->dout)), both = dx && !apart;
+    RnsJob jx, jw;
+    Need need;
+    if (apart) need = dense_need(c, rows, l->din, l->dout, l->dout);
+    if (both) jx = RnsJob(c, view(dz, l->dout, MAT_ROWS), wmat(l->W, MAT_W), rows, l->din, l->dout, false, ox);
+    if (dW) jw = RnsJob(c, view(to_p6(x), l->din, MAT_COLS), view(dz, l->dout, MAT_COLS), l->din, l->dout, rows, false, ow);
+    if (dW) need.also(both ? jobs_need(c, jx, jw) : job_need(c, l->din, l->dout, rows));
+    GTCHK(reserve(c, need));
     if (gate) {
-        int rc = ws_grow(c, c->ws_dz, n);
-        if (rc != GT_OK) return rc;
-        dz = c->ws_dz.v;
         MultArgs m{}; m.x = once(to_p6(gate)); m.y = once(to_p6(dy)); m.z = dz; m.n = n;
         m.c = kc(c, c->op++);
         if (n) GTCHK(launch(c, GT_KC_MULT, k_mult, dim3(tiles8(n)), GT_BLOCK, m));
         acct_reshare(c, n, 1);
     }
-    FinOut ox, ow;
-    if (dx) ox.y = to_p6(dx);
-    if (dW) ow.y = to_p6(dW);
-    if (dx && (rows == 0 || !dW || few_rows_apart(rows, l->din, l->dout))) GTCHK(do_dense_w(c, dz, l->dout, l->W, true, rows, false, ox));
-    else if (dx) {
-        const RnsJob jx(c, view(dz, l->dout, MAT_ROWS), wmat(l->W, MAT_W), rows, l->din, l->dout, false, ox), jw(c, view(to_p6(x), l->din, MAT_COLS), view(dz, l->dout, MAT_COLS), l->din, l->dout, rows, false, ow);
-        GTCHK(run_jobs(c, jx, jw));
-        dW = nullptr;
-    }
-    if (dW) GTCHK(run_job(c, RnsJob(c, view(to_p6(x), l->din, MAT_COLS), view(dz, l->dout, MAT_COLS), l->din, l->dout, rows, false, ow)));
+    if (apart) GTCHK(do_dense_w(c, dz, l->dout, l->W, true, rows, false, ox));
+    if (both) GTCHK(run_jobs(c, jx, jw));
+    else if (dW) GTCHK(run_job(c, jw));
     if (db) {
         ColsumArgs a{}; a.x = dz; a.out = to_p6(db); a.rows = rows; a.cols = l->dout;
         GTCHK(launch(c, GT_KC_LOCAL, k_colsum, dim3((l->dout + 15) / 16, 3), dim3(1024), a));
@@ -403,6 +451,10 @@ extern "C" int gt_moe_forward(gt_ctx *c, gt_moe *m, const gt_shares *x, size_t r
     if (!shares_ok(x, rows * d) || !shares_ok(y, rows * d) || (res && !shares_ok(res, rows * d))) return GT_EINVAL;
     Timed T(c);
     const bool few = rk && few_rows(c->simds, rk, ff, E * (d + 1), E * (d + 1)) && few_rows(c->simds, rows, d, E * (ff + 1), E * (ff + 1));     // parts of the products by k_mm_few, else results
+    Need need = few ? few_need(c, rows, E, d) : dense_need(c, rows, E, d, d);
+    need.also(dense_need(c, rk, ff, E * (d + 1), E * (d + 1)));
+    need.also(dense_need(c, rows, d, E * (ff + 1), E * (ff + 1)));
+    GTCHK(reserve(c, need));
     MoeArgs a{};
     a.s = m->s.v; a.bias = m->br.v; a.o = m->o.v; a.S = m->S.v; a.Q = m->Q.v; a.g = m->g.v; a.x = to_p6(x); a.xe = m->xe.v; a.hg = m->hg.v; a.he = m->he.v;
     a.rows = rows; a.E = (u32)E; a.k = m->k; a.d = m->d; a.ff = m->ff; a.f = c->tau; a.parts = few; a.has_bias = m->has_br;

@@ -296,6 +296,18 @@ static inline RnsSizes rns_sizes(u64 simds, u64 M, u64 N, u64 K)
     z.abytes = (z.asums ? 6 : 3) * 18 * z.narb * nkb * 1024; z.bbytes = (z.asums ? 3 : 6) * 18 * z.nbrb * nkb * 1024; z.rbytes = 3 * 18 * z.plane;
     return z;
 }
+// ... of the largest part of a planned product: full and last rows and columns
+static inline u64 rns_bytes(u64 simds, u64 M, u64 N, u64 K, const RnsPlan &p)
+{
+    const u64 m[2] = { std::min(M, p.rows), M % p.rows }, n[2] = { std::min(N, p.cols), N % p.cols };
+    u64 most = 0;
+    for (int i = 0; i < 4; i++) {
+        if (!m[i & 1] || !n[i >> 1]) continue;
+        const RnsSizes z = rns_sizes(simds, m[i & 1], n[i >> 1], K);
+        most = std::max(most, z.abytes + z.bbytes + p.keep * z.rbytes);
+    }
+    return most;
+}
 // moduli of a wavefront of k_residues: all 18, fewer where few operands leave SIMDs without work
 static inline u32 residue_range(u64 simds, u64 operands)
 {
