@@ -50,7 +50,7 @@ extern "C" {
 #define GT_OK 0
 #define GT_EINVAL (-1) /* null pointer, zero/oversized dimension, bad selector */
 #define GT_ENOMEM (-2) /* device allocation failed */
-#define GT_ESTATE (-3) /* level called out of order, object used after finish */
+#define GT_ESTATE (-3) /* level called out of order, object used after finish, workspace too small under graph capture */
 #define GT_EHIP (-4)   /* a HIP runtime call or kernel launch failed */
 
 #define GT_MAX_DEPTH 16u       /* decision levels of a tree */
@@ -282,9 +282,10 @@ int gt_dense_destroy(gt_dense *layer);
  * 2^(tau+31) (results below 2^31).  gate (NULL: not wanted, GT_EINVAL without ReLU) receives ReLU's bit, 1 where the
  * value before the activation is at least 0.  y may be the residual's buffers, not those of x.  One operation id; rounds: 6, with ReLU 8.
  * The context's workspace: up to 17 GB of residues, and 24 bytes an output of few rows or, where not all residues fit, of a pass (2^27 outputs,
- * at least 128 rows).  It grows on first use or for larger calls (then the call waits for the stream and allocates): a caller that captures
- * these calls into a graph makes the largest one eagerly first, and no larger one while the graph is in use; the captured part starts with gt_rekey
- * where replays see new inputs. */
+ * at least 128 rows).  It grows on first use or for larger calls (then the call waits for the stream and allocates).  Under graph
+ * capture it cannot: a call that would have to is refused with GT_ESTATE, so a caller makes the largest one eagerly first.  From a capture on, what the workspace
+ * outgrows stays allocated until the context is destroyed, so that larger calls do not disturb the graph.  The captured part
+ * starts with gt_rekey where replays see new inputs. */
 int gt_dense_forward(gt_ctx *ctx, const gt_dense *layer, const gt_shares *x, size_t rows, int act, const gt_shares *residual,
                      const gt_shares *y, const gt_shares *gate);
 /* dz = gate dy (gate NULL: dz = dy), dx = floor((dz W^T + 2^(tau-1)) / 2^tau), dW = the same of x^T dz, db = column sums of dz; outputs

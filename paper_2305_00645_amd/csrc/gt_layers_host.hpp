@@ -65,7 +65,7 @@ static int grow_res(gt_ctx *c, size_t need)
 {
     if (c->res_bytes >= need) return GT_OK;
     (void)hipStreamSynchronize(c->stream);
-    if (c->res) (void)hipFree(c->res);
+    workspace_drop(c, c->res);
     c->res = nullptr; c->res_bytes = 0;
     if (hipMalloc(&c->res, need) != hipSuccess) { c->res = nullptr; return GT_ENOMEM; }
     c->res_bytes = need;
@@ -79,6 +79,7 @@ struct Need {
 };
 static int reserve(gt_ctx *c, const Need &n)
 {
+    GTCHK(workspace_room(c, c->dacc_words >= n.words && c->res_bytes >= n.res));
     GTCHK(grow_dacc(c, n.words));
     return grow_res(c, n.res);
 }
@@ -354,9 +355,12 @@ extern "C" int gt_dense_forward(gt_ctx *c, const gt_dense *l, const gt_shares *x
 
 static int ws_grow(gt_ctx *c, DSh &w, size_t n)
 {
-    if (w.base && w.n >= n) return GT_OK;
+    const bool fits = w.base && w.n >= n;
+    GTCHK(workspace_room(c, fits));
+    if (fits) return GT_OK;
     (void)hipStreamSynchronize(c->stream);
-    dsh_free(w);
+    workspace_drop(c, w.base);
+    w.base = nullptr; w.n = 0;
     return dsh_alloc(w, n, c->stream);
 }
 extern "C" int gt_dense_backward(gt_ctx *c, const gt_dense *l, const gt_shares *x, const gt_shares *gate, const gt_shares *dy, size_t rows,

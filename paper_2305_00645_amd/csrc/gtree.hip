@@ -58,6 +58,8 @@ struct gt_ctx {
     DSh ws_dz;                // a layer's gradient behind its activation, likewise
     u64 *dacc;                // partial inner products of split equality grids
     size_t dacc_words;
+    bool captured;            // a graph may hold addresses of res, ws_dz and dacc: what they outgrow is kept in `held`
+    std::vector<void *> held;
     u64 *scratch_d;           // this device's copy of the static scratch array
     bool noalloc;             // inside gt_oaa_static: nothing may be allocated
 };
@@ -268,7 +270,7 @@ extern "C" int gt_ctx_create(gt_ctx **out, const gt_params *prm)
     gt_ctx *c = new (std::nothrow) gt_ctx();
     if (!c) return GT_ENOMEM;
     c->noalloc = false; c->scratch_d = nullptr;
-    c->op = 0; c->ev_used = 0; c->keys_d = nullptr; c->wire_d = nullptr; c->dacc = nullptr; c->dacc_words = 0; c->res = nullptr; c->res_bytes = 0; c->simds = 1024;
+    c->op = 0; c->ev_used = 0; c->keys_d = nullptr; c->wire_d = nullptr; c->dacc = nullptr; c->dacc_words = 0; c->res = nullptr; c->res_bytes = 0; c->captured = false; c->simds = 1024;
     memset(&c->acc, 0, sizeof c->acc); memset(&c->prof, 0, sizeof c->prof);
     c->profile = (prm->flags & GT_FLAG_PROFILE) != 0;
     c->levelwise_infer = (prm->flags & GT_FLAG_LEVELWISE_INFER) != 0;
@@ -308,6 +310,7 @@ extern "C" int gt_ctx_destroy(gt_ctx *c)
     dsh_free(c->ws_dz);
     if (c->res) (void)hipFree(c->res);
     if (c->dacc) (void)hipFree(c->dacc);
+    for (void *p : c->held) (void)hipFree(p);
     (void)hipFree(c->wire_d);
     (void)hipFree(c->keys_d);
     delete c;
@@ -437,11 +440,28 @@ extern "C" int gt_ge_a(gt_ctx *c, const gt_shares *x, const gt_shares *y, size_t
 
 // The context's workspace of partial inner products.  Zero once: its users (k_dot_fin, k_lit_fin) leave every
 // word that they have read at zero again.
+// Workspaces that captured calls may use.  A call under capture cannot wait or allocate: it is refused where its workspace would have to grow.  A graph keeps the
+// addresses that it was captured with, so from the first capture on what a workspace outgrows stays allocated until the context goes.
+static int workspace_room(gt_ctx *c, bool fits)
+{
+    hipStreamCaptureStatus s = hipStreamCaptureStatusNone;
+    if (c->stream && hipStreamIsCapturing(c->stream, &s) != hipSuccess) { (void)hipGetLastError(); return GT_EHIP; }
+    if (s == hipStreamCaptureStatusNone) return GT_OK;
+    c->captured = true;
+    return fits ? GT_OK : GT_ESTATE;
+}
+static void workspace_drop(gt_ctx *c, void *p)
+{
+    if (!p) return;
+    if (!c->captured) { (void)hipFree(p); return; }
+    try { c->held.push_back(p); } catch (...) { }                       // (no host memory for the note: it stays for good)
+}
 static int grow_dacc(gt_ctx *c, size_t need)
 {
+    GTCHK(workspace_room(c, c->dacc_words >= need));
     if (c->dacc_words >= need) return GT_OK;
     (void)hipStreamSynchronize(c->stream);
-    if (c->dacc) (void)hipFree(c->dacc);
+    workspace_drop(c, c->dacc);
     c->dacc = nullptr; c->dacc_words = 0;
     if (hipMalloc(&c->dacc, need * 8) != hipSuccess) { c->dacc = nullptr; return GT_ENOMEM; }
     c->dacc_words = need;
