@@ -189,12 +189,12 @@ __device__ __forceinline__ Sh finish_el(FWire &W, const TileT &T, u32 f, u64 z, 
 }
 
 // ---------------------------------------------------------------------------------
-// Residues.  Products of many rows run as products of small residues: words are taken as signed numbers, their products
-// added up exactly, |S| <= 2 * RNS_TERMS * 2^126, from 18 coprime moduli whose product M is 2^140.4 > 2 |S| / 0.74, and only then
-// reduced modulo 2^64 (RNS_TERMS terms at a time, two products of words each).  A modulus costs one int8 product per term, so a ring product costs 18 of them where signed limbs cost 36.
+// Residues.  Products of many rows run as products of small residues: words are taken as the numbers that their eight signed bytes stand for, -128 R to 127 R with
+// R = (256^8 - 1) / 255, their products added up exactly (RNS_TERMS terms at a time, two products of words each: |S| <= 2 * RNS_TERMS * (128 R)^2), from 18 coprime
+// moduli whose product M is 2^140.4, and only then reduced modulo 2^64.  A modulus costs one int8 product per term, so a ring product costs 18 of them where signed limbs cost 36.
 //   r_i = (sum of the products of residues, the right factor's times (M / m_i)^-1) mod m_i, balanced
 //   S = sum_i r_i M / m_i - q M,  q = round(sum_i r_i / m_i)
-// q is exact: |S / M| <= 0.367 and the fixed-point sum below is off by at most 18 * 128 / 2^15 = 0.071 < 0.5 - 0.367.
+// q is exact: |S / M| < 0.3682 and the fixed-point sum below is off by at most 18 * 128 / 2^15 = 0.0704 < 0.5 - 0.3682.
 #define RNS_N 18
 struct RnsTable {
     int m[RNS_N];                                 // moduli
