@@ -1112,7 +1112,7 @@ __global__ __launch_bounds__(256, WM == 4 ? 2 : WM == 2 ? 3 : 4) void k_rns_mm(R
     } else __syncthreads();
     step(s, 0, yes, no);
     step(s + 1, 1, no, no);
-    // |sum| < 2^28: low 13 bits and the rest times 2^13 mod m, below 2^21.1, then the balanced residue; through LDS to rows
+    // |sum| <= 2^27: low 13 bits and the rest times 2^13 mod m, below 2^21.1, then the balanced residue; through LDS to rows
     const float inv = d_rns.inv[mi];
     const u32 neg = 256 - (u32)d_rns.m[mi];
     const int c13 = d_rns.c13[mi];

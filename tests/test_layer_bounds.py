@@ -50,7 +50,8 @@ def test_the_quotient_is_exact():
     error = 18 * 128
     assert LARGEST * (1 << 15) + error * M < M * (1 << 14)
     assert 3681 * M < 10000 * LARGEST < 3682 * M
-    assert 2 * TERMS * 2 ** 14 < 2 ** 28 and (2 ** 28 // 8192) * 128 + 8191 < 2 ** 22          # int32 sums of residues, and their reduction in 24 bits
+    most = 2 * TERMS * 2 ** 14                            # int32 sums of residues, and their reduction in a float's 24 bits
+    assert most == 2 ** 27 and (most >> 13) * 128 + 8191 < 2 ** 21.1
     for S in (0, 1, -1, LARGEST, -LARGEST, LARGEST - 1, LARGEST // 3, -LARGEST // 7):
         assert join(S) == S
 
