@@ -309,7 +309,7 @@ __device__ __forceinline__ void rns_words(const Args &a, int p, u64 i0, u64 (&zw
     }
 }
 // The words of some chunks' residues, n elements of a block of `cols` columns, added to the parts: [3][parts] words, rows of `ld`, the block's first column at c0.  For products whose
-// residues are not kept until the completion.  Bound: what it reads and writes, 54 + 48 bytes an element.
+// residues are not kept until the completion.  Bound: what it reads and writes, 54 + 48 bytes an element a chunk (2^27 elements: 4.4 ms, 3.1 TB/s).
 struct JoinArgs { const unsigned char *R; u64 *Z; u64 plane, n, parts, ld, c0, cols; u32 nchunk; };
 __global__ __launch_bounds__(256) void k_join(JoinArgs a)
 {

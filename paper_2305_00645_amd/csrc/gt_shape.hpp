@@ -251,7 +251,7 @@ static inline bool few_left(u64 simds, u64 ntile, u64 ngrp, u64 steps) { return 
 // bytes a word of a factor, twice that of the one whose sums are converted, too.  `limit` outputs and words of the right factor (2^27) make up to 7.3 GB each; with
 // the left factor's 16384 rows of 4096 words below 17 GB.  rows: of a pass, a multiple of 128; cols: columns, a multiple of 256; keep: chunks whose residues are kept.
 // whole: all chunks of all columns, which the completion joins (54 bytes read an output and chunk); else k_join adds them to the parts' words first, 24
-// bytes an output of a pass (at the copy's rate a twentieth of the time of a chunk's product).
+// bytes an output of a pass.  Fewer rows, down to 4096, rather than that: 16384 rows, 8192 x 8192, by 8192 rows 134 ms, joined 139.
 #define RNS_LIMIT ((u64)1 << 27)
 #define RNS_LIMIT_SMALL ((u64)1 << 15)            // below 128 MB, beside the words of 128 rows: GT_FLAG_SMALL_WORKSPACE
 static inline u64 rns_rows(u64 N, u64 limit = RNS_LIMIT) { return std::max<u64>(128, std::min<u64>(16384, limit / N / 128 * 128)); }
@@ -262,6 +262,8 @@ static inline RnsPlan rns_plan(u64 M, u64 N, u64 K, u64 limit)
     RnsPlan p;
     p.rows = std::min(rns_rows(N, limit), rns_rows(terms, limit));
     p.cols = N * terms <= limit ? N : std::max<u64>(256, limit / terms / 256 * 256);
+    const u64 fit = rns_rows(N * std::max<u64>(1, chunks), limit);       // rows whose residues of all chunks fit
+    if (p.cols >= N && fit >= std::min<u64>(M, 4096)) p.rows = std::min(p.rows, fit);
     const u64 outputs = std::max<u64>(1280, std::min(M, p.rows) * std::min(N, p.cols));            // (planes of whole tiles)
     p.keep = (u32)std::min<u64>(chunks, std::max<u64>(1, limit / outputs));
     p.whole = p.cols >= N && p.keep == chunks;

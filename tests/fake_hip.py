@@ -2,8 +2,10 @@
 
 A child process loads it before the library (the calls of both runtimes' names then go to this one) and runs a test's code with `fake`, `L` (the library), `gtree`, `np`
 and `shares` at hand; what the code prints is returned."""
+import atexit
 import functools
 import os
+import shutil
 import subprocess
 import sys
 import tempfile
@@ -133,6 +135,7 @@ def moe(ctx, d, ff, E, top, rows):
 @functools.lru_cache(None)
 def _built():
     tmp = tempfile.mkdtemp()
+    atexit.register(shutil.rmtree, tmp, True)
     src, so = os.path.join(tmp, "fake_hip.cpp"), os.path.join(tmp, "fake_hip.so")
     with open(src, "w") as f:
         f.write(SOURCE)

@@ -31,7 +31,8 @@ def test_calls_keep_what_fits():
     for M, N, K in ((2048, 4096, 1024), (16384, 8192, 4096), (1000, 257, 294), (294, 257, 48842), (1024, 1024, 1 << 18)):
         p = plan(M, N, K)
         assert p.whole and p.rows >= M
-    assert not plan(16384, 8192, 8192).whole and not plan(1024, 1024, 1 << 20).whole and plan(1024, 1024, 1 << 20).keep == 128
+    assert plan(16384, 8192, 8192) == (8192, 8192, 2, True)               # fewer rows rather than a joining launch
+    assert not plan(16384, 8192, 20000).whole and not plan(1024, 1024, 1 << 20).whole and plan(1024, 1024, 1 << 20).keep == 128
 
 
 def test_calls_take_the_variants_that_they_name():
