@@ -15,14 +15,14 @@
  *    caller, of `n` 64-bit words.  party[p].own holds component p, party[p].next
  *    component p+1 mod 3 (Sec. II-B: P_i holds (x_i, x_{i+1})).
  *    The two copies of a component of an input are equal: where a call reads it for both of its holders (gt_mult's
- *    factors, the instances of an inference, a training's data) it may read one copy, the own one.
+ *    factors, the instances of an inference, a training's data, the factors of a layer's products) it may read one copy, the own one.
  *  - `plain` buffers are device memory too.
  *  - Calls only enqueue work on the context's HIP stream and return; gt_stats_get,
  *    gt_prof_get, gt_stats_reset and the destroy calls wait for it.  Calls on one
  *    context must not overlap.  Device memory is allocated by the create/import calls;
  *    gt_train_level, gt_train_finish and gt_train_reset allocate nothing (the tree that
  *    gt_train_finish returns uses buffers made by gt_train_create, unless the tree of an
- *    earlier finish of the same object is still alive); gt_oaa, gt_oaa_literal
+ *    earlier finish of the same object is still alive); gt_oaa, gt_oaa_literal, the layers
  *    and, level by level only, gt_infer_batch keep a workspace in the context that grows
  *    on first use or for more rows (then they wait for the stream and allocate).
  *  - Return value 0 = success, negative = error; nothing is thrown or aborted.
@@ -36,7 +36,8 @@
  *    then: every replay masks what it opens with the same words.  That is private
  *    only while the inputs stay the same; with new ones the difference of two replays' opened
  *    words is the difference of the secrets.  A graph that is replayed on new inputs
- *    starts with a captured gt_rekey, which gives every replay keys of its own.
+ *    starts with a captured gt_rekey, which gives every replay keys of its own.  Rounds and wire_bytes are counted when
+ *    a call is captured, wire_bits_dev at every replay.
  *  - Public values (leaked by design, Sec. I): all sizes, depths, tau, K.
  */
 #ifndef GTREE_H
@@ -280,7 +281,7 @@ int gt_dense_destroy(gt_dense *layer);
 /* y = act(floor((x W + (b << tau) + 2^(tau-1)) / 2^tau)) + residual, x: rows x din, y, residual (NULL: none), gate: rows x dout.
  * Sums are added up modulo 2^64 and have to stay below 2^62 in absolute value, with GT_ACT_RELU below
  * 2^(tau+31) (results below 2^31).  gate (NULL: not wanted, GT_EINVAL without ReLU) receives ReLU's bit, 1 where the
- * value before the activation is at least 0.  y may be the residual's buffers, not those of x.  One operation id; rounds: 6, with ReLU 8.
+ * value before the activation is at least 0 (at 0 itself frameworks commonly take 0).  y may be the residual's buffers, not those of x.  One operation id; rounds: 6, with ReLU 8.
  * The context's workspace: up to 17 GB of residues, and 24 bytes an output of few rows or, where not all residues fit, of a pass (2^27 outputs,
  * at least 128 rows).  It grows on first use or for larger calls (then the call waits for the stream and allocates).  Under graph
  * capture it cannot: a call that would have to is refused with GT_ESTATE, so a caller makes the largest one eagerly first.  From a capture on, what the workspace
@@ -294,7 +295,8 @@ int gt_dense_forward(gt_ctx *ctx, const gt_dense *layer, const gt_shares *x, siz
 int gt_dense_backward(gt_ctx *ctx, const gt_dense *layer, const gt_shares *x, const gt_shares *gate, const gt_shares *dy, size_t rows,
                       const gt_shares *dx, const gt_shares *dW, const gt_shares *db);
 /* Router Wr: d x experts, br: experts; W1: experts x d x ff, b1: experts x ff; W2: experts x ff x d, b2: experts x d; biases may be
- * NULL.  1 <= top <= experts <= GT_MAX_EXPERTS.  The shares are copied; the workspace for max_rows rows is allocated here. */
+ * NULL.  1 <= top <= experts <= GT_MAX_EXPERTS.  The shares are copied; the workspace for max_rows rows is allocated here, and serves
+ * one call at a time, whatever the context. */
 int gt_moe_create(gt_ctx *ctx, const gt_shares *Wr, const gt_shares *br, const gt_shares *W1, const gt_shares *b1, const gt_shares *W2,
                   const gt_shares *b2, uint32_t d, uint32_t ff, uint32_t experts, uint32_t top, uint32_t max_rows, gt_moe **out);
 int gt_moe_destroy(gt_moe *moe);
