@@ -24,7 +24,8 @@
  *    gt_train_finish returns uses buffers made by gt_train_create, unless the tree of an
  *    earlier finish of the same object is still alive); gt_oaa, gt_oaa_literal, the layers
  *    and, level by level only, gt_infer_batch keep a workspace in the context that grows
- *    on first use or for more rows (then they wait for the stream and allocate).
+ *    on first use or for more rows (then they wait for the stream and allocate; under graph
+ *    capture gt_oaa, gt_oaa_literal and the layers refuse to, with GT_ESTATE).
  *  - Return value 0 = success, negative = error; nothing is thrown or aborted.
  *    After an error the output buffers are unspecified; the context stays usable
  *    unless the error is GT_EHIP.

@@ -482,10 +482,10 @@ static int launch_grid(gt_ctx *c, int mode, int ndot, dim3 g, dim3 b, const Grid
 // rider: equality tests that may run beside the sums' completion, as the operation after this one; n = 0 afterwards: they do
 static int do_grid(gt_ctx *c, int mode, bool has_g, int ndot, GridArgs a, u64 *ext = nullptr, size_t ext_words = 0, EqArgs *rider = nullptr)
 {
-    a.c = kc(c, c->op++);
     a.ndot = ndot;
     const u64 nel = (u64)a.w * a.N;
-    if (a.N && a.w) {
+    if (!a.N || !a.w) c->op++;
+    else {
         const GridShape s = grid_shape(c->simds, mode, ndot, a.sums != 0, a.w, a.N8);
         a.rps = s.rps; a.gpt = s.gpt; a.kchunk = s.kchunk; a.nkc = s.nkc;
         u64 *const own = a.dacc;               // a training object's: zero, like the context's
@@ -499,6 +499,7 @@ static int do_grid(gt_ctx *c, int mode, bool has_g, int ndot, GridArgs a, u64 *e
             } else if (own) a.dacc = own;
             else { GTCHK(grow_dacc(c, need)); a.dacc = c->dacc; }
         }
+        a.c = kc(c, c->op++);                  // (a call that finds no workspace takes no id)
         // more wavefronts than fit at once: the hardware balances them over the compute units
         const dim3 g((unsigned)std::min<u64>(s.ntile * a.nkc, 1u << 20)), B1(GT_LANES);
         const int rc = s.alone ? launch_grid<PRF_ALONE, 2>(c, mode, ndot, g, B1, a) : s.waves == 3 ? launch_grid<PRF_PAIR_LOOP, 3>(c, mode, ndot, g, B1, a)
