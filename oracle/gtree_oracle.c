@@ -1604,16 +1604,18 @@ static void less_el(const orc_ctx *c, u32 op, u64 e, u64 cw, const u64 rw[3], co
 
 /* Completion of sums v whose additive parts the parties hold: y = floor((v + 2^(f-1)) / 2^f), with ReLU times its sign bit (the gate),
  * plus a residual.  Open c = v + 2^(f-1) + O + r with O = 2^62, or 2^(f+31) with ReLU (z_p + alpha_p + r_p to both others, one round); then
- * y = (c >> f) - (r >> f) + 2^(64-f) [c_63 = 0 and r_63 = 1] - [c mod 2^f < r mod 2^f] - (O >> f), and the sign is bit f+31 of c - r. */
-static void finish(orc_ctx *c, u32 op, const sh *z, size_t n, int relu, const sh *res, sh *y, sh *gate)
+ * y = (c >> f) - (r >> f) + 2^(64-f) [c_63 = 0 and r_63 = 1] - [c mod 2^f < r mod 2^f] - (O >> f), and the sign is bit f+31 of c - r.
+ * finish_runs: 1 <= f <= 32; the n sums lie in runs of `width`, element i of the operation is base + i / width * stride + i % width; counts messages, not
+ * rounds. */
+static void finish_runs(orc_ctx *c, u32 op, u32 f, u64 base, size_t width, u64 stride, const sh *z, size_t n, int relu, const sh *res, sh *y, sh *gate)
 {
-    const u32 f = c->tau;
     const u64 off = relu ? (u64)1 << (f + 31) : (u64)1 << 62;
 #pragma omp parallel for schedule(static)
-    for (size_t e = 0; e < n; e++) {
+    for (size_t i = 0; i < n; i++) {
+        const u64 e = base + i / width * stride + i % width;
         dealer_t D; finish_t G;
         u64 al[3], v[3], cw, low[3], all[3], rw[3], b[3], o[3];
-        sh_get(z, e, v);
+        sh_get(z, i, v);
         dealer(c, op, e, &D);
         dealer_finish(c, op, e, D.r, f, &G);
         zero_a(c, op, 0, e, al);
@@ -1636,16 +1638,20 @@ static void finish(orc_ctx *c, u32 op, const sh *z, size_t n, int relu, const sh
             zero_a(c, op, 3, e, a3);
             mult_el(sA, o, a3, r);
             memcpy(o, r, sizeof o);
-            if (gate) sh_set(gate, e, sA);
+            if (gate) sh_set(gate, i, sA);
         }
-        if (res) for (int j = 0; j < 3; j++) o[j] += res->c[j][e];
-        sh_set(y, e, o);
+        if (res) for (int j = 0; j < 3; j++) o[j] += res->c[j][i];
+        sh_set(y, i, o);
     }
     wire(c, +1, n, 64); wire(c, -1, n, 64);
     for (int v = 1; v <= 4; v++) wire(c, -1, n, (relu ? 64u : 32u) >> v);    /* the last level's E of the low half is not used: it is sent all the same */
     if (relu) wire(c, -1, n, 1);
     wire(c, +1, n, relu ? 2 : 1);
     if (relu) wire(c, -1, n, 64);
+}
+static void finish(orc_ctx *c, u32 op, const sh *z, size_t n, int relu, const sh *res, sh *y, sh *gate)
+{
+    finish_runs(c, op, c->tau, 0, n ? n : 1, 0, z, n, relu, res, y, gate);
     c->rounds += relu ? 8 : 6;
 }
 
@@ -1818,5 +1824,168 @@ void orc_moe_forward(orc_ctx *c, const uint64_t *Xf, const uint64_t *Wrf, const 
     dense(c, &he, &W2, NULL, rows, n2, d, 0, resf ? &res : NULL, &y, NULL);
     sh_to_flat(&y, yf);
     sh *all[] = { &X, &Wr, &br, &res, &W1, &W2, &s, &rank, &o, &S, &Q, &g, &xe, &h, &z, &hg, &he, &y };
+    for (size_t i = 0; i < sizeof all / sizeof *all; i++) sh_free(all[i]);
+}
+
+/* ------------------------------------------------------------------------- */
+/* Gated layer: g = (x Wg + bg) s, u = x Wu + bu, h = g u, s ReLU's bit (or 1).  Operations op (g), op + 1 (u), op + 2 (h); elements are rows of ff rounded
+ * up to a multiple of 8.  u is completed beside g. */
+static void projected(orc_ctx *c, u32 op, const sh *X, const uint64_t *Wf, const uint64_t *bf, size_t rows, size_t din, size_t ff, int relu, sh *y, sh *gate)
+{
+    sh W = sh_flat(Wf, din * ff), b = sh_flat(bf, ff), z = sh_alloc(rows * ff);
+    product_parts(X, 0, &W, 0, rows, din, ff, &z);
+    for (int p = 0; p < 3; p++) for (size_t e = 0; e < rows * ff; e++) z.c[p][e] += b.c[p][e % ff] << c->tau;
+    finish_runs(c, op, c->tau, 0, ff, pad8(ff), &z, rows * ff, relu, NULL, y, gate);
+    sh_free(&W); sh_free(&b); sh_free(&z);
+}
+static void local_product(const sh *x, const sh *y, size_t n, sh *z)
+{
+    for (size_t e = 0; e < n; e++) {
+        u64 a[3], b[3], t[3];
+        sh_get(x, e, a); sh_get(y, e, b);
+        prod3(a, b, t);
+        sh_set(z, e, t);
+    }
+}
+void orc_gated_forward(orc_ctx *c, const uint64_t *Xf, const uint64_t *Wgf, const uint64_t *bgf, const uint64_t *Wuf, const uint64_t *buf, size_t rows, size_t din,
+                       size_t ff, int relu, uint64_t *hf, uint64_t *gf, uint64_t *uf, uint64_t *sf)
+{
+    const size_t n = rows * ff;
+    const u32 op = c->op;
+    sh X = sh_flat(Xf, rows * din), g = sh_alloc(n), u = sh_alloc(n), s = sh_alloc(n), z = sh_alloc(n), h = sh_alloc(n);
+    c->op += 3;
+    projected(c, op, &X, Wgf, bgf, rows, din, ff, relu, &g, relu ? &s : NULL);
+    projected(c, op + 1, &X, Wuf, buf, rows, din, ff, 0, &u, NULL);
+    local_product(&g, &u, n, &z);
+    finish_runs(c, op + 2, c->tau, 0, ff, pad8(ff), &z, n, 0, NULL, &h, NULL);
+    c->rounds += relu ? 14 : 12;
+    sh_to_flat(&h, hf); sh_to_flat(&g, gf); sh_to_flat(&u, uf);
+    if (relu) sh_to_flat(&s, sf);
+    sh_free(&X); sh_free(&g); sh_free(&u); sh_free(&s); sh_free(&z); sh_free(&h);
+}
+/* dg = s (dh u) (operation op; the product with the bit under the zero sharing of stream 3), du = dh g (op + 1), then, each if wanted, dx = dg Wg^T + du Wu^T in one
+ * sum, dWg = x^T dg, dWu = x^T du, column sums.  sf NULL: no activation. */
+void orc_gated_backward(orc_ctx *c, const uint64_t *Xf, const uint64_t *Wgf, const uint64_t *Wuf, const uint64_t *gf, const uint64_t *uf, const uint64_t *sf,
+                        const uint64_t *dhf, size_t rows, size_t din, size_t ff, uint64_t *dxf, uint64_t *dWgf, uint64_t *dWuf, uint64_t *dbgf, uint64_t *dbuf)
+{
+    const size_t n = rows * ff;
+    const u32 op = c->op;
+    sh X = sh_flat(Xf, rows * din), Wg = sh_flat(Wgf, din * ff), Wu = sh_flat(Wuf, din * ff), g = sh_flat(gf, n), u = sh_flat(uf, n), s = sh_flat(sf, n);
+    sh dh = sh_flat(dhf, n), z = sh_alloc(n), d[2] = { sh_alloc(n), sh_alloc(n) };
+    c->op += 2;
+    local_product(&dh, &u, n, &z);
+    finish_runs(c, op, c->tau, 0, ff, pad8(ff), &z, n, 0, NULL, &d[0], NULL);
+    if (sf) {
+        for (size_t i = 0; i < n; i++) {
+            u64 a[3], b[3], al[3], t[3];
+            sh_get(&s, i, a); sh_get(&d[0], i, b);
+            zero_a(c, op, 3, i / ff * pad8(ff) + i % ff, al);
+            mult_el(a, b, al, t);
+            sh_set(&d[0], i, t);
+        }
+        wire(c, -1, n, 64);
+    }
+    local_product(&dh, &g, n, &z);
+    finish_runs(c, op + 1, c->tau, 0, ff, pad8(ff), &z, n, 0, NULL, &d[1], NULL);
+    c->rounds += sf ? 7 : 6;
+    if (dxf) {
+        sh a = sh_alloc(rows * din), b = sh_alloc(rows * din), o = sh_alloc(rows * din);
+        product_parts(&d[0], 0, &Wg, 1, rows, ff, din, &a);
+        product_parts(&d[1], 0, &Wu, 1, rows, ff, din, &b);
+        for (int p = 0; p < 3; p++) for (size_t e = 0; e < rows * din; e++) a.c[p][e] += b.c[p][e];
+        finish(c, c->op++, &a, rows * din, 0, NULL, &o, NULL);
+        sh_to_flat(&o, dxf);
+        sh_free(&a); sh_free(&b); sh_free(&o);
+    }
+    for (int i = 0; i < 2; i++) {
+        uint64_t *out = i ? dWuf : dWgf, *sum = i ? dbuf : dbgf;
+        if (out) {
+            sh a = sh_alloc(din * ff), o = sh_alloc(din * ff);
+            product_parts(&X, 1, &d[i], 0, din, rows, ff, &a);
+            finish(c, c->op++, &a, din * ff, 0, NULL, &o, NULL);
+            sh_to_flat(&o, out);
+            sh_free(&a); sh_free(&o);
+        }
+        if (sum)
+            for (int p = 0; p < 3; p++)
+                for (size_t j = 0; j < ff; j++) {
+                    u64 t = 0;
+                    for (size_t r = 0; r < rows; r++) t += d[i].c[p][r * ff + j];
+                    sum[p * ff + j] = t;
+                }
+    }
+    sh *all[] = { &X, &Wg, &Wu, &g, &u, &s, &dh, &z, &d[0], &d[1] };
+    for (size_t i = 0; i < sizeof all / sizeof *all; i++) sh_free(all[i]);
+}
+
+/* Linear attention with a decay w / 2^12 for each head, 64 tokens at a time.  D[n] = decay^n with 12 fraction bits, rounded from 46; s = tau + 12.  For a chunk of c
+ * tokens with the state S before it
+ *   P_ij = floor((D[i-j] q_i k_j + 2^(s-1)) / 2^s), j <= i                                    operation op
+ *   S'   = floor((2^tau D[c] S + sum_j D[c-1-j] k_j v_j + 2^(s-1)) / 2^s)                       op + 1
+ *   o_i  = floor((2^12 sum_j P_ij v_j + D[i+1] q_i S + 2^(s-1)) / 2^s)                          op + 2
+ * Elements, b = (sequence * heads + head) * chunks + chunk: b * 2080 + i (i + 1) / 2 + j; b * pad8(dk dv) + row * dv + column; (b * 64 + i) * pad8(dv) + column.
+ * Rounds: scores and the first state side by side, then state after state, the outputs beside the last one. */
+void orc_linattn_forward(orc_ctx *c, const uint64_t *qf, const uint64_t *kf, const uint64_t *vf, const uint64_t *Sf, const uint32_t *decay, size_t seqs, size_t T, size_t H,
+                         size_t dk, size_t dv, uint64_t *of, uint64_t *outf)
+{
+    const size_t n = seqs * T, nc = (T + 63) / 64, nS = seqs * H * dk * dv;
+    const u32 op = c->op, s = c->tau + 12, f = c->tau;
+    sh q = sh_flat(qf, n * H * dk), k = sh_flat(kf, n * H * dk), v = sh_flat(vf, n * H * dv), S = sh_flat(Sf, nS), o = sh_alloc(n * H * dv);
+    sh sc = sh_alloc(2080), P = sh_alloc(2080), zS = sh_alloc(dk * dv), nextS = sh_alloc(dk * dv), zo = sh_alloc(64 * dv), oo = sh_alloc(64 * dv);
+    c->op += 3;
+    for (size_t bh = 0; bh < seqs * H; bh++)
+        for (size_t ch = 0; ch < nc; ch++) {
+            const size_t h = bh % H, t0 = bh / H * T + ch * 64, len = T - ch * 64 < 64 ? T - ch * 64 : 64, b = bh * nc + ch;
+            u64 D[65], E = (u64)1 << 46;
+            for (int i = 0; i <= 64; i++) { D[i] = (E + ((u64)1 << 33)) >> 34; E = (E * decay[h] + (1u << 11)) >> 12; }
+            u64 x[3], y[3], t[3];
+            for (size_t i = 0; i < len; i++)
+                for (size_t j = 0; j <= i; j++) {
+                    u64 a[3] = { 0, 0, 0 };
+                    for (size_t d = 0; d < dk; d++) {
+                        sh_get(&q, ((t0 + i) * H + h) * dk + d, x); sh_get(&k, ((t0 + j) * H + h) * dk + d, y);
+                        prod3(x, y, t);
+                        for (int p = 0; p < 3; p++) a[p] += t[p] * D[i - j];
+                    }
+                    sh_set(&sc, i * (i + 1) / 2 + j, a);
+                }
+            const size_t tri = len * (len + 1) / 2;
+            finish_runs(c, op, s, b * 2080, tri, 0, &sc, tri, 0, NULL, &P, NULL);
+            for (size_t r = 0; r < dk; r++)
+                for (size_t j = 0; j < dv; j++) {
+                    u64 a[3];
+                    sh_get(&S, (bh * dk + r) * dv + j, a);
+                    for (int p = 0; p < 3; p++) a[p] = (a[p] * D[len]) << f;
+                    for (size_t i = 0; i < len; i++) {
+                        sh_get(&k, ((t0 + i) * H + h) * dk + r, x); sh_get(&v, ((t0 + i) * H + h) * dv + j, y);
+                        prod3(x, y, t);
+                        for (int p = 0; p < 3; p++) a[p] += t[p] * D[len - 1 - i];
+                    }
+                    sh_set(&zS, r * dv + j, a);
+                }
+            finish_runs(c, op + 1, s, b * pad8(dk * dv), dk * dv, 0, &zS, dk * dv, 0, NULL, &nextS, NULL);
+            for (size_t i = 0; i < len; i++)
+                for (size_t j = 0; j < dv; j++) {
+                    u64 a[3] = { 0, 0, 0 };
+                    for (size_t e = 0; e <= i; e++) {
+                        sh_get(&P, i * (i + 1) / 2 + e, x); sh_get(&v, ((t0 + e) * H + h) * dv + j, y);
+                        prod3(x, y, t);
+                        for (int p = 0; p < 3; p++) a[p] += t[p] << 12;
+                    }
+                    for (size_t d = 0; d < dk; d++) {
+                        sh_get(&q, ((t0 + i) * H + h) * dk + d, x); sh_get(&S, (bh * dk + d) * dv + j, y);
+                        prod3(x, y, t);
+                        for (int p = 0; p < 3; p++) a[p] += t[p] * D[i + 1];
+                    }
+                    sh_set(&zo, i * dv + j, a);
+                }
+            finish_runs(c, op + 2, s, b * 64 * pad8(dv), dv, pad8(dv), &zo, len * dv, 0, NULL, &oo, NULL);
+            for (size_t i = 0; i < len; i++)
+                for (size_t j = 0; j < dv; j++) { sh_get(&oo, i * dv + j, x); sh_set(&o, ((t0 + i) * H + h) * dv + j, x); }
+            for (size_t e = 0; e < dk * dv; e++) { sh_get(&nextS, e, x); sh_set(&S, bh * dk * dv + e, x); }
+        }
+    c->rounds += n ? 6 * (nc > 2 ? nc : 2) : 0;
+    sh_to_flat(&o, of); sh_to_flat(&S, outf);
+    sh *all[] = { &q, &k, &v, &S, &o, &sc, &P, &zS, &nextS, &zo, &oo };
     for (size_t i = 0; i < sizeof all / sizeof *all; i++) sh_free(all[i]);
 }

@@ -154,6 +154,12 @@ void orc_dense_forward(orc_ctx *, const uint64_t *X, const uint64_t *W, const ui
 void orc_dense_backward(orc_ctx *, const uint64_t *X, const uint64_t *W, const uint64_t *gate, const uint64_t *dy, size_t rows, size_t din,
                         size_t dout, uint64_t *dx, uint64_t *dW, uint64_t *db);
 /* mixture of experts, see the source; Wr d x E, W1 E x d x ff, W2 E x ff x d; 10 + tau ops */
+void orc_gated_forward(orc_ctx *, const uint64_t *X, const uint64_t *Wg, const uint64_t *bg, const uint64_t *Wu, const uint64_t *bu, size_t rows, size_t din, size_t ff,
+                       int relu, uint64_t *h, uint64_t *g, uint64_t *u, uint64_t *s);
+void orc_gated_backward(orc_ctx *, const uint64_t *X, const uint64_t *Wg, const uint64_t *Wu, const uint64_t *g, const uint64_t *u, const uint64_t *s, const uint64_t *dh,
+                        size_t rows, size_t din, size_t ff, uint64_t *dx, uint64_t *dWg, uint64_t *dWu, uint64_t *dbg, uint64_t *dbu);
+void orc_linattn_forward(orc_ctx *, const uint64_t *q, const uint64_t *k, const uint64_t *v, const uint64_t *S, const uint32_t *decay, size_t seqs, size_t tokens,
+                         size_t heads, size_t dk, size_t dv, uint64_t *o, uint64_t *Sout);
 void orc_moe_forward(orc_ctx *, const uint64_t *X, const uint64_t *Wr, const uint64_t *br, const uint64_t *W1, const uint64_t *b1,
                      const uint64_t *W2, const uint64_t *b2, const uint64_t *res, size_t rows, size_t d, size_t ff, size_t E, size_t k, uint64_t *y);
 

@@ -77,6 +77,9 @@ def _load():
         "orc_div": (None, [vp, _u64p, _u64p, sz, _u64p]),
         "orc_dense_forward": (None, [vp, _u64p, _u64p, _u64p, _u64p, sz, sz, sz, i, _u64p, _u64p]),
         "orc_dense_backward": (None, [vp, _u64p, _u64p, _u64p, _u64p, sz, sz, sz, _u64p, _u64p, _u64p]),
+        "orc_gated_forward": (None, [vp] + [_u64p] * 5 + [sz, sz, sz, i] + [_u64p] * 4),
+        "orc_gated_backward": (None, [vp] + [_u64p] * 7 + [sz, sz, sz] + [_u64p] * 5),
+        "orc_linattn_forward": (None, [vp] + [_u64p] * 4 + [vp] + [sz] * 5 + [_u64p] * 2),
         "orc_moe_forward": (None, [vp] + [_u64p] * 8 + [sz] * 5 + [_u64p]),
         "orc_train_create": (vp, [vp, _u64p, _u64p, sz, u32, u32]),
         "orc_train_destroy": (None, [vp]),
@@ -295,6 +298,31 @@ class Oracle:
         a = [self._flat(t) for t in (X, Wr, br, W1, b1, W2, b2, residual)]
         self.L.orc_moe_forward(self.ctx, *[_p(t) for t in a], rows, d, ff, experts, top, _p(y.reshape(-1)))
         return y
+
+    def gated_forward(self, X, Wg, Wu, rows, din, ff, bg=None, bu=None, relu=True):
+        """(h, g, u, s); s is None without ReLU."""
+        out = [np.zeros((3, rows * ff), dtype=np.uint64) for _ in range(4)]
+        a = [self._flat(t) for t in (X, Wg, bg, Wu, bu)]
+        self.L.orc_gated_forward(self.ctx, *[_p(t) for t in a], rows, din, ff, int(relu), *[_p(t.reshape(-1)) for t in out])
+        return (*out[:3], out[3] if relu else None)
+
+    def gated_backward(self, X, Wg, Wu, dh, rows, din, ff, kept, want=(True, True, True)):
+        """(dx, dWg, dWu, dbg, dbu), None where not wanted; kept: (g, u, s)."""
+        wants = (want[0], want[1], want[1], want[2], want[2])
+        out = [np.zeros((3, n), dtype=np.uint64) if w else None for n, w in zip((rows * din, din * ff, din * ff, ff, ff), wants)]
+        a = [self._flat(t) for t in (X, Wg, Wu, *kept, dh)]
+        self.L.orc_gated_backward(self.ctx, *[_p(t) for t in a], rows, din, ff, *[None if t is None else _p(t.reshape(-1)) for t in out])
+        return tuple(out)
+
+    def linattn_forward(self, q, k, v, S, decay, seqs, tokens, dk, dv):
+        """(o, state); decay: words of 12 fraction bits, one a head; S None: zeros."""
+        w = np.ascontiguousarray(decay, dtype=np.uint32)
+        H = w.size
+        S = np.zeros((3, seqs * H * dk * dv), dtype=np.uint64) if S is None else S
+        o, out = np.zeros((3, seqs * tokens * H * dv), dtype=np.uint64), np.zeros_like(S)
+        a = [self._flat(t) for t in (q, k, v, S)]
+        self.L.orc_linattn_forward(self.ctx, *[_p(t) for t in a], w.ctypes.data, seqs, tokens, H, dk, dv, _p(o.reshape(-1)), _p(out.reshape(-1)))
+        return o, out
 
     # -- training ----------------------------------------------------------
     def train_create(self, X, Y, N, d, H):
