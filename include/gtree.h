@@ -62,6 +62,8 @@ extern "C" {
 #define GT_STATIC_MAX_N (1u << 18) /* rows of gt_oaa_static */
 #define GT_MAX_DIM (1u << 20)  /* rows, inputs and outputs of a layer */
 #define GT_MAX_EXPERTS 64u     /* experts of a mixture */
+#define GT_MAX_HEADS 256u      /* heads of linear attention */
+#define GT_MAX_HEAD_DIM 256u   /* ... their keys' and values' words */
 
 typedef struct gt_ctx gt_ctx;     /* keys, operation counter, stream, scratch for partial sums */
 typedef struct gt_train gt_train; /* per-party shares of T, F, M, C, gamma and the data */
@@ -306,6 +308,43 @@ int gt_moe_destroy(gt_moe *moe);
  * plus the residual (NULL: none).  Which experts a row takes is not revealed: the row's inputs are multiplied by the shared choice and meet
  * all experts' weights.  rows <= max_rows, x, y, residual: rows x d; y may be the residual's buffers.  10 + tau operation ids. */
 int gt_moe_forward(gt_ctx *ctx, gt_moe *moe, const gt_shares *x, size_t rows, const gt_shares *residual, const gt_shares *y);
+
+/* Gated layer: both projections of a gated feed-forward block, the activation and the product.  Wg, Wu: din x ff, bg, bu: ff words, both or none.
+ * ff <= GT_MAX_DIM / 2.  The shares are copied. */
+typedef struct gt_gated gt_gated;
+int gt_gated_create(gt_ctx *ctx, const gt_shares *Wg, const gt_shares *bg, const gt_shares *Wu, const gt_shares *bu, uint32_t din, uint32_t ff, gt_gated **out);
+/* new weights of the same sizes; biases as at creation.  Allocates nothing. */
+int gt_gated_set(gt_ctx *ctx, gt_gated *layer, const gt_shares *Wg, const gt_shares *bg, const gt_shares *Wu, const gt_shares *bu);
+int gt_gated_destroy(gt_gated *layer);
+/* G = floor((x Wg + (bg << tau) + 2^(tau-1)) / 2^tau), g = G [G >= 0] (GT_ACT_NONE: G), u = floor((x Wu + (bu << tau) + 2^(tau-1)) / 2^tau),
+ * h = floor((g u + 2^(tau-1)) / 2^tau).  x: rows x din, h: rows x ff.  g, u (rows x ff, both or NULL) and, where they are wanted with GT_ACT_RELU, the gate (ReLU's bit,
+ * else NULL) are what gt_gated_backward takes.  Bounds as in gt_dense_forward, for x Wg (with GT_ACT_RELU), x Wu and g u (2^62).  Three operation ids; rounds: 12,
+ * with ReLU 14.  Workspace, graph capture and gt_rekey as in gt_dense_forward. */
+int gt_gated_forward(gt_ctx *ctx, const gt_gated *layer, const gt_shares *x, size_t rows, int act, const gt_shares *h, const gt_shares *g, const gt_shares *u,
+                     const gt_shares *gate);
+/* dg = floor((dh u + 2^(tau-1)) / 2^tau), times the gate unless it is NULL (GT_ACT_NONE), du = the same of dh g; dx = the same of dg Wg^T + du Wu^T in one sum,
+ * dWg, dWu = the same of x^T dg, x^T du; dbg, dbu = column sums of dg, du.  dx, dWg and dWu, dbg and dbu may be NULL: not computed (x is needed for dWg, dWu alone).  Two
+ * operation ids, then one for dx and two for dWg, dWu, each if computed.  All sums stay below 2^62. */
+int gt_gated_backward(gt_ctx *ctx, const gt_gated *layer, const gt_shares *x, const gt_shares *g, const gt_shares *u, const gt_shares *gate, const gt_shares *dh,
+                      size_t rows, const gt_shares *dx, const gt_shares *dWg, const gt_shares *dWu, const gt_shares *dbg, const gt_shares *dbu);
+
+/* Linear attention with a decay for each head: per head a state S of dk x dv words, S <- decay S + k^T v, o = q S, token after token, without softmax or
+ * normaliser.  decay: `heads` words in host memory of 12 fraction bits, 0 .. 2^12 (the state's weight from one token to the next, public).  heads <=
+ * GT_MAX_HEADS, dk, dv <= GT_MAX_HEAD_DIM. */
+typedef struct gt_linattn gt_linattn;
+int gt_linattn_create(gt_ctx *ctx, const uint32_t *decay, uint32_t heads, uint32_t dk, uint32_t dv, gt_linattn **out);
+int gt_linattn_destroy(gt_linattn *attention);
+/* q, k: rows of heads x dk words, v: of heads x dv, row `sequence * tokens + token`; rows are ld words apart (parts of one projection's output; 0: without gaps), o:
+ * heads x dv without gaps.  state_in, state_out: seqs x heads x dk x dv; state_in NULL: zeros; both may be the same buffers, o and the states share
+ * none with q, k, v.  A sequence's tokens are taken in chunks of 64 from its first one on (the last may be shorter; a single token is a chunk).  With D[n] = decay^n rounded to
+ * 12 bits, s = tau + 12 and a chunk's c tokens counted from 0:
+ *   P_ij = floor((D[i-j] q_i k_j + 2^(s-1)) / 2^s) for j <= i, o_i = floor((2^12 sum_j P_ij v_j + D[i+1] q_i S + 2^(s-1)) / 2^s),
+ *   S <- floor((2^tau D[c] S + sum_j D[c-1-j] k_j v_j + 2^(s-1)) / 2^s)
+ * so other chunks round otherwise; all sums stay below 2^62, real numbers below 2^(50 - 2 tau).  Without tokens the states are copied.
+ * Three operation ids; rounds: 6 for every chunk, at least 12.  Workspace (up to 2 GB, with GT_FLAG_SMALL_WORKSPACE 64 MB), graph capture and gt_rekey as in
+ * gt_dense_forward.  seqs * tokens <= GT_MAX_DIM. */
+int gt_linattn_forward(gt_ctx *ctx, const gt_linattn *attention, const gt_shares *q, const gt_shares *k, const gt_shares *v, size_t ld, size_t seqs, size_t tokens,
+                       const gt_shares *state_in, const gt_shares *state_out, const gt_shares *o);
 
 #ifdef __cplusplus
 }

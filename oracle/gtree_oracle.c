@@ -1605,8 +1605,8 @@ static void less_el(const orc_ctx *c, u32 op, u64 e, u64 cw, const u64 rw[3], co
 /* Completion of sums v whose additive parts the parties hold: y = floor((v + 2^(f-1)) / 2^f), with ReLU times its sign bit (the gate),
  * plus a residual.  Open c = v + 2^(f-1) + O + r with O = 2^62, or 2^(f+31) with ReLU (z_p + alpha_p + r_p to both others, one round); then
  * y = (c >> f) - (r >> f) + 2^(64-f) [c_63 = 0 and r_63 = 1] - [c mod 2^f < r mod 2^f] - (O >> f), and the sign is bit f+31 of c - r.
- * finish_runs: 1 <= f <= 32; the n sums lie in runs of `width`, element i of the operation is base + i / width * stride + i % width; counts messages, not
- * rounds. */
+ * finish_runs: 1 <= f <= 32; the n sums lie in runs of `width`, element i of the operation is base + i / width * stride + i % width; messages (wire_finish)
+ * and rounds are the caller's to count. */
 static void finish_runs(orc_ctx *c, u32 op, u32 f, u64 base, size_t width, u64 stride, const sh *z, size_t n, int relu, const sh *res, sh *y, sh *gate)
 {
     const u64 off = relu ? (u64)1 << (f + 31) : (u64)1 << 62;
@@ -1643,6 +1643,9 @@ static void finish_runs(orc_ctx *c, u32 op, u32 f, u64 base, size_t width, u64 s
         if (res) for (int j = 0; j < 3; j++) o[j] += res->c[j][i];
         sh_set(y, i, o);
     }
+}
+static void wire_finish(orc_ctx *c, size_t n, int relu)
+{
     wire(c, +1, n, 64); wire(c, -1, n, 64);
     for (int v = 1; v <= 4; v++) wire(c, -1, n, (relu ? 64u : 32u) >> v);    /* the last level's E of the low half is not used: it is sent all the same */
     if (relu) wire(c, -1, n, 1);
@@ -1652,6 +1655,7 @@ static void finish_runs(orc_ctx *c, u32 op, u32 f, u64 base, size_t width, u64 s
 static void finish(orc_ctx *c, u32 op, const sh *z, size_t n, int relu, const sh *res, sh *y, sh *gate)
 {
     finish_runs(c, op, c->tau, 0, n ? n : 1, 0, z, n, relu, res, y, gate);
+    wire_finish(c, n, relu);
     c->rounds += relu ? 8 : 6;
 }
 
@@ -1858,6 +1862,7 @@ void orc_gated_forward(orc_ctx *c, const uint64_t *Xf, const uint64_t *Wgf, cons
     projected(c, op + 1, &X, Wuf, buf, rows, din, ff, 0, &u, NULL);
     local_product(&g, &u, n, &z);
     finish_runs(c, op + 2, c->tau, 0, ff, pad8(ff), &z, n, 0, NULL, &h, NULL);
+    wire_finish(c, n, relu); wire_finish(c, n, 0); wire_finish(c, n, 0);
     c->rounds += relu ? 14 : 12;
     sh_to_flat(&h, hf); sh_to_flat(&g, gf); sh_to_flat(&u, uf);
     if (relu) sh_to_flat(&s, sf);
@@ -1887,6 +1892,7 @@ void orc_gated_backward(orc_ctx *c, const uint64_t *Xf, const uint64_t *Wgf, con
     }
     local_product(&dh, &g, n, &z);
     finish_runs(c, op + 1, c->tau, 0, ff, pad8(ff), &z, n, 0, NULL, &d[1], NULL);
+    wire_finish(c, n, 0); wire_finish(c, n, 0);
     c->rounds += sf ? 7 : 6;
     if (dxf) {
         sh a = sh_alloc(rows * din), b = sh_alloc(rows * din), o = sh_alloc(rows * din);
@@ -1984,7 +1990,13 @@ void orc_linattn_forward(orc_ctx *c, const uint64_t *qf, const uint64_t *kf, con
                 for (size_t j = 0; j < dv; j++) { sh_get(&oo, i * dv + j, x); sh_set(&o, ((t0 + i) * H + h) * dv + j, x); }
             for (size_t e = 0; e < dk * dv; e++) { sh_get(&nextS, e, x); sh_set(&S, bh * dk * dv + e, x); }
         }
-    c->rounds += n ? 6 * (nc > 2 ? nc : 2) : 0;
+    if (n) {
+        const size_t full = T / 64, rest = T % 64;
+        wire_finish(c, seqs * H * (full * 2080 + rest * (rest + 1) / 2), 0);
+        for (size_t ch = 0; ch < nc; ch++) wire_finish(c, nS, 0);
+        wire_finish(c, n * H * dv, 0);
+        c->rounds += 6 * (nc > 2 ? nc : 2);
+    }
     sh_to_flat(&o, of); sh_to_flat(&S, outf);
     sh *all[] = { &q, &k, &v, &S, &o, &sc, &P, &zS, &nextS, &zo, &oo };
     for (size_t i = 0; i < sizeof all / sizeof *all; i++) sh_free(all[i]);

@@ -1,0 +1,442 @@
+// A block of a network in fixed point on shares: the gated layer and its gradients, and linear attention with a decay for each head.
+#pragma once
+#include "gt_layers.hpp"
+
+// ---------------------------------------------------------------------------------
+// Gated layer: g = (x Wg + bg) s, u = x Wu + bu, h = g u, s ReLU's bit (or 1), f = tau fraction bits.  Both projections are one product with the weights side by side,
+// ffp (ff rounded up to 64) columns each; one kernel completes g (operation c.op), u (c.op + 1) and h (c.op + 2), so that neither projection is written and
+// read again.  Elements are rows of ff8 (ff rounded up to 8), so that eight adjacent ones lie in a row.
+// Z: the parts, [3][rows][2 ffp], left at zero, or R: residues, planes of rows x 2 ffp.  first: the pass's first row.
+struct GatedArgs {
+    KCommon c;
+    u64 *Z;
+    const unsigned char *R;
+    u64 plane, first, rows;
+    u32 nchunk, ff, ff8, ffp, f, per, nbig;
+    P6 bias, h, g, u, s;                          // bias: bg, behind it bu; s: with ReLU
+    int has_bias, keep;
+};
+// row and column of an element of the pass
+struct GatedAt { u64 row; u32 col; };
+__device__ __forceinline__ GatedAt gated_at(u64 i, u32 ff8, bool narrow)
+{
+    const u64 row = narrow ? (u64)((u32)i / ff8) : i / ff8;
+    return GatedAt{ row, (u32)(i - row * ff8) };
+}
+template <int SRC, bool RELU>
+__global__ __launch_bounds__(64) void k_gated(GatedArgs a)
+{
+    constexpr int NS = RELU ? 3 : 2;
+    __shared__ uint4 s_msg[GT_LANES];
+    __shared__ u64 s_mat[(22 + 3 * NS) * GT_FP_ROW];
+    __shared__ u64 s_cnt[6];
+    WWire W; W.init(s_msg, s_cnt);
+    const int p = W.p;
+    const u32 f = a.f, t = W.t < 20 ? W.t : 19, block = blockIdx.x;
+    const u64 n = a.rows * a.ff8, ld = 2 * (u64)a.ffp;
+    const bool mine = W.real && W.t < 20, narrow = n <= 0xffffffffu;
+    const u32 per = SRC == FIN_RES && block < a.nbig ? a.per : 1, chunk = per * GT_FP_EL;
+    const u64 c0 = (SRC == FIN_RES ? (block < a.nbig ? (u64)block * a.per : (u64)a.nbig * (a.per - 1) + block) : (u64)block) * GT_FP_EL;
+    // residues: lane t of a party joins eight adjacent words, of g in the first 5 per lanes, of u in the next
+    const u32 half = t >= 5 * per ? 1 : 0, grp = half ? t - 5 * per : t;
+    u64 zw[8];
+    if (SRC == FIN_RES) {
+        const u64 i = c0 + 8 * (grp < 5 * per ? grp : 5 * per - 1);
+        const GatedAt at = gated_at(i < n ? i : n - 8, a.ff8, narrow);
+        rns_words(a, p, at.row * ld + half * a.ffp + at.col, zw);
+    }
+    for (u32 k0 = 0; k0 < chunk && c0 + k0 < n; k0 += GT_FP_EL) {
+        const u32 el[2] = { t, t + 20 };
+        bool act[2];
+        u64 zg[2], zu[2], e[2], from[2];
+#pragma unroll
+        for (int q = 0; q < 2; q++) {
+            const u64 i = c0 + k0 + el[q];
+            GatedAt at = gated_at(i < n ? i : n - 1, a.ff8, narrow);
+            act[q] = W.t < 20 && i < n && at.col < a.ff;
+            if (at.col >= a.ff) at.col = a.ff - 1;                   // (words that exist where these do not)
+            e[q] = (a.first + at.row) * a.ff + at.col;
+            from[q] = at.row * ld + at.col;
+            if (a.has_bias) { const u64 *b = own_of(a.bias, p); zg[q] = b[at.col] << f; zu[q] = b[a.ff + at.col] << f; }
+            else zg[q] = zu[q] = 0;
+        }
+        if (SRC == FIN_PARTS) {
+            u64 *Z = a.Z + (u64)p * a.rows * ld;
+#pragma unroll
+            for (int q = 0; q < 2; q++) { zg[q] += Z[from[q]]; zu[q] += Z[from[q] + a.ffp]; }
+#pragma unroll
+            for (int q = 0; q < 2; q++) if (mine && act[q]) { Z[from[q]] = 0; Z[from[q] + a.ffp] = 0; }
+        } else {
+            // the tile's words from the lanes that joined them, through the message region
+            u64 *words = (u64 *)s_msg + GT_FP_EL * p;
+            const u32 at = 8 * grp - k0;                              // (wraps for the lanes of tiles before)
+#pragma unroll
+            for (u32 w = 0; w < 2; w++) {
+                wave_sync();
+                if (half == w && grp < 5 * per && at < GT_FP_EL)
+#pragma unroll
+                    for (int i = 0; i < 8; i++) words[at + i] = zw[i];
+                wave_sync();
+                (w ? zu : zg)[0] += words[t]; (w ? zu : zg)[1] += words[t + 20];
+            }
+        }
+        const u32 na = (u32)act[0] + (u32)act[1];
+        const u64 e0 = a.first * a.ff8 + c0 + k0;
+        Sh g[2], u[2], h[2], s[2], none[2];
+        {
+            FinPair<NS> T; T.keys = a.c.keys; T.mat = s_mat; T.f = f;
+            T.deal(W, a.c.op, e0);
+            finish_two<RELU>(W, T, f, zg, el, na, g, s);
+        }
+        FinPair<2> T; T.keys = a.c.keys; T.mat = s_mat; T.f = f;
+        T.deal(W, a.c.op + 1, e0);
+        finish_two<false>(W, T, f, zu, el, na, u, none);
+        const u64 zh[2] = { prod3(g[0], u[0]), prod3(g[1], u[1]) };
+        T.deal(W, a.c.op + 2, e0);
+        finish_two<false>(W, T, f, zh, el, na, h, none);
+#pragma unroll
+        for (int q = 0; q < 2; q++)
+            if (mine && act[q]) {
+                st(a.h, p, e[q], h[q]);
+                if (a.keep) { st(a.g, p, e[q], g[q]); st(a.u, p, e[q], u[q]); }
+                if (RELU && a.keep) st(a.s, p, e[q], s[q]);
+            }
+        W.drain();
+    }
+    W.flush(a.c.wire);
+}
+
+// Gradients behind the product and the activation: dg = s (dh u) (operation c.op, the product with the bit under its stream 3), du = dh g (c.op + 1), the components
+// side by side, rows of 2 ffp: operands of the products that follow (columns behind ff are not written; they meet weights that are zero).
+struct GatedBackArgs { KCommon c; P6 dh, g, u, s; u64 *dz[3]; u64 rows; u32 ff, ff8, ffp, f; };
+template <bool RELU>
+__global__ __launch_bounds__(64) void k_gated_back(GatedBackArgs a)
+{
+    constexpr int NS = RELU ? 3 : 2;
+    __shared__ uint4 s_msg[GT_LANES];
+    __shared__ u64 s_mat[(22 + 3 * NS) * GT_FP_ROW];
+    __shared__ u64 s_cnt[6];
+    WWire W; W.init(s_msg, s_cnt);
+    const int p = W.p;
+    const u32 f = a.f, t = W.t < 20 ? W.t : 19;
+    const u64 n = a.rows * a.ff8, c0 = (u64)blockIdx.x * GT_FP_EL;
+    const bool mine = W.real && W.t < 20, narrow = n <= 0xffffffffu;
+    const u32 el[2] = { t, t + 20 };
+    bool act[2];
+    u64 zg[2], zu[2], to[2];
+    Sh s[2], dg[2], du[2], none[2];
+#pragma unroll
+    for (int q = 0; q < 2; q++) {
+        const u64 i = c0 + el[q];
+        GatedAt at = gated_at(i < n ? i : n - 1, a.ff8, narrow);
+        act[q] = W.t < 20 && i < n && at.col < a.ff;
+        if (at.col >= a.ff) at.col = a.ff - 1;
+        const u64 e = at.row * a.ff + at.col;
+        to[q] = at.row * 2 * a.ffp + at.col;
+        const Sh dh = ld(a.dh, p, e);
+        zg[q] = prod3(dh, ld(a.u, p, e)); zu[q] = prod3(dh, ld(a.g, p, e));
+        if (RELU) s[q] = ld(a.s, p, e);
+    }
+    const u32 na = (u32)act[0] + (u32)act[1];
+    {
+        FinPair<NS> T; T.keys = a.c.keys; T.mat = s_mat; T.f = f;
+        T.deal(W, a.c.op, c0);
+        finish_two<false>(W, T, f, zg, el, na, dg, none);
+        if (RELU) {
+            u64 m[2], rcv[2];
+#pragma unroll
+            for (int q = 0; q < 2; q++) m[q] = prod3(s[q], dg[q]) + T.za(W, 2, el[q]);
+            W.reshare64<2>(m, rcv);
+            W.nresh += 64u * na;
+#pragma unroll
+            for (int q = 0; q < 2; q++) dg[q] = Sh{ m[q], rcv[q] };
+        }
+    }
+    FinPair<2> T; T.keys = a.c.keys; T.mat = s_mat; T.f = f;
+    T.deal(W, a.c.op + 1, c0);
+    finish_two<false>(W, T, f, zu, el, na, du, none);
+    u64 *dz = p == 0 ? a.dz[0] : (p == 1 ? a.dz[1] : a.dz[2]);
+#pragma unroll
+    for (int q = 0; q < 2; q++) if (mine && act[q]) { dz[to[q]] = dg[q].o; dz[to[q] + a.ffp] = du[q].o; }
+    W.flush(a.c.wire);
+}
+
+// ---------------------------------------------------------------------------------
+// Linear attention, 64 tokens (a chunk) at a time, s = f + 12, D[n] = decay^n with 12 fraction bits:
+//   P_ij = floor((D[i-j] q_i k_j + 2^(s-1)) / 2^s), j <= i                       operation c.op,     element b * 2080 + i (i + 1) / 2 + j
+//   S'   = floor((2^f D[c] S + sum_j D[c-1-j] k_j v_j + 2^(s-1)) / 2^s)            c.op + 1,           element b * pk + row * dv + column
+//   o_i  = floor((2^12 sum_j P_ij v_j + D[i+1] q_i S + 2^(s-1)) / 2^s)             c.op + 2,           element (b * 64 + i) * dv8 + column
+// for chunk b = (sequence * heads + head) * chunks + chunk, c tokens of it, S the state before it; pk, dv8: dk dv and dv rounded up to 8.
+//   k_lin_parts    the parts of D q k^T and of (D k)^T v, every chunk by itself
+//   k_lin_states   the states one after the other, an element's chain in one wavefront; beside them the scores' completion
+//   k_lin_out      the parts of [2^12 P, D q] [v; S]
+//   k_lin_finish   their completion
+// A pass takes chunks ch0 .. ch0 + nch - 1 of sequences' heads bh0 .. bh0 + nbh - 1; b' = (bh - bh0) * nch + chunk - ch0 counts in its workspace.
+#define GT_LIN_CHUNK 64
+#define GT_LIN_TRI 2080
+#define GT_LIN_DECAY 12
+struct LinArgs {
+    KCommon c;
+    const u64 *q[3], *k[3], *v[3];
+    P6 in, out, o;                                // states before and after, outputs
+    const u32 *D;                                 // [head][65]
+    u64 ldq, ldk, ldv, T;
+    u32 H, dk, dv, dv8, pk, f, has_in;
+    u64 nc, bh0;                                  // chunks of a sequence
+    u32 ch0, nch, nbh;
+    u64 *Zs, *Zk, *Zo, *P, *S;                    // parts [3][b'][2080], [pk], [64 dv8]; scores [3][b'][2080], states before a chunk [3][b'][pk]
+    u32 tiles, each;                              // k_lin_states: workgroups of chains; k_lin_states, k_lin_finish: tiles of 40 of a head's chunks in the pass
+};
+
+struct LinChunk { u64 t0; u32 bh, h, len; };     // first row of q, k, v; head; tokens
+__device__ __forceinline__ LinChunk lin_chunk(const LinArgs &a, u32 bhl, u32 ch)
+{
+    LinChunk r;
+    const u64 bh = a.bh0 + bhl, t = (u64)ch * GT_LIN_CHUNK;
+    r.bh = (u32)bh; r.h = (u32)(bh % a.H);
+    r.t0 = bh / a.H * a.T + t;
+    r.len = a.T - t < GT_LIN_CHUNK ? (u32)(a.T - t) : GT_LIN_CHUNK;
+    return r;
+}
+__device__ __forceinline__ const u64 *comp_of(const u64 *const (&x)[3], int j) { return j == 0 ? x[0] : (j == 1 ? x[1] : x[2]); }
+
+// Limbs of a lane's 16 words, as operands of v_mfma_i32_16x16x64_i8.
+__device__ __forceinline__ void lin_limbs(const u64 (&x)[16], v4i (&B)[8])
+{
+    u64 y[8], z[8];
+#pragma unroll
+    for (int i = 0; i < 8; i++) { y[i] = (x[i] + GT_BIAS) ^ GT_BIAS; z[i] = (x[8 + i] + GT_BIAS) ^ GT_BIAS; }
+    transpose8x8(y); transpose8x8(z);
+#pragma unroll
+    for (int i = 0; i < 8; i++) B[i] = v4i{ (int)(u32)y[i], (int)(u32)(y[i] >> 32), (int)(u32)z[i], (int)(u32)(z[i] >> 32) };
+}
+
+enum { LIN_SCORES = 0, LIN_KV = 1, LIN_OUT = 2 };
+#define GT_LIN_LDS (3 * 2 * 8 * 1024)
+// Parts of 32 rows x 64 columns of a chunk's product, on the matrix cores in signed 8-bit limbs (36 products of limbs a ring product):
+// z_p = x_p (y_p + y_{p+1}) + x_{p+1} y_p.  A wavefront owns 16 columns; the rows' limbs go through LDS, [component][16 rows][limb][lane][16 bytes], the columns' stay in registers.
+template <int JOB>
+__device__ __forceinline__ void lin_tile(const LinArgs &a, u32 lb, u32 r0, u32 c0, unsigned char *s_a)
+{
+    const u32 lane = threadIdx.x & 63, lr = lane & 15, kq = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const u32 bhl = lb / a.nch, nb = a.nbh * a.nch;
+    const LinChunk ck = lin_chunk(a, bhl, a.ch0 + lb % a.nch);
+    const u32 len = ck.len, dk = a.dk, dv = a.dv, M = JOB == LIN_KV ? dk : len, N = JOB == LIN_SCORES ? len : dv;
+    if (r0 >= M || c0 >= N) return;
+    const u32 *D = a.D + ck.h * (GT_LIN_CHUNK + 1);
+    const u32 nstep = JOB == LIN_KV ? 1 : (dk + 63) / 64 + (JOB == LIN_OUT ? 1 : 0), first = c0 + 16 * wave, col = first + lr;
+    const bool cols = first < N && (JOB != LIN_SCORES || first <= r0 + 31);
+    const u64 hq = ck.t0 * a.ldq + (u64)ck.h * dk, hk = ck.t0 * a.ldk + (u64)ck.h * dk, hv = ck.t0 * a.ldv + (u64)ck.h * dv;
+    // a lane's 16 words of a row of the left factor, or a column of the right one, from term 64 step + 16 kq on; zero where there are none
+    auto left = [&](int j, u32 row, u32 step, u64 (&x)[16]) {
+        const bool tokens = JOB == LIN_KV || (JOB == LIN_OUT && step == 0);
+        const u32 k0 = 16 * kq + (JOB == LIN_KV ? 0 : 64 * (JOB == LIN_OUT ? (step ? step - 1 : 0) : step)), K = tokens ? len : dk;
+        const u32 r = row < M ? row : M - 1;
+        const u64 *q = comp_of(a.q, j) + hq, *k = comp_of(a.k, j) + hk, *P = a.P + ((u64)j * nb + lb) * GT_LIN_TRI;
+        const u32 scale = JOB == LIN_OUT ? (step ? D[r + 1] : 1u << GT_LIN_DECAY) : 1u;
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+            const u32 t = k0 + i, at = t < K ? t : K - 1;
+            bool in = t < K && row < M;
+            u64 v;
+            if (JOB == LIN_SCORES) v = q[r * a.ldq + at];
+            else if (JOB == LIN_KV) v = k[at * a.ldk + r] * D[len - 1 - at];
+            else if (step == 0) { in = in && t <= r; v = P[r * (r + 1) / 2 + (t <= r ? t : r)] * scale; }
+            else v = q[r * a.ldq + at] * scale;
+            x[i] = in ? v : 0;
+        }
+    };
+    auto right = [&](int j, u32 step, u64 (&y)[16]) {
+        const bool tokens = JOB == LIN_KV || (JOB == LIN_OUT && step == 0);
+        const u32 k0 = 16 * kq + (JOB == LIN_KV ? 0 : 64 * (JOB == LIN_OUT ? (step ? step - 1 : 0) : step)), K = tokens ? len : dk;
+        const u32 c = col < N ? col : N - 1;
+        const u64 *k = comp_of(a.k, j) + hk, *v = comp_of(a.v, j) + hv, *S = a.S + ((u64)j * nb + lb) * a.pk;
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+            const u32 t = k0 + i, at = t < K ? t : K - 1;
+            const u64 w = JOB == LIN_SCORES ? k[c * a.ldk + at] : tokens ? v[at * a.ldv + c] : S[(u64)at * dv + c];
+            y[i] = t < K && col < N ? w : 0;
+        }
+    };
+    u64 z[3][2][4];
+#pragma unroll
+    for (int p = 0; p < 3; p++)
+#pragma unroll
+        for (int i = 0; i < 8; i++) z[p][i >> 2][i & 3] = 0;
+    for (u32 step = 0; step < nstep; step++) {
+        __syncthreads();
+        for (u32 q = wave; q < 6; q += 4) {
+            const u32 j = q % 3, rt = q / 3;
+            u64 x[16];
+            v4i L[8];
+            left((int)j, r0 + rt * 16 + lr, step, x);
+            lin_limbs(x, L);
+#pragma unroll
+            for (int sl = 0; sl < 8; sl++) *(v4i *)(s_a + ((j * 2 + rt) * 8 + sl) * 1024 + lane * 16) = L[sl];
+        }
+        __syncthreads();
+        if (!cols) continue;
+#pragma unroll
+        for (int p = 0; p < 3; p++) {
+            const int pn = p == 2 ? 0 : p + 1;
+            v4i acc[2][8];
+#pragma unroll
+            for (int i = 0; i < 16; i++) acc[i >> 3][i & 7] = v4i{ 0, 0, 0, 0 };
+            u64 y[16], yn[16];
+            right(p, step, y); right(pn, step, yn);
+#pragma unroll
+            for (int i = 0; i < 16; i++) yn[i] += y[i];
+#pragma unroll
+            for (int w = 0; w < 2; w++) {
+                v4i B[8];
+                lin_limbs(w ? y : yn, B);
+                const unsigned char *A0 = s_a + (w ? pn : p) * 16384 + lane * 16;
+#pragma unroll
+                for (int rt = 0; rt < 2; rt++)
+#pragma unroll
+                    for (int sl = 0; sl < 8; sl++) {
+                        const v4i A = *(const v4i *)(A0 + (rt * 8 + sl) * 1024);
+#pragma unroll
+                        for (int t = 0; t < 8 - sl; t++) acc[rt][sl + t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(A, B[t], acc[rt][sl + t], 0, 0, 0);
+                    }
+            }
+#pragma unroll
+            for (int rt = 0; rt < 2; rt++)
+#pragma unroll
+                for (int v = 0; v < 4; v++)
+#pragma unroll
+                    for (int u = 0; u < 8; u++) z[p][rt][v] += (u64)(long long)acc[rt][u][v] << (8 * u);
+        }
+    }
+    if (!cols) return;
+#pragma unroll
+    for (int rt = 0; rt < 2; rt++)
+#pragma unroll
+        for (int v = 0; v < 4; v++) {
+            const u32 row = r0 + rt * 16 + 4 * kq + v;
+            if (row >= M || col >= N || (JOB == LIN_SCORES && col > row)) continue;
+            const u64 factor = JOB == LIN_SCORES ? D[row - col] : 1;
+#pragma unroll
+            for (int p = 0; p < 3; p++) {
+                const u64 at = (u64)p * nb + lb;
+                if (JOB == LIN_SCORES) a.Zs[at * GT_LIN_TRI + row * (row + 1) / 2 + col] = z[p][rt][v] * factor;
+                else if (JOB == LIN_KV) a.Zk[at * a.pk + (u64)row * dv + col] = z[p][rt][v];
+                else a.Zo[(at * GT_LIN_CHUNK + row) * a.dv8 + col] = z[p][rt][v];
+            }
+        }
+}
+// a chunk's workgroups: two of its scores, then its products k^T v
+__global__ __launch_bounds__(256) void k_lin_parts(LinArgs a)
+{
+    __shared__ __align__(16) unsigned char s_a[GT_LIN_LDS];
+    const u32 ct = (a.dv + 63) / 64, per = 2 + (a.dk + 31) / 32 * ct, lb = blockIdx.x / per, t = blockIdx.x % per;
+    if (t < 2) lin_tile<LIN_SCORES>(a, lb, 32 * t, 0, s_a);
+    else lin_tile<LIN_KV>(a, lb, (t - 2) / ct * 32, (t - 2) % ct * 64, s_a);
+}
+__global__ __launch_bounds__(256) void k_lin_out(LinArgs a)
+{
+    __shared__ __align__(16) unsigned char s_a[GT_LIN_LDS];
+    const u32 ct = (a.dv + 63) / 64, per = 2 * ct, lb = blockIdx.x / per, t = blockIdx.x % per;
+    lin_tile<LIN_OUT>(a, lb, t / ct * 32, t % ct * 64, s_a);
+}
+
+// Workgroups below `tiles`: 40 elements of a head's state, all chunks of the pass; the others: 40 scores of a chunk.
+__global__ __launch_bounds__(64) void k_lin_states(LinArgs a)
+{
+    __shared__ uint4 s_msg[GT_LANES];
+    __shared__ u64 s_mat[28 * GT_FP_ROW];
+    __shared__ u64 s_cnt[6];
+    WWire W; W.init(s_msg, s_cnt);
+    const u32 s = a.f + GT_LIN_DECAY, t = W.t < 20 ? W.t : 19, nb = a.nbh * a.nch;
+    FinPair<2> T; T.keys = a.c.keys; T.mat = s_mat; T.f = s;
+    const int p = W.p;
+    const bool mine = W.real && W.t < 20;
+    const u32 el[2] = { t, t + 20 };
+    bool act[2];
+    u64 z[2];
+    Sh none[2];
+    if (blockIdx.x >= a.tiles) {
+        const u32 b = blockIdx.x - a.tiles, bhl = b / a.each, tile = b % a.each, chl = tile / (GT_LIN_TRI / GT_FP_EL), i0 = tile % (GT_LIN_TRI / GT_FP_EL) * GT_FP_EL;
+        const LinChunk ck = lin_chunk(a, bhl, a.ch0 + chl);
+        const u32 n = ck.len * (ck.len + 1) / 2;
+        const u64 at = ((u64)p * nb + bhl * a.nch + chl) * GT_LIN_TRI + i0;
+        Sh y[2];
+#pragma unroll
+        for (int q = 0; q < 2; q++) { act[q] = W.t < 20 && i0 + el[q] < n; z[q] = act[q] ? a.Zs[at + el[q]] : 0; }
+        T.deal(W, a.c.op, ((u64)ck.bh * a.nc + a.ch0 + chl) * GT_LIN_TRI + i0);
+        finish_two<false>(W, T, s, z, el, (u32)act[0] + (u32)act[1], y, none);
+#pragma unroll
+        for (int q = 0; q < 2; q++) if (mine && act[q]) a.P[at + el[q]] = y[q].o;
+        W.flush(a.c.wire);
+        return;
+    }
+    const u32 dkv = a.dk * a.dv, per = (dkv + GT_FP_EL - 1) / GT_FP_EL, bhl = blockIdx.x / per, i0 = blockIdx.x % per * GT_FP_EL;
+    const u64 bh = a.bh0 + bhl;
+    const u32 *D = a.D + (u32)(bh % a.H) * (GT_LIN_CHUNK + 1);
+    Sh y[2];
+    u64 next[2];
+#pragma unroll
+    for (int q = 0; q < 2; q++) {
+        act[q] = W.t < 20 && i0 + el[q] < dkv;
+        y[q] = act[q] && a.has_in ? ld(a.in, p, bh * dkv + i0 + el[q]) : Sh{ 0, 0 };
+        next[q] = act[q] ? a.Zk[((u64)p * nb + bhl * a.nch) * a.pk + i0 + el[q]] : 0;
+    }
+    for (u32 chl = 0; chl < a.nch; chl++) {
+        const LinChunk ck = lin_chunk(a, bhl, a.ch0 + chl);
+        const u64 at = ((u64)p * nb + bhl * a.nch + chl) * a.pk + i0;
+#pragma unroll
+        for (int q = 0; q < 2; q++) {
+            z[q] = ((y[q].o * D[ck.len]) << a.f) + next[q];
+            if (mine && act[q]) a.S[at + el[q]] = y[q].o;
+            if (chl + 1 < a.nch) next[q] = act[q] ? a.Zk[at + a.pk + el[q]] : 0;
+        }
+        T.deal(W, a.c.op + 1, (bh * a.nc + a.ch0 + chl) * a.pk + i0);
+        finish_two<false>(W, T, s, z, el, (u32)act[0] + (u32)act[1], y, none);
+    }
+#pragma unroll
+    for (int q = 0; q < 2; q++) if (mine && act[q]) st(a.out, p, bh * dkv + i0 + el[q], y[q]);
+    W.flush(a.c.wire);
+}
+
+__global__ __launch_bounds__(64) void k_lin_finish(LinArgs a)
+{
+    __shared__ uint4 s_msg[GT_LANES];
+    __shared__ u64 s_mat[28 * GT_FP_ROW];
+    __shared__ u64 s_cnt[6];
+    WWire W; W.init(s_msg, s_cnt);
+    const u32 s = a.f + GT_LIN_DECAY, t = W.t < 20 ? W.t : 19, nb = a.nbh * a.nch, full = (GT_LIN_CHUNK * a.dv8 + GT_FP_EL - 1) / GT_FP_EL;
+    const u32 bhl = blockIdx.x / a.each, tile = blockIdx.x % a.each, chl = tile / full, i0 = tile % full * GT_FP_EL;
+    const LinChunk ck = lin_chunk(a, bhl, a.ch0 + chl);
+    FinPair<2> T; T.keys = a.c.keys; T.mat = s_mat; T.f = s;
+    const int p = W.p;
+    const u32 el[2] = { t, t + 20 };
+    const u64 b = (u64)bhl * a.nch + chl, from = ((u64)p * nb + b) * GT_LIN_CHUNK * a.dv8;
+    bool act[2];
+    u64 z[2], to[2];
+    Sh y[2], none[2];
+#pragma unroll
+    for (int q = 0; q < 2; q++) {
+        const u32 i = i0 + el[q], row = i / a.dv8, col = i % a.dv8;
+        act[q] = W.t < 20 && row < ck.len && col < a.dv;
+        z[q] = act[q] ? a.Zo[from + i] : 0;
+        to[q] = (ck.t0 + row) * ((u64)a.H * a.dv) + (u64)ck.h * a.dv + col;
+    }
+    T.deal(W, a.c.op + 2, ((u64)ck.bh * a.nc + a.ch0 + chl) * GT_LIN_CHUNK * a.dv8 + i0);
+    finish_two<false>(W, T, s, z, el, (u32)act[0] + (u32)act[1], y, none);
+#pragma unroll
+    for (int q = 0; q < 2; q++) if (W.real && act[q]) st(a.o, p, to[q], y[q]);
+    W.flush(a.c.wire);
+}
+
+// Powers of the heads' decays, 12 fraction bits, rounded from 46: D[n] = round(E[n] / 2^34), E[0] = 2^46, E[n + 1] = round(E[n] w / 2^12).
+struct DecayArgs { u32 w[256]; u32 *D; u32 heads; };
+__global__ __launch_bounds__(256) void k_lin_decays(DecayArgs a)
+{
+    const u32 h = threadIdx.x;
+    if (h >= a.heads) return;
+    u64 E = 1ull << 46;
+    for (u32 n = 0; n <= GT_LIN_CHUNK; n++) {
+        a.D[h * (GT_LIN_CHUNK + 1) + n] = (u32)((E + (1ull << 33)) >> 34);
+        E = (E * a.w[h] + (1u << (GT_LIN_DECAY - 1))) >> GT_LIN_DECAY;
+    }
+}

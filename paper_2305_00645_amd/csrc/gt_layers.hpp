@@ -486,6 +486,67 @@ __device__ __forceinline__ void less_pair(WWire &W, const u64 (&c)[2], const Sh 
     W.nresh += nresh * live2;
 }
 
+// Completion of two elements a lane, el[0] and el[1] of the tile: z the party's parts, material dealt for the operation; na: how many of them exist.
+template <bool RELU, class TileT>
+__device__ __forceinline__ void finish_two(WWire &W, const TileT &T, u32 f, const u64 (&z)[2], const u32 (&el)[2], u32 na, Sh (&y)[2], Sh (&gate)[2])
+{
+    const int p = W.p;
+    const u64 off = RELU ? 1ull << (f + 31) : 1ull << 62;
+    const Sh one = pub(p, 1);
+    u64 m[2], c[2];
+#pragma unroll
+    for (int q = 0; q < 2; q++) m[q] = z[q] + T.za(W, 0, el[q]) + T.mat[p * GT_FP_ROW + el[q]];
+    wave_sync();
+    W.buf[W.m] = make_uint4((u32)m[0], (u32)(m[0] >> 32), (u32)m[1], (u32)(m[1] >> 32));
+    wave_sync();
+    {
+        const uint4 x = W.buf[W.nx], v = W.buf[W.pv];
+        c[0] = m[0] + ((u64)x.x | ((u64)x.y << 32)) + ((u64)v.x | ((u64)v.y << 32)) + ((1ull << (f - 1)) + off);
+        c[1] = m[1] + ((u64)x.z | ((u64)x.w << 32)) + ((u64)v.z | ((u64)v.w << 32)) + ((1ull << (f - 1)) + off);
+        W.nopen += 64u * na; W.nresh += 64u * na;
+    }
+    const Sh rho[2] = { T.pair(W, 3, el[0]), T.pair(W, 3, el[1]) }, pr[2] = { T.pair(W, 19, el[0]), T.pair(W, 19, el[1]) };
+    const u64 A[2] = { T.zb(W, 1, el[0]), T.zb(W, 1, el[1]) }, cw[2] = { c[0] << (32 - f), c[1] << (32 - f) };
+    u32 lo[2], ln[2], ao[2], an[2];
+    less_pair<RELU ? 2 : 1>(W, cw, rho, pr, A, na, lo, ln, ao, an);
+    u32 fo[1] = { 0 }, fr[1], fn = 0;
+#pragma unroll
+    for (int q = 0; q < 2; q++) {
+        const u32 bits = (u32)T.mat[9 * GT_FP_ROW + el[q]];
+        u32 o = (lo[q] ^ (bits >> p)) & 1, n = (ln[q] ^ (bits >> W.pn)) & 1;
+        if (RELU) {
+            const u32 ct = (u32)(c[q] >> (f + 31)) & 1;
+            const u32 so = (u32)(rho[q].o >> 63) ^ ao[q] ^ (p == 0 ? ct : 0), sn = (u32)(rho[q].n >> 63) ^ an[q] ^ (p == 2 ? ct : 0);
+            o |= ((so ^ (bits >> (3 + p))) & 1) << 1;
+            n |= ((sn ^ (bits >> (3 + W.pn))) & 1) << 1;
+        }
+        fo[0] |= o << (2 * q); fn |= n << (2 * q);
+    }
+    W.pass<1>(fo, fr, W.pv);
+    W.nopen += (RELU ? 2u : 1u) * na;
+    const u32 ff = fo[0] ^ fn ^ fr[0];
+#pragma unroll
+    for (int q = 0; q < 2; q++) {
+        const Sh d = T.pair(W, 6, el[q]), b = (ff >> (2 * q)) & 1 ? one - d : d;
+        y[q] = pub(p, (c[q] >> f) - (off >> f)) - T.pair(W, 10, el[q]) - b;
+        const Sh top = T.pair(W, 13, el[q]);
+        const u64 wrap = 0 - (u64)!(c[q] >> 63);
+        y[q].o += top.o & wrap; y[q].n += top.n & wrap;
+        if (RELU) {
+            const Sh d2 = T.pair(W, 16, el[q]);
+            gate[q] = (ff >> (2 * q)) & 2 ? one - d2 : d2;
+            m[q] = prod3(gate[q], y[q]) + T.za(W, 2, el[q]);
+        }
+    }
+    if (RELU) {
+        u64 rcv[2];
+        W.reshare64<2>(m, rcv);
+        W.nresh += 64u * na;
+#pragma unroll
+        for (int q = 0; q < 2; q++) y[q] = Sh{ m[q], rcv[q] };
+    }
+}
+
 // One or two completions in a launch: workgroups below na are the first one's.
 struct FinSet { FinArgs f[2]; u32 na; };
 template <int SRC, bool RELU>
@@ -503,8 +564,6 @@ __global__ __launch_bounds__(64) void k_finish_pair(FinSet set)
     const int p = W.p;
     const u32 f = a.f, t = W.t < 20 ? W.t : 19;
     const bool mine = W.real && W.t < 20, narrow = a.first + a.n <= 0xffffffffu;
-    const u64 off = RELU ? 1ull << (f + 31) : 1ull << 62;
-    const Sh one = pub(p, 1);
     // the party's planes, chosen once
     u64 *const yo = own_of(a.y, p), *const yn = nxt_of(a.y, p), *const go = own_of(a.gate, p), *const gn = nxt_of(a.gate, p);
     const u64 *const ro = own_of(a.res, p), *const rn = nxt_of(a.res, p), *const bo = own_of(a.bias, p);
@@ -550,59 +609,8 @@ __global__ __launch_bounds__(64) void k_finish_pair(FinSet set)
 #pragma unroll
                 for (int q = 0; q < 2; q++) res[q] = Sh{ ro[e[q]], rn[e[q]] };
             T.deal(W, a.c.op, e0);
-            u64 m[2], c[2];
-            {
-#pragma unroll
-                for (int q = 0; q < 2; q++) m[q] = z[q] + T.za(W, 0, el[q]) + T.mat[p * GT_FP_ROW + el[q]];
-                wave_sync();
-                s_msg[W.m] = make_uint4((u32)m[0], (u32)(m[0] >> 32), (u32)m[1], (u32)(m[1] >> 32));
-                wave_sync();
-                const uint4 x = s_msg[W.nx], y = s_msg[W.pv];
-                c[0] = m[0] + ((u64)x.x | ((u64)x.y << 32)) + ((u64)y.x | ((u64)y.y << 32)) + ((1ull << (f - 1)) + off);
-                c[1] = m[1] + ((u64)x.z | ((u64)x.w << 32)) + ((u64)y.z | ((u64)y.w << 32)) + ((1ull << (f - 1)) + off);
-                W.nopen += 64u * na; W.nresh += 64u * na;
-            }
-            const Sh rho[2] = { T.pair(W, 3, el[0]), T.pair(W, 3, el[1]) }, pr[2] = { T.pair(W, 19, el[0]), T.pair(W, 19, el[1]) };
-            const u64 A[2] = { T.zb(W, 1, el[0]), T.zb(W, 1, el[1]) }, cw[2] = { c[0] << (32 - f), c[1] << (32 - f) };
-            u32 lo[2], ln[2], ao[2], an[2];
-            less_pair<RELU ? 2 : 1>(W, cw, rho, pr, A, na, lo, ln, ao, an);
-            u32 fo[1] = { 0 }, fr[1], fn = 0;
-#pragma unroll
-            for (int q = 0; q < 2; q++) {
-                const u32 bits = (u32)T.mat[9 * GT_FP_ROW + el[q]];
-                u32 o = (lo[q] ^ (bits >> p)) & 1, n = (ln[q] ^ (bits >> W.pn)) & 1;
-                if (RELU) {
-                    const u32 ct = (u32)(c[q] >> (f + 31)) & 1;
-                    const u32 so = (u32)(rho[q].o >> 63) ^ ao[q] ^ (p == 0 ? ct : 0), sn = (u32)(rho[q].n >> 63) ^ an[q] ^ (p == 2 ? ct : 0);
-                    o |= ((so ^ (bits >> (3 + p))) & 1) << 1;
-                    n |= ((sn ^ (bits >> (3 + W.pn))) & 1) << 1;
-                }
-                fo[0] |= o << (2 * q); fn |= n << (2 * q);
-            }
-            W.pass<1>(fo, fr, W.pv);
-            W.nopen += (RELU ? 2u : 1u) * na;
-            const u32 ff = fo[0] ^ fn ^ fr[0];
             Sh y[2], gate[2];
-#pragma unroll
-            for (int q = 0; q < 2; q++) {
-                const Sh d = T.pair(W, 6, el[q]), b = (ff >> (2 * q)) & 1 ? one - d : d;
-                y[q] = pub(p, (c[q] >> f) - (off >> f)) - T.pair(W, 10, el[q]) - b;
-                const Sh top = T.pair(W, 13, el[q]);
-                const u64 wrap = 0 - (u64)!(c[q] >> 63);
-                y[q].o += top.o & wrap; y[q].n += top.n & wrap;
-                if (RELU) {
-                    const Sh d2 = T.pair(W, 16, el[q]);
-                    gate[q] = (ff >> (2 * q)) & 2 ? one - d2 : d2;
-                    m[q] = prod3(gate[q], y[q]) + T.za(W, 2, el[q]);
-                }
-            }
-            if (RELU) {
-                u64 rcv[2];
-                W.reshare64<2>(m, rcv);
-                W.nresh += 64u * na;
-#pragma unroll
-                for (int q = 0; q < 2; q++) y[q] = Sh{ m[q], rcv[q] };
-            }
+            finish_two<RELU>(W, T, f, z, el, na, y, gate);
             if (a.has_res)
 #pragma unroll
                 for (int q = 0; q < 2; q++) y[q] = y[q] + res[q];
@@ -1148,14 +1156,14 @@ __global__ __launch_bounds__(256, WM == 4 ? 2 : WM == 2 ? 3 : 4) void k_rns_mm(R
     }
 }
 
-// Components (own planes) of a rows x cols matrix into the tiles of weights, rows from row0 on; padding stays at zero.  A thread takes a pair of rows, whose words
+// Components (own planes) of a rows x cols matrix into the tiles of weights, rows from row0 and columns from col0 on; padding stays at zero.  A thread takes a pair of rows, whose words
 // are adjacent there, so that 16 columns are 256 bytes on end (1024 x 4096: 30 us; a word at a time 188).
-struct PutArgs { P6 src; u64 *dst; u64 row0, rows, cols; u32 nst; };
+struct PutArgs { P6 src; u64 *dst; u64 row0, rows, col0, cols; u32 nst; };
 __global__ __launch_bounds__(256) void k_put(PutArgs a)
 {
     const u64 first = a.row0 / 2, n = ((a.row0 + a.rows + 1) / 2 - first) * a.cols;
     for (u64 e = (u64)blockIdx.x * blockDim.x + threadIdx.x; e < n; e += (u64)gridDim.x * blockDim.x) {
-        const u64 pair = e / a.cols, c = e - pair * a.cols, k = 2 * (first + pair), to = wtile_at(k, c, a.nst);
+        const u64 pair = e / a.cols, c = e - pair * a.cols, k = 2 * (first + pair), to = wtile_at(k, a.col0 + c, a.nst);
         const bool low = k >= a.row0, high = k + 1 < a.row0 + a.rows;
         const u64 from = (k - a.row0) * a.cols + c;                   // (wraps where the pair's first row is the one before; not read then)
 #pragma unroll
@@ -1170,7 +1178,7 @@ __global__ __launch_bounds__(256) void k_put(PutArgs a)
 }
 
 // Column sums of a shared matrix (local): a workgroup per 16 columns and component, 64 rows at a time.  Bound: reading the matrix (2048 x 1024, 50 MB).
-struct ColsumArgs { P6 x, out; u64 rows; u32 cols; };
+struct ColsumArgs { P6 x, out; u64 rows, ld; u32 cols; };
 __global__ __launch_bounds__(1024) void k_colsum(ColsumArgs a)
 {
     __shared__ u64 s_sum[64][17];
@@ -1180,7 +1188,7 @@ __global__ __launch_bounds__(1024) void k_colsum(ColsumArgs a)
     u64 s = 0;
     if (col < a.cols) {
 #pragma unroll 8
-        for (u64 r = g; r < a.rows; r += 64) s += x[r * a.cols + col];
+        for (u64 r = g; r < a.rows; r += 64) s += x[r * a.ld + col];
     }
     s_sum[g][c] = s;
     __syncthreads();

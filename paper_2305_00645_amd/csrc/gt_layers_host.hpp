@@ -15,12 +15,13 @@ static int wmat_alloc(WMat &w, u64 K, u64 N, hipStream_t st)
     HIPCHK(hipMemsetAsync(w.base, 0, words * 8, st));
     return GT_OK;
 }
-static int wmat_put(gt_ctx *c, const WMat &w, const gt_shares *src, u64 row0, u64 rows)
+static int wmat_put(gt_ctx *c, const WMat &w, const gt_shares *src, u64 row0, u64 rows, u64 col0, u64 cols)
 {
     PutArgs a{};
-    a.src = to_p6(src); a.dst = w.base; a.row0 = row0; a.rows = rows; a.cols = w.N; a.nst = w.nst;
-    return launch(c, GT_KC_LOCAL, k_put, g1(((row0 + rows + 1) / 2 - row0 / 2) * w.N), B256, a);
+    a.src = to_p6(src); a.dst = w.base; a.row0 = row0; a.rows = rows; a.col0 = col0; a.cols = cols; a.nst = w.nst;
+    return launch(c, GT_KC_LOCAL, k_put, g1(((row0 + rows + 1) / 2 - row0 / 2) * cols), B256, a);
 }
+static int wmat_put(gt_ctx *c, const WMat &w, const gt_shares *src, u64 row0, u64 rows) { return wmat_put(c, w, src, row0, rows, 0, w.N); }
 static MatView wmat(const WMat &w, u32 kind)
 { MatView v{}; for (int j = 0; j < 3; j++) v.c[j] = w.base + (u64)j * GT_WTILE; v.kind = kind; v.nst = w.nst; return v; }
 static MatView view(P6 a, u64 ld, u32 kind) { MatView v{}; for (int j = 0; j < 3; j++) v.c[j] = a.o[j]; v.ld = ld; v.kind = kind; return v; }
@@ -33,15 +34,15 @@ struct gt_moe {
     DSh br, s, o, S, Q, g, xe, h, hg, he;
 };
 
-static void acct_finish(gt_ctx *c, u64 n, bool relu)
+static void acct_finished(gt_ctx *c, u64 n, bool relu)
 {
     wire_add(c, +1, n, 64); wire_add(c, -1, n, 64);
     for (int v = 1; v <= 4; v++) wire_add(c, -1, n, (relu ? 64u : 32u) >> v);
     if (relu) wire_add(c, -1, n, 1);
     wire_add(c, +1, n, relu ? 2 : 1);
     if (relu) wire_add(c, -1, n, 64);
-    c->acc.rounds += relu ? 8 : 6;
 }
+static void acct_finish(gt_ctx *c, u64 n, bool relu) { acct_finished(c, n, relu); c->acc.rounds += relu ? 8 : 6; }
 
 struct FinOut { P6 y{}, gate{}, res{}, bias{}; bool has_res = false, has_gate = false, has_bias = false; };
 static dim3 gF(u64 n) { return dim3((unsigned)std::min<u64>((n + GT_FIN_EL - 1) / GT_FIN_EL, 1u << 16)); }
@@ -183,14 +184,17 @@ static int rmm_launch(gt_ctx *c, u32 wm, const RmmSet &m, u32 blocks)
     return wm == 4 ? launch(c, GT_KC_DENSE, k_rns_mm<4, 2>, dim3(blocks), B256, m) : wm == 2 ? launch(c, GT_KC_DENSE, k_rns_mm<2, 2>, dim3(blocks), B256, m)
            : launch(c, GT_KC_DENSE, k_rns_mm<1, 1>, dim3(blocks), B256, m);
 }
-// rows and columns in blocks, the long axis in chunks of RNS_TERMS (see rns_plan); its workspace is there
-static int run_taken(gt_ctx *c, const RnsJob &all)
+// rows and columns in blocks, the long axis in chunks of RNS_TERMS (see rns_plan); its workspace is there.  done(r0, rows, whole, R, plane, nchunk) completes the product's
+// rows from r0 on: from residues R of all chunks (none of a product without terms, whatever R is), or unless whole from the parts' words.
+template <class Done>
+static int run_products(gt_ctx *c, const RnsJob &all, Done done)
 {
     const RnsPlan &plan = all.plan;
     for (u64 r0 = 0; r0 < all.M; r0 += plan.rows) {
         const u64 rows = std::min<u64>(all.M - r0, plan.rows), n = rows * all.N;
-        FinSet f{};
-        f.f[0] = all.f;
+        const unsigned char *R = nullptr;
+        u64 plane = 0;
+        u32 nchunk = 0;
         for (u64 c0 = 0; c0 < all.N; c0 += plan.cols) {
             RnsJob j = all.part(c, r0, rows, c0, std::min<u64>(all.N - c0, plan.cols));
             j.at = c->res;
@@ -208,17 +212,26 @@ static int run_taken(gt_ctx *c, const RnsJob &all)
                 a.R = j.at + j.abytes + j.bbytes; a.Z = c->dacc; a.plane = j.plane; a.n = rows * j.N; a.parts = n; a.ld = all.N; a.c0 = c0; a.cols = j.N; a.nchunk = ch % plan.keep + 1;
                 GTCHK(launch(c, GT_KC_DENSE, k_join, dim3((unsigned)((a.n + 2047) / 2048), 3), B256, a));
             }
-            if (plan.whole) f.na = fin_residues(c, f.f[0], j.at + j.abytes + j.bbytes, r0 * all.N, n, j.plane, j.nchunk);
+            if (plan.whole) { R = j.at + j.abytes + j.bbytes; plane = j.plane; nchunk = j.nchunk; }
         }
-        if (plan.whole) {
-            GTCHK(all.relu ? launch(c, GT_KC_FINISH, k_finish_pair<FIN_RES, true>, dim3(f.na), B64, f) : launch(c, GT_KC_FINISH, k_finish_pair<FIN_RES, false>, dim3(f.na), B64, f));
-            continue;
+        GTCHK(done(r0, rows, plan.whole, R, plane, nchunk));
+    }
+    return GT_OK;
+}
+static int run_taken(gt_ctx *c, const RnsJob &all)
+{
+    return run_products(c, all, [&](u64 r0, u64 rows, bool whole, const unsigned char *R, u64 plane, u32 nchunk) {
+        const u64 n = rows * all.N;
+        FinSet f{};
+        f.f[0] = all.f;
+        if (whole) {
+            f.na = fin_residues(c, f.f[0], R, r0 * all.N, n, plane, nchunk);
+            return all.relu ? launch(c, GT_KC_FINISH, k_finish_pair<FIN_RES, true>, dim3(f.na), B64, f) : launch(c, GT_KC_FINISH, k_finish_pair<FIN_RES, false>, dim3(f.na), B64, f);
         }
         f.f[0].Z = c->dacc; f.f[0].first = r0 * all.N; f.f[0].n = n;
         f.na = (u32)((n + GT_FP_EL - 1) / GT_FP_EL);
-        GTCHK(all.relu ? launch(c, GT_KC_FINISH, k_finish_pair<FIN_PARTS, true>, dim3(f.na), B64, f) : launch(c, GT_KC_FINISH, k_finish_pair<FIN_PARTS, false>, dim3(f.na), B64, f));
-    }
-    return GT_OK;
+        return all.relu ? launch(c, GT_KC_FINISH, k_finish_pair<FIN_PARTS, true>, dim3(f.na), B64, f) : launch(c, GT_KC_FINISH, k_finish_pair<FIN_PARTS, false>, dim3(f.na), B64, f);
+    });
 }
 static int run_job(gt_ctx *c, RnsJob j)
 {
@@ -394,7 +407,7 @@ extern "C" int gt_dense_backward(gt_ctx *c, const gt_dense *l, const gt_shares *
     if (both) GTCHK(run_jobs(c, jx, jw));
     else if (dW) GTCHK(run_job(c, jw));
     if (db) {
-        ColsumArgs a{}; a.x = dz; a.out = to_p6(db); a.rows = rows; a.cols = l->dout;
+        ColsumArgs a{}; a.x = dz; a.out = to_p6(db); a.rows = rows; a.cols = l->dout; a.ld = l->dout;
         GTCHK(launch(c, GT_KC_LOCAL, k_colsum, dim3((l->dout + 15) / 16, 3), dim3(1024), a));
     }
     return T.finish(GT_OK);

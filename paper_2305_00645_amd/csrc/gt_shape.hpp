@@ -327,6 +327,27 @@ static inline FinShape fin_shape(u64 simds, u64 n)
     s.waves = (u32)(tiles - (u64)s.nbig * (s.per - 1));
     return s;
 }
+// Completion of a gated layer's residues (k_gated): as fin_shape, with at most two tiles a wavefront (their words of both projections are 20 lanes' joins).
+static inline FinShape gated_shape(u64 simds, u64 n)
+{
+    const u64 tiles = (n + 39) / 40, slots = 3 * simds;
+    FinShape s = { tiles >= slots ? 2u : 1u, 0, 0 };
+    if (s.per > 1) s.nbig = (u32)((tiles - slots / 2) / s.per);
+    s.waves = (u32)(tiles - (u64)s.nbig * (s.per - 1));
+    return s;
+}
+// What linear attention does at a time: heads of sequences (nbh of them) and chunks of 64 tokens (nc), so that its workspace (2 GB, with GT_FLAG_SMALL_WORKSPACE
+// 64 MB) does not grow with the prompt.
+struct LinPass { u64 nbh, nch; };
+static inline LinPass lin_pass(u64 nbh, u64 nc, u64 dk, u64 dv, u64 limit)
+{
+    const u64 each = 24 * (2 * 2080 + 2 * ((dk * dv + 7) / 8 * 8) + 64 * ((dv + 7) / 8 * 8)), bytes = std::max<u64>(16 * limit, (u64)1 << 26);
+    const u64 most = std::max<u64>(1, bytes / each);
+    LinPass p;
+    p.nbh = std::min(nbh, most);
+    p.nch = std::min(nc, std::max<u64>(1, most / std::max<u64>(1, p.nbh)));
+    return p;
+}
 // completion of parts: by two elements a lane (k_finish_pair) or by one (k_finish)?  64 terms with ReLU, the whole layer, us: 32768 elements 16.5, 15.4, 65536 18, 18,
 // 98304 20, 21, 393216 46, 51
 static inline bool fin_pairs(u64 simds, u64 n) { return n >= 80 * simds; }

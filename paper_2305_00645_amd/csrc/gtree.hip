@@ -6,6 +6,7 @@
 #include "gt_infer.hpp"
 #include "gt_partmm.hpp"
 #include "gt_layers.hpp"
+#include "gt_block.hpp"
 #include <algorithm>
 #include <cstdio>
 #include <cstring>
@@ -1337,3 +1338,4 @@ extern "C" int gt_infer_forest(gt_ctx *c, const gt_forest *f, const gt_shares *I
 }
 
 #include "gt_layers_host.hpp"
+#include "gt_block_host.hpp"

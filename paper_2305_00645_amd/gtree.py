@@ -122,6 +122,14 @@ def load():
         "gt_moe_create": (i, [vp, S, S, S, S, S, S, u32, u32, u32, u32, u32, C.POINTER(vp)]),
         "gt_moe_destroy": (i, [vp]),
         "gt_moe_forward": (i, [vp, vp, S, sz, S, S]),
+        "gt_gated_create": (i, [vp, S, S, S, S, u32, u32, C.POINTER(vp)]),
+        "gt_gated_set": (i, [vp, vp, S, S, S, S]),
+        "gt_gated_destroy": (i, [vp]),
+        "gt_gated_forward": (i, [vp, vp, S, sz, i, S, S, S, S]),
+        "gt_gated_backward": (i, [vp, vp, S, S, S, S, S, sz, S, S, S, S, S]),
+        "gt_linattn_create": (i, [vp, C.POINTER(u32), u32, u32, u32, C.POINTER(vp)]),
+        "gt_linattn_destroy": (i, [vp]),
+        "gt_linattn_forward": (i, [vp, vp, S, S, S, sz, sz, sz, S, S, S]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -151,9 +159,10 @@ class Shares:
         self.n = int(n)
         self.t = t if t is not None else torch.zeros((3, 2, max(self.n, 1)), dtype=torch.int64, device=device)
 
-    def c_struct(self):
-        a, b = self.t.data_ptr(), self.t.stride(1) * 8
-        return _Shares.from_buffer_copy(_SHARES_WORDS(a, a + b, a + 2 * b, a + 3 * b, a + 4 * b, a + 5 * b, self.n))
+    def c_struct(self, first=0):
+        """The words from `first` on."""
+        a, b = self.t.data_ptr() + 8 * first, self.t.stride(1) * 8
+        return _Shares.from_buffer_copy(_SHARES_WORDS(a, a + b, a + 2 * b, a + 3 * b, a + 4 * b, a + 5 * b, self.n - first))
 
     def planes(self):
         """numpy uint64 array (3, 2, n)."""
@@ -420,6 +429,57 @@ class GTree:
         _chk(self.L.gt_moe_forward(self.ctx, moe.h, _ref(x), rows, _ref(residual), _ref(y)), "gt_moe_forward")
         return y
 
+    def gated_create(self, Wg, Wu, din, ff, bg=None, bu=None):
+        h = C.c_void_p()
+        _chk(self.L.gt_gated_create(self.ctx, _ref(Wg), _ref(bg), _ref(Wu), _ref(bu), din, ff, C.byref(h)), "gt_gated_create")
+        return Gated(self, h, din, ff)
+
+    def gated_set(self, layer, Wg, Wu, bg=None, bu=None):
+        """New weights in place, as after a training step."""
+        _chk(self.L.gt_gated_set(self.ctx, layer.h, _ref(Wg), _ref(bg), _ref(Wu), _ref(bu)), "gt_gated_set")
+
+    def gated_forward(self, layer, x, rows, relu=True, keep=False):
+        """h, or (h, kept) with keep: (g, u, gate) for gated_backward, gate None without ReLU."""
+        n = rows * layer.ff
+        h = self._out(n)
+        kept = (self._out(n), self._out(n), self._out(n) if relu else None) if keep else (None, None, None)
+        _chk(self.L.gt_gated_forward(self.ctx, layer.h, _ref(x), rows, int(bool(relu)), _ref(h), *[_ref(t) for t in kept]), "gt_gated_forward")
+        return (h, kept) if keep else h
+
+    def gated_backward(self, layer, x, dh, rows, kept, want=(True, True, True)):
+        """(dx, dWg, dWu, dbg, dbu); want: dx, both dW, both db; None in the place of the others."""
+        w = (want[0], want[1], want[1], want[2], want[2])
+        nw = layer.din * layer.ff
+        out = [self._out(n) if on else None for n, on in zip((rows * layer.din, nw, nw, layer.ff, layer.ff), w)]
+        _chk(self.L.gt_gated_backward(self.ctx, layer.h, _ref(x), *[_ref(t) for t in kept], _ref(dh), rows, *[_ref(t) for t in out]), "gt_gated_backward")
+        return tuple(out)
+
+    def linattn_create(self, decay, dk, dv):
+        """decay: a number in [0, 1] for each head, rounded to 12 fraction bits."""
+        w = [int(round(float(d) * 4096)) for d in decay]
+        if any(x < 0 for x in w):
+            raise GtError(GT_EINVAL, "gt_linattn_create")
+        h = C.c_void_p()
+        _chk(self.L.gt_linattn_create(self.ctx, (C.c_uint32 * max(len(w), 1))(*w), len(w), dk, dv, C.byref(h)), "gt_linattn_create")
+        return LinearAttention(self, h, len(w), dk, dv)
+
+    def linattn_forward(self, layer, q, k=None, v=None, seqs=1, tokens=1, state=None, inplace=False):
+        """(o, state) of `tokens` tokens of `seqs` sequences.  q alone: rows [q | k | v], as one projection gives them.  state None: zeros; inplace: the
+        given state is overwritten and returned."""
+        wk, wv = layer.heads * layer.dk, layer.heads * layer.dv
+        rows, ld = seqs * tokens, 0
+        if k is None:
+            ld = 2 * wk + wv
+            if q.n < rows * ld:
+                raise GtError(GT_EINVAL, "gt_linattn_forward")
+            parts = [q.c_struct(off) if q.n else q.c_struct() for off in (0, wk, 2 * wk)]
+        else:
+            parts = [t.c_struct() for t in (q, k, v)]
+        out = state if inplace else self._out(seqs * layer.heads * layer.dk * layer.dv)
+        o = self._out(rows * wv)
+        _chk(self.L.gt_linattn_forward(self.ctx, layer.h, *[C.byref(t) for t in parts], ld, seqs, tokens, _ref(state), _ref(out), _ref(o)), "gt_linattn_forward")
+        return o, out
+
 
 class Dense:
     def __init__(self, g, h, din, dout):
@@ -444,6 +504,38 @@ class Moe:
     def close(self):
         if self.h:
             self.g.L.gt_moe_destroy(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Gated:
+    def __init__(self, g, h, din, ff):
+        self.g, self.h, self.din, self.ff = g, h, din, ff
+
+    def close(self):
+        if self.h:
+            self.g.L.gt_gated_destroy(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class LinearAttention:
+    def __init__(self, g, h, heads, dk, dv):
+        self.g, self.h, self.heads, self.dk, self.dv = g, h, heads, dk, dv
+
+    def close(self):
+        if self.h:
+            self.g.L.gt_linattn_destroy(self.h)
             self.h = None
 
     def __del__(self):
