@@ -210,134 +210,183 @@ __device__ __forceinline__ void lin_limbs(const u64 (&x)[16], v4i (&B)[8])
 #pragma unroll
     for (int i = 0; i < 8; i++) B[i] = v4i{ (int)(u32)y[i], (int)(u32)(y[i] >> 32), (int)(u32)z[i], (int)(u32)(z[i] >> 32) };
 }
+// The word that sums of products of limbs stand for, sum of D_u 256^u: bytes with carries below 2^32, above it modulo 2^32.
+__device__ __forceinline__ u64 lin_word(const v4i (&acc)[8], int v)
+{
+    const int t0 = acc[0][v], t1 = acc[1][v] + (t0 >> 8), t2 = acc[2][v] + (t1 >> 8), t3 = acc[3][v] + (t2 >> 8), t4 = acc[4][v] + (t3 >> 8);
+    const u32 high = (u32)t4 + ((u32)acc[5][v] << 8) + ((u32)acc[6][v] << 16) + ((u32)acc[7][v] << 24);
+    return (u64)low_bytes((u32)t0, (u32)t1, (u32)t2, (u32)t3) | ((u64)high << 32);
+}
 
 enum { LIN_SCORES = 0, LIN_KV = 1, LIN_OUT = 2 };
-#define GT_LIN_LDS (3 * 2 * 8 * 1024)
-// Parts of 32 rows x 64 columns of a chunk's product, on the matrix cores in signed 8-bit limbs (36 products of limbs a ring product):
-// z_p = x_p (y_p + y_{p+1}) + x_{p+1} y_p.  A wavefront owns 16 columns; the rows' limbs go through LDS, [component][16 rows][limb][lane][16 bytes], the columns' stay in registers.
+#define GT_LIN_LDS (2 * 2 * 8 * 1024 + 64 * 4)
+// A party's parts of 32 rows x 64 columns of a chunk's product, on the matrix cores in signed 8-bit limbs (36 products of limbs a ring product):
+// z_p = x_p (y_p + y_{p+1}) + x_{p+1} y_p, terms in steps of 64.  A wavefront owns 16 columns, whose words stay in registers and become limbs there; the rows' limbs go through LDS,
+// [component p or p + 1][16 rows][limb][lane][16 bytes], a block of them made by each wavefront.  A block of 16 rows (or columns) whose terms are adjacent in memory is loaded
+// a row at a time, whole lines, and turned in LDS, where its limbs go afterwards.
+// Bound: the vector units that make limbs and words around the matrix instructions (144 of them a wavefront and step).
 template <int JOB>
-__device__ __forceinline__ void lin_tile(const LinArgs &a, u32 lb, u32 r0, u32 c0, unsigned char *s_a)
+__device__ __forceinline__ void lin_tile(const LinArgs &a, u32 lb, u32 p, u32 r0, u32 c0, unsigned char *s_a)
 {
-    const u32 lane = threadIdx.x & 63, lr = lane & 15, kq = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const u32 wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    u32 lane = threadIdx.x & 63, lr = lane & 15, kq = lane >> 4;
     const u32 bhl = lb / a.nch, nb = a.nbh * a.nch;
     const LinChunk ck = lin_chunk(a, bhl, a.ch0 + lb % a.nch);
     const u32 len = ck.len, dk = a.dk, dv = a.dv, M = JOB == LIN_KV ? dk : len, N = JOB == LIN_SCORES ? len : dv;
     if (r0 >= M || c0 >= N) return;
     const u32 *D = a.D + ck.h * (GT_LIN_CHUNK + 1);
-    const u32 nstep = JOB == LIN_KV ? 1 : (dk + 63) / 64 + (JOB == LIN_OUT ? 1 : 0), first = c0 + 16 * wave, col = first + lr;
+    const u32 nstep = JOB == LIN_KV ? 1 : (dk + 63) / 64 + (JOB == LIN_OUT ? 1 : 0), pn = p == 2 ? 0 : p + 1, first = c0 + 16 * wave;
     const bool cols = first < N && (JOB != LIN_SCORES || first <= r0 + 31);
     const u64 hq = ck.t0 * a.ldq + (u64)ck.h * dk, hk = ck.t0 * a.ldk + (u64)ck.h * dk, hv = ck.t0 * a.ldv + (u64)ck.h * dv;
-    // a lane's 16 words of a row of the left factor, or a column of the right one, from term 64 step + 16 kq on; zero where there are none
-    auto left = [&](int j, u32 row, u32 step, u64 (&x)[16]) {
-        const bool tokens = JOB == LIN_KV || (JOB == LIN_OUT && step == 0);
-        const u32 k0 = 16 * kq + (JOB == LIN_KV ? 0 : 64 * (JOB == LIN_OUT ? (step ? step - 1 : 0) : step)), K = tokens ? len : dk;
-        const u32 r = row < M ? row : M - 1;
-        const u64 *q = comp_of(a.q, j) + hq, *k = comp_of(a.k, j) + hk, *P = a.P + ((u64)j * nb + lb) * GT_LIN_TRI;
-        const u32 scale = JOB == LIN_OUT ? (step ? D[r + 1] : 1u << GT_LIN_DECAY) : 1u;
+    u32 *s_D = (u32 *)(s_a + 2 * 2 * 8 * 1024);                           // powers by the tokens between, or of a token's age (the loop's first barrier is theirs)
+    if (JOB != LIN_OUT && threadIdx.x < 64) s_D[threadIdx.x] = threadIdx.x < len ? D[JOB == LIN_KV ? len - 1 - threadIdx.x : threadIdx.x] : 0;
+    // 16 rows of 64 words through 8 KB of LDS: row i's word at(i) by lane, blocks of two words exchanged by row against bank conflicts
+    auto turn = [&](unsigned char *to, u64 (&x)[16]) {
+        wave_sync();
 #pragma unroll
-        for (int i = 0; i < 16; i++) {
-            const u32 t = k0 + i, at = t < K ? t : K - 1;
-            bool in = t < K && row < M;
-            u64 v;
-            if (JOB == LIN_SCORES) v = q[r * a.ldq + at];
-            else if (JOB == LIN_KV) v = k[at * a.ldk + r] * D[len - 1 - at];
-            else if (step == 0) { in = in && t <= r; v = P[r * (r + 1) / 2 + (t <= r ? t : r)] * scale; }
-            else v = q[r * a.ldq + at] * scale;
-            x[i] = in ? v : 0;
+        for (int i = 0; i < 16; i++) *(u64 *)(to + i * 512 + (((lane >> 1) ^ i) * 16) + (lane & 1) * 8) = x[i];
+        wave_sync();
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const ulonglong2 v = *(const ulonglong2 *)(to + lr * 512 + (((kq * 8 + i) ^ lr) * 16));
+            x[2 * i] = v.x; x[2 * i + 1] = v.y;
         }
+        wave_sync();
     };
-    auto right = [&](int j, u32 step, u64 (&y)[16]) {
-        const bool tokens = JOB == LIN_KV || (JOB == LIN_OUT && step == 0);
-        const u32 k0 = 16 * kq + (JOB == LIN_KV ? 0 : 64 * (JOB == LIN_OUT ? (step ? step - 1 : 0) : step)), K = tokens ? len : dk;
-        const u32 c = col < N ? col : N - 1;
-        const u64 *k = comp_of(a.k, j) + hk, *v = comp_of(a.v, j) + hv, *S = a.S + ((u64)j * nb + lb) * a.pk;
+    // terms k0 + lane of rows first .. first + 15 of a matrix of `rows` rows of K terms (zero where there are none)
+    auto by_rows = [&](const u64 *m, u64 ld, u32 f, u32 rows, u32 k0, u32 K, u64 (&x)[16]) {
+        const u32 k = k0 + lane, at = (k < K ? k : K - 1) * 8;
 #pragma unroll
-        for (int i = 0; i < 16; i++) {
-            const u32 t = k0 + i, at = t < K ? t : K - 1;
-            const u64 w = JOB == LIN_SCORES ? k[c * a.ldk + at] : tokens ? v[at * a.ldv + c] : S[(u64)at * dv + c];
-            y[i] = t < K && col < N ? w : 0;
-        }
+        for (int i = 0; i < 16; i++) x[i] = ld_at<u64>(m + (u64)(f + i < rows ? f + i : rows - 1) * ld, at);
+#pragma unroll
+        for (int i = 0; i < 16; i++) x[i] = k < K && f + i < rows ? x[i] : 0;
     };
-    u64 z[3][2][4];
+    // terms k0 + 16 kq .. of column c (of `columns`) of a matrix whose rows are terms (a chunk's rows lie within 32-bit offsets)
+    auto by_terms = [&](const u64 *m, u32 ld, u32 c, u32 columns, u32 k0, u32 K, u64 (&x)[16]) {
+        const u32 k = k0 + 16 * kq, cc = c < columns ? c : columns - 1;
 #pragma unroll
-    for (int p = 0; p < 3; p++)
+        for (int i = 0; i < 16; i++) x[i] = ld_at<u64>(m, ((k + i < K ? k + i : K - 1) * ld + cc) * 8);
 #pragma unroll
-        for (int i = 0; i < 8; i++) z[p][i >> 2][i & 3] = 0;
+        for (int i = 0; i < 16; i++) x[i] = k + i < K && c < columns ? x[i] : 0;
+    };
+    v4i acc[2][8];
+#pragma unroll
+    for (int i = 0; i < 16; i++) acc[i >> 3][i & 7] = v4i{ 0, 0, 0, 0 };
+#pragma unroll 1
     for (u32 step = 0; step < nstep; step++) {
+        const bool scores = JOB == LIN_OUT && step == 0;                  // the step of the scores and values
+        const u32 k0 = JOB == LIN_KV || scores ? 0 : 64 * (JOB == LIN_OUT ? step - 1 : step);
+        // (a step works its addresses out again: kept over the steps they take the registers of the sums)
+        asm volatile("" : "+v"(lane));
+        lr = lane & 15; kq = lane >> 4;
+        const u32 col = first + lr;
+        u64 y[16], t[16];
         __syncthreads();
-        for (u32 q = wave; q < 6; q += 4) {
-            const u32 j = q % 3, rt = q / 3;
-            u64 x[16];
-            v4i L[8];
-            left((int)j, r0 + rt * 16 + lr, step, x);
-            lin_limbs(x, L);
-#pragma unroll
-            for (int sl = 0; sl < 8; sl++) *(v4i *)(s_a + ((j * 2 + rt) * 8 + sl) * 1024 + lane * 16) = L[sl];
-        }
-        __syncthreads();
-        if (!cols) continue;
-#pragma unroll
-        for (int p = 0; p < 3; p++) {
-            const int pn = p == 2 ? 0 : p + 1;
-            v4i acc[2][8];
-#pragma unroll
-            for (int i = 0; i < 16; i++) acc[i >> 3][i & 7] = v4i{ 0, 0, 0, 0 };
-            u64 y[16], yn[16];
-            right(p, step, y); right(pn, step, yn);
-#pragma unroll
-            for (int i = 0; i < 16; i++) yn[i] += y[i];
+        auto right = [&]() {
+            if (!cols) return;
 #pragma unroll
             for (int w = 0; w < 2; w++) {
-                v4i B[8];
-                lin_limbs(w ? y : yn, B);
-                const unsigned char *A0 = s_a + (w ? pn : p) * 16384 + lane * 16;
-#pragma unroll
-                for (int rt = 0; rt < 2; rt++)
-#pragma unroll
-                    for (int sl = 0; sl < 8; sl++) {
-                        const v4i A = *(const v4i *)(A0 + (rt * 8 + sl) * 1024);
-#pragma unroll
-                        for (int t = 0; t < 8 - sl; t++) acc[rt][sl + t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(A, B[t], acc[rt][sl + t], 0, 0, 0);
-                    }
+                const int j = (int)(w ? pn : p);
+                if (JOB == LIN_SCORES) {
+                    by_rows(comp_of(a.k, j) + hk, a.ldk, first, N, k0, dk, w ? t : y);
+                    turn(s_a + wave * 8192, w ? t : y);
+                } else {
+                    const bool tokens = JOB == LIN_KV || scores;
+                    by_terms(tokens ? comp_of(a.v, j) + hv : a.S + ((u64)j * nb + lb) * a.pk, tokens ? (u32)a.ldv : dv, col, N, k0, tokens ? len : dk, w ? t : y);
+                }
             }
+#pragma unroll
+            for (int i = 0; i < 16; i++) t[i] += y[i];
+        };
+        if (JOB == LIN_SCORES) right();                                // (through the LDS that the rows' limbs go to)
+        {
+            const u32 j = wave >> 1 ? pn : p, row = r0 + (wave & 1) * 16;
+            unsigned char *to = s_a + wave * 8192;
+            u64 x[16];
+            v4i L[8];
+            if (JOB == LIN_KV) {
+                by_terms(comp_of(a.k, (int)j) + hk, (u32)a.ldk, row + lr, M, 0, len, x);
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    const uint4 w = *(const uint4 *)(s_D + 16 * kq + i);
+                    x[i] *= w.x; x[i + 1] *= w.y; x[i + 2] *= w.z; x[i + 3] *= w.w;
+                }
+            } else if (scores) {
+                const u64 *P = a.P + ((u64)j * nb + lb) * GT_LIN_TRI;
+#pragma unroll
+                for (int i = 0; i < 16; i++) {
+                    const u32 r = row + i < M ? row + i : M - 1;
+                    x[i] = ld_at<u64>(P + r * (r + 1) / 2, (lane <= r ? lane : r) * 8);
+                }
+#pragma unroll
+                for (int i = 0; i < 16; i++) x[i] = row + i < M && lane <= row + i ? x[i] << GT_LIN_DECAY : 0;
+                turn(to, x);
+            } else {
+                by_rows(comp_of(a.q, (int)j) + hq, a.ldq, row, M, k0, dk, x);
+                if (JOB == LIN_OUT)
+#pragma unroll
+                    for (int i = 0; i < 16; i++) x[i] *= D[row + i < M ? row + i + 1 : M];
+                turn(to, x);
+            }
+            lin_limbs(x, L);
+#pragma unroll
+            for (int sl = 0; sl < 8; sl++) *(v4i *)(to + sl * 1024 + lane * 16) = L[sl];
+        }
+        if (JOB != LIN_SCORES) right();
+        __syncthreads();
+        if (!cols) continue;
+        v4i B[8];
+#pragma unroll
+        for (int w = 0; w < 2; w++) {
+            lin_limbs(w ? y : t, B);
+            const unsigned char *A0 = s_a + w * 16384 + lane * 16;
 #pragma unroll
             for (int rt = 0; rt < 2; rt++)
 #pragma unroll
-                for (int v = 0; v < 4; v++)
+                for (int sl = 0; sl < 8; sl++) {
+                    const v4i A = *(const v4i *)(A0 + (rt * 8 + sl) * 1024);
 #pragma unroll
-                    for (int u = 0; u < 8; u++) z[p][rt][v] += (u64)(long long)acc[rt][u][v] << (8 * u);
+                    for (int u = 0; u < 8 - sl; u++) acc[rt][sl + u] = __builtin_amdgcn_mfma_i32_16x16x64_i8(A, B[u], acc[rt][sl + u], 0, 0, 0);
+                }
         }
     }
     if (!cols) return;
+    // (at most 320 terms of two products: |sums| < 2^27)
+    const u32 col = first + lr, ld = JOB == LIN_KV ? dv : a.dv8;
+    const u64 at = (u64)p * nb + lb;
+    u64 *const Z = JOB == LIN_SCORES ? a.Zs + at * GT_LIN_TRI : JOB == LIN_KV ? a.Zk + at * a.pk : a.Zo + at * GT_LIN_CHUNK * a.dv8;
 #pragma unroll
     for (int rt = 0; rt < 2; rt++)
 #pragma unroll
         for (int v = 0; v < 4; v++) {
             const u32 row = r0 + rt * 16 + 4 * kq + v;
-            if (row >= M || col >= N || (JOB == LIN_SCORES && col > row)) continue;
-            const u64 factor = JOB == LIN_SCORES ? D[row - col] : 1;
-#pragma unroll
-            for (int p = 0; p < 3; p++) {
-                const u64 at = (u64)p * nb + lb;
-                if (JOB == LIN_SCORES) a.Zs[at * GT_LIN_TRI + row * (row + 1) / 2 + col] = z[p][rt][v] * factor;
-                else if (JOB == LIN_KV) a.Zk[at * a.pk + (u64)row * dv + col] = z[p][rt][v];
-                else a.Zo[(at * GT_LIN_CHUNK + row) * a.dv8 + col] = z[p][rt][v];
-            }
+            u64 z = lin_word(acc[rt], v);
+            if (JOB == LIN_SCORES) z *= s_D[col <= row ? row - col : 0];
+            if (row < M && col < N && (JOB != LIN_SCORES || col <= row))
+                *(u64 *)((char *)Z + (JOB == LIN_SCORES ? row * (row + 1) / 2 + col : row * ld + col) * 8) = z;
         }
 }
-// a chunk's workgroups: two of its scores, then its products k^T v
-__global__ __launch_bounds__(256) void k_lin_parts(LinArgs a)
+// Workgroups go to the XCDs in turn: XCD x takes the x-th eighth of the work, so that a chunk's words are in one L2 (16 heads, 4096 tokens, 64 x 128: XXX).
+__device__ __forceinline__ u32 lin_block(u32 total)
 {
-    __shared__ __align__(16) unsigned char s_a[GT_LIN_LDS];
-    const u32 ct = (a.dv + 63) / 64, per = 2 + (a.dk + 31) / 32 * ct, lb = blockIdx.x / per, t = blockIdx.x % per;
-    if (t < 2) lin_tile<LIN_SCORES>(a, lb, 32 * t, 0, s_a);
-    else lin_tile<LIN_KV>(a, lb, (t - 2) / ct * 32, (t - 2) % ct * 64, s_a);
+    const u32 per = (total + 7) / 8, id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    return (blockIdx.x >> 3) < per && id < total ? id : ~0u;
 }
-__global__ __launch_bounds__(256) void k_lin_out(LinArgs a)
+// a chunk's workgroups, for each party: two of its scores, then its products k^T v
+__global__ __launch_bounds__(256, 3) void k_lin_parts(LinArgs a)
 {
     __shared__ __align__(16) unsigned char s_a[GT_LIN_LDS];
-    const u32 ct = (a.dv + 63) / 64, per = 2 * ct, lb = blockIdx.x / per, t = blockIdx.x % per;
-    lin_tile<LIN_OUT>(a, lb, t / ct * 32, t % ct * 64, s_a);
+    const u32 ct = (a.dv + 63) / 64, per = 3 * (2 + (a.dk + 31) / 32 * ct), id = lin_block(a.nbh * a.nch * per), lb = id / per, t = id % per / 3, p = id % 3;
+    if (id == ~0u) return;
+    if (t < 2) lin_tile<LIN_SCORES>(a, lb, p, 32 * t, 0, s_a);
+    else lin_tile<LIN_KV>(a, lb, p, (t - 2) / ct * 32, (t - 2) % ct * 64, s_a);
+}
+__global__ __launch_bounds__(256, 3) void k_lin_out(LinArgs a)
+{
+    __shared__ __align__(16) unsigned char s_a[GT_LIN_LDS];
+    const u32 ct = (a.dv + 63) / 64, per = 6 * ct, id = lin_block(a.nbh * a.nch * per), lb = id / per, t = id % per / 3, p = id % 3;
+    if (id == ~0u) return;
+    lin_tile<LIN_OUT>(a, lb, p, t / ct * 32, t % ct * 64, s_a);
 }
 
 // Workgroups below `tiles`: 40 elements of a head's state, all chunks of the pass; the others: 40 scores of a chunk.

@@ -211,11 +211,11 @@ extern "C" int gt_linattn_forward(gt_ctx *c, const gt_linattn *l, const gt_share
             const gt_shares *from = ch0 ? out : in;
             a.has_in = from != nullptr;
             if (from) a.in = to_p6(from);
-            GTCHK(launch(c, GT_KC_DENSE, k_lin_parts, dim3(nb * (2 + (l->dk + 31) / 32 * ct)), B256, a));
+            GTCHK(launch(c, GT_KC_DENSE, k_lin_parts, dim3((nb * 3 * (2 + (l->dk + 31) / 32 * ct) + 7) / 8 * 8), B256, a));
             a.tiles = a.nbh * (u32)((dkv + GT_FP_EL - 1) / GT_FP_EL);
             a.each = (a.nch - 1) * (GT_LIN_TRI / GT_FP_EL) + (last * (last + 1) / 2 + GT_FP_EL - 1) / GT_FP_EL;
             GTCHK(launch(c, GT_KC_FINISH, k_lin_states, dim3(a.tiles + a.nbh * a.each), B64, a));
-            GTCHK(launch(c, GT_KC_DENSE, k_lin_out, dim3(nb * 2 * ct), B256, a));
+            GTCHK(launch(c, GT_KC_DENSE, k_lin_out, dim3((nb * 6 * ct + 7) / 8 * 8), B256, a));
             a.each = (a.nch - 1) * per_o + (last * a.dv8 + GT_FP_EL - 1) / GT_FP_EL;
             GTCHK(launch(c, GT_KC_FINISH, k_lin_finish, dim3(a.nbh * a.each), B64, a));
         }
