@@ -185,7 +185,7 @@ struct LinArgs {
     u64 nc, bh0;                                  // chunks of a sequence
     u32 ch0, nch, nbh;
     u64 *Zs, *Zk, *Zo, *P, *S;                    // parts [3][b'][2080], [pk], [64 dv8]; scores [3][b'][2080], states before a chunk [3][b'][pk]
-    u32 tiles, each;                              // k_lin_states: workgroups of chains; k_lin_states, k_lin_finish: tiles of 40 of a head's chunks in the pass
+    u32 tiles, each, per;                         // k_lin_states: workgroups of chains; k_lin_states, k_lin_finish: tiles of 40 of a head's chunks in the pass; tiles of a wavefront
 };
 
 struct LinChunk { u64 t0; u32 bh, h, len; };     // first row of q, k, v; head; tokens
@@ -239,7 +239,7 @@ __device__ __forceinline__ void lin_tile(const LinArgs &a, u32 lb, u32 p, u32 r0
     const bool cols = first < N && (JOB != LIN_SCORES || first <= r0 + 31);
     const u64 hq = ck.t0 * a.ldq + (u64)ck.h * dk, hk = ck.t0 * a.ldk + (u64)ck.h * dk, hv = ck.t0 * a.ldv + (u64)ck.h * dv;
     u32 *s_D = (u32 *)(s_a + 2 * 2 * 8 * 1024);                           // powers by the tokens between, or of a token's age (the loop's first barrier is theirs)
-    if (JOB != LIN_OUT && threadIdx.x < 64) s_D[threadIdx.x] = threadIdx.x < len ? D[JOB == LIN_KV ? len - 1 - threadIdx.x : threadIdx.x] : 0;
+    if (threadIdx.x < 64) s_D[threadIdx.x] = threadIdx.x < len ? D[JOB == LIN_KV ? len - 1 - threadIdx.x : threadIdx.x + (JOB == LIN_OUT ? 1 : 0)] : 0;
     // 16 rows of 64 words through 8 KB of LDS: row i's word at(i) by lane, blocks of two words exchanged by row against bank conflicts
     auto turn = [&](unsigned char *to, u64 (&x)[16]) {
         wave_sync();
@@ -269,6 +269,7 @@ __device__ __forceinline__ void lin_tile(const LinArgs &a, u32 lb, u32 p, u32 r0
 #pragma unroll
         for (int i = 0; i < 16; i++) x[i] = k + i < K && c < columns ? x[i] : 0;
     };
+    u32 here = r0;
     v4i acc[2][8];
 #pragma unroll
     for (int i = 0; i < 16; i++) acc[i >> 3][i & 7] = v4i{ 0, 0, 0, 0 };
@@ -277,7 +278,7 @@ __device__ __forceinline__ void lin_tile(const LinArgs &a, u32 lb, u32 p, u32 r0
         const bool scores = JOB == LIN_OUT && step == 0;                  // the step of the scores and values
         const u32 k0 = JOB == LIN_KV || scores ? 0 : 64 * (JOB == LIN_OUT ? step - 1 : step);
         // (a step works its addresses out again: kept over the steps they take the registers of the sums)
-        asm volatile("" : "+v"(lane));
+        asm volatile("" : "+v"(lane), "+s"(here));
         lr = lane & 15; kq = lane >> 4;
         const u32 col = first + lr;
         u64 y[16], t[16];
@@ -300,7 +301,7 @@ __device__ __forceinline__ void lin_tile(const LinArgs &a, u32 lb, u32 p, u32 r0
         };
         if (JOB == LIN_SCORES) right();                                // (through the LDS that the rows' limbs go to)
         {
-            const u32 j = wave >> 1 ? pn : p, row = r0 + (wave & 1) * 16;
+            const u32 j = wave >> 1 ? pn : p, row = here + (wave & 1) * 16;
             unsigned char *to = s_a + wave * 8192;
             u64 x[16];
             v4i L[8];
@@ -319,14 +320,18 @@ __device__ __forceinline__ void lin_tile(const LinArgs &a, u32 lb, u32 p, u32 r0
                     x[i] = ld_at<u64>(P + r * (r + 1) / 2, (lane <= r ? lane : r) * 8);
                 }
 #pragma unroll
-                for (int i = 0; i < 16; i++) x[i] = row + i < M && lane <= row + i ? x[i] << GT_LIN_DECAY : 0;
+                for (int i = 0; i < 16; i++) x[i] = row + i < M && lane <= row + i ? x[i] : 0;
                 turn(to, x);
+#pragma unroll
+                for (int i = 0; i < 16; i++) x[i] <<= GT_LIN_DECAY;
             } else {
                 by_rows(comp_of(a.q, (int)j) + hq, a.ldq, row, M, k0, dk, x);
-                if (JOB == LIN_OUT)
-#pragma unroll
-                    for (int i = 0; i < 16; i++) x[i] *= D[row + i < M ? row + i + 1 : M];
                 turn(to, x);
+                if (JOB == LIN_OUT) {
+                    const u32 w = s_D[row + lr];
+#pragma unroll
+                    for (int i = 0; i < 16; i++) x[i] *= w;
+                }
             }
             lin_limbs(x, L);
 #pragma unroll
@@ -366,7 +371,7 @@ __device__ __forceinline__ void lin_tile(const LinArgs &a, u32 lb, u32 p, u32 r0
                 *(u64 *)((char *)Z + (JOB == LIN_SCORES ? row * (row + 1) / 2 + col : row * ld + col) * 8) = z;
         }
 }
-// Workgroups go to the XCDs in turn: XCD x takes the x-th eighth of the work, so that a chunk's words are in one L2 (16 heads, 4096 tokens, 64 x 128: XXX).
+// Workgroups go to the XCDs in turn: XCD x takes the x-th eighth of the work, so that a chunk's words are in one L2 (16 heads, 4096 tokens, 64 x 128: 467 -> 414 us).
 __device__ __forceinline__ u32 lin_block(u32 total)
 {
     const u32 per = (total + 7) / 8, id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
@@ -381,7 +386,7 @@ __global__ __launch_bounds__(256, 3) void k_lin_parts(LinArgs a)
     if (t < 2) lin_tile<LIN_SCORES>(a, lb, p, 32 * t, 0, s_a);
     else lin_tile<LIN_KV>(a, lb, p, (t - 2) / ct * 32, (t - 2) % ct * 64, s_a);
 }
-__global__ __launch_bounds__(256, 3) void k_lin_out(LinArgs a)
+__global__ __launch_bounds__(256, 2) void k_lin_out(LinArgs a)
 {
     __shared__ __align__(16) unsigned char s_a[GT_LIN_LDS];
     const u32 ct = (a.dv + 63) / 64, per = 6 * ct, id = lin_block(a.nbh * a.nch * per), lb = id / per, t = id % per / 3, p = id % 3;
@@ -389,46 +394,62 @@ __global__ __launch_bounds__(256, 3) void k_lin_out(LinArgs a)
     lin_tile<LIN_OUT>(a, lb, p, t / ct * 32, t % ct * 64, s_a);
 }
 
-// Workgroups below `tiles`: 40 elements of a head's state, all chunks of the pass; the others: 40 scores of a chunk.
+// Completion of tiles of 40, a wavefront's `per` tiles one after the other.
+struct LinTile {
+    WWire W;
+    FinPair<2> T;
+    u32 t, s, el[2];
+    bool mine;
+    __device__ __forceinline__ LinTile(const LinArgs &a, uint4 *msg, u64 *mat, u64 *cnt)
+    {
+        W.init(msg, cnt);
+        T.keys = a.c.keys; T.mat = mat; T.f = s = a.f + GT_LIN_DECAY;
+        t = W.t < 20 ? W.t : 19; el[0] = t; el[1] = t + 20;
+        mine = W.real && W.t < 20;
+    }
+    __device__ __forceinline__ void finish(u32 op, u64 e0, const u64 (&z)[2], u32 na, Sh (&y)[2])
+    {
+        Sh none[2];
+        T.deal(W, op, e0);
+        finish_two<false>(W, T, s, z, el, na, y, none);
+    }
+};
+#define GT_LIN_SHARED __shared__ uint4 s_msg[GT_LANES]; __shared__ u64 s_mat[28 * GT_FP_ROW]; __shared__ u64 s_cnt[6]; LinTile L(a, s_msg, s_mat, s_cnt);
+
+// Workgroups below `tiles`: 40 elements of a head's state, all chunks of the pass; the others: `per` tiles of 40 scores.
 __global__ __launch_bounds__(64) void k_lin_states(LinArgs a)
 {
-    __shared__ uint4 s_msg[GT_LANES];
-    __shared__ u64 s_mat[28 * GT_FP_ROW];
-    __shared__ u64 s_cnt[6];
-    WWire W; W.init(s_msg, s_cnt);
-    const u32 s = a.f + GT_LIN_DECAY, t = W.t < 20 ? W.t : 19, nb = a.nbh * a.nch;
-    FinPair<2> T; T.keys = a.c.keys; T.mat = s_mat; T.f = s;
-    const int p = W.p;
-    const bool mine = W.real && W.t < 20;
-    const u32 el[2] = { t, t + 20 };
+    GT_LIN_SHARED
+    const int p = L.W.p;
+    const u32 nb = a.nbh * a.nch, row = GT_LIN_TRI / GT_FP_EL;
     bool act[2];
     u64 z[2];
-    Sh none[2];
+    Sh y[2];
     if (blockIdx.x >= a.tiles) {
-        const u32 b = blockIdx.x - a.tiles, bhl = b / a.each, tile = b % a.each, chl = tile / (GT_LIN_TRI / GT_FP_EL), i0 = tile % (GT_LIN_TRI / GT_FP_EL) * GT_FP_EL;
-        const LinChunk ck = lin_chunk(a, bhl, a.ch0 + chl);
-        const u32 n = ck.len * (ck.len + 1) / 2;
-        const u64 at = ((u64)p * nb + bhl * a.nch + chl) * GT_LIN_TRI + i0;
-        Sh y[2];
+        for (u32 i = 0; i < a.per; i++) {
+            const u32 b = (blockIdx.x - a.tiles) * a.per + i, bhl = b / a.each, tile = b % a.each, chl = tile / row, i0 = tile % row * GT_FP_EL;
+            if (bhl >= a.nbh) break;
+            const LinChunk ck = lin_chunk(a, bhl, a.ch0 + chl);
+            const u32 n = ck.len * (ck.len + 1) / 2;
+            const u64 at = ((u64)p * nb + bhl * a.nch + chl) * GT_LIN_TRI + i0;
 #pragma unroll
-        for (int q = 0; q < 2; q++) { act[q] = W.t < 20 && i0 + el[q] < n; z[q] = act[q] ? a.Zs[at + el[q]] : 0; }
-        T.deal(W, a.c.op, ((u64)ck.bh * a.nc + a.ch0 + chl) * GT_LIN_TRI + i0);
-        finish_two<false>(W, T, s, z, el, (u32)act[0] + (u32)act[1], y, none);
+            for (int q = 0; q < 2; q++) { act[q] = L.W.t < 20 && i0 + L.el[q] < n; z[q] = act[q] ? a.Zs[at + L.el[q]] : 0; }
+            L.finish(a.c.op, ((u64)ck.bh * a.nc + a.ch0 + chl) * GT_LIN_TRI + i0, z, (u32)act[0] + (u32)act[1], y);
 #pragma unroll
-        for (int q = 0; q < 2; q++) if (mine && act[q]) a.P[at + el[q]] = y[q].o;
-        W.flush(a.c.wire);
+            for (int q = 0; q < 2; q++) if (L.mine && act[q]) a.P[at + L.el[q]] = y[q].o;
+        }
+        L.W.flush(a.c.wire);
         return;
     }
     const u32 dkv = a.dk * a.dv, per = (dkv + GT_FP_EL - 1) / GT_FP_EL, bhl = blockIdx.x / per, i0 = blockIdx.x % per * GT_FP_EL;
     const u64 bh = a.bh0 + bhl;
     const u32 *D = a.D + (u32)(bh % a.H) * (GT_LIN_CHUNK + 1);
-    Sh y[2];
     u64 next[2];
 #pragma unroll
     for (int q = 0; q < 2; q++) {
-        act[q] = W.t < 20 && i0 + el[q] < dkv;
-        y[q] = act[q] && a.has_in ? ld(a.in, p, bh * dkv + i0 + el[q]) : Sh{ 0, 0 };
-        next[q] = act[q] ? a.Zk[((u64)p * nb + bhl * a.nch) * a.pk + i0 + el[q]] : 0;
+        act[q] = L.W.t < 20 && i0 + L.el[q] < dkv;
+        y[q] = act[q] && a.has_in ? ld(a.in, p, bh * dkv + i0 + L.el[q]) : Sh{ 0, 0 };
+        next[q] = act[q] ? a.Zk[((u64)p * nb + bhl * a.nch) * a.pk + i0 + L.el[q]] : 0;
     }
     for (u32 chl = 0; chl < a.nch; chl++) {
         const LinChunk ck = lin_chunk(a, bhl, a.ch0 + chl);
@@ -436,45 +457,130 @@ __global__ __launch_bounds__(64) void k_lin_states(LinArgs a)
 #pragma unroll
         for (int q = 0; q < 2; q++) {
             z[q] = ((y[q].o * D[ck.len]) << a.f) + next[q];
-            if (mine && act[q]) a.S[at + el[q]] = y[q].o;
-            if (chl + 1 < a.nch) next[q] = act[q] ? a.Zk[at + a.pk + el[q]] : 0;
+            if (L.mine && act[q]) a.S[at + L.el[q]] = y[q].o;
+            if (chl + 1 < a.nch) next[q] = act[q] ? a.Zk[at + a.pk + L.el[q]] : 0;
         }
-        T.deal(W, a.c.op + 1, (bh * a.nc + a.ch0 + chl) * a.pk + i0);
-        finish_two<false>(W, T, s, z, el, (u32)act[0] + (u32)act[1], y, none);
+        L.finish(a.c.op + 1, (bh * a.nc + a.ch0 + chl) * a.pk + i0, z, (u32)act[0] + (u32)act[1], y);
     }
 #pragma unroll
-    for (int q = 0; q < 2; q++) if (mine && act[q]) st(a.out, p, bh * dkv + i0 + el[q], y[q]);
-    W.flush(a.c.wire);
+    for (int q = 0; q < 2; q++) if (L.mine && act[q]) st(a.out, p, bh * dkv + i0 + L.el[q], y[q]);
+    L.W.flush(a.c.wire);
 }
 
 __global__ __launch_bounds__(64) void k_lin_finish(LinArgs a)
 {
-    __shared__ uint4 s_msg[GT_LANES];
-    __shared__ u64 s_mat[28 * GT_FP_ROW];
-    __shared__ u64 s_cnt[6];
-    WWire W; W.init(s_msg, s_cnt);
-    const u32 s = a.f + GT_LIN_DECAY, t = W.t < 20 ? W.t : 19, nb = a.nbh * a.nch, full = (GT_LIN_CHUNK * a.dv8 + GT_FP_EL - 1) / GT_FP_EL;
-    const u32 bhl = blockIdx.x / a.each, tile = blockIdx.x % a.each, chl = tile / full, i0 = tile % full * GT_FP_EL;
-    const LinChunk ck = lin_chunk(a, bhl, a.ch0 + chl);
-    FinPair<2> T; T.keys = a.c.keys; T.mat = s_mat; T.f = s;
-    const int p = W.p;
-    const u32 el[2] = { t, t + 20 };
-    const u64 b = (u64)bhl * a.nch + chl, from = ((u64)p * nb + b) * GT_LIN_CHUNK * a.dv8;
-    bool act[2];
-    u64 z[2], to[2];
-    Sh y[2], none[2];
+    GT_LIN_SHARED
+    const int p = L.W.p;
+    const u32 nb = a.nbh * a.nch, full = (GT_LIN_CHUNK * a.dv8 + GT_FP_EL - 1) / GT_FP_EL;
+    for (u32 j = 0; j < a.per; j++) {
+        const u32 id = blockIdx.x * a.per + j, bhl = id / a.each, tile = id % a.each, chl = tile / full, i0 = tile % full * GT_FP_EL;
+        if (bhl >= a.nbh) break;
+        const LinChunk ck = lin_chunk(a, bhl, a.ch0 + chl);
+        const u64 from = ((u64)p * nb + bhl * a.nch + chl) * GT_LIN_CHUNK * a.dv8;
+        bool act[2];
+        u64 z[2], to[2];
+        Sh y[2];
 #pragma unroll
-    for (int q = 0; q < 2; q++) {
-        const u32 i = i0 + el[q], row = i / a.dv8, col = i % a.dv8;
-        act[q] = W.t < 20 && row < ck.len && col < a.dv;
-        z[q] = act[q] ? a.Zo[from + i] : 0;
-        to[q] = (ck.t0 + row) * ((u64)a.H * a.dv) + (u64)ck.h * a.dv + col;
+        for (int q = 0; q < 2; q++) {
+            const u32 i = i0 + L.el[q], row = i / a.dv8, col = i % a.dv8;
+            act[q] = L.W.t < 20 && row < ck.len && col < a.dv;
+            z[q] = act[q] ? a.Zo[from + i] : 0;
+            to[q] = (ck.t0 + row) * ((u64)a.H * a.dv) + (u64)ck.h * a.dv + col;
+        }
+        L.finish(a.c.op + 2, ((u64)ck.bh * a.nc + a.ch0 + chl) * GT_LIN_CHUNK * a.dv8 + i0, z, (u32)act[0] + (u32)act[1], y);
+#pragma unroll
+        for (int q = 0; q < 2; q++) if (L.W.real && act[q]) st(a.o, p, to[q], y[q]);
     }
-    T.deal(W, a.c.op + 2, ((u64)ck.bh * a.nc + a.ch0 + chl) * GT_LIN_CHUNK * a.dv8 + i0);
-    finish_two<false>(W, T, s, z, el, (u32)act[0] + (u32)act[1], y, none);
+    L.W.flush(a.c.wire);
+}
+
+// A token of every sequence: its score, output and state in one launch, without a workspace.  Workgroups below nout: 40 outputs of a head, whose one score, q k, the first
+// wavefront works out (each such workgroup for itself) while the others make q S, a third of the state's rows each; the other workgroups: `per` tiles of 40 words of a
+// state for each wavefront.  Where the new states take the place of the old ones, two launches: outputs first.
+// Bound: many sequences: the completions' block function; few: the outputs' two chains of messages.
+__global__ __launch_bounds__(256, 4) void k_lin_token(LinArgs a, u32 nout)
+{
+    __shared__ uint4 s_msg[4][GT_LANES];
+    __shared__ u64 s_mat[4][28 * GT_FP_ROW], s_cnt[4][6];
+    const u32 wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    LinTile L(a, s_msg[wave], s_mat[wave], s_cnt[wave]);
+    const int p = L.W.p, pn = L.W.pn;
+    const u32 dk = a.dk, dv = a.dv, dkv = dk * dv;
+    const u64 *q0 = comp_of(a.q, p), *q1 = comp_of(a.q, pn), *k0 = comp_of(a.k, p), *k1 = comp_of(a.k, pn), *v0 = comp_of(a.v, p), *v1 = comp_of(a.v, pn);
+    bool act[2];
+    u64 z[2];
+    Sh y[2];
+    if (blockIdx.x < nout) {
+        const u32 ct = (a.dv8 + GT_FP_EL - 1) / GT_FP_EL, bh = blockIdx.x / ct, tile = blockIdx.x % ct, h = bh % a.H, seq = bh / a.H;
+        const u64 hq = seq * a.ldq + (u64)h * dk, hk = seq * a.ldk + (u64)h * dk, hv = seq * a.ldv + (u64)h * dv;
+        const u64 w = a.D[h * (GT_LIN_CHUNK + 1) + 1];
+        u32 col[2];
 #pragma unroll
-    for (int q = 0; q < 2; q++) if (W.real && act[q]) st(a.o, p, to[q], y[q]);
-    W.flush(a.c.wire);
+        for (int i = 0; i < 2; i++) {
+            const u32 c = tile * GT_FP_EL + L.el[i];
+            act[i] = L.W.t < 20 && c < dv;
+            col[i] = c < dv ? c : dv - 1;
+        }
+        if (wave) {
+            u64 acc[2] = { 0, 0 };
+            if (a.has_in) {
+                const u64 *s0 = own_of(a.in, p) + (u64)bh * dkv, *s1 = nxt_of(a.in, p) + (u64)bh * dkv;
+                const u32 each = (dk + 2) / 3, d0 = (wave - 1) * each, d1 = d0 + each < dk ? d0 + each : dk;
+#pragma unroll 8
+                for (u32 d = d0; d < d1; d++) {
+                    const Sh x = { q0[hq + d], q1[hq + d] };
+#pragma unroll
+                    for (int i = 0; i < 2; i++) acc[i] += prod3(x, Sh{ s0[d * dv + col[i]], s1[d * dv + col[i]] });
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 2; i++) if (L.mine) s_mat[wave][GT_FP_EL * p + L.el[i]] = acc[i];
+            __syncthreads();
+            return;
+        }
+        const Sh v[2] = { { v0[hv + col[0]], v1[hv + col[0]] }, { v0[hv + col[1]], v1[hv + col[1]] } };
+        u64 dot = 0;
+        if (L.mine) for (u32 d = L.t; d < dk; d += 20) dot += prod3(Sh{ q0[hq + d], q1[hq + d] }, Sh{ k0[hk + d], k1[hk + d] });
+        u64 *sum = (u64 *)s_msg[0];
+        wave_sync();
+        if (L.mine) sum[20 * p + L.t] = dot;
+        wave_sync();
+        z[0] = 0; z[1] = 0;
+#pragma unroll
+        for (int i = 0; i < 20; i++) z[0] += sum[20 * p + i];
+        z[0] <<= GT_LIN_DECAY;
+        L.finish(a.c.op, (u64)bh * GT_LIN_TRI, z, tile == 0 && L.W.t == 0 ? 1u : 0u, y);
+        const int from = (int)L.W.lane_of(0);
+        const Sh P = { (u64)__shfl((unsigned long long)y[0].o, from, GT_LANES), (u64)__shfl((unsigned long long)y[0].n, from, GT_LANES) };
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            const u32 e = GT_FP_EL * p + L.el[i];
+            z[i] = (prod3(P, v[i]) << GT_LIN_DECAY) + (s_mat[1][e] + s_mat[2][e] + s_mat[3][e]) * w;
+        }
+        L.finish(a.c.op + 2, (u64)bh * GT_LIN_CHUNK * a.dv8 + tile * GT_FP_EL, z, (u32)act[0] + (u32)act[1], y);
+#pragma unroll
+        for (int i = 0; i < 2; i++) if (L.mine && act[i]) st(a.o, p, (u64)bh * dv + col[i], y[i]);
+        L.W.flush(a.c.wire);
+        return;
+    }
+    const u32 tiles = (dkv + GT_FP_EL - 1) / GT_FP_EL;
+    for (u32 j = 0; j < a.per; j++) {
+        const u32 id = ((blockIdx.x - nout) * 4 + wave) * a.per + j, bh = id / tiles, i0 = id % tiles * GT_FP_EL, h = bh % a.H, seq = bh / a.H;
+        if (bh >= a.nbh) break;
+        const u64 hk = seq * a.ldk + (u64)h * dk, hv = seq * a.ldv + (u64)h * dv, w = a.D[h * (GT_LIN_CHUNK + 1) + 1], at = (u64)bh * dkv + i0;
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            const u32 e = i0 + L.el[i] < dkv ? i0 + L.el[i] : dkv - 1, d = e / dv, c = e - d * dv;
+            act[i] = L.W.t < 20 && i0 + L.el[i] < dkv;
+            z[i] = prod3(Sh{ k0[hk + d], k1[hk + d] }, Sh{ v0[hv + c], v1[hv + c] }) << GT_LIN_DECAY;
+            if (a.has_in) z[i] += (own_of(a.in, p)[(u64)bh * dkv + e] * w) << a.f;
+        }
+        L.finish(a.c.op + 1, (u64)bh * a.pk + i0, z, (u32)act[0] + (u32)act[1], y);
+#pragma unroll
+        for (int i = 0; i < 2; i++) if (L.mine && act[i]) st(a.out, p, at + L.el[i], y[i]);
+    }
+    L.W.flush(a.c.wire);
 }
 
 // Powers of the heads' decays, 12 fraction bits, rounded from 46: D[n] = round(E[n] / 2^34), E[0] = 2^46, E[n + 1] = round(E[n] w / 2^12).

@@ -190,7 +190,23 @@ extern "C" int gt_linattn_forward(gt_ctx *c, const gt_linattn *l, const gt_share
     a.out = to_p6(out); a.o = to_p6(o);
     a.D = l->D; a.ldq = a.ldk = ldk; a.ldv = ldv; a.T = tokens; a.H = l->heads; a.dk = l->dk; a.dv = l->dv; a.dv8 = (l->dv + 7) / 8 * 8;
     a.pk = (u32)((dkv + 7) / 8 * 8); a.f = c->tau; a.nc = (tokens + GT_LIN_CHUNK - 1) / GT_LIN_CHUNK;
-    const u64 nbh = seqs * l->heads, sizes[5] = { GT_LIN_TRI, a.pk, (u64)GT_LIN_CHUNK * a.dv8, GT_LIN_TRI, a.pk };
+    const u64 nbh = seqs * l->heads;
+    if (tokens == 1) {
+        const u64 nout = nbh * ((a.dv8 + GT_FP_EL - 1) / GT_FP_EL), tiles = nbh * ((dkv + GT_FP_EL - 1) / GT_FP_EL);
+        a.c = kc(c, c->op); c->op += 3;
+        a.nbh = (u32)nbh; a.per = tiles_of_wave(c->simds, tiles);
+        a.has_in = in != nullptr;
+        if (in) a.in = to_p6(in);
+        acct_finished(c, nbh, false); acct_finished(c, nS, false); acct_finished(c, wv * seqs, false);
+        c->acc.rounds += 12;
+        const u32 nstate = (u32)((tiles + 4 * a.per - 1) / (4 * a.per));
+        if (in && in->party[0].own == out->party[0].own) {
+            GTCHK(launch(c, GT_KC_FINISH, k_lin_token, dim3((unsigned)nout), B256, a, (u32)nout));
+            return T.finish(launch(c, GT_KC_FINISH, k_lin_token, dim3(nstate), B256, a, 0u));
+        }
+        return T.finish(launch(c, GT_KC_FINISH, k_lin_token, dim3((unsigned)nout + nstate), B256, a, (u32)nout));
+    }
+    const u64 sizes[5] = { GT_LIN_TRI, a.pk, (u64)GT_LIN_CHUNK * a.dv8, GT_LIN_TRI, a.pk };
     const LinPass pass = lin_pass(nbh, a.nc, l->dk, l->dv, c->rns_limit);
     Need need;
     for (u64 w : sizes) need.res += 24 * w * pass.nbh * pass.nch;
@@ -214,10 +230,12 @@ extern "C" int gt_linattn_forward(gt_ctx *c, const gt_linattn *l, const gt_share
             GTCHK(launch(c, GT_KC_DENSE, k_lin_parts, dim3((nb * 3 * (2 + (l->dk + 31) / 32 * ct) + 7) / 8 * 8), B256, a));
             a.tiles = a.nbh * (u32)((dkv + GT_FP_EL - 1) / GT_FP_EL);
             a.each = (a.nch - 1) * (GT_LIN_TRI / GT_FP_EL) + (last * (last + 1) / 2 + GT_FP_EL - 1) / GT_FP_EL;
-            GTCHK(launch(c, GT_KC_FINISH, k_lin_states, dim3(a.tiles + a.nbh * a.each), B64, a));
+            a.per = tiles_of_wave(c->simds, (u64)a.nbh * a.each);
+            GTCHK(launch(c, GT_KC_FINISH, k_lin_states, dim3(a.tiles + (a.nbh * a.each + a.per - 1) / a.per), B64, a));
             GTCHK(launch(c, GT_KC_DENSE, k_lin_out, dim3((nb * 6 * ct + 7) / 8 * 8), B256, a));
             a.each = (a.nch - 1) * per_o + (last * a.dv8 + GT_FP_EL - 1) / GT_FP_EL;
-            GTCHK(launch(c, GT_KC_FINISH, k_lin_finish, dim3(a.nbh * a.each), B64, a));
+            a.per = tiles_of_wave(c->simds, (u64)a.nbh * a.each);
+            GTCHK(launch(c, GT_KC_FINISH, k_lin_finish, dim3((a.nbh * a.each + a.per - 1) / a.per), B64, a));
         }
     return T.finish(GT_OK);
 }

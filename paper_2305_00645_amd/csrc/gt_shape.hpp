@@ -336,6 +336,13 @@ static inline FinShape gated_shape(u64 simds, u64 n)
     s.waves = (u32)(tiles - (u64)s.nbig * (s.per - 1));
     return s;
 }
+// Tiles of 40 that a wavefront of linear attention's completions takes one after the other: at most 16, so that the wavefronts are as few and whole rounds of the
+// four that a SIMD has at a time.
+static inline u32 tiles_of_wave(u64 simds, u64 tiles)
+{
+    const u64 slots = 4 * simds, rounds = std::max<u64>(1, (tiles + 16 * slots - 1) / (16 * slots));
+    return (u32)std::max<u64>(1, (tiles + rounds * slots - 1) / (rounds * slots));
+}
 // What linear attention does at a time: heads of sequences (nbh of them) and chunks of 64 tokens (nc), so that its workspace (2 GB, with GT_FLAG_SMALL_WORKSPACE
 // 64 MB) does not grow with the prompt.
 struct LinPass { u64 nbh, nch; };

@@ -326,13 +326,13 @@ def test_refused_under_capture(mods, seed):
     with torch.cuda.stream(st):
         g = gtree.GTree(seed, stream=st)
         layer, gl = g.linattn_create([0.5], 4, 4), g.gated_create(g.new(4 * 9), g.new(4 * 9), 4, 9)
-        q, S, y, h = g.new(12), g.new(16), g.new(4), g.new(9)
+        q, S, y, h = g.new(12), g.new(16), g.new(8), g.new(9)
         st.synchronize()
         graph, got = torch.cuda.CUDAGraph(), []
         with torch.cuda.graph(graph, stream=st):
             op = g.op_counter()
             r = gtree._ref
-            got.append(g.L.gt_linattn_forward(g.ctx, layer.h, r(q), r(q), r(q), 0, 1, 1, None, r(S), r(y)))
+            got.append(g.L.gt_linattn_forward(g.ctx, layer.h, r(q), r(q), r(q), 0, 1, 2, None, r(S), r(y)))
             got.append(g.L.gt_gated_forward(g.ctx, gl.h, r(q), 1, 1, r(h), None, None, None))
             got.append(g.L.gt_gated_backward(g.ctx, gl.h, None, r(h), r(h), r(h), r(h), 1, r(q), None, None, None, None))
             got.append(g.op_counter() - op)
