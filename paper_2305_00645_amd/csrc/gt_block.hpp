@@ -24,7 +24,7 @@ __device__ __forceinline__ GatedAt gated_at(u64 i, u32 ff8, bool narrow)
     return GatedAt{ row, (u32)(i - row * ff8) };
 }
 template <int SRC, bool RELU>
-__global__ __launch_bounds__(64) void k_gated(GatedArgs a)
+__global__ __launch_bounds__(64, 3) void k_gated(GatedArgs a)
 {
     constexpr int NS = RELU ? 3 : 2;
     __shared__ uint4 s_msg[GT_LANES];
