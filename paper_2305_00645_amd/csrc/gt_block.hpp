@@ -106,6 +106,50 @@ __global__ __launch_bounds__(64, 3) void k_gated(GatedArgs a)
     W.flush(a.c.wire);
 }
 
+// The same for few elements, 16 a workgroup, from parts: the first wavefront completes g, the second u beside it, whose material for h is there when both are: one chain of
+// messages after the other, but one PRF pass before them.
+template <bool RELU>
+__global__ __launch_bounds__(128) void k_gated_few(GatedArgs a)
+{
+    constexpr int NS = RELU ? 3 : 2;
+    __shared__ uint4 s_msg[2][GT_LANES];
+    __shared__ u64 s_mat[3][GT_FIN_WORDS(3)], s_cnt[2][6], s_g[6][GT_FIN_EL];
+    const u32 wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    FWire W; W.init(s_msg[wave], s_cnt[wave]);
+    const int p = W.p;
+    const u64 n = a.rows * a.ff8, ld = 2 * (u64)a.ffp, e0 = (u64)blockIdx.x * GT_FIN_EL, i = e0 + W.t;
+    GatedAt at = gated_at(i < n ? i : n - 1, a.ff8, n <= 0xffffffffu);
+    const bool act = i < n && at.col < a.ff;
+    if (at.col >= a.ff) at.col = a.ff - 1;
+    const u64 e = (a.first + at.row) * a.ff + at.col, id = a.first * a.ff8 + e0;
+    u64 *Z = a.Z + ((u64)p * a.rows + at.row) * ld + at.col + (wave ? a.ffp : 0);
+    u64 z = *Z;
+    if (act && W.real) *Z = 0;
+    if (a.has_bias) z += own_of(a.bias, p)[(wave ? a.ff : 0) + at.col] << a.f;
+    Sh y, s, h;
+    if (wave == 0) {
+        FinTile<NS> T; T.keys = a.c.keys; T.mat = s_mat[0]; T.f = a.f;
+        T.deal(a.c.op, id);
+        y = finish_el<RELU>(W, T, a.f, z, act, s);
+        if (W.real) { s_g[2 * p][W.t] = y.o; s_g[2 * p + 1][W.t] = y.n; }
+        if (act && W.real && a.keep) { st(a.g, p, e, y); if (RELU) st(a.s, p, e, s); }
+    } else {
+        FinTile<2> T; T.keys = a.c.keys; T.mat = s_mat[1]; T.f = a.f;
+        T.deal(a.c.op + 1, id);
+        y = finish_el<false>(W, T, a.f, z, act, s);
+        if (act && W.real && a.keep) st(a.u, p, e, y);
+        T.mat = s_mat[2];
+        T.deal(a.c.op + 2, id);
+    }
+    __syncthreads();
+    if (wave) {
+        FinTile<2> T; T.keys = a.c.keys; T.mat = s_mat[2]; T.f = a.f; T.w = ((u32)id & 7) + (threadIdx.x & 15);
+        h = finish_el<false>(W, T, a.f, prod3(Sh{ s_g[2 * p][W.t], s_g[2 * p + 1][W.t] }, y), act, s);
+        if (act && W.real) st(a.h, p, e, h);
+    }
+    W.flush(a.c.wire);
+}
+
 // Gradients behind the product and the activation: dg = s (dh u) (operation c.op, the product with the bit under its stream 3), du = dh g (c.op + 1), the components
 // side by side, rows of 2 ffp: operands of the products that follow (columns behind ff are not written; they meet weights that are zero).
 struct GatedBackArgs { KCommon c; P6 dh, g, u, s; u64 *dz[3]; u64 rows; u32 ff, ff8, ffp, f; };
@@ -158,6 +202,39 @@ __global__ __launch_bounds__(64) void k_gated_back(GatedBackArgs a)
     u64 *dz = p == 0 ? a.dz[0] : (p == 1 ? a.dz[1] : a.dz[2]);
 #pragma unroll
     for (int q = 0; q < 2; q++) if (mine && act[q]) { dz[to[q]] = dg[q].o; dz[to[q] + a.ffp] = du[q].o; }
+    W.flush(a.c.wire);
+}
+
+// The same for few elements, 16 a workgroup: the first wavefront completes dg, the second du.
+template <bool RELU>
+__global__ __launch_bounds__(128) void k_gated_back_few(GatedBackArgs a)
+{
+    __shared__ uint4 s_msg[2][GT_LANES];
+    __shared__ u64 s_mat[2][GT_FIN_WORDS(3)], s_cnt[2][6];
+    const u32 wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    FWire W; W.init(s_msg[wave], s_cnt[wave]);
+    const int p = W.p;
+    const u64 n = a.rows * a.ff8, e0 = (u64)blockIdx.x * GT_FIN_EL, i = e0 + W.t;
+    GatedAt at = gated_at(i < n ? i : n - 1, a.ff8, n <= 0xffffffffu);
+    const bool act = i < n && at.col < a.ff;
+    if (at.col >= a.ff) at.col = a.ff - 1;
+    const u64 e = at.row * a.ff + at.col;
+    const u64 z = prod3(ld(a.dh, p, e), wave ? ld(a.g, p, e) : ld(a.u, p, e));
+    Sh y, none;
+    if (wave == 0) {
+        Sh s = { 0, 0 };
+        if (RELU) s = ld(a.s, p, e);
+        FinTile<RELU ? 3 : 2> T; T.keys = a.c.keys; T.mat = s_mat[0]; T.f = a.f;
+        T.deal(a.c.op, e0);
+        y = finish_el<false>(W, T, a.f, z, act, none);
+        if (RELU) y = mult_sh(W, s, y, T.za(W, 2), act);
+    } else {
+        FinTile<2> T; T.keys = a.c.keys; T.mat = s_mat[1]; T.f = a.f;
+        T.deal(a.c.op + 1, e0);
+        y = finish_el<false>(W, T, a.f, z, act, none);
+    }
+    u64 *dz = p == 0 ? a.dz[0] : (p == 1 ? a.dz[1] : a.dz[2]);
+    if (act && W.real) dz[at.row * 2 * a.ffp + at.col + (wave ? a.ffp : 0)] = y.o;
     W.flush(a.c.wire);
 }
 
@@ -416,18 +493,24 @@ struct LinTile {
 };
 #define GT_LIN_SHARED __shared__ uint4 s_msg[GT_LANES]; __shared__ u64 s_mat[28 * GT_FP_ROW]; __shared__ u64 s_cnt[6]; LinTile L(a, s_msg, s_mat, s_cnt);
 
-// Workgroups below `tiles`: 40 elements of a head's state, all chunks of the pass; the others: `per` tiles of 40 scores.
-__global__ __launch_bounds__(64) void k_lin_states(LinArgs a)
+// Workgroups below `tiles`: 40 elements of a head's state, all chunks of the pass; the others: `per` tiles of 40 scores for each wavefront.
+// PAIR: of a chain's two wavefronts one deals the material of the next chunk while the other completes this one; for chains that are too few to fill the SIMDs.
+template <bool PAIR>
+__global__ __launch_bounds__(PAIR ? 128 : 64) void k_lin_states(LinArgs a)
 {
-    GT_LIN_SHARED
+    constexpr int NW = PAIR ? 2 : 1;
+    __shared__ uint4 s_msg[NW][GT_LANES];
+    __shared__ u64 s_mat[NW][28 * GT_FP_ROW], s_cnt[NW][6];
+    const u32 wave = PAIR ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
+    LinTile L(a, s_msg[wave], s_mat[wave], s_cnt[wave]);
     const int p = L.W.p;
     const u32 nb = a.nbh * a.nch, row = GT_LIN_TRI / GT_FP_EL;
     bool act[2];
     u64 z[2];
-    Sh y[2];
+    Sh y[2], none[2];
     if (blockIdx.x >= a.tiles) {
         for (u32 i = 0; i < a.per; i++) {
-            const u32 b = (blockIdx.x - a.tiles) * a.per + i, bhl = b / a.each, tile = b % a.each, chl = tile / row, i0 = tile % row * GT_FP_EL;
+            const u32 b = ((blockIdx.x - a.tiles) * NW + wave) * a.per + i, bhl = b / a.each, tile = b % a.each, chl = tile / row, i0 = tile % row * GT_FP_EL;
             if (bhl >= a.nbh) break;
             const LinChunk ck = lin_chunk(a, bhl, a.ch0 + chl);
             const u32 n = ck.len * (ck.len + 1) / 2;
@@ -442,8 +525,16 @@ __global__ __launch_bounds__(64) void k_lin_states(LinArgs a)
         return;
     }
     const u32 dkv = a.dk * a.dv, per = (dkv + GT_FP_EL - 1) / GT_FP_EL, bhl = blockIdx.x / per, i0 = blockIdx.x % per * GT_FP_EL;
-    const u64 bh = a.bh0 + bhl;
+    const u64 bh = a.bh0 + bhl, e0 = (bh * a.nc + a.ch0) * a.pk + i0;
     const u32 *D = a.D + (u32)(bh % a.H) * (GT_LIN_CHUNK + 1);
+    if (PAIR && wave) {
+        for (u32 chl = 0; chl < a.nch; chl++) {
+            L.T.mat = s_mat[chl & 1];
+            L.T.deal(L.W, a.c.op + 1, e0 + (u64)chl * a.pk);
+            __syncthreads();                                          // (dealt; and the chunk before is completed)
+        }
+        return;
+    }
     u64 next[2];
 #pragma unroll
     for (int q = 0; q < 2; q++) {
@@ -460,7 +551,9 @@ __global__ __launch_bounds__(64) void k_lin_states(LinArgs a)
             if (L.mine && act[q]) a.S[at + L.el[q]] = y[q].o;
             if (chl + 1 < a.nch) next[q] = act[q] ? a.Zk[at + a.pk + L.el[q]] : 0;
         }
-        L.finish(a.c.op + 1, (bh * a.nc + a.ch0 + chl) * a.pk + i0, z, (u32)act[0] + (u32)act[1], y);
+        if (PAIR) { L.T.mat = s_mat[chl & 1]; __syncthreads(); }
+        else L.T.deal(L.W, a.c.op + 1, e0 + (u64)chl * a.pk);
+        finish_two<false>(L.W, L.T, L.s, z, L.el, (u32)act[0] + (u32)act[1], y, none);
     }
 #pragma unroll
     for (int q = 0; q < 2; q++) if (L.mine && act[q]) st(a.out, p, bh * dkv + i0 + L.el[q], y[q]);
@@ -495,7 +588,7 @@ __global__ __launch_bounds__(64) void k_lin_finish(LinArgs a)
 }
 
 // A token of every sequence: its score, output and state in one launch, without a workspace.  Workgroups below nout: 40 outputs of a head, whose one score, q k, the first
-// wavefront works out (each such workgroup for itself) while the others make q S, a third of the state's rows each; the other workgroups: `per` tiles of 40 words of a
+// wavefront works out (each such workgroup for itself) while the second deals the outputs' material and the others make q S, half of the state's rows each; the other workgroups: `per` tiles of 40 words of a
 // state for each wavefront.  Where the new states take the place of the old ones, two launches: outputs first.
 // Bound: many sequences: the completions' block function; few: the outputs' two chains of messages.
 __global__ __launch_bounds__(256, 4) void k_lin_token(LinArgs a, u32 nout)
@@ -521,11 +614,17 @@ __global__ __launch_bounds__(256, 4) void k_lin_token(LinArgs a, u32 nout)
             act[i] = L.W.t < 20 && c < dv;
             col[i] = c < dv ? c : dv - 1;
         }
+        const u64 eo = (u64)bh * GT_LIN_CHUNK * a.dv8 + tile * GT_FP_EL;
+        if (wave == 1) {
+            L.T.deal(L.W, a.c.op + 2, eo);
+            __syncthreads();
+            return;
+        }
         if (wave) {
             u64 acc[2] = { 0, 0 };
             if (a.has_in) {
                 const u64 *s0 = own_of(a.in, p) + (u64)bh * dkv, *s1 = nxt_of(a.in, p) + (u64)bh * dkv;
-                const u32 each = (dk + 2) / 3, d0 = (wave - 1) * each, d1 = d0 + each < dk ? d0 + each : dk;
+                const u32 each = (dk + 1) / 2, d0 = (wave - 2) * each, d1 = d0 + each < dk ? d0 + each : dk;
 #pragma unroll 8
                 for (u32 d = d0; d < d1; d++) {
                     const Sh x = { q0[hq + d], q1[hq + d] };
@@ -556,9 +655,11 @@ __global__ __launch_bounds__(256, 4) void k_lin_token(LinArgs a, u32 nout)
 #pragma unroll
         for (int i = 0; i < 2; i++) {
             const u32 e = GT_FP_EL * p + L.el[i];
-            z[i] = (prod3(P, v[i]) << GT_LIN_DECAY) + (s_mat[1][e] + s_mat[2][e] + s_mat[3][e]) * w;
+            z[i] = (prod3(P, v[i]) << GT_LIN_DECAY) + (s_mat[2][e] + s_mat[3][e]) * w;
         }
-        L.finish(a.c.op + 2, (u64)bh * GT_LIN_CHUNK * a.dv8 + tile * GT_FP_EL, z, (u32)act[0] + (u32)act[1], y);
+        L.T.mat = s_mat[1];
+        Sh none[2];
+        finish_two<false>(L.W, L.T, L.s, z, L.el, (u32)act[0] + (u32)act[1], y, none);
 #pragma unroll
         for (int i = 0; i < 2; i++) if (L.mine && act[i]) st(a.o, p, (u64)bh * dv + col[i], y[i]);
         L.W.flush(a.c.wire);

@@ -54,6 +54,10 @@ static int gated_finish(gt_ctx *c, GatedArgs a, bool relu, u64 first, u64 rows, 
 {
     a.first = first; a.rows = rows; a.R = R; a.plane = plane; a.nchunk = nchunk; a.Z = c->dacc;
     const u64 n = rows * a.ff8;
+    if (!whole && gated_few(c->simds, n)) {
+        const dim3 g((unsigned)((n + GT_FIN_EL - 1) / GT_FIN_EL));
+        return relu ? launch(c, GT_KC_FINISH, k_gated_few<true>, g, dim3(128), a) : launch(c, GT_KC_FINISH, k_gated_few<false>, g, dim3(128), a);
+    }
     if (!whole) {
         const dim3 g((unsigned)((n + GT_FP_EL - 1) / GT_FP_EL));
         return relu ? launch(c, GT_KC_FINISH, k_gated<FIN_PARTS, true>, g, B64, a) : launch(c, GT_KC_FINISH, k_gated<FIN_PARTS, false>, g, B64, a);
@@ -123,8 +127,10 @@ extern "C" int gt_gated_backward(gt_ctx *c, const gt_gated *l, const gt_shares *
     if (gate) a.s = once(to_p6(gate));
     for (int p = 0; p < 3; p++) a.dz[p] = dz.o[p];
     a.rows = rows; a.ff = l->ff; a.ff8 = (l->ff + 7) / 8 * 8; a.ffp = l->ffp; a.f = c->tau;
-    const dim3 grid((unsigned)((rows * a.ff8 + GT_FP_EL - 1) / GT_FP_EL));
-    if (rows) GTCHK(gate ? launch(c, GT_KC_FINISH, k_gated_back<true>, grid, B64, a) : launch(c, GT_KC_FINISH, k_gated_back<false>, grid, B64, a));
+    const u64 elements = rows * a.ff8;
+    const dim3 grid((unsigned)((elements + GT_FP_EL - 1) / GT_FP_EL)), few((unsigned)((elements + GT_FIN_EL - 1) / GT_FIN_EL));
+    if (rows && gated_few(c->simds, elements)) GTCHK(gate ? launch(c, GT_KC_FINISH, k_gated_back_few<true>, few, dim3(128), a) : launch(c, GT_KC_FINISH, k_gated_back_few<false>, few, dim3(128), a));
+    else if (rows) GTCHK(gate ? launch(c, GT_KC_FINISH, k_gated_back<true>, grid, B64, a) : launch(c, GT_KC_FINISH, k_gated_back<false>, grid, B64, a));
     acct_finished(c, n, false); acct_finished(c, n, false);
     if (gate) wire_add(c, -1, n, 64);
     c->acc.rounds += gate ? 7 : 6;
@@ -231,7 +237,9 @@ extern "C" int gt_linattn_forward(gt_ctx *c, const gt_linattn *l, const gt_share
             a.tiles = a.nbh * (u32)((dkv + GT_FP_EL - 1) / GT_FP_EL);
             a.each = (a.nch - 1) * (GT_LIN_TRI / GT_FP_EL) + (last * (last + 1) / 2 + GT_FP_EL - 1) / GT_FP_EL;
             a.per = tiles_of_wave(c->simds, (u64)a.nbh * a.each);
-            GTCHK(launch(c, GT_KC_FINISH, k_lin_states, dim3(a.tiles + (a.nbh * a.each + a.per - 1) / a.per), B64, a));
+            const u32 waves = (a.nbh * a.each + a.per - 1) / a.per;
+            GTCHK(lin_pairs(c->simds, a.tiles) ? launch(c, GT_KC_FINISH, k_lin_states<true>, dim3(a.tiles + (waves + 1) / 2), dim3(128), a)
+                  : launch(c, GT_KC_FINISH, k_lin_states<false>, dim3(a.tiles + waves), B64, a));
             GTCHK(launch(c, GT_KC_DENSE, k_lin_out, dim3((nb * 6 * ct + 7) / 8 * 8), B256, a));
             a.each = (a.nch - 1) * per_o + (last * a.dv8 + GT_FP_EL - 1) / GT_FP_EL;
             a.per = tiles_of_wave(c->simds, (u64)a.nbh * a.each);

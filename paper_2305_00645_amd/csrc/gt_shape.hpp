@@ -336,6 +336,10 @@ static inline FinShape gated_shape(u64 simds, u64 n)
     s.waves = (u32)(tiles - (u64)s.nbig * (s.per - 1));
     return s;
 }
+// Whether a gated layer's completions (n elements) take 16 elements a workgroup of two wavefronts (k_gated_few) rather than 40 a wavefront.
+static inline bool gated_few(u64 simds, u64 n) { return n < 40 * simds; }
+// Whether a state's chain takes two wavefronts (k_lin_states): up to this many chains.
+static inline bool lin_pairs(u64 simds, u64 chains) { return chains <= 2 * simds; }
 // Tiles of 40 that a wavefront of linear attention's completions takes one after the other: at most 16, so that the wavefronts are as few and whole rounds of the
 // four that a SIMD has at a time.
 static inline u32 tiles_of_wave(u64 simds, u64 tiles)
