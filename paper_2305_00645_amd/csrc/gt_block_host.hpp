@@ -110,16 +110,19 @@ extern "C" int gt_gated_backward(gt_ctx *c, const gt_gated *l, const gt_shares *
     for (int p = 0; p < 3; p++) half[1].o[p] += l->ffp;
     FinOut ox, og, ou;
     if (dx) ox.y = to_p6(dx);
-    RnsJob jg, ju;
+    // dx joins the others' launches unless the conversion of its weights is much (few_rows_apart)
+    const bool apart = dx && (rows == 0 || !dWg || few_rows_apart(rows, l->din, N));
+    RnsJobs jobs;
     Need need;
-    if (dx) need = dense_need(c, rows, l->din, N, N);
+    if (apart) need = dense_need(c, rows, l->din, N, N);
+    else if (dx) jobs.add(RnsJob(c, view(dz, N, MAT_ROWS), wmat(l->W, MAT_W), rows, l->din, N, false, ox));
     if (dWg) {
         og.y = to_p6(dWg); ou.y = to_p6(dWu);
         const MatView xt = view(to_p6(x), l->din, MAT_COLS);
-        jg = RnsJob(c, xt, view(half[0], N, MAT_COLS), l->din, l->ff, rows, false, og);
-        ju = RnsJob(c, xt, view(half[1], N, MAT_COLS), l->din, l->ff, rows, false, ou);
-        need.also(jobs_need(c, jg, ju));
+        jobs.add(RnsJob(c, xt, view(half[0], N, MAT_COLS), l->din, l->ff, rows, false, og));
+        jobs.add(RnsJob(c, xt, view(half[1], N, MAT_COLS), l->din, l->ff, rows, false, ou), true);
     }
+    need.also(jobs_need(c, jobs));
     GTCHK(reserve(c, need));
     GatedBackArgs a{};
     a.c = kc(c, c->op); c->op += 2;
@@ -134,11 +137,11 @@ extern "C" int gt_gated_backward(gt_ctx *c, const gt_gated *l, const gt_shares *
     acct_finished(c, n, false); acct_finished(c, n, false);
     if (gate) wire_add(c, -1, n, 64);
     c->acc.rounds += gate ? 7 : 6;
-    if (dx) GTCHK(do_dense_w(c, dz, N, l->W, true, rows, false, ox));
-    if (dWg) GTCHK(run_jobs(c, jg, ju));
-    for (int i = 0; i < 2 && dbg; i++) {
-        ColsumArgs s{}; s.x = half[i]; s.out = to_p6(i ? dbu : dbg); s.rows = rows; s.cols = l->ff; s.ld = N;
-        GTCHK(launch(c, GT_KC_LOCAL, k_colsum, dim3((l->ff + 15) / 16, 3), dim3(1024), s));
+    if (apart) GTCHK(do_dense_w(c, dz, N, l->W, true, rows, false, ox));
+    GTCHK(run_jobs(c, jobs));
+    if (dbg) {
+        ColsumArgs s{}; s.x = dz; s.out = to_p6(dbg); s.out2 = to_p6(dbu); s.rows = rows; s.ld = N; s.apart = l->ffp; s.cols = l->ff; s.half = (l->ff + 15) / 16;
+        GTCHK(launch(c, GT_KC_LOCAL, k_colsum, dim3(2 * s.half, 3), dim3(1024), s));
     }
     return T.finish(GT_OK);
 }

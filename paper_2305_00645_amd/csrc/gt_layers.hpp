@@ -547,14 +547,14 @@ __device__ __forceinline__ void finish_two(WWire &W, const TileT &T, u32 f, cons
     }
 }
 
-// One or two completions in a launch: workgroups below na are the first one's.
-struct FinSet { FinArgs f[2]; u32 na; };
+// Up to three completions in a launch: workgroups below na are the first one's, below nb the second one's.
+struct FinSet { FinArgs f[3]; u32 na = ~0u, nb = ~0u; };
 template <int SRC, bool RELU>
 __global__ __launch_bounds__(64) void k_finish_pair(FinSet set)
 {
-    const bool second = blockIdx.x >= set.na;
-    const FinArgs &a = set.f[second ? 1 : 0];
-    const u32 block = second ? blockIdx.x - set.na : blockIdx.x;
+    const u32 which = (blockIdx.x >= set.na ? 1u : 0u) + (blockIdx.x >= set.nb ? 1u : 0u);
+    const FinArgs &a = set.f[which];
+    const u32 block = blockIdx.x - (which == 2 ? set.nb : which ? set.na : 0);
     constexpr int NS = RELU ? 3 : 2;
     __shared__ uint4 s_msg[GT_LANES];
     __shared__ u64 s_mat[(22 + 3 * NS) * GT_FP_ROW];
@@ -995,12 +995,15 @@ __device__ __forceinline__ void residue_block(const ResArgs &a, u32 block, u64 (
     }
 }
 
-// the factors of one or two products: left, right, left, right; end: their workgroups, added up
-struct ResSet { ResArgs r[4]; u32 end[4]; };
+// the factors of up to three products: left, right, left, right ...; end: their workgroups, added up (no workgroups: a factor that is there already)
+struct ResSet { ResArgs r[6]; u32 end[6]; };
 __global__ __launch_bounds__(256) void k_residues(ResSet set)
 {
     __shared__ u64 s_t[4][32 * 33];
-    const u32 b = blockIdx.x, i = (b >= set.end[0] ? 1u : 0u) + (b >= set.end[1] ? 1u : 0u) + (b >= set.end[2] ? 1u : 0u);
+    const u32 b = blockIdx.x;
+    u32 i = 0;
+#pragma unroll
+    for (int e = 0; e < 5; e++) i += b >= set.end[e] ? 1u : 0u;
     const ResArgs &a = set.r[i];
     const u32 block = b - (i ? set.end[i - 1] : 0);
     if (!(i & 1)) { if (a.x.kind == MAT_ROWS) residue_block<false, MAT_ROWS>(a, block, s_t); else residue_block<false, MAT_COLS>(a, block, s_t); }
@@ -1019,14 +1022,14 @@ __global__ __launch_bounds__(256) void k_residues(ResSet set)
 // of the vendor's library 2.4-2.5; these matrix instructions alone on random registers 3.3, with this LDS traffic and a barrier a step 2.5; zeros 4.5).
 // With the words to LDS behind the matrix instructions and loads a step ahead 1.09 ms; 256 x 256 outputs by eight wavefronts 0.97.
 struct RmmArgs { const unsigned char *A, *B; unsigned char *R; u64 amat, bmat, plane; u32 M, N, narb, nbrb, nstep, ntm, ntn, total; int asums; };   // amat, bmat: bytes of a modulus's matrix; narb: blocks of 32 rows
-// One or two products in a launch: workgroups below na are the first one's.
-struct RmmSet { RmmArgs m[2]; u32 na; };
+// Up to three products in a launch: workgroups below na are the first one's, below nb the second one's.
+struct RmmSet { RmmArgs m[3]; u32 na = ~0u, nb = ~0u; };
 template <int WM, int WN>
 __global__ __launch_bounds__(256, WM == 4 ? 2 : WM == 2 ? 3 : 4) void k_rns_mm(RmmSet set)
 {
-    const bool second = blockIdx.x >= set.na;
-    const RmmArgs &a = set.m[second ? 1 : 0];
-    const u32 block = second ? blockIdx.x - set.na : blockIdx.x;
+    const u32 which = (blockIdx.x >= set.na ? 1u : 0u) + (blockIdx.x >= set.nb ? 1u : 0u);
+    const RmmArgs &a = set.m[which];
+    const u32 block = blockIdx.x - (which == 2 ? set.nb : which ? set.na : 0);
     constexpr int FA = 2 * WM, FB = 2 * WN, STEP = 2 * (FA + FB) * 1024;       // operands of 32 rows a workgroup, bytes of a step
     constexpr int LD = 64 * WN + 16, OUT = 64 * WM * LD;
     constexpr int LOADS = STEP / 4096;                                         // of 16 bytes a lane
@@ -1178,13 +1181,16 @@ __global__ __launch_bounds__(256) void k_put(PutArgs a)
 }
 
 // Column sums of a shared matrix (local): a workgroup per 16 columns and component, 64 rows at a time.  Bound: reading the matrix (2048 x 1024, 50 MB).
-struct ColsumArgs { P6 x, out; u64 rows, ld; u32 cols; };
+// With `half` workgroups of columns a second matrix, `apart` words behind the first, goes to out2.
+struct ColsumArgs { P6 x, out, out2; u64 rows, ld, apart; u32 cols, half; };
 __global__ __launch_bounds__(1024) void k_colsum(ColsumArgs a)
 {
     __shared__ u64 s_sum[64][17];
     const u32 c = threadIdx.x & 15, g = threadIdx.x >> 4, pl = blockIdx.y;
-    const u64 col = (u64)blockIdx.x * 16 + c;
-    const u64 *x = pl == 0 ? a.x.o[0] : (pl == 1 ? a.x.o[1] : a.x.o[2]);
+    const bool second = blockIdx.x >= a.half;
+    const u64 col = (u64)(blockIdx.x - (second ? a.half : 0)) * 16 + c;
+    const u64 *x = (pl == 0 ? a.x.o[0] : (pl == 1 ? a.x.o[1] : a.x.o[2])) + (second ? a.apart : 0);
+    const P6 &out = second ? a.out2 : a.out;
     u64 s = 0;
     if (col < a.cols) {
 #pragma unroll 8
@@ -1202,7 +1208,7 @@ __global__ __launch_bounds__(1024) void k_colsum(ColsumArgs a)
 #pragma unroll
         for (int i = 1; i < 8; i++) s += s_sum[i][c];
         // component pl: party pl's own, its predecessor's next one
-        own_of(a.out, (int)pl)[col] = s; nxt_of(a.out, pl == 0 ? 2 : (int)pl - 1)[col] = s;
+        own_of(out, (int)pl)[col] = s; nxt_of(out, pl == 0 ? 2 : (int)pl - 1)[col] = s;
     }
 }
 

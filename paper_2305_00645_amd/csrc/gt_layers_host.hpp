@@ -186,8 +186,9 @@ static int rmm_launch(gt_ctx *c, u32 wm, const RmmSet &m, u32 blocks)
 }
 // rows and columns in blocks, the long axis in chunks of RNS_TERMS (see rns_plan); its workspace is there.  done(r0, rows, whole, R, plane, nchunk) completes the product's
 // rows from r0 on: from residues R of all chunks (none of a product without terms, whatever R is), or unless whole from the parts' words.
+// left_there: the left factor's residues are, from the product before (of one pass, see RnsJobs).
 template <class Done>
-static int run_products(gt_ctx *c, const RnsJob &all, Done done)
+static int run_products(gt_ctx *c, const RnsJob &all, Done done, bool left_there = false)
 {
     const RnsPlan &plan = all.plan;
     for (u64 r0 = 0; r0 < all.M; r0 += plan.rows) {
@@ -202,7 +203,9 @@ static int run_products(gt_ctx *c, const RnsJob &all, Done done)
                 ResSet r{};
                 u32 na, nb;
                 r.r[0] = j.left(c, ch, &na); r.r[1] = j.right(c, ch, &nb);
-                r.end[0] = na; r.end[1] = r.end[2] = r.end[3] = na + nb;
+                if (left_there) na = 0;
+                r.end[0] = na;
+                for (int e = 1; e < 6; e++) r.end[e] = na + nb;
                 GTCHK(launch(c, GT_KC_DENSE, k_residues, dim3(na + nb), B256, r));
                 RmmSet m{};
                 m.m[0] = j.product(ch); m.na = rmm_blocks(m.m[0]);
@@ -218,7 +221,7 @@ static int run_products(gt_ctx *c, const RnsJob &all, Done done)
     }
     return GT_OK;
 }
-static int run_taken(gt_ctx *c, const RnsJob &all)
+static int run_taken(gt_ctx *c, const RnsJob &all, bool left_there = false)
 {
     return run_products(c, all, [&](u64 r0, u64 rows, bool whole, const unsigned char *R, u64 plane, u32 nchunk) {
         const u64 n = rows * all.N;
@@ -231,53 +234,83 @@ static int run_taken(gt_ctx *c, const RnsJob &all)
         f.f[0].Z = c->dacc; f.f[0].first = r0 * all.N; f.f[0].n = n;
         f.na = (u32)((n + GT_FP_EL - 1) / GT_FP_EL);
         return all.relu ? launch(c, GT_KC_FINISH, k_finish_pair<FIN_PARTS, true>, dim3(f.na), B64, f) : launch(c, GT_KC_FINISH, k_finish_pair<FIN_PARTS, false>, dim3(f.na), B64, f);
-    });
+    }, left_there);
 }
 static int run_job(gt_ctx *c, RnsJob j)
 {
     j.take(c);
     return run_taken(c, j);
 }
-// Two products that do not wait for each other, without activation: side by side in the same three launches where neither fills the chip alone (267 x 22 -> 16:
-// 12 launches of a backward pass, 66 us, where the host's calls count, to 9).
-static bool joined(const RnsJob &x, const RnsJob &y)
-{
-    const auto once = [](const RnsJob &j) { return j.nchunk == 1 && j.M <= j.plan.rows && j.plan.whole; };
-    return once(x) && once(y) && x.s.wm == y.s.wm && x.s.wm != 4;
-}
-static Need jobs_need(gt_ctx *c, const RnsJob &x, const RnsJob &y)
+// Up to three products that do not wait for each other, without activation: side by side in the same three launches where none fills the chip alone (267 x 22 -> 16:
+// 12 launches of a backward pass, 66 us, where the host's calls count, to 9).  Where one has the same left factor as the one before (same_left, the same sizes too), its
+// residues are made once.
+struct RnsJobs {
+    RnsJob j[3];
+    bool same_left[3] = { false, false, false };
+    int n = 0;
+    void add(const RnsJob &x, bool same = false) { j[n] = x; same_left[n++] = same; }
+    static bool once(const RnsJob &x) { return x.nchunk == 1 && x.M <= x.plan.rows && x.plan.whole; }
+    bool joined(int from, int to) const
+    {
+        for (int i = from; i < to; i++) if (!once(j[i]) || j[i].s.wm != j[from].s.wm || j[i].s.wm == 4) return false;
+        return to - from > 1;
+    }
+    // the jobs that share their launches with the first one of `from`
+    int group(int from) const { return joined(from, n) ? n : from + 2 <= n && joined(from, from + 2) ? from + 2 : from + 1; }
+};
+static Need jobs_need(gt_ctx *c, const RnsJobs &all)
 {
     Need n;
-    if (joined(x, y)) n.res = x.bytes() + y.bytes();
-    else { n = job_need(c, x.M, x.N, x.K); n.also(job_need(c, y.M, y.N, y.K)); }
+    for (int from = 0, to; from < all.n; from = to) {
+        to = all.group(from);
+        Need g;
+        if (to - from == 1) g = job_need(c, all.j[from].M, all.j[from].N, all.j[from].K);
+        else for (int i = from; i < to; i++) g.res += all.j[i].bytes();
+        n.also(g);
+    }
     return n;
 }
-static int run_jobs(gt_ctx *c, RnsJob x, RnsJob y)
+static int run_jobs(gt_ctx *c, RnsJobs all)
 {
-    x.take(c); y.take(c);
-    if (!joined(x, y)) {
-        GTCHK(run_taken(c, x));
-        return run_taken(c, y);
+    for (int i = 0; i < all.n; i++) all.j[i].take(c);
+    bool alone = false;                           // the job before had the workspace for itself
+    for (int from = 0, to; from < all.n; from = to) {
+        to = all.group(from);
+        RnsJob *j = all.j;
+        if (to - from == 1) {
+            GTCHK(run_taken(c, j[from], alone && all.same_left[from] && RnsJobs::once(j[from]) && RnsJobs::once(j[from - 1])));
+            alone = true;
+            continue;
+        }
+        alone = false;
+        ResSet r{};
+        RmmSet m{};
+        FinSet f{};
+        u32 rblocks = 0, mblocks = 0, fblocks = 0;
+        unsigned char *at = c->res;
+        for (int i = from; i < to; i++) {
+            const int k = i - from;
+            const bool shared = k && all.same_left[i];
+            j[i].at = at;
+            at += j[i].bytes();
+            u32 na, nb;
+            r.r[2 * k] = j[i].left(c, 0, &na); r.r[2 * k + 1] = j[i].right(c, 0, &nb);
+            r.end[2 * k] = rblocks += shared ? 0 : na;
+            r.end[2 * k + 1] = rblocks += nb;
+            m.m[k] = j[i].product(0);
+            if (shared) m.m[k].A = m.m[k - 1].A;
+            mblocks += rmm_blocks(m.m[k]);
+            f.f[k] = j[i].f;
+            fblocks += fin_residues(c, f.f[k], j[i].at + j[i].abytes + j[i].bbytes, 0, j[i].M * j[i].N, j[i].plane, 1);
+            if (k == 0) { m.na = mblocks; f.na = fblocks; }
+            if (k == 1) { m.nb = mblocks; f.nb = fblocks; }
+        }
+        for (int k = 2 * (to - from); k < 6; k++) r.end[k] = rblocks;
+        GTCHK(launch(c, GT_KC_DENSE, k_residues, dim3(rblocks), B256, r));
+        GTCHK(rmm_launch(c, j[from].s.wm, m, mblocks));
+        GTCHK(launch(c, GT_KC_FINISH, k_finish_pair<FIN_RES, false>, dim3(fblocks), B64, f));
     }
-    RnsJob j[2] = { x, y };
-    j[0].at = c->res; j[1].at = c->res + x.bytes();
-    ResSet r{};
-    RmmSet m{};
-    FinSet f{};
-    u32 rblocks = 0, mblocks = 0, fblocks = 0;
-    for (int i = 0; i < 2; i++) {
-        u32 na, nb;
-        r.r[2 * i] = j[i].left(c, 0, &na); r.r[2 * i + 1] = j[i].right(c, 0, &nb);
-        r.end[2 * i] = rblocks + na; r.end[2 * i + 1] = rblocks += na + nb;
-        m.m[i] = j[i].product(0);
-        mblocks += rmm_blocks(m.m[i]);
-        f.f[i] = j[i].f;
-        fblocks += fin_residues(c, f.f[i], j[i].at + j[i].abytes + j[i].bbytes, 0, j[i].M * j[i].N, j[i].plane, 1);
-        if (i == 0) { m.na = mblocks; f.na = fblocks; }
-    }
-    GTCHK(launch(c, GT_KC_DENSE, k_residues, dim3(rblocks), B256, r));
-    GTCHK(rmm_launch(c, x.s.wm, m, mblocks));
-    return launch(c, GT_KC_FINISH, k_finish_pair<FIN_RES, false>, dim3(fblocks), B64, f);
+    return GT_OK;
 }
 // Parts of the product of few rows x (M rows of K words) and weights, or, transposed, the weights' rows as columns, in the workspace of
 // partial inner products; div: a division that may run beside it.
@@ -390,12 +423,12 @@ extern "C" int gt_dense_backward(gt_ctx *c, const gt_dense *l, const gt_shares *
     if (dx) ox.y = to_p6(dx);
     if (dW) ow.y = to_p6(dW);
     const bool apart = dx && (rows == 0 || !dW || few_rows_apart(rows, l->din, l->dout)), both = dx && !apart;
-    RnsJob jx, jw;
+    RnsJobs jobs;
     Need need;
     if (apart) need = dense_need(c, rows, l->din, l->dout, l->dout);
-    if (both) jx = RnsJob(c, view(dz, l->dout, MAT_ROWS), wmat(l->W, MAT_W), rows, l->din, l->dout, false, ox);
-    if (dW) jw = RnsJob(c, view(to_p6(x), l->din, MAT_COLS), view(dz, l->dout, MAT_COLS), l->din, l->dout, rows, false, ow);
-    if (dW) need.also(both ? jobs_need(c, jx, jw) : job_need(c, l->din, l->dout, rows));
+    if (both) jobs.add(RnsJob(c, view(dz, l->dout, MAT_ROWS), wmat(l->W, MAT_W), rows, l->din, l->dout, false, ox));
+    if (dW) jobs.add(RnsJob(c, view(to_p6(x), l->din, MAT_COLS), view(dz, l->dout, MAT_COLS), l->din, l->dout, rows, false, ow));
+    need.also(jobs_need(c, jobs));
     GTCHK(reserve(c, need));
     if (gate) {
         MultArgs m{}; m.x = once(to_p6(gate)); m.y = once(to_p6(dy)); m.z = dz; m.n = n;
@@ -404,10 +437,9 @@ extern "C" int gt_dense_backward(gt_ctx *c, const gt_dense *l, const gt_shares *
         acct_reshare(c, n, 1);
     }
     if (apart) GTCHK(do_dense_w(c, dz, l->dout, l->W, true, rows, false, ox));
-    if (both) GTCHK(run_jobs(c, jx, jw));
-    else if (dW) GTCHK(run_job(c, jw));
+    GTCHK(run_jobs(c, jobs));
     if (db) {
-        ColsumArgs a{}; a.x = dz; a.out = to_p6(db); a.rows = rows; a.cols = l->dout; a.ld = l->dout;
+        ColsumArgs a{}; a.x = dz; a.out = to_p6(db); a.rows = rows; a.cols = l->dout; a.ld = l->dout; a.half = ~0u;
         GTCHK(launch(c, GT_KC_LOCAL, k_colsum, dim3((l->dout + 15) / 16, 3), dim3(1024), a));
     }
     return T.finish(GT_OK);
