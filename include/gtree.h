@@ -342,7 +342,7 @@ int gt_linattn_destroy(gt_linattn *attention);
  *   S <- floor((2^tau D[c] S + sum_j D[c-1-j] k_j v_j + 2^(s-1)) / 2^s)
  * so other chunks round otherwise; all sums stay below 2^62, real numbers below 2^(50 - 2 tau).  Without tokens the states are copied.
  * Three operation ids; rounds: 6 for every chunk, at least 12.  Workspace (up to 2 GB, with GT_FLAG_SMALL_WORKSPACE 64 MB), graph capture and gt_rekey as in
- * gt_dense_forward.  seqs * tokens <= GT_MAX_DIM. */
+ * gt_dense_forward; a single token takes none and can be captured at once.  seqs * tokens and seqs * heads <= GT_MAX_DIM. */
 int gt_linattn_forward(gt_ctx *ctx, const gt_linattn *attention, const gt_shares *q, const gt_shares *k, const gt_shares *v, size_t ld, size_t seqs, size_t tokens,
                        const gt_shares *state_in, const gt_shares *state_out, const gt_shares *o);
 

@@ -152,7 +152,7 @@ __global__ __launch_bounds__(128) void k_gated_few(GatedArgs a)
 
 // Gradients behind the product and the activation: dg = s (dh u) (operation c.op, the product with the bit under its stream 3), du = dh g (c.op + 1), the components
 // side by side, rows of 2 ffp: operands of the products that follow (columns behind ff are not written; they meet weights that are zero).
-struct GatedBackArgs { KCommon c; P6 dh, g, u, s; u64 *dz[3]; u64 rows; u32 ff, ff8, ffp, f; };
+struct GatedBackArgs { KCommon c; P6 dh, g, u, s; u64 *dz[3]; u64 rows, first; u32 ff, ff8, ffp, f; };           // first: the launch's first element
 template <bool RELU>
 __global__ __launch_bounds__(64) void k_gated_back(GatedBackArgs a)
 {
@@ -163,7 +163,7 @@ __global__ __launch_bounds__(64) void k_gated_back(GatedBackArgs a)
     WWire W; W.init(s_msg, s_cnt);
     const int p = W.p;
     const u32 f = a.f, t = W.t < 20 ? W.t : 19;
-    const u64 n = a.rows * a.ff8, c0 = (u64)blockIdx.x * GT_FP_EL;
+    const u64 n = a.rows * a.ff8, c0 = a.first + (u64)blockIdx.x * GT_FP_EL;
     const bool mine = W.real && W.t < 20, narrow = n <= 0xffffffffu;
     const u32 el[2] = { t, t + 20 };
     bool act[2];
@@ -588,13 +588,15 @@ __global__ __launch_bounds__(64) void k_lin_finish(LinArgs a)
 }
 
 // A token of every sequence: its score, output and state in one launch, without a workspace.  Workgroups below nout: 40 outputs of a head, whose one score, q k, the first
-// wavefront works out (each such workgroup for itself) while the second deals the outputs' material and the others make q S, half of the state's rows each; the other workgroups: `per` tiles of 40 words of a
+// wavefront works out (each such workgroup for itself) while the second deals the outputs' material and the others make q S, a sixth of the state's rows each
+// (states come from memory, where the token before has put them: with two wavefronts for it 25 us a launch of one sequence, with six 12); the other workgroups: `per` tiles of 40 words of a
 // state for each wavefront.  Where the new states take the place of the old ones, two launches: outputs first.
 // Bound: many sequences: the completions' block function; few: the outputs' two chains of messages.
-__global__ __launch_bounds__(256, 4) void k_lin_token(LinArgs a, u32 nout)
+#define GT_LIN_TOKEN 8
+__global__ __launch_bounds__(64 * GT_LIN_TOKEN, 4) void k_lin_token(LinArgs a, u32 nout)
 {
-    __shared__ uint4 s_msg[4][GT_LANES];
-    __shared__ u64 s_mat[4][28 * GT_FP_ROW], s_cnt[4][6];
+    __shared__ uint4 s_msg[GT_LIN_TOKEN][GT_LANES];
+    __shared__ u64 s_mat[GT_LIN_TOKEN][28 * GT_FP_ROW], s_cnt[GT_LIN_TOKEN][6];
     const u32 wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     LinTile L(a, s_msg[wave], s_mat[wave], s_cnt[wave]);
     const int p = L.W.p, pn = L.W.pn;
@@ -623,8 +625,8 @@ __global__ __launch_bounds__(256, 4) void k_lin_token(LinArgs a, u32 nout)
         if (wave) {
             u64 acc[2] = { 0, 0 };
             if (a.has_in) {
-                const u64 *s0 = own_of(a.in, p) + (u64)bh * dkv, *s1 = nxt_of(a.in, p) + (u64)bh * dkv;
-                const u32 each = (dk + 1) / 2, d0 = (wave - 2) * each, d1 = d0 + each < dk ? d0 + each : dk;
+                const u64 *s0 = own_of(a.in, p) + (u64)bh * dkv, *s1 = own_of(a.in, pn) + (u64)bh * dkv;
+                const u32 each = (dk + GT_LIN_TOKEN - 3) / (GT_LIN_TOKEN - 2), d0 = (wave - 2) * each, d1 = d0 + each < dk ? d0 + each : dk;
 #pragma unroll 8
                 for (u32 d = d0; d < d1; d++) {
                     const Sh x = { q0[hq + d], q1[hq + d] };
@@ -654,8 +656,10 @@ __global__ __launch_bounds__(256, 4) void k_lin_token(LinArgs a, u32 nout)
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 2; i++) {
-            const u32 e = GT_FP_EL * p + L.el[i];
-            z[i] = (prod3(P, v[i]) << GT_LIN_DECAY) + (s_mat[2][e] + s_mat[3][e]) * w;
+            u64 qs = 0;
+#pragma unroll
+            for (int j = 2; j < GT_LIN_TOKEN; j++) qs += s_mat[j][GT_FP_EL * p + L.el[i]];
+            z[i] = (prod3(P, v[i]) << GT_LIN_DECAY) + qs * w;
         }
         L.T.mat = s_mat[1];
         Sh none[2];
@@ -667,7 +671,7 @@ __global__ __launch_bounds__(256, 4) void k_lin_token(LinArgs a, u32 nout)
     }
     const u32 tiles = (dkv + GT_FP_EL - 1) / GT_FP_EL;
     for (u32 j = 0; j < a.per; j++) {
-        const u32 id = ((blockIdx.x - nout) * 4 + wave) * a.per + j, bh = id / tiles, i0 = id % tiles * GT_FP_EL, h = bh % a.H, seq = bh / a.H;
+        const u32 id = ((blockIdx.x - nout) * GT_LIN_TOKEN + wave) * a.per + j, bh = id / tiles, i0 = id % tiles * GT_FP_EL, h = bh % a.H, seq = bh / a.H;
         if (bh >= a.nbh) break;
         const u64 hk = seq * a.ldk + (u64)h * dk, hv = seq * a.ldv + (u64)h * dv, w = a.D[h * (GT_LIN_CHUNK + 1) + 1], at = (u64)bh * dkv + i0;
 #pragma unroll

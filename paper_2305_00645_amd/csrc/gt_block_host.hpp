@@ -131,9 +131,12 @@ extern "C" int gt_gated_backward(gt_ctx *c, const gt_gated *l, const gt_shares *
     for (int p = 0; p < 3; p++) a.dz[p] = dz.o[p];
     a.rows = rows; a.ff = l->ff; a.ff8 = (l->ff + 7) / 8 * 8; a.ffp = l->ffp; a.f = c->tau;
     const u64 elements = rows * a.ff8;
-    const dim3 grid((unsigned)((elements + GT_FP_EL - 1) / GT_FP_EL)), few((unsigned)((elements + GT_FIN_EL - 1) / GT_FIN_EL));
+    const dim3 few((unsigned)((elements + GT_FIN_EL - 1) / GT_FIN_EL));
     if (rows && gated_few(c->simds, elements)) GTCHK(gate ? launch(c, GT_KC_FINISH, k_gated_back_few<true>, few, dim3(128), a) : launch(c, GT_KC_FINISH, k_gated_back_few<false>, few, dim3(128), a));
-    else if (rows) GTCHK(gate ? launch(c, GT_KC_FINISH, k_gated_back<true>, grid, B64, a) : launch(c, GT_KC_FINISH, k_gated_back<false>, grid, B64, a));
+    else for (; a.first < elements; a.first += (u64)GT_FP_EL << 24) {
+        const dim3 grid((unsigned)std::min<u64>((elements - a.first + GT_FP_EL - 1) / GT_FP_EL, 1u << 24));
+        GTCHK(gate ? launch(c, GT_KC_FINISH, k_gated_back<true>, grid, B64, a) : launch(c, GT_KC_FINISH, k_gated_back<false>, grid, B64, a));
+    }
     acct_finished(c, n, false); acct_finished(c, n, false);
     if (gate) wire_add(c, -1, n, 64);
     c->acc.rounds += gate ? 7 : 6;
@@ -175,10 +178,18 @@ extern "C" int gt_linattn_destroy(gt_linattn *l)
     return GT_OK;
 }
 
+// whether two sharings of n words have memory in common
+static bool shares_meet(const gt_shares *a, const gt_shares *b, size_t n)
+{
+    const u64 *x[6], *y[6];
+    for (int p = 0; p < 3; p++) { x[2 * p] = a->party[p].own; x[2 * p + 1] = a->party[p].next; y[2 * p] = b->party[p].own; y[2 * p + 1] = b->party[p].next; }
+    for (int i = 0; i < 36; i++) if (x[i / 6] < y[i % 6] + n && y[i % 6] < x[i / 6] + n) return true;
+    return false;
+}
 extern "C" int gt_linattn_forward(gt_ctx *c, const gt_linattn *l, const gt_shares *q, const gt_shares *k, const gt_shares *v, size_t ld, size_t seqs, size_t tokens,
                                   const gt_shares *in, const gt_shares *out, const gt_shares *o)
 {
-    if (!c || !l || seqs > GT_MAX_DIM || tokens > GT_MAX_DIM || seqs * tokens > GT_MAX_DIM) return GT_EINVAL;
+    if (!c || !l || seqs > GT_MAX_DIM || tokens > GT_MAX_DIM || seqs * tokens > GT_MAX_DIM || seqs * l->heads > GT_MAX_DIM) return GT_EINVAL;
     const size_t rows = seqs * tokens, wk = (size_t)l->heads * l->dk, wv = (size_t)l->heads * l->dv, dkv = (size_t)l->dk * l->dv, nS = seqs * l->heads * dkv;
     if (ld && (ld < wk || ld < wv || ld > 4 * (size_t)GT_MAX_DIM)) return GT_EINVAL;
     const size_t ldk = ld ? ld : wk, ldv = ld ? ld : wv;
@@ -186,7 +197,7 @@ extern "C" int gt_linattn_forward(gt_ctx *c, const gt_linattn *l, const gt_share
     if (!shares_ok(q, nk) || !shares_ok(k, nk) || !shares_ok(v, nv) || (in && !shares_ok(in, nS)) || !shares_ok(out, nS) || !shares_ok(o, rows * wv)) return GT_EINVAL;
     Timed T(c);
     if (!rows) {                                  // the states stay as they are
-        if (nS && in && in->party[0].own != out->party[0].own) GTCHK(copy6(c, to_p6(out), 0, to_p6(in), 0, nS));
+        if (nS && in && !shares_meet(in, out, nS)) GTCHK(copy6(c, to_p6(out), 0, to_p6(in), 0, nS));
         if (nS && !in) for (int p = 0; p < 3; p++) {
             GTCHK(launch(c, GT_KC_LOCAL, k_fill_words, g1(nS), B256, out->party[p].own, (u64)nS, (u64)0));
             GTCHK(launch(c, GT_KC_LOCAL, k_fill_words, g1(nS), B256, out->party[p].next, (u64)nS, (u64)0));
@@ -208,12 +219,12 @@ extern "C" int gt_linattn_forward(gt_ctx *c, const gt_linattn *l, const gt_share
         if (in) a.in = to_p6(in);
         acct_finished(c, nbh, false); acct_finished(c, nS, false); acct_finished(c, wv * seqs, false);
         c->acc.rounds += 12;
-        const u32 nstate = (u32)((tiles + 4 * a.per - 1) / (4 * a.per));
-        if (in && in->party[0].own == out->party[0].own) {
-            GTCHK(launch(c, GT_KC_FINISH, k_lin_token, dim3((unsigned)nout), B256, a, (u32)nout));
-            return T.finish(launch(c, GT_KC_FINISH, k_lin_token, dim3(nstate), B256, a, 0u));
+        const u32 nstate = (u32)((tiles + GT_LIN_TOKEN * a.per - 1) / (GT_LIN_TOKEN * a.per));
+        if (in && shares_meet(in, out, nS)) {
+            GTCHK(launch(c, GT_KC_FINISH, k_lin_token, dim3((unsigned)nout), dim3(64 * GT_LIN_TOKEN), a, (u32)nout));
+            return T.finish(launch(c, GT_KC_FINISH, k_lin_token, dim3(nstate), dim3(64 * GT_LIN_TOKEN), a, 0u));
         }
-        return T.finish(launch(c, GT_KC_FINISH, k_lin_token, dim3((unsigned)nout + nstate), B256, a, (u32)nout));
+        return T.finish(launch(c, GT_KC_FINISH, k_lin_token, dim3((unsigned)nout + nstate), dim3(64 * GT_LIN_TOKEN), a, (u32)nout));
     }
     const u64 sizes[5] = { GT_LIN_TRI, a.pk, (u64)GT_LIN_CHUNK * a.dv8, GT_LIN_TRI, a.pk };
     const LinPass pass = lin_pass(nbh, a.nc, l->dk, l->dv, c->rns_limit);

@@ -336,10 +336,12 @@ static inline FinShape gated_shape(u64 simds, u64 n)
     s.waves = (u32)(tiles - (u64)s.nbig * (s.per - 1));
     return s;
 }
-// Whether a gated layer's completions (n elements) take 16 elements a workgroup of two wavefronts (k_gated_few) rather than 40 a wavefront.
+// Whether a gated layer's completions (n elements) take 16 elements a workgroup of two wavefronts (k_gated_few) rather than 40 a wavefront.  64 terms with ReLU, the whole
+// layer, us: 8192 elements 15.4, 20.7, 32768 19.1, 22.9, 65536 28.4, 25.3; gradients' completions 8.0, 9.3, 8.5, 10.3, 13.4, 11.8.
 static inline bool gated_few(u64 simds, u64 n) { return n < 40 * simds; }
-// Whether a state's chain takes two wavefronts (k_lin_states): up to this many chains.
-static inline bool lin_pairs(u64 simds, u64 chains) { return chains <= 2 * simds; }
+// Whether a state's chain takes two wavefronts (k_lin_states).  Attention, 64 x 64, 512 tokens, with two and with one, us: 4 heads (412 chains) 61, 72, 16 (1648) 122, 123, 20
+// (2060) 149, 146, 32 213, 206; 8192 tokens of 2 heads 420, 594.
+static inline bool lin_pairs(u64 simds, u64 chains) { return 2 * chains <= 3 * simds; }
 // Tiles of 40 that a wavefront of linear attention's completions takes one after the other: at most 16, so that the wavefronts are as few and whole rounds of the
 // four that a SIMD has at a time (outputs of 4096 tokens, 16 x 128: a tile each 455 us, so 396).
 static inline u32 tiles_of_wave(u64 simds, u64 tiles)
