@@ -330,21 +330,32 @@ __device__ __forceinline__ void lin_tile(const LinArgs &a, u32 lb, u32 p, u32 r0
         }
         wave_sync();
     };
-    // terms k0 + lane of rows first .. first + 15 of a matrix of `rows` rows of K terms (zero where there are none)
+    // terms k0 + lane of rows f .. f + 15 of a matrix of `rows` rows of K terms (zero where there are none)
     auto by_rows = [&](const u64 *m, u64 ld, u32 f, u32 rows, u32 k0, u32 K, u64 (&x)[16]) {
+        if (k0 + 64 <= K && f + 16 <= rows) {
+#pragma unroll
+            for (int i = 0; i < 16; i++) x[i] = ld_at<u64>(m + k0 + (u64)(f + i) * ld, lane * 8);
+            return;
+        }
         const u32 k = k0 + lane, at = (k < K ? k : K - 1) * 8;
 #pragma unroll
         for (int i = 0; i < 16; i++) x[i] = ld_at<u64>(m + (u64)(f + i < rows ? f + i : rows - 1) * ld, at);
 #pragma unroll
         for (int i = 0; i < 16; i++) x[i] = k < K && f + i < rows ? x[i] : 0;
     };
-    // terms k0 + 16 kq .. of column c (of `columns`) of a matrix whose rows are terms (a chunk's rows lie within 32-bit offsets)
+    // terms k0 + 16 kq .. of column c + lr (of `columns`) of a matrix whose rows are terms (a chunk's rows lie within 32-bit offsets)
     auto by_terms = [&](const u64 *m, u32 ld, u32 c, u32 columns, u32 k0, u32 K, u64 (&x)[16]) {
-        const u32 k = k0 + 16 * kq, cc = c < columns ? c : columns - 1;
+        if (k0 + 64 <= K && c + 16 <= columns) {                          // (uniform addresses)
+            const u32 off = (16 * kq * ld + lr) * 8;
+#pragma unroll
+            for (int i = 0; i < 16; i++) x[i] = ld_at<u64>(m + c + (u64)(k0 + i) * ld, off);
+            return;
+        }
+        const u32 k = k0 + 16 * kq, cc = c + lr < columns ? c + lr : columns - 1;
 #pragma unroll
         for (int i = 0; i < 16; i++) x[i] = ld_at<u64>(m, ((k + i < K ? k + i : K - 1) * ld + cc) * 8);
 #pragma unroll
-        for (int i = 0; i < 16; i++) x[i] = k + i < K && c < columns ? x[i] : 0;
+        for (int i = 0; i < 16; i++) x[i] = k + i < K && c + lr < columns ? x[i] : 0;
     };
     u32 here = r0;
     v4i acc[2][8];
@@ -357,7 +368,6 @@ __device__ __forceinline__ void lin_tile(const LinArgs &a, u32 lb, u32 p, u32 r0
         // (a step works its addresses out again: kept over the steps they take the registers of the sums)
         asm volatile("" : "+v"(lane), "+s"(here));
         lr = lane & 15; kq = lane >> 4;
-        const u32 col = first + lr;
         u64 y[16], t[16];
         __syncthreads();
         auto right = [&]() {
@@ -370,7 +380,7 @@ __device__ __forceinline__ void lin_tile(const LinArgs &a, u32 lb, u32 p, u32 r0
                     turn(s_a + wave * 8192, w ? t : y);
                 } else {
                     const bool tokens = JOB == LIN_KV || scores;
-                    by_terms(tokens ? comp_of(a.v, j) + hv : a.S + ((u64)j * nb + lb) * a.pk, tokens ? (u32)a.ldv : dv, col, N, k0, tokens ? len : dk, w ? t : y);
+                    by_terms(tokens ? comp_of(a.v, j) + hv : a.S + ((u64)j * nb + lb) * a.pk, tokens ? (u32)a.ldv : dv, first, N, k0, tokens ? len : dk, w ? t : y);
                 }
             }
 #pragma unroll
@@ -383,7 +393,7 @@ __device__ __forceinline__ void lin_tile(const LinArgs &a, u32 lb, u32 p, u32 r0
             u64 x[16];
             v4i L[8];
             if (JOB == LIN_KV) {
-                by_terms(comp_of(a.k, (int)j) + hk, (u32)a.ldk, row + lr, M, 0, len, x);
+                by_terms(comp_of(a.k, (int)j) + hk, (u32)a.ldk, row, M, 0, len, x);
 #pragma unroll
                 for (int i = 0; i < 16; i += 4) {
                     const uint4 w = *(const uint4 *)(s_D + 16 * kq + i);
