@@ -45,9 +45,9 @@ def check_gated(mods, seed, rows, din, ff, relu, bias, keep, f=16, calls=2, smal
     layer.close(); g.close()
 
 
-# few rows; more than 192 rows; odd widths, below 8, at the borders of 64; many tiles
+# few rows; more than 192 rows; odd widths, below 8, at the borders of 64; many parts; residues, one tile and two a wavefront (see tests/block_shapes.py)
 GATED = [(1, 1, 1), (1, 64, 128), (1, 300, 7), (2, 65, 33), (7, 31, 64), (8, 64, 65), (16, 130, 9), (33, 294, 257), (100, 22, 16), (193, 70, 24), (193, 70, 25),
-         (267, 22, 3), (300, 200, 127), (1000, 50, 130)]
+         (267, 22, 3), (300, 200, 127), (1000, 50, 130), (400, 300, 301), (700, 150, 260), (1000, 294, 257)]
 
 
 @pytest.mark.parametrize("rows,din,ff", GATED)
@@ -105,7 +105,7 @@ def check_gated_back(mods, seed, rows, din, ff, relu, f=16, want=(True, True, Tr
 
 
 @pytest.mark.parametrize("rows,din,ff", [(0, 3, 4), (1, 1, 1), (1, 50, 70), (5, 33, 20), (16, 64, 17), (40, 3, 129), (129, 70, 65), (267, 22, 16), (300, 64, 33),
-                                         (300, 300, 90)])
+                                         (300, 300, 90), (600, 70, 90), (70, 1000, 1030)])
 @pytest.mark.parametrize("relu", [False, True])
 def test_gated_backward(mods, seed, rows, din, ff, relu):
     check_gated_back(mods, seed, rows, din, ff, relu)
@@ -149,7 +149,7 @@ def check_lin(mods, seed, seqs, tokens, heads, dk, dv, f=16, fused=False, state=
 
 
 LIN = [(1, 1, 1, 1, 1), (1, 1, 4, 64, 64), (5, 1, 3, 20, 77), (2, 1, 2, 130, 9), (1, 2, 1, 3, 2), (3, 7, 2, 16, 8), (2, 31, 2, 5, 12), (1, 32, 1, 64, 16), (1, 33, 1, 8, 65),
-       (2, 63, 1, 40, 30), (1, 64, 2, 64, 64), (3, 77, 5, 33, 65), (1, 129, 2, 65, 130), (2, 200, 1, 9, 24), (1, 1, 1, 256, 256), (1, 70, 1, 200, 250)]
+       (2, 63, 1, 40, 30), (1, 64, 2, 64, 64), (3, 77, 5, 33, 65), (1, 129, 2, 65, 130), (2, 200, 1, 9, 24), (1, 1, 1, 256, 256), (1, 70, 1, 200, 250), (3, 1, 16, 64, 64), (1, 65, 16, 64, 64), (1, 300, 16, 16, 40), (2, 320, 8, 4, 4)]
 
 
 @pytest.mark.parametrize("seqs,tokens,heads,dk,dv", LIN)
@@ -341,3 +341,106 @@ def test_refused_under_capture(mods, seed):
         g.linattn_forward(layer, q, q, q)
         st.synchronize()
         g.close()
+
+
+def test_another_stream_and_planes_of_odd_alignment(mods, seed):
+    """Work on the context's own stream; planes that start 8 but not 16 bytes aligned; q, k and v as parts of rows of an odd length; q and k the same words."""
+    import torch
+    Oracle, gtree = mods
+    st = torch.cuda.Stream()
+    with torch.cuda.stream(st):
+        o, g = Oracle(seed), gtree.GTree(seed, stream=st)
+        rng = np.random.default_rng(6)
+
+        def odd(s):
+            t = torch.empty((3, 2, s.n + 3 - s.n % 2), dtype=torch.int64, device="cuda")[:, :, 1:s.n + 1]
+            t.copy_(s.t)
+            return gtree.Shares(s.n, t=t)
+
+        for rows in (3, 300):
+            x, Wg, Wu, dh = (shared(o, g, pl.fixed(rng, 16, 0.5, *s)) for s in ((rows, 21), (21, 113), (21, 113), (rows, 113)))
+            layer = g.gated_create(odd(Wg[1]), odd(Wu[1]), 21, 113)
+            want = o.gated_forward(x[0], Wg[0], Wu[0], rows, 21, 113)
+            h, kept = g.gated_forward(layer, odd(x[1]), rows, keep=True)
+            same(h, want[0])
+            got = g.gated_backward(layer, odd(x[1]), odd(dh[1]), rows, tuple(odd(t) for t in kept))
+            for a, b in zip(got, o.gated_backward(x[0], Wg[0], Wu[0], dh[0], rows, 21, 113, want[1:])):
+                same(a, b)
+            layer.close()
+        for tokens in (1, 64, 67):
+            q, v = (shared(o, g, pl.fixed(rng, 16, 0.5, *s)) for s in ((tokens, 2 * 33), (tokens, 2 * 31)))
+            S = shared(o, g, pl.fixed(rng, 16, 0.5, 2, 33, 31))
+            layer = g.linattn_create([0.75, 1.0], 33, 31)
+            yo, So = o.linattn_forward(q[0], q[0], v[0], S[0], [3072, 4096], 1, tokens, 33, 31)
+            y, Sg = g.linattn_forward(layer, odd(q[1]), odd(q[1]), odd(v[1]), tokens=tokens, state=odd(S[1]))
+            same(y, yo); same(Sg, So)
+            n, ld = tokens, 2 * 33 * 2 + 2 * 31
+            rows = np.concatenate([t.reshape(3, n, -1) for t in (q[0], q[0], v[0])], 2).reshape(3, -1)
+            t = torch.from_numpy(np.stack([rows, np.roll(rows, -1, 0)], 1).view(np.int64)).cuda()
+            yo, So = o.linattn_forward(q[0], q[0], v[0], So, [3072, 4096], 1, tokens, 33, 31)
+            y, Sg = g.linattn_forward(layer, odd(gtree.Shares(n * ld, t=t)), tokens=tokens, state=Sg, inplace=True)
+            same(y, yo); same(Sg, So)
+            layer.close()
+        st.synchronize()
+        g.close()
+
+
+def test_two_graphs_of_one_context(mods, seed):
+    """Two captured graphs share the context's workspaces: replayed in turns, with eager calls between them, each gives the eager values."""
+    import torch
+    _, gtree = mods
+    st = torch.cuda.Stream()
+    with torch.cuda.stream(st):
+        g = gtree.GTree(seed, stream=st)
+        rng = np.random.default_rng(8)
+        s = lambda *shape: g.share_a(pl.words(pl.fixed(rng, 16, 0.5, *shape)))  # noqa: E731
+        rows, din, ff = 250, 30, 70
+        layer, att = g.gated_create(s(din, ff), s(din, ff), din, ff), g.linattn_create([0.9, 0.5], 10, 15)
+        x, dh, qkv, S = s(rows, din), s(rows, ff), s(rows, 2 * 35), s(2, 10, 15)
+
+        def first():
+            h, kept = g.gated_forward(layer, x, rows, keep=True)
+            return [h, *kept, *g.gated_backward(layer, x, dh, rows, kept)]
+
+        def second():
+            return list(g.linattn_forward(att, qkv, seqs=1, tokens=rows, state=S))
+
+        want = [[g.rec(t) for t in f()] for f in (first, second)]
+        graphs, outs = [torch.cuda.CUDAGraph() for _ in range(2)], []
+        for graph, f in zip(graphs, (first, second)):
+            with torch.cuda.graph(graph, stream=st):
+                g.rekey()
+                outs.append(f())
+        for turn in range(3):
+            for i in (0, 1, 1, 0):
+                for t in outs[i]:
+                    t.t.zero_()
+                graphs[i].replay()
+                st.synchronize()
+                for a, b in zip(outs[i], want[i]):
+                    assert np.array_equal(g.rec(a), b), (turn, i)
+            first() if turn else second()
+        g.close()
+
+
+def test_offsets_past_32_bits(mods, seed):
+    """Planes of more than 4 GiB, several passes: with decays of zero and zero states the last tokens' values are those of a call on them alone."""
+    import torch
+    _, gtree = mods
+    g = gtree.GTree(seed)
+    tokens, heads, d, last = 1 << 17, 33, 128, 128
+    n = tokens * heads * d
+    assert n * 8 > 1 << 32
+    own = torch.randint(-(1 << 16), 1 << 16, (3, n), device="cuda")
+    t = torch.empty((3, 2, n), dtype=torch.int64, device="cuda")
+    for p in range(3):
+        t[p, 0], t[p, 1] = own[p], own[(p + 1) % 3]
+    del own
+    x = gtree.Shares(n, t=t)
+    layer = g.linattn_create([0.0] * heads, d, d)
+    o, S = g.linattn_forward(layer, x, x, x, tokens=tokens)
+    tail = gtree.Shares(last * heads * d, t=t[:, :, n - last * heads * d:].contiguous())
+    want, state = g.linattn_forward(layer, tail, tail, tail, tokens=last)
+    got = gtree.Shares(tail.n, t=o.t[:, :, n - tail.n:].contiguous())
+    assert np.array_equal(g.rec(got), g.rec(want)) and np.array_equal(g.rec(S), g.rec(state))
+    layer.close(); g.close()
