@@ -7,6 +7,7 @@
 // ffp (ff rounded up to 64) columns each; one kernel completes g (operation c.op), u (c.op + 1) and h (c.op + 2), so that neither projection is written and
 // read again.  Elements are rows of ff8 (ff rounded up to 8), so that eight adjacent ones lie in a row.
 // Z: the parts, [3][rows][2 ffp], left at zero, or R: residues, planes of rows x 2 ffp.  first: the pass's first row.
+// Bound: the vector units, half of them on the block function (2048 x 1024 -> 2048 with ReLU, 1.3e7 completions: 0.79 ms with three wavefronts a SIMD, 0.85 with two).
 struct GatedArgs {
     KCommon c;
     u64 *Z;
@@ -107,7 +108,7 @@ __global__ __launch_bounds__(64, 3) void k_gated(GatedArgs a)
 }
 
 // The same for few elements, 16 a workgroup, from parts: the first wavefront completes g, the second u beside it, whose material for h is there when both are: one chain of
-// messages after the other, but one PRF pass before them.
+// messages after the other, but one PRF pass before them.  Bound: those chains (1 x 128: 6.9 us, as tiles of 40 12.6).
 template <bool RELU>
 __global__ __launch_bounds__(128) void k_gated_few(GatedArgs a)
 {
@@ -152,6 +153,7 @@ __global__ __launch_bounds__(128) void k_gated_few(GatedArgs a)
 
 // Gradients behind the product and the activation: dg = s (dh u) (operation c.op, the product with the bit under its stream 3), du = dh g (c.op + 1), the components
 // side by side, rows of 2 ffp: operands of the products that follow (columns behind ff are not written; they meet weights that are zero).
+// Bound: the vector units (2048 x 1024, 4.2e6 completions: 0.27 ms).
 struct GatedBackArgs { KCommon c; P6 dh, g, u, s; u64 *dz[3]; u64 rows, first; u32 ff, ff8, ffp, f; };           // first: the launch's first element
 template <bool RELU>
 __global__ __launch_bounds__(64) void k_gated_back(GatedBackArgs a)
@@ -248,6 +250,8 @@ __global__ __launch_bounds__(128) void k_gated_back_few(GatedBackArgs a)
 //   k_lin_states   the states one after the other, an element's chain in one wavefront; beside them the scores' completion
 //   k_lin_out      the parts of [2^12 P, D q] [v; S]
 //   k_lin_finish   their completion
+// Bound: the completions' vector instructions, 1,170 to 1,270 a tile of 40, 770 of them the block function's (16 heads, 4096 tokens, 64 x 128: states and scores 456 us,
+// outputs 402), then the products (286 and 385 us).
 // A pass takes chunks ch0 .. ch0 + nch - 1 of sequences' heads bh0 .. bh0 + nbh - 1; b' = (bh - bh0) * nch + chunk - ch0 counts in its workspace.
 #define GT_LIN_CHUNK 64
 #define GT_LIN_TRI 2080
@@ -301,7 +305,8 @@ enum { LIN_SCORES = 0, LIN_KV = 1, LIN_OUT = 2 };
 // z_p = x_p (y_p + y_{p+1}) + x_{p+1} y_p, terms in steps of 64.  A wavefront owns 16 columns, whose words stay in registers and become limbs there; the rows' limbs go through LDS,
 // [component p or p + 1][16 rows][limb][lane][16 bytes], a block of them made by each wavefront.  A block of 16 rows (or columns) whose terms are adjacent in memory is loaded
 // a row at a time, whole lines, and turned in LDS, where its limbs go afterwards.
-// Bound: the vector units that make limbs and words around the matrix instructions (144 of them a wavefront and step).
+// Bound: instructions of the vector units around the matrix instructions, which a SIMD's two or three wavefronts overlap in part (outputs of 16 heads, 4096 tokens, 64 x 128: 1.0e8 and
+// 1.4e7 of them, 47 and 27 % of 385 us).  Three parties a workgroup, six wavefronts: 414 and 691 us instead of 286 and 385, as one such workgroup fits a compute unit.
 template <int JOB>
 __device__ __forceinline__ void lin_tile(const LinArgs &a, u32 lb, u32 p, u32 r0, u32 c0, unsigned char *s_a)
 {
