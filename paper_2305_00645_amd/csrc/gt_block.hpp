@@ -255,7 +255,7 @@ __global__ __launch_bounds__(128) void k_gated_back_few(GatedBackArgs a)
 // A pass takes chunks ch0 .. ch0 + nch - 1 of sequences' heads bh0 .. bh0 + nbh - 1; b' = (bh - bh0) * nch + chunk - ch0 counts in its workspace.
 #define GT_LIN_CHUNK 64
 #define GT_LIN_TRI 2080
-#define GT_LIN_DECAY 12
+#define GT_LIN_DECAY 12                           // fraction bits of a decay: with tau <= 20 a completion's shift stays within 32, one half of the tree of ANDs
 struct LinArgs {
     KCommon c;
     const u64 *q[3], *k[3], *v[3];
@@ -704,8 +704,8 @@ __global__ __launch_bounds__(64 * GT_LIN_TOKEN, 4) void k_lin_token(LinArgs a, u
 }
 
 // Powers of the heads' decays, 12 fraction bits, rounded from 46: D[n] = round(E[n] / 2^34), E[0] = 2^46, E[n + 1] = round(E[n] w / 2^12).
-struct DecayArgs { u32 w[256]; u32 *D; u32 heads; };
-__global__ __launch_bounds__(256) void k_lin_decays(DecayArgs a)
+struct DecayArgs { u32 w[GT_MAX_HEADS]; u32 *D; u32 heads; };
+__global__ __launch_bounds__(GT_MAX_HEADS) void k_lin_decays(DecayArgs a)
 {
     const u32 h = threadIdx.x;
     if (h >= a.heads) return;

@@ -165,7 +165,7 @@ extern "C" int gt_linattn_create(gt_ctx *c, const uint32_t *decay, uint32_t head
     l->heads = heads; l->dk = dk; l->dv = dv;
     if (hipMalloc(&l->D, (size_t)heads * (GT_LIN_CHUNK + 1) * 4) != hipSuccess) { delete l; return GT_ENOMEM; }
     a.D = l->D; a.heads = heads;
-    const int rc = launch(c, GT_KC_LOCAL, k_lin_decays, dim3(1), B256, a);
+    const int rc = launch(c, GT_KC_LOCAL, k_lin_decays, dim3(1), dim3(GT_MAX_HEADS), a);
     if (rc != GT_OK) { (void)hipFree(l->D); delete l; return rc; }
     *out = l;
     return GT_OK;

@@ -468,6 +468,8 @@ class GTree:
         given state is overwritten and returned."""
         wk, wv = layer.heads * layer.dk, layer.heads * layer.dv
         rows, ld = seqs * tokens, 0
+        if (k is None) != (v is None):
+            raise GtError(GT_EINVAL, "gt_linattn_forward")
         if k is None:
             ld = 2 * wk + wv
             if q.n < rows * ld:

@@ -370,14 +370,14 @@ def test_another_stream_and_planes_of_odd_alignment(mods, seed):
         for tokens in (1, 64, 67):
             q, v = (shared(o, g, pl.fixed(rng, 16, 0.5, *s)) for s in ((tokens, 2 * 33), (tokens, 2 * 31)))
             S = shared(o, g, pl.fixed(rng, 16, 0.5, 2, 33, 31))
-            layer = g.linattn_create([0.75, 1.0], 33, 31)
-            yo, So = o.linattn_forward(q[0], q[0], v[0], S[0], [3072, 4096], 1, tokens, 33, 31)
+            layer = g.linattn_create([0.7, 1.0], 33, 31)
+            yo, So = o.linattn_forward(q[0], q[0], v[0], S[0], [2867, 4096], 1, tokens, 33, 31)
             y, Sg = g.linattn_forward(layer, odd(q[1]), odd(q[1]), odd(v[1]), tokens=tokens, state=odd(S[1]))
             same(y, yo); same(Sg, So)
             n, ld = tokens, 2 * 33 * 2 + 2 * 31
             rows = np.concatenate([t.reshape(3, n, -1) for t in (q[0], q[0], v[0])], 2).reshape(3, -1)
             t = torch.from_numpy(np.stack([rows, np.roll(rows, -1, 0)], 1).view(np.int64)).cuda()
-            yo, So = o.linattn_forward(q[0], q[0], v[0], So, [3072, 4096], 1, tokens, 33, 31)
+            yo, So = o.linattn_forward(q[0], q[0], v[0], So, [2867, 4096], 1, tokens, 33, 31)
             y, Sg = g.linattn_forward(layer, odd(gtree.Shares(n * ld, t=t)), tokens=tokens, state=Sg, inplace=True)
             same(y, yo); same(Sg, So)
             layer.close()
