@@ -110,8 +110,8 @@ extern "C" int gt_gated_backward(gt_ctx *c, const gt_gated *l, const gt_shares *
     for (int p = 0; p < 3; p++) half[1].o[p] += l->ffp;
     FinOut ox, og, ou;
     if (dx) ox.y = to_p6(dx);
-    // dx joins the others' launches unless the conversion of its weights is much (few_rows_apart)
-    const bool apart = dx && (rows == 0 || !dWg || few_rows_apart(rows, l->din, N));
+    // dx joins the others' launches unless the conversion of its weights is much
+    const bool apart = dx && (rows == 0 || !dWg || gated_apart(rows, l->din, N));
     RnsJobs jobs;
     Need need;
     if (apart) need = dense_need(c, rows, l->din, N, N);

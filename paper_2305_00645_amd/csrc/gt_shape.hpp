@@ -226,6 +226,9 @@ static inline bool few_rows(u64 simds, u64 M, u64 N, u64 K, u64 ldx)
 // dx of a backward pass that computes dW too, whose product by residues dx's can join: apart from it only where the conversion of the weights is much (both
 // gradients, us, apart and joined: 33 rows, 32 x 32 32, 23, 64 x 1024 45, 39, 600 x 600 80, 94, 1024 x 1024 133, 155; 128 rows 178, 162)
 static inline bool few_rows_apart(u64 rows, u64 din, u64 dout) { return rows <= 64 && din * dout >= (1u << 17); }
+// ... and of a gated layer, whose weights are n = 2 ff wide (all gradients, us, apart and joined: 33 rows, 64 -> 512 52, 45, 600 -> 300 88, 102, 1024 -> 512 140, 161; 64 rows,
+// 300 -> 300 71, 84, 1024 -> 1024 265, 320; 128 rows, 300 -> 300 85, 100, 1024 -> 512 189, 191; 190 rows, 600 -> 600 196, 187; 267 rows, 22 -> 16 42, 32)
+static inline bool gated_apart(u64 rows, u64 din, u64 n) { return rows <= 128 && din * n >= (1u << 17); }
 struct FewShape { u32 rows; u64 ntile, ngrp; u32 nsplit, per; };
 static inline FewShape few_shape(u64 simds, u64 M, u64 N, u64 K)
 {

@@ -162,7 +162,7 @@ class Shares:
     def c_struct(self, first=0):
         """The words from `first` on."""
         a, b = self.t.data_ptr() + 8 * first, self.t.stride(1) * 8
-        return _Shares.from_buffer_copy(_SHARES_WORDS(a, a + b, a + 2 * b, a + 3 * b, a + 4 * b, a + 5 * b, self.n - first))
+        return _Shares.from_buffer_copy(_SHARES_WORDS(a, a + b, a + 2 * b, a + 3 * b, a + 4 * b, a + 5 * b, max(self.n - first, 0)))
 
     def planes(self):
         """numpy uint64 array (3, 2, n)."""

@@ -105,7 +105,7 @@ def check_gated_back(mods, seed, rows, din, ff, relu, f=16, want=(True, True, Tr
 
 
 @pytest.mark.parametrize("rows,din,ff", [(0, 3, 4), (1, 1, 1), (1, 50, 70), (5, 33, 20), (16, 64, 17), (40, 3, 129), (129, 70, 65), (267, 22, 16), (300, 64, 33),
-                                         (300, 300, 90), (600, 70, 90), (70, 1000, 1030)])
+                                         (300, 300, 90), (600, 70, 90), (70, 1000, 1030), (140, 600, 500)])
 @pytest.mark.parametrize("relu", [False, True])
 def test_gated_backward(mods, seed, rows, din, ff, relu):
     check_gated_back(mods, seed, rows, din, ff, relu)
