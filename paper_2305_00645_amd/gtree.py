@@ -456,9 +456,10 @@ class GTree:
 
     def linattn_create(self, decay, dk, dv):
         """decay: a number in [0, 1] for each head, rounded to 12 fraction bits."""
-        w = [int(round(float(d) * 4096)) for d in decay]
-        if any(x < 0 for x in w):
+        decay = [float(d) for d in decay]
+        if not all(0 <= d <= 1 for d in decay):                               # (before they are words, which wrap; NaN too)
             raise GtError(GT_EINVAL, "gt_linattn_create")
+        w = [int(round(d * 4096)) for d in decay]
         h = C.c_void_p()
         _chk(self.L.gt_linattn_create(self.ctx, (C.c_uint32 * max(len(w), 1))(*w), len(w), dk, dv, C.byref(h)), "gt_linattn_create")
         return LinearAttention(self, h, len(w), dk, dv)

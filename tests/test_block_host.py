@@ -196,3 +196,24 @@ def test_refusals_without_a_gpu():
     assert L.gt_gated_create(None, None, None, None, None, 1, 1, C.byref(h)) == gtree.GT_EINVAL
     assert L.gt_linattn_create(None, None, 1, 1, 1, C.byref(h)) == gtree.GT_EINVAL
     assert not h.value
+
+
+def test_decays_outside_their_range():
+    """A decay's word has 32 bits at the library's border: one that does not fit must not arrive there as another."""
+    run(SETUP % 0 + """
+import math
+g = object.__new__(gtree.GTree)
+g.L, g.ctx = L, ctx
+before, n = counted(ctx), fake.fake_launches()
+for w in (2.0 ** 20, 2.0 ** 20 + 0.5, -2.0 ** 20, 1e300, -0.001, 1.001, 2, math.nan, math.inf, -math.inf):
+    for decay in ([w], [0.5, w], [w, 0.5]):
+        try:
+            g.linattn_create(decay, 4, 4)
+        except gtree.GtError as e:
+            assert e.code == gtree.GT_EINVAL, (w, e.code)
+        else:
+            raise AssertionError(w)
+assert counted(ctx) == before and fake.fake_launches() == n
+for decay in ([0, 1], [0.0, 1.0], [0.25], np.array([0.5, 1.0])):
+    g.linattn_create(decay, 4, 4).close()
+""")
