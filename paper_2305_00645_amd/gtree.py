@@ -455,11 +455,14 @@ class GTree:
         return tuple(out)
 
     def linattn_create(self, decay, dk, dv):
-        """decay: a number in [0, 1] for each head, rounded to 12 fraction bits."""
+        """decay: a number in [0, 1] for each head, rounded to 12 fraction bits.  One below 1 that would be rounded to 1 (from 4095.5 / 4096 on) is refused: its head
+        would never forget."""
         decay = [float(d) for d in decay]
         if not all(0 <= d <= 1 for d in decay):                               # (before they are words, which wrap; NaN too)
             raise GtError(GT_EINVAL, "gt_linattn_create")
         w = [int(round(d * 4096)) for d in decay]
+        if any(x == 4096 and d < 1 for x, d in zip(w, decay)):
+            raise GtError(GT_EINVAL, "gt_linattn_create")
         h = C.c_void_p()
         _chk(self.L.gt_linattn_create(self.ctx, (C.c_uint32 * max(len(w), 1))(*w), len(w), dk, dv, C.byref(h)), "gt_linattn_create")
         return LinearAttention(self, h, len(w), dk, dv)

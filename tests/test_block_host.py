@@ -217,3 +217,23 @@ assert counted(ctx) == before and fake.fake_launches() == n
 for decay in ([0, 1], [0.0, 1.0], [0.25], np.array([0.5, 1.0])):
     g.linattn_create(decay, 4, 4).close()
 """)
+
+
+def test_a_decay_below_one_that_rounds_to_one():
+    """A head that forgets slowly must not become one that never does: its state would grow without bound."""
+    run(SETUP % 0 + """
+g = object.__new__(gtree.GTree)
+g.L, g.ctx = L, ctx
+n = fake.fake_launches()
+for w in (4095.5 / 4096, 0.9999, 1 - 2.0 ** -20, 1 - 2.0 ** -53):
+    for decay in ([w], [1.0, w]):
+        try:
+            g.linattn_create(decay, 4, 4)
+        except gtree.GtError as e:
+            assert e.code == gtree.GT_EINVAL, (w, e.code)
+        else:
+            raise AssertionError(w)
+assert fake.fake_launches() == n
+for w in (1.0, 4095 / 4096, 4095.49 / 4096, 2.0 ** -14, 0.0):
+    g.linattn_create([w], 4, 4).close()
+""")
