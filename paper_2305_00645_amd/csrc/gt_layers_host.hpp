@@ -250,13 +250,13 @@ struct RnsJobs {
     int n = 0;
     void add(const RnsJob &x, bool same = false) { j[n] = x; same_left[n++] = same; }
     static bool once(const RnsJob &x) { return x.nchunk == 1 && x.M <= x.plan.rows && x.plan.whole; }
-    bool joined(int from, int to) const
+    bool joined(int from) const
     {
-        for (int i = from; i < to; i++) if (!once(j[i]) || j[i].s.wm != j[from].s.wm || j[i].s.wm == 4) return false;
-        return to - from > 1;
+        for (int i = from; i < n; i++) if (!once(j[i]) || j[i].s.wm != j[from].s.wm || j[i].s.wm == 4) return false;
+        return n - from > 1;
     }
-    // the jobs that share their launches with the first one of `from`
-    int group(int from) const { return joined(from, n) ? n : from + 2 <= n && joined(from, from + 2) ? from + 2 : from + 1; }
+    // end of the jobs that share their launches with `from`: all of the others or none.  (Two of three never would: the last two are of the same sizes.)
+    int group(int from) const { return joined(from) ? n : from + 1; }
 };
 static Need jobs_need(gt_ctx *c, const RnsJobs &all)
 {
