@@ -5,7 +5,7 @@ import pytest
 
 import block_shapes as bs
 import layer_shapes as ls
-from test_gpu_block import GATED, LIN
+from test_gpu_block import GATED, LIN, PASSES
 
 
 def pad8(n):
@@ -61,3 +61,20 @@ def test_the_gpu_tests_take_every_variant():
         seen.add("wide" if dk > 64 else "narrow")
         seen.add("whole" if dk % 64 == 0 and dv % 16 == 0 and tokens % 64 == 0 else "ragged")
     assert seen == {"token 1", "token 2", "pairs", "chains", "scores 1", "scores 2", "outputs 1", "outputs 2", "wide", "narrow", "whole", "ragged"}
+
+
+def test_the_gpu_tests_take_every_kind_of_pass():
+    seen = set()
+    for seqs, tokens, heads, dk, dv in PASSES:
+        nbh, nc = seqs * heads, (tokens + 63) // 64
+        h, c = bs.lin_pass(nbh, nc, dk, dv, True)
+        if h < nbh:
+            seen.add("heads")
+            seen.add("fewer heads last" if nbh % h else "equal heads")
+        if c < nc:
+            seen.add("chunks" if c > 1 else "a chunk")
+            if c > 1:
+                seen.add("fewer chunks last" if nc % c else "equal chunks")
+        seen.add("short last chunk" if tokens % 64 else "full")
+        seen.add("pairs" if bs.pairs(h * tiles(dk * dv)) else "chains")
+    assert seen >= {"heads", "fewer heads last", "chunks", "a chunk", "fewer chunks last", "equal chunks", "short last chunk", "pairs", "chains"}

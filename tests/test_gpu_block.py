@@ -175,6 +175,17 @@ def test_linattn_passes(mods, seed, seqs, tokens, heads):
     check_lin(mods, seed, seqs, tokens, heads, 256, 250, small=True, inplace=True)
 
 
+# several chunks a pass and passes behind them (2, 2 and 1 chunks, 2 and 2), a short last chunk; passes over heads, a chunk each (see tests/test_block_shapes.py)
+PASSES = [(16, 300, 16, 8, 9), (5, 200, 16, 64, 50), (3, 65, 7, 256, 250)]
+
+
+@pytest.mark.parametrize("seqs,tokens,heads,dk,dv", PASSES)
+@pytest.mark.parametrize("state,inplace", [(True, True), (True, False), (False, False)])
+def test_linattn_state_from_pass_to_pass(mods, seed, seqs, tokens, heads, dk, dv, state, inplace):
+    """The first pass takes the given state or zeros, the later ones what the one before has left."""
+    check_lin(mods, seed, seqs, tokens, heads, dk, dv, state=state, inplace=inplace, calls=1, small=True)
+
+
 @pytest.mark.parametrize("tokens", [1, 70])
 def test_linattn_words_of_any_size(mods, seed, tokens):
     """Words over the whole ring: sums wrap, results are what the protocol makes of them on both sides."""
