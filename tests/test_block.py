@@ -55,6 +55,20 @@ def test_gated_backward(seed, rows, din, ff, relu):
     assert o.op_counter() == op + 5 and o.stats()[0] == rounds + (7 if relu else 6) + 18
 
 
+@pytest.mark.parametrize("f", [1, 9, 20])
+@pytest.mark.parametrize("relu", [False, True])
+def test_gated_backward_fraction_widths(seed, f, relu):
+    rows, din, ff = 5, 7, 9
+    x, Wg, Wu, _, _ = gated_inputs(f, rows, din, ff, False)
+    dh = pl.fixed(np.random.default_rng(f), f, 0.5, rows, ff)
+    _, g, u, s = pb.gated(x, Wg, Wu, f, relu=relu)
+    s = s if relu else None
+    o = Oracle(seed, tau=f)
+    X, G, U, D, gs, us, ss = shared(o, x, Wg, Wu, dh, g, u, s)
+    for a, w in zip(o.gated_backward(X, G, U, D, rows, din, ff, (gs, us, ss)), pb.gated_back(x, Wg, Wu, dh, g, u, s, f)):
+        assert np.array_equal(o.rec(a), pl.words(w))
+
+
 def test_gated_gradients_against_differences(seed):
     """Gradients of sum(h c) against central differences of the real function.  A value of the backward pass is rounded by at most half a word per
     completion: with two factors of at most M in absolute value and K terms it is off by K M / 2 + 1 words; the differences of a bilinear function are exact but for

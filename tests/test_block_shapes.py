@@ -5,7 +5,7 @@ import pytest
 
 import block_shapes as bs
 import layer_shapes as ls
-from test_gpu_block import GATED, LIN, PASSES
+from test_gpu_block import BACK_WIDTHS, GATED, LIN, PASSES
 
 
 def pad8(n):
@@ -78,3 +78,7 @@ def test_the_gpu_tests_take_every_kind_of_pass():
         seen.add("short last chunk" if tokens % 64 else "full")
         seen.add("pairs" if bs.pairs(h * tiles(dk * dv)) else "chains")
     assert seen >= {"heads", "fewer heads last", "chunks", "a chunk", "fewer chunks last", "equal chunks", "short last chunk", "pairs", "chains"}
+
+
+def test_gradients_of_every_width_by_both_kernels():
+    assert [bs.few(rows * pad8(ff)) for rows, _, ff in BACK_WIDTHS] == [True, False]

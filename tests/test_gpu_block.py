@@ -111,6 +111,17 @@ def test_gated_backward(mods, seed, rows, din, ff, relu):
     check_gated_back(mods, seed, rows, din, ff, relu)
 
 
+# few elements (k_gated_back_few) and at least 40 a SIMD (k_gated_back); see tests/test_block_shapes.py
+BACK_WIDTHS = [(9, 20, 37), (700, 30, 61)]
+
+
+@pytest.mark.parametrize("rows,din,ff", BACK_WIDTHS)
+@pytest.mark.parametrize("relu", [False, True])
+@pytest.mark.parametrize("f", [1, 9, 20])
+def test_gated_backward_fraction_widths(mods, seed, rows, din, ff, relu, f):
+    check_gated_back(mods, seed, rows, din, ff, relu, f=f)
+
+
 @pytest.mark.parametrize("want", [(True, False, False), (False, True, False), (False, False, True), (True, False, True), (False, False, False)])
 def test_gated_backward_parts(mods, seed, want):
     check_gated_back(mods, seed, 9, 20, 30, True, want=want)
