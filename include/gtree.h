@@ -341,6 +341,9 @@ int gt_linattn_destroy(gt_linattn *attention);
  *   P_ij = floor((D[i-j] q_i k_j + 2^(s-1)) / 2^s) for j <= i, o_i = floor((2^12 sum_j P_ij v_j + D[i+1] q_i S + 2^(s-1)) / 2^s),
  *   S <- floor((2^tau D[c] S + sum_j D[c-1-j] k_j v_j + 2^(s-1)) / 2^s)
  * so other chunks round otherwise; all sums stay below 2^62, real numbers below 2^(50 - 2 tau).  Without tokens the states are copied.
+ * Precision: a chunk's powers are off by up to 2^-13 whatever tau is (a single token's decay is exact), and with them each term of a prompt's sums: some 2^-13
+ * of an output's usual size, unless the decay is 0 or 1 (q, k, v of unit variance, 128 tokens of 16 x 4, decays 0.95 to 0.9998, words rms: tau = 12 7 to 9, 16 120 to
+ * 150, 20 1900 to 2400; token by token 3 to 10 at each).  Bits of tau beyond 12 widen a prompt's words, not what it knows.
  * Three operation ids; rounds: 6 for every chunk, at least 12.  Workspace (up to 2 GB, with GT_FLAG_SMALL_WORKSPACE 64 MB), graph capture and gt_rekey as in
  * gt_dense_forward; a single token takes none and can be captured at once.  seqs * tokens and seqs * heads <= GT_MAX_DIM. */
 int gt_linattn_forward(gt_ctx *ctx, const gt_linattn *attention, const gt_shares *q, const gt_shares *k, const gt_shares *v, size_t ld, size_t seqs, size_t tokens,

@@ -469,7 +469,7 @@ class GTree:
 
     def linattn_forward(self, layer, q, k=None, v=None, seqs=1, tokens=1, state=None, inplace=False):
         """(o, state) of `tokens` tokens of `seqs` sequences.  q alone: rows [q | k | v], as one projection gives them.  state None: zeros; inplace: the
-        given state is overwritten and returned."""
+        given state is overwritten and returned.  Powers of a decay have 12 fraction bits: several tokens at a time carry about 13 bits, whatever tau is."""
         wk, wv = layer.heads * layer.dk, layer.heads * layer.dv
         rows, ld = seqs * tokens, 0
         if (k is None) != (v is None):

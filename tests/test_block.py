@@ -171,3 +171,43 @@ def test_chunks_are_the_recurrence(seed):
     # (a token's own score is rounded by half a word, times |v|)
     assert np.abs(np.array(rows) / 2.0 ** f - want).max() <= reach * one + (np.abs(V).max() + 1) / 2.0 ** f
     assert np.abs(o.rec(whole).astype(np.int64).reshape(T, dv) / 2.0 ** f - want).max() <= reach * many + score + 2.0 ** -f
+
+
+@pytest.mark.parametrize("f", [8, 16, 20])
+@pytest.mark.parametrize("w", [0, 2048, 3900, 4095, 4096])
+@pytest.mark.parametrize("size", [1, 64])
+def test_how_far_a_prompt_is_from_the_recurrence(seed, f, w, size):
+    """Against the recurrence in real numbers, term by term.  A power of the decay is off by at most d = 2^-13 (12 fraction bits, from 46, whose own roundings add less than
+    2^-40), of a single token by nothing; every completion by r = 2^-(f+1).  So with e the state's error, P_ij = q_i k_j in real numbers:
+      an output by    sum_j (d |P_ij| + r) |v_j| + sum |q_i| (d (|S| + e) + D[i+1] e) + r
+      a state by      d (|S| + e) + D[c] e + sum_j d |k_j v_j| + r
+    and the sums in double precision by less than 2^-40 of theirs."""
+    T, dk, dv = 128, 6, 4
+    q, k, v, S = lin_inputs(f, 1, T, 1, dk, dv, seed=w)
+    o = Oracle(seed, tau=f)
+    shares = shared(o, q, k, v, S)
+    if size == 1:
+        state, rows = shares[3], []
+        for t in range(T):
+            y, state = o.linattn_forward(*shared(o, q[:, t], k[:, t], v[:, t]), state, [w], 1, 1, dk, dv)
+            rows.append(o.rec(y))
+        got = np.concatenate(rows)
+    else:
+        y, state = o.linattn_forward(*shares, [w], 1, T, dk, dv)
+        got = o.rec(y)
+    Q, K, V = (np.asarray(a[0, :, 0], dtype=np.float64) / 2.0 ** f for a in (q, k, v))
+    R, e, decay, r = np.asarray(S[0, 0], dtype=np.float64) / 2.0 ** f, np.zeros((dk, dv)), w / 4096, 2.0 ** -(f + 1)
+    d = 0.0 if size == 1 else 2.0 ** -13 + 2.0 ** -40
+    want, off = np.zeros((T, dv)), np.zeros((T, dv))
+    for t0 in range(0, T, size):
+        qc, kc, vc = Q[t0:t0 + size], K[t0:t0 + size], V[t0:t0 + size]
+        n = np.arange(size)
+        low = np.tri(size)
+        P, D = qc @ kc.T, decay ** (n + 1.0)[:, None]
+        want[t0:t0 + size] = (P * low * decay ** np.maximum(n[:, None] - n, 0)) @ vc + D * (qc @ R)
+        off[t0:t0 + size] = ((d * np.abs(P) + r) * low) @ np.abs(vc) + d * (np.abs(qc) @ (np.abs(R) + e)) + D * (np.abs(qc) @ e) + r
+        e = d * (np.abs(R) + e) + decay ** size * e + d * (np.abs(kc).T @ np.abs(vc)) + r
+        R = decay ** size * R + (kc * decay ** (size - 1.0 - n)[:, None]).T @ vc
+    slack = 2.0 ** -40 * (np.abs(want).max() + np.abs(R).max() + dk * T)
+    assert (np.abs(got.astype(np.int64).reshape(T, dv) / 2.0 ** f - want) <= off + slack).all()
+    assert (np.abs(o.rec(state).astype(np.int64).reshape(dk, dv) / 2.0 ** f - R) <= e + slack).all()
