@@ -8,6 +8,7 @@
 // read again.  Elements are rows of ff8 (ff rounded up to 8), so that eight adjacent ones lie in a row.
 // Z: the parts, [3][rows][2 ffp], left at zero, or R: residues, planes of rows x 2 ffp.  first: the pass's first row.
 // Bound: the vector units, half of them on the block function (2048 x 1024 -> 2048 with ReLU, 1.3e7 completions: 0.79 ms with three wavefronts a SIMD, 0.85 with two).
+// Three were measured with ReLU, where 2 vector registers are spilled; without it 22 are (92 bytes a lane), and the same rows take longer (0.75 ms, with ReLU 0.69 on that card).
 struct GatedArgs {
     KCommon c;
     u64 *Z;
@@ -306,7 +307,7 @@ enum { LIN_SCORES = 0, LIN_KV = 1, LIN_OUT = 2 };
 // [component p or p + 1][16 rows][limb][lane][16 bytes], a block of them made by each wavefront.  A block of 16 rows (or columns) whose terms are adjacent in memory is loaded
 // a row at a time, whole lines, and turned in LDS, where its limbs go afterwards.
 // Bound: instructions of the vector units around the matrix instructions, which a SIMD's two or three wavefronts overlap in part (outputs of 16 heads, 4096 tokens, 64 x 128: 1.0e8 and
-// 1.4e7 of them, 47 and 27 % of 385 us).  Three parties a workgroup, six wavefronts: 414 and 691 us instead of 286 and 385, as one such workgroup fits a compute unit.
+// 1.4e7 of them, 47 and 27 % of 385 us).  k_lin_parts spills 12 vector registers (52 bytes a lane) at its three wavefronts a SIMD, k_lin_out none at its two.  Three parties a workgroup, six wavefronts: 414 and 691 us instead of 286 and 385, as one such workgroup fits a compute unit.
 template <int JOB>
 __device__ __forceinline__ void lin_tile(const LinArgs &a, u32 lb, u32 p, u32 r0, u32 c0, unsigned char *s_a)
 {
@@ -604,8 +605,9 @@ __global__ __launch_bounds__(64) void k_lin_finish(LinArgs a)
 
 // A token of every sequence: its score, output and state in one launch, without a workspace.  Workgroups below nout: 40 outputs of a head, whose one score, q k, the first
 // wavefront works out (each such workgroup for itself) while the second deals the outputs' material and the others make q S, a sixth of the state's rows each
-// (states come from memory, where the token before has put them: with two wavefronts for it 25 us a launch of one sequence, with six 12); the other workgroups: `per` tiles of 40 words of a
-// state for each wavefront.  Where the new states take the place of the old ones, two launches: outputs first.
+// (states come from memory, where the token before has put them: in place, one sequence of 16 heads of 64 x 64, both launches 21 us, with two wavefronts for it 35); the other workgroups: `per` tiles of 40 words of a
+// state for each wavefront.  Where the new states take the place of the old ones, two launches: outputs first (4 heads of 64 x 64: 9.1 us in one launch, in place 11.8 + 8.5;
+// 16 heads 10.2, 11.9 + 9.3).
 // Bound: many sequences: the completions' block function; few: the outputs' two chains of messages.
 #define GT_LIN_TOKEN 8
 __global__ __launch_bounds__(64 * GT_LIN_TOKEN, 4) void k_lin_token(LinArgs a, u32 nout)
